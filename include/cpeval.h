@@ -64,6 +64,9 @@ extern "C" {
 #define CP_STATUS_BAD_TIE        8   /* cp_simulate: tie is not a permutation of 0 .. n-1: nothing was simulated */
 #define CP_STATUS_INCOMPLETE     16  /* cp_simulate: a partition ended with vertices that never started (cannot
                                         happen on a graph that cp_graph_create accepted) */
+#define CP_STATUS_BAD_TOKEN      32  /* cp_token_logprobs: a token >= vocab; it counts as one that is to be ignored */
+#define CP_STATUS_BAD_SEQUENCE   64  /* cp_recurrence: seq_ptr does not rise from 0 to rows: the outputs are meaningless */
+#define CP_STATUS_BAD_SLOT       128 /* cp_recurrence_step: a slot >= num_slots; its row was left out */
 
 /* ---- enums ---- */
 #define CP_TICK_I32  4   /* b-level / t-level stored as int32 (only if the graph's bound allows) */
@@ -470,6 +473,165 @@ int cp_search(const cp_graph *g, int32_t k, const int64_t *speeds, const int64_t
 int cp_ranks_workspace_bytes(const cp_graph *g, size_t *out_bytes);
 int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *stream,
              int64_t *up_out, int64_t *down_out, int64_t *total_out);
+
+/*
+ * ---- Operators of a learned placement policy ----
+ *
+ * A policy that learns where to place a graph's vertices reads them in topological order as a
+ * sequence and gives each a row of logits over the devices; partitions are drawn from the rows,
+ * cp_eval rates them, and the gradient of their log probabilities, weighted by the ratings,
+ * trains the policy.  The entry points below are its sequence layer (cp_recurrence), the joint
+ * between its blocks (cp_norm_gate) and its head (cp_token_logprobs), each with its gradient; the
+ * matrix products between them are left to the caller's library.
+ *
+ * Common to them: all arrays are device memory; matrices have rows of contiguous elements and
+ * a distance ld between rows, in elements, at least the row's length.  Element types are
+ * CP_TYPE_*; vectors of parameters, states and statistics are float where nothing else is said.
+ * States, sums and statistics are formed in 32 bits or more and a result is rounded once, to its
+ * type.  The calls only enqueue work on `stream`, allocate nothing and record no memset or copy,
+ * so that they may be captured into a graph; results do not depend on the order in which
+ * workgroups run.  Workspaces are scratch, 256-byte aligned; two calls that may overlap in time
+ * need distinct ones.
+ */
+#define CP_TYPE_F32  0
+#define CP_TYPE_BF16 1
+#define CP_TYPE_F16  2
+
+#define CP_RECURRENCE_CHUNK      128
+#define CP_RECURRENCE_MAX_WIDTH  65536
+
+/*
+ * Gated linear recurrence along `rows` rows of `width` channels, for each channel on its own:
+ *     a_t = sigmoid(f_t + bias),   h_t = a_t h_{t-1} + (1 - a_t) x_t
+ *
+ *   num_seq, seq_ptr   the rows are cut into num_seq sequences: seq_ptr int32 [num_seq + 1], rising
+ *                 from 0 to rows (sequences may be empty), or NULL: num_seq equal parts (rows is a
+ *                 multiple of num_seq)
+ *   type          CP_TYPE_* of f, x and h
+ *   reverse       0: from each sequence's first row to its last, 1: from the last to the first
+ *   bias          [width], or NULL (0)
+ *   h0            [num_seq][width], the state that each sequence begins with, or NULL (0)
+ *   h             [rows][width]
+ *   last          [num_seq][width], the state that each sequence ends in (h0's where it is empty), or NULL
+ *   carry         [ceil(rows / CP_RECURRENCE_CHUNK)][width] for the backward pass, or NULL
+ *   status_out    device int32, required with seq_ptr: CP_STATUS_BAD_SEQUENCE after the stream has
+ *                 drained where seq_ptr is not what it has to be (no access leaves the arrays)
+ * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, width, num_seq < 1, rows no
+ * multiple of num_seq without seq_ptr, a distance below width), CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.
+ */
+int cp_recurrence_workspace_bytes(int64_t rows, int32_t width, int backward, size_t *out_bytes);
+int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_ptr, int type, int reverse,
+                  const void *f, int64_t ldf, const void *x, int64_t ldx, const float *bias, const float *h0,
+                  void *h, int64_t ldh, float *last, float *carry, void *workspace, size_t workspace_bytes,
+                  void *stream, int32_t *status_out);
+
+/*
+ * Gradient of cp_recurrence: dh [rows][width] and dlast [num_seq][width] (or NULL) are the gradients
+ * of h and last; carry and the inputs are those of the forward call.  df, dx [rows][width] of the
+ * element type; dbias [width] and dh0 [num_seq][width] float, or NULL.  h is not read: it is computed
+ * again from the states in carry.  Errors as cp_recurrence's; carry is required from more than
+ * CP_RECURRENCE_CHUNK rows on.
+ */
+int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_ptr, int type, int reverse,
+                           const void *dh, int64_t lddh, const float *dlast, const void *f, int64_t ldf,
+                           const void *x, int64_t ldx, const float *bias, const float *h0, const float *carry,
+                           void *df, int64_t lddf, void *dx, int64_t lddx, float *dbias, float *dh0,
+                           void *workspace, size_t workspace_bytes, void *stream, int32_t *status_out);
+
+/*
+ * One more row of each of num_seq sequences: state [num_slots][width] is updated in place and
+ * h [num_seq][width] gets the new states.  slots int32 [num_seq]: the state row of each sequence, all
+ * different, or NULL (row i for sequence i); a negative slot leaves its sequence out (its h is 0).
+ * status_out: device int32, required with slots (CP_STATUS_BAD_SLOT).  Errors as cp_recurrence's.
+ */
+int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, int64_t ldf, const void *x, int64_t ldx,
+                       const float *bias, float *state, int32_t num_slots, const int32_t *slots, void *h, int64_t ldh,
+                       void *stream, int32_t *status_out);
+
+#define CP_GATE_NONE     0   /* the gate as it is */
+#define CP_GATE_SIGMOID  1
+#define CP_GATE_SILU     2
+#define CP_NORM_MAX_WIDTH 16384
+
+/*
+ * The joint between two blocks: the norm behind the block that gave y, its gate, the residual
+ * stream x and the norm in front of the next block, row by row of `width` values:
+ *     u = y / rms(y) * w_post,   r = x + scale * act(gate) * u,   z = r / rms(r) * w_pre
+ * with rms(v) = sqrt(mean(v^2) + eps).  z is formed from r before it is rounded.
+ *
+ *   stream_type   of x and r: `type`, or CP_TYPE_F32
+ *   type          of y, gate and z
+ *   weight_type   of w_pre and w_post, [width]
+ *   gate_act      CP_GATE_*
+ *   y             NULL: no block yet, z is the norm of x (gate, w_post NULL; r may be)
+ *   gate          NULL: 1;   w_post NULL: u = y
+ *   stats         [2][rows] for the backward pass (1 / rms of y and of r), or NULL
+ * Errors: CP_ERR_ARG, CP_ERR_SIZE (rows < 0, width, a distance below width), CP_ERR_NULL, CP_ERR_HIP.
+ */
+int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int weight_type, int gate_act,
+                 const void *x, int64_t ldx, const void *y, int64_t ldy, const void *gate, int64_t ldg,
+                 const void *w_pre, const void *w_post, float scale, float eps,
+                 void *r, int64_t ldr, void *z, int64_t ldz, float *stats, void *stream);
+
+/*
+ * Gradient of cp_norm_gate: dr (of r, or NULL: 0) and dz (of z) in; dx, dy, dgate, dw_pre, dw_post out,
+ * each of the type of what it is the gradient of; dy is required with y, the last three may be
+ * NULL.  The inputs and stats are those of the forward call; workspace is needed for dw_pre and dw_post.
+ */
+int cp_norm_gate_backward_workspace_bytes(int64_t rows, int32_t width, size_t *out_bytes);
+int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type, int weight_type, int gate_act,
+                          const void *dr, int64_t lddr, const void *dz, int64_t lddz,
+                          const void *x, int64_t ldx, const void *y, int64_t ldy, const void *gate, int64_t ldg,
+                          const void *w_pre, const void *w_post, float scale, const float *stats,
+                          void *dx, int64_t lddx, void *dy, int64_t lddy, void *dgate, int64_t lddg,
+                          void *dw_pre, void *dw_post, void *workspace, size_t workspace_bytes, void *stream);
+
+#define CP_TOKEN_U8  1
+#define CP_TOKEN_I32 4
+#define CP_TOKEN_I64 8
+#define CP_LOGPROBS_MAX_VOCAB (1 << 26)
+#define CP_LOGPROBS_MAX_TOP   64
+
+/*
+ * Log probabilities of given tokens, with the rows' entropy and their best alternatives, under
+ * softmax(scale * logits) over the allowed places of each row.
+ *
+ *   logits        [rows][vocab] of `type`; scale > 0 (1 / temperature)
+ *   allow         uint64 [rows][ceil(vocab / 64)], bit i of word w = place 64 w + i may be taken, or NULL
+ *                 (all).  What lies at a place that may not is not looked at.
+ *   given, tokens `given` tokens of each row: token g of row i at i * token_row_stride + g * token_stride, of
+ *                 CP_TOKEN_*.  cp_eval's assignments of a batch of partitions are such tokens, in either
+ *                 layout.  A negative token is ignored: its logp is 0 and it has no gradient.
+ *   logp          [rows][given]; -inf at a place that is not allowed
+ *   entropy       [rows]
+ *   stats         [rows][3] for the backward pass
+ *   top           alternatives of each row, at most CP_LOGPROBS_MAX_TOP: top_idx int32 [rows][top], by falling
+ *                 logit, equal ones by rising place, and top_logp; -1 and -inf where fewer have a probability
+ *   status_out    device int32, required: CP_STATUS_BAD_TOKEN after the stream has drained
+ * A row with nothing allowed has entropy 0, logp -inf and no alternatives.  A NaN or +inf at an allowed
+ * place makes its row's results NaN.
+ * Errors: CP_ERR_ARG (type, token_type, scale), CP_ERR_SIZE (rows, vocab, given, top, ld < vocab),
+ * CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.
+ */
+int cp_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top, size_t *out_bytes);
+int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, float scale,
+                      const uint64_t *allow, int32_t given, const void *tokens, int token_type,
+                      int64_t token_row_stride, int64_t token_stride, float *logp, float *entropy, float *stats,
+                      int32_t top, float *top_logp, int32_t *top_idx, void *workspace, size_t workspace_bytes,
+                      void *stream, int32_t *status_out);
+
+/*
+ * Gradient of cp_token_logprobs with respect to the logits, [rows][vocab] of their type: dlogp is the
+ * gradient of logp, at i * dlogp_row_stride + g * dlogp_stride (a stride of 0: the same for all rows or
+ * tokens), dentropy that of entropy at i * dentropy_stride, or NULL; stats are the forward call's.  Tokens
+ * that are ignored, out of range or without a probability pass nothing on; places that are not allowed
+ * and rows with nothing allowed get 0.  The alternatives have no gradient.
+ */
+int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, float scale,
+                               const uint64_t *allow, int32_t given, const void *tokens, int token_type,
+                               int64_t token_row_stride, int64_t token_stride, const float *stats,
+                               const float *dlogp, int64_t dlogp_row_stride, int64_t dlogp_stride,
+                               const float *dentropy, int64_t dentropy_stride, void *dlogits, int64_t ldd, void *stream);
 
 /*
  * Stage timing with HIP events recorded on the stream the kernels run on.

@@ -36,3 +36,12 @@ from .binding import (  # noqa: F401
     error_string,
     load_library,
 )
+from .policy import (  # noqa: F401
+    cp_norm_gate,
+    cp_norm_gate_backward,
+    cp_recurrence,
+    cp_recurrence_backward,
+    cp_recurrence_step,
+    cp_token_logprobs,
+    cp_token_logprobs_backward,
+)

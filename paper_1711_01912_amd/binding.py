@@ -35,6 +35,9 @@ EXPORTS = (
     "cp_profile_create", "cp_profile_reset",
     "cp_profile_count", "cp_profile_read", "cp_profile_plan", "cp_profile_destroy", "cp_cost_magic",
     "cp_error_string", "cp_cost_compact", "cp_window_shape",
+    "cp_recurrence_workspace_bytes", "cp_recurrence", "cp_recurrence_backward", "cp_recurrence_step",
+    "cp_norm_gate", "cp_norm_gate_backward_workspace_bytes", "cp_norm_gate_backward",
+    "cp_token_logprobs_workspace_bytes", "cp_token_logprobs", "cp_token_logprobs_backward",
 )
 
 
@@ -150,6 +153,24 @@ def load_library():
     lib.cp_cost_compact.restype = C.c_int
     lib.cp_cost_compact.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_uint32)]
     lib.cp_error_string.argtypes = [C.c_int]
+    i32, i64, szp = C.c_int32, C.c_int64, C.POINTER(C.c_size_t)
+    lib.cp_recurrence_workspace_bytes.argtypes = [i64, i32, C.c_int, szp]
+    lib.cp_recurrence.argtypes = [i64, i32, i32, vp, C.c_int, C.c_int, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp,
+                                  C.c_size_t, vp, vp]
+    lib.cp_recurrence_backward.argtypes = [i64, i32, i32, vp, C.c_int, C.c_int, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp,
+                                           vp, i64, vp, i64, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.cp_recurrence_step.argtypes = [i32, i32, C.c_int, vp, i64, vp, i64, vp, vp, i32, vp, vp, i64, vp, vp]
+    lib.cp_norm_gate.argtypes = [i64, i32, C.c_int, C.c_int, C.c_int, C.c_int, vp, i64, vp, i64, vp, i64, vp, vp,
+                                 C.c_float, C.c_float, vp, i64, vp, i64, vp, vp]
+    lib.cp_norm_gate_backward_workspace_bytes.argtypes = [i64, i32, szp]
+    lib.cp_norm_gate_backward.argtypes = [i64, i32, C.c_int, C.c_int, C.c_int, C.c_int, vp, i64, vp, i64, vp, i64, vp, i64,
+                                          vp, i64, vp, vp, C.c_float, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp,
+                                          C.c_size_t, vp]
+    lib.cp_token_logprobs_workspace_bytes.argtypes = [i64, i32, i32, szp]
+    lib.cp_token_logprobs.argtypes = [i64, i32, C.c_int, vp, i64, C.c_float, vp, i32, vp, C.c_int, i64, i64, vp, vp, vp, i32,
+                                      vp, vp, vp, C.c_size_t, vp, vp]
+    lib.cp_token_logprobs_backward.argtypes = [i64, i32, C.c_int, vp, i64, C.c_float, vp, i32, vp, C.c_int, i64, i64, vp, vp,
+                                               i64, i64, vp, i64, vp, i64, vp]
     _lib = lib
     return lib
 
