@@ -18,9 +18,10 @@ constexpr size_t kPolicyAlign = 256;     // of workspaces, as cp_eval's
 using bf16 = __bf16;
 using f16 = _Float16;
 
-// V values as one load or store; aligned to their own size
+// V values as one load or store, wherever a value may lie: global memory takes wide accesses at any element's address, and
+// rows of odd widths and distances are read as those of even ones
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Pack {
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
     T v[V];
 };
 
