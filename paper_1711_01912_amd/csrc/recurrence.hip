@@ -13,7 +13,7 @@
 // States, products and sums are floats; a row's result is rounded once, to the element type.
 //
 // Bound by memory, and laid out to read every input once: a workgroup takes a tile of rows x 128 bytes of channels (a cache
-// line of each row) into registers, 16 lanes a row, `kRun` rows a lane.  It publishes what its tile does to a state, looks
+// line of each row) into registers, two channels a lane.  It publishes what its tile does to a state, looks
 // back over the tiles before it until it meets a state that is known, publishes its own, and writes its rows.  Narrow and
 // long tiles keep what is read in looking back small beside a tile's own bytes, and the number of tiles that the chain of
 // states has to pass.
@@ -28,13 +28,16 @@ namespace cpeval {
 
 namespace {
 
-constexpr int kLanes = 16;                          // lanes of a row: with 8 bytes each, 128 bytes
-constexpr int kSides = kWave / kLanes;              // runs side by side in a wavefront
 constexpr int kWaves = 8;
-constexpr int kRuns = kWaves * kSides;              // runs of a workgroup, one behind the other
-constexpr int kForwardRun = 16, kBackwardRun = 8;   // rows of a run, held in registers
+constexpr int kWide = 2;                                // channels of a lane (of a width of one: one)
+constexpr int kForwardSpan = 64, kBackwardSpan = 32;    // rows of a wavefront
+
+// How a wavefront's lanes share its rows: 128 bytes of each, kSides runs of them side by side, held in registers
 template <typename T>
-constexpr int kWide = 8 / sizeof(T);                // channels of a lane
+struct Shape {
+    static constexpr int kLanes = 128 / (kWide * (int)sizeof(T)), kSides = kWave / kLanes, kRuns = kWaves * kSides;
+    static constexpr int kForwardRun = kForwardSpan / kSides, kBackwardRun = kBackwardSpan / kSides;
+};
 
 // Where sequences begin, in positions
 struct Sequences {
@@ -69,13 +72,17 @@ struct Sequences {
     }
 };
 
+// Whether all of a tile's rows are there and lie inside one sequence, which neither begins nor ends with them
+__device__ __forceinline__ bool is_inside(const Sequences &s, int64_t first, int64_t rows) {
+    return first > 0 && first + rows < s.rows && s.begun(first - 1) == s.begun(first + rows);
+}
+
 // The sequence starts among a wavefront's rows, of which each lane has the `run` from its own position on
-template <int RUN>
+template <int RUN, int SIDES>
 struct Starts {
-    static constexpr int kSpan = kSides * RUN;
+    static constexpr int kSpan = SIDES * RUN;
     static_assert(kSpan <= 64, "a wavefront's rows are bits of a word");
-    uint32_t first;          // bit i: the lane's i-th row is a sequence's first, or lies behind the last row; i = 0 .. RUN
-    bool any;                // whether any lane of the wavefront has one, or less than RUN rows
+    uint64_t first;          // bit i: the lane's i-th row is a sequence's first, or lies behind the last row; i = 0 .. RUN
     int32_t *begins, *ends;  // of the lane's rows: the sequence that begins with a marked row, the one that ends in front of it
 
     __device__ __forceinline__ void find(const Sequences &s, int64_t wave0, int wave, int side) {
@@ -116,10 +123,9 @@ struct Starts {
             if (s.rows < wave0 + kSpan) bits |= 1ull << (s.rows - wave0);
             else next = true;
         }
-        any = some || s.rows < wave0 + kSpan;            // (also of wavefronts that lie behind the last row)
-        first = (uint32_t)(bits >> (side * RUN)) & ((1u << RUN) - 1);
-        const bool behind = side + 1 < kSides ? bits >> ((side + 1) * RUN) & 1 : next;
-        first |= behind ? 1u << RUN : 0u;
+        first = bits >> (side * RUN) & ((1ull << RUN) - 1);
+        const bool behind = side + 1 < SIDES ? bits >> (side + 1 < SIDES ? (side + 1) * RUN : 0) & 1 : next;
+        first |= behind ? 1ull << RUN : 0ull;
         begins = first_of + side * RUN;
         ends = last_of + side * RUN;
     }
@@ -164,7 +170,9 @@ __device__ __forceinline__ void publish(uint64_t *at, Effect e) {
 __device__ __forceinline__ uint64_t look(const uint64_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ Effect effect_of(uint64_t w) { return {__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32))}; }
 
-__device__ __forceinline__ float keep_not(float f, float bias) { return fast_rcp(1.0f + fast_exp(f + bias)); }   // z
+// e^(f + bias), with the bias in units of ln 2, and z = 1 / (1 + e^(f + bias))
+__device__ __forceinline__ float odds(float f, float bias2) { return __builtin_amdgcn_exp2f(fmaf(f, kLog2e, bias2)); }
+__device__ __forceinline__ float keep_not(float f, float bias2) { return fast_rcp(1.0f + odds(f, bias2)); }
 
 // (1 - z) h + z x, with h - z h rounded once: 1 - z, rounded, would be off by more than z where z is small
 __device__ __forceinline__ float next(float z, float h, float x) { return fmaf(z, x, fmaf(-z, h, h)); }
@@ -181,17 +189,6 @@ __device__ __forceinline__ void put(float *rows, int64_t row, int32_t width, int
     for (int k = 0; k < V; k++) rows[row * width + c + k] = from[k];
 }
 
-// f for wavefronts with a sequence's start or the last row among their rows, or the same without looking for them
-template <typename F>
-__device__ __forceinline__ void either(bool any, F f) {
-    if (any) f(std::true_type{});
-    else f(std::false_type{});
-}
-
-// The compiler does not move instructions over this: left to itself it starts the exponentials of all rows at once and
-// spills what they give.
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
-
 struct Scan {
     Sequences seq;
     int32_t width, strips, lookers;      // lookers: wavefronts that look back, kSides tiles each at a time
@@ -206,7 +203,10 @@ struct Scan {
 // A lane's place: its channels and its run.  The last lane of a row that is no multiple of V takes its last V channels, some
 // of them as its neighbour does, to the same values.
 template <typename T, int V>
-struct Place {
+struct Place : Shape<T> {
+    using Shape<T>::kLanes;
+    using Shape<T>::kSides;
+    using Shape<T>::kRuns;
     int64_t tile, wave0, p0;
     int32_t strip, c;
     int lane, side, wave, run;
@@ -257,9 +257,9 @@ struct Raw {
 #pragma unroll
         for (uint32_t &one : w) one = word;
     }
-    // what was computed from them (conversions, z) is computed again where it is needed again: the compiler takes them as
-    // unknown from here on.  Kept in registers it would be twice the values themselves, and half the wavefronts.
-    __device__ __forceinline__ void forget() {
+    // The compiler takes them as new from here on, and in this order.  Without this it converts the rows of a whole run at
+    // once, and once for all passes, and spills what it cannot hold.
+    __device__ __forceinline__ void renew() {
 #pragma unroll
         for (uint32_t &one : w) asm volatile("" : "+v"(one));
     }
@@ -271,6 +271,7 @@ constexpr uint32_t kInfinite = sizeof(T) == 4 ? 0x7f800000u : std::is_same_v<T, 
 // lane's own part in one.
 template <typename T, int V, int RUN>
 struct Run {
+    static constexpr int kSides = Shape<T>::kSides;
     const char *base;        // the lowest row that a lane of the wavefront has at its i = 0, column 0
     int64_t step;            // bytes from a lane's row to its next one
     uint32_t off;
@@ -298,17 +299,12 @@ struct Run {
     }
 };
 
-template <typename T, int V, int RUN>
-__device__ __forceinline__ void forget(Raw<T, V> (&of)[RUN]) {
-#pragma unroll
-    for (int i = 0; i < RUN; i++) of[i].forget();
-}
-
 // From the effects of a workgroup's runs (forward: in their order, backward: in the opposite one) to the state that enters
 // each: they are joined inside the wavefronts, then over the tiles before, and applied from there.  What has to wait
 // meanwhile waits in LDS: registers are full of rows.
 template <typename T, int V, bool BACK>
 struct Join {
+    static constexpr int kLanes = Shape<T>::kLanes, kSides = Shape<T>::kSides;
     Effect (*waves)[V][kLanes];          // what each wavefront's runs do, in the order of the chain
     Effect (*before)[kWaves * kWave];    // what the runs of the wavefront before the lane's do
 
@@ -343,9 +339,11 @@ struct Join {
         return all;
     }
 
-    // the state that enters the tile
+    // The state that enters the tile.  Each looking wavefront joins kSides tiles, the first one joins what they found.
     __device__ __forceinline__ void behind(const Place<T, V> &p, const Scan &s, float (&state)[V]) {
-        __shared__ Effect lds[kRuns][V][kLanes];
+        __shared__ Effect lds[kWaves][V][kLanes];
+        __shared__ float lds_state[V][kLanes];
+        __shared__ int lds_known;
         const int64_t tile = BACK ? s.tiles - 1 - p.tile : p.tile;          // in the order of the chain
         const bool tells = p.run == 0 && p.live && tile + 1 < s.tiles;
         if (tells) {
@@ -355,42 +353,62 @@ struct Join {
                 publish(p.word(s, p.tile) + k, {tile ? all.A : -1.0f, all.H});
             }
         }
-        Effect all[V];
+        if (tile == 0) {
+#pragma unroll
+            for (int k = 0; k < V; k++) state[k] = 0.0f;
+            return;
+        }
+        Effect all[V];                   // (the first wavefront's)
 #pragma unroll
         for (int k = 0; k < V; k++) all[k] = {1.0f, 0.0f};
-        const int at_once = s.lookers * kSides;
-        for (int64_t near = tile - 1; near >= 0; near -= at_once) {
+        for (int64_t near = tile - 1;; near -= s.lookers * kSides) {
             if (p.wave < s.lookers) {
                 const int64_t of = near - p.run;
                 const bool there = of >= 0 && p.live;
                 const uint64_t *at = p.word(s, there ? BACK ? s.tiles - 1 - of : of : p.tile);
+                const int here = threadIdx.x & (kWave - 1);
+                uint64_t w[V];
+#pragma unroll
+                for (int k = 0; k < V; k++) w[k] = there ? look(at + k) : 0;
 #pragma unroll
                 for (int k = 0; k < V; k++) {
-                    uint64_t w = there ? look(at + k) : 0;
-                    while (w == kNotYet) w = look(at + k);
-                    lds[p.run][k][p.lane] = there ? effect_of(w) : Effect{-1.0f, 0.0f};
+                    while (w[k] == kNotYet) w[k] = look(at + k);
+                    Effect e = there ? effect_of(w[k]) : Effect{-1.0f, 0.0f};
+#pragma unroll
+                    for (int d = 1; d < kSides; d <<= 1) {
+                        const Effect o = {__shfl(e.A, here + d * kLanes), __shfl(e.H, here + d * kLanes)};
+                        e = then(o, e);          // (of side 0, in the end, all sides)
+                    }
+                    if (p.side == 0) lds[p.wave][k][p.lane] = e;
                 }
             }
             __syncthreads();
-            bool known = false;
-            for (int q = 0; q < at_once && !known; q++) {
-                known = true;
+            if (p.wave == 0) {
+                bool known = false;
+                for (int q = 0; q < s.lookers && !known; q++) {
+                    known = true;
 #pragma unroll
-                for (int k = 0; k < V; k++) {
-                    all[k] = then(lds[q][k][p.lane], all[k]);
-                    known &= all[k].A < 0;
+                    for (int k = 0; k < V; k++) {
+                        all[k] = then(lds[q][k][p.lane], all[k]);
+                        known &= all[k].A < 0;
+                    }
+                    known = __all(known);
                 }
-                known = __all(known);
+                if (known && tells) {
+#pragma unroll
+                    for (int k = 0; k < V; k++) publish(p.word(s, p.tile) + k, {-1.0f, whole(p, k).of(all[k].H)});
+                }
+                if (p.side == 0) {
+#pragma unroll
+                    for (int k = 0; k < V; k++) lds_state[k][p.lane] = all[k].H;
+                }
+                if (threadIdx.x == 0) lds_known = known;
             }
-            if (known) break;            // (every wavefront sees the same)
             __syncthreads();
+            if (lds_known) break;
         }
 #pragma unroll
-        for (int k = 0; k < V; k++) state[k] = tile ? all[k].H : 0.0f;
-        if (tells && tile) {
-#pragma unroll
-            for (int k = 0; k < V; k++) publish(p.word(s, p.tile) + k, {-1.0f, whole(p, k).of(state[k])});
-        }
+        for (int k = 0; k < V; k++) state[k] = lds_state[k][p.lane];
     }
 
     // from the state that enters the tile to the one that enters the lane's run
@@ -405,51 +423,45 @@ struct Join {
     }
 };
 
-template <typename T, int V>
-__global__ __launch_bounds__(kWaves *kWave, 4) void scan_kernel(Scan s, T *h, int64_t ldh, float *last, float *carry, int32_t *status) {
-    constexpr int RUN = kForwardRun;
-    Place<T, V> p;
-    p.template take<RUN>(s, false);
+// One tile.  INSIDE: of the inside of a sequence, the common case; else its wavefronts look for sequences' ends and for rows
+// that are not there.
+template <typename T, int V, bool INSIDE>
+__device__ __forceinline__ void scan(const Scan &s, const Place<T, V> &p, T *h, int64_t ldh, float *last, float *carry) {
+    constexpr int RUN = Shape<T>::kForwardRun;
     const Sequences &seq = s.seq;
     const int32_t c = p.c;
-    const bool full = p.wave0 + kSides * RUN <= seq.rows;
     const int64_t left = seq.rows - p.p0;
-    const int rows = left <= 0 ? 0 : left < RUN ? (int)left : RUN;
+    const int rows = INSIDE || left >= RUN ? RUN : left <= 0 ? 0 : (int)left;
 
     Raw<T, V> fr[RUN], xr[RUN];
     // (z is 0 where f is infinite: rows behind the last leave the state as it is)
-    Run<T, V, RUN>(s.f, s.ldf, seq, p).load(fr, full, rows, kInfinite<T>);
-    Run<T, V, RUN>(s.x, s.ldx, seq, p).load(xr, full, rows, 0u);
-    Starts<RUN> starts;
-    starts.find(seq, p.wave0, p.wave, p.side);
-    if (status && blockIdx.x == 0) check_sequences(seq, status);
+    Run<T, V, RUN>(s.f, s.ldf, seq, p).load(fr, INSIDE, rows, kInfinite<T>);
+    Run<T, V, RUN>(s.x, s.ldx, seq, p).load(xr, INSIDE, rows, 0u);
+    Starts<RUN, Shape<T>::kSides> starts;
+    if (!INSIDE) starts.find(seq, p.wave0, p.wave, p.side);
     float bias[V];
 #pragma unroll
-    for (int k = 0; k < V; k++) bias[k] = s.bias ? s.bias[c + k] : 0.0f;
+    for (int k = 0; k < V; k++) bias[k] = s.bias ? s.bias[c + k] * kLog2e : 0.0f;
 
-    const uint32_t mine = (1u << rows) - 1;
-    const bool begins = starts.first & mine;
+    const uint64_t mine = (1ull << rows) - 1, firsts = INSIDE ? 0 : starts.first & mine, lasts = INSIDE ? 0 : starts.first >> 1 & mine;
     float state[V], A[V];
 #pragma unroll
     for (int k = 0; k < V; k++) state[k] = 0.0f, A[k] = 1.0f;
-    either(starts.any, [&](auto any) {
 #pragma unroll
         for (int i = 0; i < RUN; i++) {
-            if (any && (starts.first & mine) >> i & 1) start_from<V>(state, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
+            fr[i].renew();
+            xr[i].renew();
+            if (firsts >> i & 1) start_from<V>(state, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
 #pragma unroll
             for (int k = 0; k < V; k++) {
                 const float z = keep_not(fr[i][k], bias[k]);
                 state[k] = next(z, state[k], xr[i][k]);
                 A[k] = fmaf(-z, A[k], A[k]);
             }
-            in_order();
         }
-    });
     Effect e[V];
 #pragma unroll
-    for (int k = 0; k < V; k++) e[k] = {begins ? -1.0f : fmaxf(A[k], 0.0f), state[k]};
-    forget<T, V, RUN>(fr);
-    forget<T, V, RUN>(xr);
+    for (int k = 0; k < V; k++) e[k] = {firsts ? -1.0f : fmaxf(A[k], 0.0f), state[k]};
     Join<T, V, false> join;
     join.inside(p, e);
     if (s.ticket) join.behind(p, s, state);
@@ -463,93 +475,105 @@ __global__ __launch_bounds__(kWaves *kWave, 4) void scan_kernel(Scan s, T *h, in
         for (int k = 0; k < V; k++) carry[p.p0 / CP_RECURRENCE_CHUNK * s.width + c + k] = state[k];
     }
     const Run<T, V, RUN> to(h, ldh, seq, p);
-    either(starts.any, [&](auto any) {
 #pragma unroll
         for (int i = 0; i < RUN; i++) {
-            if (any && (starts.first & mine) >> i & 1) start_from<V>(state, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
+            fr[i].renew();
+            xr[i].renew();
+            if (firsts >> i & 1) start_from<V>(state, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
             Pack<T, V> out;
 #pragma unroll
             for (int k = 0; k < V; k++) {
                 state[k] = next(keep_not(fr[i][k], bias[k]), state[k], xr[i][k]);
                 out.v[k] = (T)state[k];
             }
-            in_order();
-            if (!any) {          // (and then all rows are there)
-                if (p.live) store_pack<T, V>(to.row(i), out);
-            } else if (p.live && i < rows) {
+            if (p.live && i < rows) {
                 store_pack<T, V>(to.row(i), out);
-                if (last && (starts.first >> (i + 1) & 1)) put<V>(last, starts.ended_by(seq, i), s.width, c, state);
+                if (last && lasts >> i & 1) put<V>(last, starts.ended_by(seq, i), s.width, c, state);
             }
         }
-    });
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kWaves *kWave, 4) void scan_kernel(Scan s, T *h, int64_t ldh, float *last, float *carry, int32_t *status) {
+    constexpr int RUN = Shape<T>::kForwardRun, kRuns = Shape<T>::kRuns;
+    Place<T, V> p;
+    p.template take<RUN>(s, false);
+    const Sequences &seq = s.seq;
+    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan<T, V, true>(s, p, h, ldh, last, carry);
+    else scan<T, V, false>(s, p, h, ldh, last, carry);
+    if (status && blockIdx.x == 0) check_sequences(seq, status);
     // a sequence without rows ends in the state that it begins with
     if (last && p.live && (seq.ptr || seq.each == 0)) {
         for (int64_t j = p.tile * kRuns + p.run; j < seq.count; j += s.tiles * kRuns) {
             if (seq.ptr && seq.ptr[j] < seq.ptr[j + 1]) continue;
 #pragma unroll
-            for (int k = 0; k < V; k++) last[j * s.width + c + k] = s.h0 ? s.h0[j * s.width + c + k] : 0.0f;
+            for (int k = 0; k < V; k++) last[j * s.width + p.c + k] = s.h0 ? s.h0[j * s.width + p.c + k] : 0.0f;
         }
     }
 }
 
-template <typename T, int V>
-__global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s, const T *dh, int64_t lddh, const float *dlast, const float *carry,
-                                                                         T *df, int64_t lddf, T *dx, int64_t lddx, float *dbias_part,
-                                                                         float *dh0, int32_t *status) {
-    constexpr int RUN = kBackwardRun;
+template <typename T>
+struct Gradient {
+    const T *dh;
+    int64_t lddh;
+    const float *dlast, *carry;
+    T *df, *dx;
+    int64_t lddf, lddx;
+    float *dbias_part, *dh0;
+};
+
+template <typename T, int V, bool INSIDE>
+__device__ __forceinline__ void scan_backward(const Scan &s, const Gradient<T> &g, const Place<T, V> &p, float (&sum)[V]) {
+    constexpr int RUN = Shape<T>::kBackwardRun, kRuns = Shape<T>::kRuns;
     static_assert(kRuns * RUN % CP_RECURRENCE_CHUNK == 0, "a tile begins where a state was kept");
-    Place<T, V> p;
-    p.template take<RUN>(s, true);
     const Sequences &seq = s.seq;
     const int32_t c = p.c;
-    const bool full = p.wave0 + kSides * RUN <= seq.rows;
     const int64_t left = seq.rows - p.p0;
-    const int rows = left <= 0 ? 0 : left < RUN ? (int)left : RUN;
+    const int rows = INSIDE || left >= RUN ? RUN : left <= 0 ? 0 : (int)left;
 
     Raw<T, V> fr[RUN], xr[RUN], dr[RUN];
-    Run<T, V, RUN>(s.f, s.ldf, seq, p).load(fr, full, rows, kInfinite<T>);
-    Run<T, V, RUN>(dh, lddh, seq, p).load(dr, full, rows, 0u);
-    Run<T, V, RUN>(s.x, s.ldx, seq, p).load(xr, full, rows, 0u);
+    Run<T, V, RUN>(s.f, s.ldf, seq, p).load(fr, INSIDE, rows, kInfinite<T>);
+    Run<T, V, RUN>(g.dh, g.lddh, seq, p).load(dr, INSIDE, rows, 0u);
+    Run<T, V, RUN>(s.x, s.ldx, seq, p).load(xr, INSIDE, rows, 0u);
     float state[V], bias[V];
 #pragma unroll
     for (int k = 0; k < V; k++) {
-        bias[k] = s.bias ? s.bias[c + k] : 0.0f;
+        bias[k] = s.bias ? s.bias[c + k] * kLog2e : 0.0f;
         // the state that enters the tile was kept
-        state[k] = p.tile ? carry[p.tile * (kRuns * RUN / CP_RECURRENCE_CHUNK) * s.width + c + k] : 0.0f;
+        state[k] = p.tile ? g.carry[p.tile * (kRuns * RUN / CP_RECURRENCE_CHUNK) * s.width + c + k] : 0.0f;
     }
-    Starts<RUN> starts;
-    starts.find(seq, p.wave0, p.wave, p.side);
-    if (status && blockIdx.x == 0) check_sequences(seq, status);
+    Starts<RUN, Shape<T>::kSides> starts;
+    if (!INSIDE) starts.find(seq, p.wave0, p.wave, p.side);
 
-    const uint32_t mine = (1u << rows) - 1, firsts = starts.first & mine, lasts = starts.first >> 1 & mine;
-    float u[V];
+    const uint64_t mine = (1ull << rows) - 1, firsts = INSIDE ? 0 : starts.first & mine, lasts = INSIDE ? 0 : starts.first >> 1 & mine;
+    float z[RUN][V], u[V];               // (z's registers are the states' below)
     Effect e[V], d[V];
     {
-        float z[RUN][V], run[V], A[V];
+        float run[V], A[V];
 #pragma unroll
         for (int k = 0; k < V; k++) run[k] = 0.0f, A[k] = 1.0f, u[k] = 0.0f;
-        either(starts.any, [&](auto any) {
 #pragma unroll
             for (int i = 0; i < RUN; i++) {
-                if (any && firsts >> i & 1) start_from<V>(run, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
+                fr[i].renew();
+                xr[i].renew();
+                if (firsts >> i & 1) start_from<V>(run, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
 #pragma unroll
                 for (int k = 0; k < V; k++) {
                     z[i][k] = keep_not(fr[i][k], bias[k]);
                     run[k] = next(z[i][k], run[k], xr[i][k]);
                     A[k] = fmaf(-z[i][k], A[k], A[k]);
                 }
-                in_order();
-            }
+                }
 #pragma unroll
             for (int i = RUN - 1; i >= 0; i--) {
-                if (any && lasts >> i & 1) start_from<V>(u, dlast, dlast ? starts.ended_by(seq, i) : 0, s.width, c);
+                dr[i].renew();
+                if (lasts >> i & 1) start_from<V>(u, g.dlast, g.dlast ? starts.ended_by(seq, i) : 0, s.width, c);
 #pragma unroll
                 for (int k = 0; k < V; k++) {
-                    const float g = u[k] + dr[i][k];
-                    u[k] = fmaf(-z[i][k], g, g);
+                    const float to = u[k] + dr[i][k];
+                    u[k] = fmaf(-z[i][k], to, to);
                 }
             }
-        });
 #pragma unroll
         for (int k = 0; k < V; k++) {
             const float a = fmaxf(A[k], 0.0f);
@@ -557,9 +581,6 @@ __global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s,
             d[k] = {lasts ? -1.0f : a, u[k]};
         }
     }
-    forget<T, V, RUN>(fr);
-    forget<T, V, RUN>(xr);
-    forget<T, V, RUN>(dr);
     {
         Join<T, V, true> join;
         join.inside(p, d);
@@ -574,52 +595,62 @@ __global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s,
         join.inside(p, e);
         join.enter(p, state);
     }
-    float before[RUN][V], sum[V];
+    float before[RUN][V];
 #pragma unroll
     for (int k = 0; k < V; k++) sum[k] = 0.0f;
-    const Run<T, V, RUN> to_f(df, lddf, seq, p), to_x(dx, lddx, seq, p);
-    either(starts.any, [&](auto any) {
+    const Run<T, V, RUN> to_f(g.df, g.lddf, seq, p), to_x(g.dx, g.lddx, seq, p);
 #pragma unroll
         for (int i = 0; i < RUN; i++) {
-            if (any && firsts >> i & 1) start_from<V>(state, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
+            xr[i].renew();
+            if (firsts >> i & 1) start_from<V>(state, s.h0, s.h0 ? starts.begun_by(seq, i) : 0, s.width, c);
 #pragma unroll
             for (int k = 0; k < V; k++) {
                 before[i][k] = state[k];
-                state[k] = next(keep_not(fr[i][k], bias[k]), state[k], xr[i][k]);
+                state[k] = next(z[i][k], state[k], xr[i][k]);
             }
-            in_order();
         }
-        forget<T, V, RUN>(fr);
-        forget<T, V, RUN>(xr);
 #pragma unroll
         for (int i = RUN - 1; i >= 0; i--) {
-            if (any && lasts >> i & 1) start_from<V>(u, dlast, dlast ? starts.ended_by(seq, i) : 0, s.width, c);
+            fr[i].renew();
+            xr[i].renew();
+            dr[i].renew();
+            if (lasts >> i & 1) start_from<V>(u, g.dlast, g.dlast ? starts.ended_by(seq, i) : 0, s.width, c);
             Pack<T, V> of, ox;
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                const float ef = fast_exp(fr[i][k] + bias[k]), z = fast_rcp(1.0f + ef);
+                const float ef = odds(fr[i][k], bias[k]), z = fast_rcp(1.0f + ef);
                 const float a = ef < 1.0f ? ef * z : 1.0f - z;      // (exact to its size at both ends)
-                const float g = dr[i][k] + u[k], gz = g * z;
+                const float to = dr[i][k] + u[k], gz = to * z;
                 const float v = gz * a * (before[i][k] - xr[i][k]);
                 ox.v[k] = (T)gz;
                 of.v[k] = (T)v;
-                sum[k] += !any || i < rows ? v : 0.0f;
-                u[k] = g - gz;
+                sum[k] += i < rows ? v : 0.0f;
+                u[k] = to - gz;
             }
-            in_order();
-            if (p.live && (!any || i < rows)) {
+            if (p.live && i < rows) {
                 store_pack<T, V>(to_x.row(i), ox);
                 store_pack<T, V>(to_f.row(i), of);
-                if (any && dh0 && firsts >> i & 1) put<V>(dh0, starts.begun_by(seq, i), s.width, c, u);
+                if (g.dh0 && firsts >> i & 1) put<V>(g.dh0, starts.begun_by(seq, i), s.width, c, u);
             }
         }
-    });
-    if (dbias_part) {
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s, Gradient<T> g, int32_t *status) {
+    constexpr int RUN = Shape<T>::kBackwardRun, kRuns = Shape<T>::kRuns, kLanes = Shape<T>::kLanes;
+    Place<T, V> p;
+    p.template take<RUN>(s, true);
+    const Sequences &seq = s.seq;
+    float sum[V];                        // of df over the lane's rows
+    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan_backward<T, V, true>(s, g, p, sum);
+    else scan_backward<T, V, false>(s, g, p, sum);
+    if (status && blockIdx.x == 0) check_sequences(seq, status);
+    if (g.dbias_part) {
         __shared__ float lds[kWaves][V][kLanes];
 #pragma unroll
         for (int k = 0; k < V; k++) {
-            sum[k] += __shfl_xor(sum[k], kLanes);
-            sum[k] += __shfl_xor(sum[k], 2 * kLanes);
+#pragma unroll
+            for (int off = kLanes; off < kWave; off <<= 1) sum[k] += __shfl_xor(sum[k], off);
             if (p.side == 0) lds[p.wave][k][p.lane] = sum[k];
         }
         __syncthreads();
@@ -628,15 +659,15 @@ __global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s,
             for (int k = 0; k < V; k++) {
                 float all = 0.0f;
                 for (int w = 0; w < kWaves; w++) all += lds[w][k][p.lane];
-                dbias_part[p.tile * s.width + c + k] = all;
+                g.dbias_part[p.tile * s.width + p.c + k] = all;
             }
         }
     }
-    if (dh0 && p.live && (seq.ptr || seq.each == 0)) {
+    if (g.dh0 && p.live && (seq.ptr || seq.each == 0)) {
         for (int64_t j = p.tile * kRuns + p.run; j < seq.count; j += s.tiles * kRuns) {
             if (seq.ptr && seq.ptr[j] < seq.ptr[j + 1]) continue;
 #pragma unroll
-            for (int k = 0; k < V; k++) dh0[j * s.width + c + k] = dlast ? dlast[j * s.width + c + k] : 0.0f;
+            for (int k = 0; k < V; k++) g.dh0[j * s.width + p.c + k] = g.dlast ? g.dlast[j * s.width + p.c + k] : 0.0f;
         }
     }
 }
@@ -685,7 +716,7 @@ __global__ __launch_bounds__(256) void step_kernel(int32_t count, int32_t width,
             Pack<float, V> st = load_pack<float, V>(at);
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                const float z = keep_not((float)fv.v[k], bias ? bias[c + k] : 0.0f);
+                const float z = keep_not((float)fv.v[k], bias ? bias[c + k] * kLog2e : 0.0f);
                 st.v[k] = next(z, st.v[k], (float)xv.v[k]);
                 out.v[k] = (T)st.v[k];
             }
@@ -711,29 +742,32 @@ int check_scan(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_
     return CP_OK;
 }
 
-int64_t tiles_of(int64_t rows, int run) { return std::max<int64_t>(1, (rows + kRuns * run - 1) / (kRuns * run)); }
-
-// A ticket, and an effect for each tile and channel, channels counted up to whole strips of the widest type's lanes
-size_t words_bytes(int64_t rows, int32_t width, bool backward) {
-    const size_t channels = ((size_t)width + kLanes * kWide<bf16> - 1) / (kLanes * kWide<bf16>) * (kLanes * kWide<bf16>);
-    return kPolicyAlign + align_up(tiles_of(rows, backward ? kBackwardRun : kForwardRun) * channels * sizeof(uint64_t));
+int64_t tiles_of(int64_t rows, bool backward) {
+    const int64_t tile = kWaves * (backward ? kBackwardSpan : kForwardSpan);
+    return std::max<int64_t>(1, (rows + tile - 1) / tile);
 }
-size_t part_bytes(int64_t rows, int32_t width) { return align_up((size_t)tiles_of(rows, kBackwardRun) * width * sizeof(float)); }
+
+// A ticket, and an effect for each tile and channel, channels counted up to whole strips of the narrower types' lanes
+size_t words_bytes(int64_t rows, int32_t width, bool backward) {
+    constexpr size_t strip = Shape<bf16>::kLanes * kWide;
+    return kPolicyAlign + align_up(tiles_of(rows, backward) * ((width + strip - 1) / strip * strip) * sizeof(uint64_t));
+}
+size_t part_bytes(int64_t rows, int32_t width) { return align_up((size_t)tiles_of(rows, true) * width * sizeof(float)); }
 
 // Wavefronts that look back.  The chain of states passes as many tiles a round as are looked at; the fewer strips there are,
 // the more tiles of each are under way at once, and the faster it has to be.
 int lookers_of(int32_t strips) { return std::max(1, std::min(kWaves, 32 / strips)); }
 
-void split_over(Scan &s, int run, int v, void *workspace) {
-    s.strips = (s.width + kLanes * v - 1) / (kLanes * v);
-    s.tiles = tiles_of(s.seq.rows, run);
+void split_over(Scan &s, bool backward, int strip, void *workspace) {
+    s.strips = (s.width + strip - 1) / strip;
+    s.tiles = tiles_of(s.seq.rows, backward);
     s.lookers = lookers_of(s.strips);
     s.ticket = s.tiles > 1 ? (uint32_t *)workspace : nullptr;
     s.words = s.tiles > 1 ? (uint64_t *)((char *)workspace + kPolicyAlign) : nullptr;
 }
 
-void clear_words(const Scan &s, int v, hipStream_t stream) {
-    const int64_t count = s.tiles * s.strips * kLanes * v;
+void clear_words(const Scan &s, int strip, hipStream_t stream) {
+    const int64_t count = s.tiles * s.strips * strip;
     hipLaunchKernelGGL(clear_words_kernel, dim3((unsigned)std::min<int64_t>((count + 255) / 256, 2048)), dim3(256), 0, stream, s.ticket, s.words, count);
 }
 
@@ -772,14 +806,15 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
         using T = decltype(t);
         auto go = [&](auto v) {
             constexpr int V = decltype(v)::value;
-            split_over(s, kForwardRun, V, workspace);
+            constexpr int strip = Shape<T>::kLanes * V;
+            split_over(s, false, strip, workspace);
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
-            if (s.ticket) clear_words(s, V, st);
+            if (s.ticket) clear_words(s, strip, st);
             hipLaunchKernelGGL((scan_kernel<T, V>), dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
                                seq_ptr ? status_out : nullptr);
             return launched();
         };
-        if (width >= kWide<T>) return go(std::integral_constant<int, kWide<T>>{});
+        if (width >= kWide) return go(std::integral_constant<int, kWide>{});
         return go(std::integral_constant<int, 1>{});
     });
 }
@@ -808,16 +843,17 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
         using T = decltype(t);
         auto go = [&](auto v) {
             constexpr int V = decltype(v)::value;
-            split_over(s, kBackwardRun, V, workspace);
+            constexpr int strip = Shape<T>::kLanes * V;
+            split_over(s, true, strip, workspace);
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
-            if (s.ticket) clear_words(s, V, st);
-            hipLaunchKernelGGL((scan_backward_kernel<T, V>), dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (const T *)dh, lddh,
-                               dlast, carry, (T *)df, lddf, (T *)dx, lddx, part, dh0, seq_ptr ? status_out : nullptr);
+            if (s.ticket) clear_words(s, strip, st);
+            hipLaunchKernelGGL((scan_backward_kernel<T, V>), dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
+                               Gradient<T>{(const T *)dh, lddh, dlast, carry, (T *)df, (T *)dx, lddf, lddx, part, dh0}, seq_ptr ? status_out : nullptr);
             if (dbias)
                 hipLaunchKernelGGL(column_sum_kernel, dim3((width + 15) / 16), dim3(1024), 0, st, part, s.tiles, width, dbias);
             return launched();
         };
-        if (width >= kWide<T>) return go(std::integral_constant<int, kWide<T>>{});
+        if (width >= kWide) return go(std::integral_constant<int, kWide>{});
         return go(std::integral_constant<int, 1>{});
     });
 }
