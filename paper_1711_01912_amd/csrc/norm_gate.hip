@@ -8,8 +8,10 @@
 //
 //   dx = q,  du = q scale act(gate),  dgate = q scale u act'(gate),  dw_pre = sum dz r/rms(r),  dw_post = sum du y/rms(y)
 //
-// Bound by memory: a row is held in registers by one workgroup, so that every input is read once and every output written
-// once.  Sums are floats; a result is rounded once, to its type.
+// Bound by memory: a row is held in registers by one workgroup, the smallest that has room for it at 16 bytes a load, so
+// that every input is read once and every output written once.  Workgroups go over many rows: weights stay in registers, and
+// so do the sums of the weights' gradients, which are joined over the workgroups at the end, in a fixed order.  Sums are
+// floats; a result is rounded once, to its type.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,97 +33,122 @@ struct Joint {
     float *stats;            // [2][rows]: 1 / rms of y and of r
 };
 
-__device__ __forceinline__ float weight(const void *w, int type, int64_t c) {
-    if (type == CP_TYPE_F32) return ((const float *)w)[c];
-    return type == CP_TYPE_BF16 ? (float)((const bf16 *)w)[c] : (float)((const f16 *)w)[c];
+// Where a thread's values lie: NV vectors of V.  The last vector of a row that is no multiple of V is the row's last V
+// values; those that are another vector's are `skip`ped in sums (and written twice, to the same).
+template <int NT, int V, int NV>
+struct Columns {
+    int32_t c[NV], skip[NV];
+    bool live[NV];
+    __device__ __forceinline__ Columns(int32_t width) {
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const int32_t first = (i * NT + (int32_t)threadIdx.x) * V;
+            live[i] = first < width;
+            c[i] = live[i] ? min(first, width - V) : 0;
+            skip[i] = live[i] ? first - c[i] : V;
+        }
+    }
+};
+
+// V weights as floats
+template <int V>
+__device__ __forceinline__ void load_weights(float (&to)[V], const void *w, int type, int32_t c) {
+    auto from = [&](auto t) {
+        using T = decltype(t);
+        const Pack<T, V> p = load_pack<T, V>((const T *)w + c);
+#pragma unroll
+        for (int k = 0; k < V; k++) to[k] = (float)p.v[k];
+    };
+    if (type == CP_TYPE_F32) from(float{});
+    else if (type == CP_TYPE_BF16) from(bf16{});
+    else from(f16{});
 }
 
-// sum over a workgroup, in every thread
+// Sum over a workgroup, in every thread.  `slot`: no two sums between which no other lies may have the same (a slow wavefront
+// may still read what the last one left).
 template <int NT>
-__device__ __forceinline__ float group_sum(float v, float *lds) {
+__device__ __forceinline__ float group_sum(float v, int slot) {
     v = wave_sum(v);
-    if (NT == kWave) return v;
-    const int wave = threadIdx.x / kWave;
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) lds[wave] = v;
-    __syncthreads();
-    float all = 0.0f;
+    if constexpr (NT > kWave) {
+        __shared__ float lds[4][NT / kWave];
+        if ((threadIdx.x & (kWave - 1)) == 0) lds[slot][threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < NT / kWave; w++) all += lds[w];
-    return all;
+        for (int w = 0; w < NT / kWave; w++) v += lds[slot][w];
+    }
+    return v;
 }
 
 // act(gate) and its slope
 __device__ __forceinline__ void gate_of(float g, int act, float &value, float &slope) {
-    const float sg = fast_rcp(1.0f + fast_exp(-g));
-    if (act == CP_GATE_SIGMOID) {
-        value = sg;
-        slope = sg * (1.0f - sg);
-    } else if (act == CP_GATE_SILU) {
-        value = g * sg;
-        slope = sg * (1.0f + g * (1.0f - sg));
-    } else {
+    if (act == CP_GATE_NONE) {
         value = g;
         slope = 1.0f;
+        return;
     }
+    const float sg = fast_rcp(1.0f + fast_exp(-g));
+    value = act == CP_GATE_SIGMOID ? sg : g * sg;
+    slope = act == CP_GATE_SIGMOID ? sg * (1.0f - sg) : sg * (1.0f + g * (1.0f - sg));
 }
 
 // TS: the stream's type (x, r, dx, dr), TB: the block's (y, gate, z and their gradients)
 template <typename TS, typename TB, int NT, int V, int NV>
 __global__ __launch_bounds__(NT) void joint_kernel(Joint j, TS *r_out, int64_t ldr, TB *z_out, int64_t ldz) {
-    __shared__ float lds[NT / kWave];
+    const Columns<NT, V, NV> at(j.width);
     const float inv = 1.0f / j.width;
-    for (int64_t row = blockIdx.x; row < j.rows; row += gridDim.x) {
-        Pack<TS, V> x[NV];
-        Pack<TB, V> y[NV], g[NV];
+    float w_pre[NV][V], w_post[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        load_weights<V>(w_pre[i], j.w_pre, j.weight_type, at.c[i]);
+        if (j.w_post) load_weights<V>(w_post[i], j.w_post, j.weight_type, at.c[i]);
+        else
+#pragma unroll
+            for (int k = 0; k < V; k++) w_post[i][k] = 1.0f;
+    }
+    int slot = 0;
+    for (int64_t row = blockIdx.x; row < j.rows; row += gridDim.x, slot ^= 2) {
+        Raw<TS, V> x[NV];
+        Raw<TB, V> y[NV], g[NV];
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
-            x[i] = load_pack<TS, V>((const TS *)j.x + row * j.ldx + c);
-            if (j.y) y[i] = load_pack<TB, V>((const TB *)j.y + row * j.ldy + c);
-            if (j.gate) g[i] = load_pack<TB, V>((const TB *)j.gate + row * j.ldg + c);
+            if (j.y) y[i].load((const TB *)j.y + row * j.ldy + at.c[i]);
+            x[i].load((const TS *)j.x + row * j.ldx + at.c[i]);
+            if (j.gate) g[i].load((const TB *)j.gate + row * j.ldg + at.c[i]);
         }
         float ry = 1.0f;
-        if (j.y && j.w_post) {
+        if (j.w_post) {
             float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NV; i++) {
-                if (((int64_t)i * NT + threadIdx.x) * V >= j.width) continue;
+            for (int i = 0; i < NV; i++)
 #pragma unroll
-                for (int k = 0; k < V; k++) sum = fmaf((float)y[i].v[k], (float)y[i].v[k], sum);
-            }
-            ry = 1.0f / sqrtf(group_sum<NT>(sum, lds) * inv + j.eps);
+                for (int k = 0; k < V; k++) sum = k >= at.skip[i] ? fmaf(y[i][k], y[i][k], sum) : sum;
+            ry = 1.0f / sqrtf(group_sum<NT>(sum, slot) * inv + j.eps);
         }
         float r[NV][V], sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
             Pack<TS, V> out;
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                r[i][k] = (float)x[i].v[k];
+                r[i][k] = x[i][k];
                 if (j.y) {
-                    float value = 1.0f, slope, u = (float)y[i].v[k];
-                    if (j.gate) gate_of((float)g[i].v[k], j.act, value, slope);
-                    if (j.w_post) u = u * ry * weight(j.w_post, j.weight_type, c + k);
-                    r[i][k] = fmaf(j.scale * value, u, r[i][k]);
+                    float value = 1.0f, slope;
+                    if (j.gate) gate_of(g[i][k], j.act, value, slope);
+                    r[i][k] = fmaf(j.scale * value, y[i][k] * ry * w_post[i][k], r[i][k]);
                 }
                 out.v[k] = (TS)r[i][k];
-                sum = fmaf(r[i][k], r[i][k], sum);
+                sum = k >= at.skip[i] ? fmaf(r[i][k], r[i][k], sum) : sum;
             }
-            if (r_out) store_pack<TS, V>(r_out + row * ldr + c, out);
+            if (r_out && at.live[i]) store_pack<TS, V>(r_out + row * ldr + at.c[i], out);
         }
-        const float rr = 1.0f / sqrtf(group_sum<NT>(sum, lds) * inv + j.eps);
+        const float rr = 1.0f / sqrtf(group_sum<NT>(sum, slot + 1) * inv + j.eps);
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
             Pack<TB, V> out;
 #pragma unroll
-            for (int k = 0; k < V; k++) out.v[k] = (TB)(r[i][k] * rr * weight(j.w_pre, j.weight_type, c + k));
-            store_pack<TB, V>(z_out + row * ldz + c, out);
+            for (int k = 0; k < V; k++) out.v[k] = (TB)(r[i][k] * rr * w_pre[i][k]);
+            if (at.live[i]) store_pack<TB, V>(z_out + row * ldz + at.c[i], out);
         }
         if (j.stats && threadIdx.x == 0) {
             j.stats[row] = ry;
@@ -130,159 +157,182 @@ __global__ __launch_bounds__(NT) void joint_kernel(Joint j, TS *r_out, int64_t l
     }
 }
 
+template <typename TS, typename TB>
+struct JointGrad {
+    const TS *dr;
+    const TB *dz;
+    TS *dx;
+    TB *dy, *dg;
+    int64_t lddr, lddz, lddx, lddy, lddg;
+    float *part_pre, *part_post;         // [workgroups][width]
+};
+
 template <typename TS, typename TB, int NT, int V, int NV>
-__global__ __launch_bounds__(NT) void joint_backward_kernel(Joint j, const TS *dr, int64_t lddr, const TB *dz, int64_t lddz, TS *dx,
-                                                            int64_t lddx, TB *dy, int64_t lddy, TB *dg, int64_t lddg, float *part_pre,
-                                                            float *part_post) {
-    __shared__ float lds[NT / kWave];
+__global__ __launch_bounds__(NT) void joint_backward_kernel(Joint j, JointGrad<TS, TB> b) {
+    const Columns<NT, V, NV> at(j.width);
     const float inv = 1.0f / j.width;
-    float acc_pre[NV][V], acc_post[NV][V];
+    // (the longest rows leave no registers for weights and sums: these are kept in LDS, those loaded again for every row)
+    constexpr bool APART = NV * V > 8;
+    extern __shared__ float lds_acc[];               // APART: [2][NV * V][NT]
+    float w_pre[NV][V], w_post[NV][V], acc_pre[NV][V], acc_post[NV][V];
+    auto weights = [&](int i) {
+        load_weights<V>(w_pre[i], j.w_pre, j.weight_type, at.c[i]);
+        if (j.w_post) load_weights<V>(w_post[i], j.w_post, j.weight_type, at.c[i]);
+        else
 #pragma unroll
-    for (int i = 0; i < NV; i++)
+            for (int k = 0; k < V; k++) w_post[i][k] = 1.0f;
+    };
+    auto pre = [&](int i, int k) -> float & { return APART ? lds_acc[(i * V + k) * NT + threadIdx.x] : acc_pre[i][k]; };
+    auto post = [&](int i, int k) -> float & { return APART ? lds_acc[((NV + i) * V + k) * NT + threadIdx.x] : acc_post[i][k]; };
 #pragma unroll
-        for (int k = 0; k < V; k++) acc_pre[i][k] = acc_post[i][k] = 0.0f;
-    for (int64_t row = blockIdx.x; row < j.rows; row += gridDim.x) {
+    for (int i = 0; i < NV; i++) {
+        if (!APART) weights(i);
+#pragma unroll
+        for (int k = 0; k < V; k++) pre(i, k) = post(i, k) = 0.0f;
+    }
+    int slot = 0;
+    for (int64_t row = blockIdx.x; row < j.rows; row += gridDim.x, slot ^= 2) {
         const float ry = j.w_post ? j.stats[row] : 1.0f, rr = j.stats[j.rows + row];
-        Pack<TS, V> x[NV], d[NV];
-        Pack<TB, V> y[NV], g[NV], e[NV];
+        Raw<TS, V> x[NV], d[NV];
+        Raw<TB, V> y[NV], g[NV], e[NV];
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            if (j.y) y[i].load((const TB *)j.y + row * j.ldy + at.c[i]);
+            x[i].load((const TS *)j.x + row * j.ldx + at.c[i]);
+            if (j.gate) g[i].load((const TB *)j.gate + row * j.ldg + at.c[i]);
+            e[i].load(b.dz + row * b.lddz + at.c[i]);
+            if (b.dr) d[i].load(b.dr + row * b.lddr + at.c[i]);
+            else d[i].fill(0);
+        }
         float rh[NV][V], dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
-            x[i] = load_pack<TS, V>((const TS *)j.x + row * j.ldx + c);
-            if (j.y) y[i] = load_pack<TB, V>((const TB *)j.y + row * j.ldy + c);
-            if (j.gate) g[i] = load_pack<TB, V>((const TB *)j.gate + row * j.ldg + c);
-            if (dr) d[i] = load_pack<TS, V>(dr + row * lddr + c);
-            e[i] = load_pack<TB, V>(dz + row * lddz + c);
-        }
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
+            if (APART) weights(i);
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                float r = (float)x[i].v[k];
+                float r = x[i][k];
                 if (j.y) {
-                    float value = 1.0f, slope, u = (float)y[i].v[k];
-                    if (j.gate) gate_of((float)g[i].v[k], j.act, value, slope);
-                    if (j.w_post) u = u * ry * weight(j.w_post, j.weight_type, c + k);
-                    r = fmaf(j.scale * value, u, r);
+                    float value = 1.0f, slope;
+                    if (j.gate) gate_of(g[i][k], j.act, value, slope);
+                    r = fmaf(j.scale * value, y[i][k] * ry * w_post[i][k], r);
                 }
                 rh[i][k] = r * rr;
-                const float dzv = (float)e[i].v[k];
-                acc_pre[i][k] = fmaf(dzv, rh[i][k], acc_pre[i][k]);
-                dot = fmaf(dzv * weight(j.w_pre, j.weight_type, c + k), rh[i][k], dot);
+                pre(i, k) = fmaf(e[i][k], rh[i][k], pre(i, k));
+                dot = k >= at.skip[i] ? fmaf(e[i][k] * w_pre[i][k], rh[i][k], dot) : dot;
             }
         }
-        dot = group_sum<NT>(dot, lds) * inv;
+        dot = group_sum<NT>(dot, slot) * inv;
         float du[NV][V], dot2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
             Pack<TS, V> ox;
             Pack<TB, V> og;
+            if (APART) weights(i);
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                float q = rr * ((float)e[i].v[k] * weight(j.w_pre, j.weight_type, c + k) - rh[i][k] * dot);
-                if (dr) q += (float)d[i].v[k];
+                const float q = fmaf(rr, fmaf(-rh[i][k], dot, e[i][k] * w_pre[i][k]), d[i][k]);
                 ox.v[k] = (TS)q;
                 if (j.y) {
-                    float value = 1.0f, slope = 0.0f, yh = (float)y[i].v[k], w = 1.0f;
-                    if (j.gate) gate_of((float)g[i].v[k], j.act, value, slope);
-                    if (j.w_post) {
-                        yh *= ry;
-                        w = weight(j.w_post, j.weight_type, c + k);
-                    }
-                    const float qs = q * j.scale;
-                    og.v[k] = (TB)(qs * yh * w * slope);
-                    const float dv = qs * value;
-                    acc_post[i][k] = fmaf(dv, yh, acc_post[i][k]);
-                    du[i][k] = dv * w;
-                    dot2 = fmaf(du[i][k], yh, dot2);
+                    float value = 1.0f, slope = 0.0f;
+                    if (j.gate) gate_of(g[i][k], j.act, value, slope);
+                    const float yh = y[i][k] * ry, qs = q * j.scale, dv = qs * value;
+                    og.v[k] = (TB)(qs * yh * w_post[i][k] * slope);
+                    post(i, k) = fmaf(dv, yh, post(i, k));
+                    du[i][k] = dv * w_post[i][k];
+                    dot2 = k >= at.skip[i] ? fmaf(du[i][k], yh, dot2) : dot2;
                 }
             }
-            store_pack<TS, V>(dx + row * lddx + c, ox);
-            if (dg) store_pack<TB, V>(dg + row * lddg + c, og);
+            if (at.live[i]) {
+                store_pack<TS, V>(b.dx + row * b.lddx + at.c[i], ox);
+                if (b.dg) store_pack<TB, V>(b.dg + row * b.lddg + at.c[i], og);
+            }
         }
         if (!j.y) continue;
-        if (j.w_post) dot2 = group_sum<NT>(dot2, lds) * inv;
+        if (j.w_post) dot2 = group_sum<NT>(dot2, slot + 1) * inv;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-            if (c >= j.width) continue;
             Pack<TB, V> oy;
 #pragma unroll
-            for (int k = 0; k < V; k++) oy.v[k] = (TB)(j.w_post ? ry * (du[i][k] - (float)y[i].v[k] * ry * dot2) : du[i][k]);
-            store_pack<TB, V>(dy + row * lddy + c, oy);
+            for (int k = 0; k < V; k++) oy.v[k] = (TB)(j.w_post ? ry * fmaf(-y[i][k] * ry, dot2, du[i][k]) : du[i][k]);
+            if (at.live[i]) store_pack<TB, V>(b.dy + row * b.lddy + at.c[i], oy);
         }
     }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-        const int64_t c = ((int64_t)i * NT + threadIdx.x) * V;
-        if (c >= j.width) continue;
+        if (!at.live[i]) continue;
+        const int64_t to = (int64_t)blockIdx.x * j.width + at.c[i];
 #pragma unroll
         for (int k = 0; k < V; k++) {
-            if (part_pre) part_pre[(int64_t)blockIdx.x * j.width + c + k] = acc_pre[i][k];
-            if (part_post) part_post[(int64_t)blockIdx.x * j.width + c + k] = acc_post[i][k];
+            if (k < at.skip[i]) continue;            // (their owner has summed them too)
+            if (b.part_pre) b.part_pre[to + k] = pre(i, k);
+            if (b.part_post) b.part_post[to + k] = post(i, k);
         }
     }
 }
 
-// a weight's gradient from the workgroups' sums, in a fixed order and in 64 bits
-__global__ __launch_bounds__(256) void weight_sum_kernel(const float *part, int32_t groups, int32_t width, void *out, int type) {
-    __shared__ double lds[4][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+// The weights' gradients from the workgroups' sums, 16 columns a workgroup, in a fixed order and in 64 bits
+struct WeightSum {
+    const float *part;
+    void *out;
+};
+__global__ __launch_bounds__(1024) void weight_sum_kernel(WeightSum pre, WeightSum post, int32_t groups, int32_t width, int type) {
+    __shared__ double lds[64][16];
+    const WeightSum &w = blockIdx.y ? post : pre;
+    const int lane = threadIdx.x & 15, first = threadIdx.x / 16;
+    const int32_t c = blockIdx.x * 16 + lane;
     double sum = 0.0;
-    if (c < width)
-        for (int32_t i = wave; i < groups; i += 4) sum += part[(int64_t)i * width + c];
-    lds[wave][lane] = sum;
+    if (c < width) {
+#pragma unroll 4
+        for (int32_t i = first; i < groups; i += 64) sum += w.part[(int64_t)i * width + c];
+    }
+    lds[first][lane] = sum;
     __syncthreads();
-    if (wave != 0 || c >= width) return;
-    const float all = (float)(((lds[0][lane] + lds[1][lane]) + lds[2][lane]) + lds[3][lane]);
-    if (type == CP_TYPE_F32) ((float *)out)[c] = all;
-    else if (type == CP_TYPE_BF16) ((bf16 *)out)[c] = (bf16)all;
-    else ((f16 *)out)[c] = (f16)all;
+    if (first != 0 || c >= width) return;
+    for (int i = 1; i < 64; i++) sum += lds[i][lane];
+    if (type == CP_TYPE_F32) ((float *)w.out)[c] = (float)sum;
+    else if (type == CP_TYPE_BF16) ((bf16 *)w.out)[c] = (bf16)(float)sum;
+    else ((f16 *)w.out)[c] = (f16)(float)sum;
 }
 
-constexpr int32_t kMostGroups = 2048;
+constexpr int kMostWaves = 16 * 256;         // that go over rows at once: what registers leave room for on 256 compute units
 
-// calls f(threads, values a load, loads a thread) for the smallest workgroup that holds a row
-template <typename F>
-int by_shape(bool wide, int32_t width, F f) {
+// Calls f(threads, values a load, loads a thread) for the smallest workgroup that holds a row.  16 bytes a load, of the wider
+// of the two types; a thread holds at most 16 values, so that a workgroup's registers leave room for others.
+template <int WIDE, typename F>
+int by_shape(int32_t width, F f) {
     auto of = [&](auto v) {
-        constexpr int V = decltype(v)::value;
-        auto go = [&](auto nt, auto nv) { return f(nt, v, nv); };
+        constexpr int V = decltype(v)::value, MOST = V == 1 ? 1 : 16 / V;
         using std::integral_constant;
+        auto go = [&](auto nt, auto nv) { return f(nt, v, nv); };
         if (width <= 64 * V) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-        if (width <= 256 * V) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-        if (width <= 512 * V) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-        if (width <= 1024 * V) return go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-        if (width <= 2048 * V) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-        if (width <= 4096 * V) return go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-        if (V == 1 && width <= 8192) return go(integral_constant<int, 1024>{}, integral_constant<int, V == 1 ? 8 : 4>{});
-        if (V == 1 && width <= 16384) return go(integral_constant<int, 1024>{}, integral_constant<int, V == 1 ? 16 : 4>{});
+        if constexpr (V > 1) {
+            if (width <= 128 * V) return go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+            if (width <= 256 * V) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+            if (width <= 512 * V) return go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+            if (width <= 1024 * V) return go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+            if (width <= 2048 * V) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+            return go(integral_constant<int, 1024>{}, integral_constant<int, MOST>{});
+        }
         return (int)CP_ERR_SIZE;
     };
-    if (wide) return of(std::integral_constant<int, 4>{});
+    if (width >= WIDE) return of(std::integral_constant<int, WIDE>{});
     return of(std::integral_constant<int, 1>{});
 }
+static_assert(1024 * 16 >= CP_NORM_MAX_WIDTH, "the largest workgroup holds the longest row");
+
+// threads of the workgroup that by_shape takes
+int shape_threads(int wide, int32_t width) {
+    int nt = 64;
+    while (nt < 1024 && width > nt * wide) nt *= 2;
+    return nt;
+}
+int groups_of(int64_t rows, int32_t width, int wide) { return (int)std::min<int64_t>(rows, kMostWaves / (shape_threads(wide, width) / kWave)); }
 
 int check_joint(int64_t rows, int32_t width, int stream_type, int type, int weight_type, int act) {
     if (!known_type(stream_type) || !known_type(type) || !known_type(weight_type)) return CP_ERR_ARG;
     if ((stream_type != type && stream_type != CP_TYPE_F32) || act < CP_GATE_NONE || act > CP_GATE_SILU) return CP_ERR_ARG;
     if (rows < 0 || width < 1 || width > CP_NORM_MAX_WIDTH) return CP_ERR_SIZE;
     return CP_OK;
-}
-
-bool aligned(size_t bytes, std::initializer_list<const void *> at, std::initializer_list<int64_t> ld) {
-    for (const void *p : at)
-        if ((uintptr_t)p % (4 * bytes)) return false;
-    for (int64_t d : ld)
-        if (d % 4) return false;
-    return true;
 }
 
 // the pairs of element types: the stream as the block, or in 32 bits
@@ -311,15 +361,14 @@ int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int wei
     if (!w_pre || (rows > 0 && (!x || !z || (y && !r)))) return CP_ERR_NULL;
     if (rows > 1 && (ldx < width || ldz < width || (y && ldy < width) || (gate && ldg < width) || (r && ldr < width))) return CP_ERR_SIZE;
     if (rows == 0) return CP_OK;
-    const Joint j{rows, width, x, y, gate, ldx, y ? ldy : 0, gate ? ldg : 0, w_pre, w_post, weight_type, gate_act, scale, eps, stats};
-    const bool wide = width % 4 == 0 && aligned(type_bytes(stream_type), {x, r}, {ldx, r ? ldr : 0}) &&
-                      aligned(type_bytes(type), {y, gate, z}, {j.ldy, j.ldg, ldz});
+    const Joint j{rows, width, x, y, gate, ldx, ldy, ldg, w_pre, w_post, weight_type, gate_act, scale, eps, stats};
     return by_types(stream_type, type, [&](auto ts, auto tb) {
         using TS = decltype(ts);
         using TB = decltype(tb);
-        return by_shape(wide, width, [&](auto nt, auto v, auto nv) {
+        return by_shape<16 / sizeof(TS)>(width, [&](auto nt, auto v, auto nv) {
             constexpr int NT = decltype(nt)::value, V = decltype(v)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((joint_kernel<TS, TB, NT, V, NV>), dim3((unsigned)std::min<int64_t>(rows, 256 * 64)), dim3(NT), 0,
+            const int groups = groups_of(rows, width, 16 / sizeof(TS)) * 2;
+            hipLaunchKernelGGL((joint_kernel<TS, TB, NT, V, NV>), dim3((unsigned)std::min<int64_t>(rows, groups)), dim3(NT), 0,
                                (hipStream_t)stream, j, (TS *)r, ldr, (TB *)z, ldz);
             return launched();
         });
@@ -329,7 +378,7 @@ int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int wei
 int cp_norm_gate_backward_workspace_bytes(int64_t rows, int32_t width, size_t *out_bytes) {
     if (!out_bytes) return CP_ERR_NULL;
     if (rows < 0 || width < 1 || width > CP_NORM_MAX_WIDTH) return CP_ERR_SIZE;
-    *out_bytes = 2 * align_up((size_t)std::min<int64_t>(rows, kMostGroups) * width * sizeof(float));
+    *out_bytes = 2 * align_up((size_t)groups_of(rows, width, 8) * width * sizeof(float));
     return CP_OK;
 }
 
@@ -340,41 +389,45 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
                           size_t workspace_bytes, void *stream) {
     int rc = check_joint(rows, width, stream_type, type, weight_type, gate_act);
     if (rc) return rc;
-    if (rows > 0 && !y && (gate || w_post)) return CP_ERR_ARG;      // (tensors without rows have no address)
+    if (rows > 0 && !y && (gate || w_post)) return CP_ERR_ARG;
     if (!w_pre || (dw_post && !w_post) || (rows > 0 && dgate && !gate)) return CP_ERR_NULL;
     if (rows > 0 && (!dz || !x || !stats || !dx || (y && !dy))) return CP_ERR_NULL;
     if (rows > 1 && ((dr && lddr < width) || lddz < width || ldx < width || (y && (ldy < width || lddy < width)) || (gate && ldg < width) ||
                      (dgate && lddg < width) || lddx < width))
         return CP_ERR_SIZE;
-    const int32_t groups = (int32_t)std::min<int64_t>(rows, kMostGroups);
-    const size_t one = align_up((size_t)groups * width * sizeof(float));
+    const size_t one = align_up((size_t)groups_of(rows, width, 8) * width * sizeof(float));
     if (dw_pre || dw_post) {
         if (!workspace && rows > 0) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < 2 * one) return CP_ERR_WORKSPACE;
     }
     float *part_pre = dw_pre ? (float *)workspace : nullptr;
     float *part_post = dw_post ? (float *)((char *)workspace + one) : nullptr;
-    const Joint j{rows, width, x, y, gate, ldx, y ? ldy : 0, gate ? ldg : 0, w_pre, w_post, weight_type, gate_act, scale, 0.0f, (float *)stats};
-    const bool wide = width % 4 == 0 && aligned(type_bytes(stream_type), {x, dx, dr}, {ldx, lddx, dr ? lddr : 0}) &&
-                      aligned(type_bytes(type), {y, gate, dz, y ? dy : nullptr, dgate}, {j.ldy, j.ldg, lddz, y ? lddy : 0, dgate ? lddg : 0});
+    const Joint j{rows, width, x, y, gate, ldx, ldy, ldg, w_pre, w_post, weight_type, gate_act, scale, 0.0f, (float *)stats};
     const hipStream_t st = (hipStream_t)stream;
+    int32_t groups = 0;
     if (rows > 0) {
         rc = by_types(stream_type, type, [&](auto ts, auto tb) {
             using TS = decltype(ts);
             using TB = decltype(tb);
-            return by_shape(wide, width, [&](auto nt, auto v, auto nv) {
+            groups = groups_of(rows, width, 16 / sizeof(TS));
+            return by_shape<16 / sizeof(TS)>(width, [&](auto nt, auto v, auto nv) {
                 constexpr int NT = decltype(nt)::value, V = decltype(v)::value, NV = decltype(nv)::value;
-                hipLaunchKernelGGL((joint_backward_kernel<TS, TB, NT, V, NV>), dim3((unsigned)groups), dim3(NT), 0, st, j, (const TS *)dr, lddr,
-                                   (const TB *)dz, lddz, (TS *)dx, lddx, (TB *)dy, lddy, (TB *)dgate, lddg, part_pre, part_post);
+                const JointGrad<TS, TB> b{(const TS *)dr, (const TB *)dz, (TS *)dx, (TB *)dy, (TB *)dgate, lddr, lddz, lddx, lddy, lddg,
+                                          part_pre, part_post};
+                constexpr size_t lds = NV * V > 8 ? 2 * NV * V * NT * sizeof(float) : 0;
+                auto *kernel = joint_backward_kernel<TS, TB, NT, V, NV>;
+                if (lds && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+                    return (int)CP_ERR_HIP;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(NT), lds, st, j, b);
                 return launched();
             });
         });
         if (rc) return rc;
     }
-    if (dw_pre)
-        hipLaunchKernelGGL(weight_sum_kernel, dim3((width + kWave - 1) / kWave), dim3(256), 0, st, part_pre, groups, width, dw_pre, weight_type);
-    if (dw_post)
-        hipLaunchKernelGGL(weight_sum_kernel, dim3((width + kWave - 1) / kWave), dim3(256), 0, st, part_post, groups, width, dw_post, weight_type);
+    const WeightSum pre{part_pre, dw_pre}, post{part_post, dw_post};
+    if (dw_pre || dw_post)
+        hipLaunchKernelGGL(weight_sum_kernel, dim3((width + 15) / 16, dw_pre && dw_post ? 2 : 1), dim3(1024), 0, st, dw_pre ? pre : post, post, groups,
+                           width, weight_type);
     return launched();
 }
 

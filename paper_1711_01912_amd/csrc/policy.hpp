@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/cpeval.h"
 
@@ -35,11 +36,47 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &a) {
     *reinterpret_cast<Pack<T, V> *>(p) = a;
 }
 
-// sums and maxima over a wavefront's 64 lanes, in every lane
-__device__ __forceinline__ float wave_sum(float v) {
+// V values as the words they are loaded in.  (As values of 16 bits the compiler gives each a register of its own.)
+template <typename T, int V>
+struct Raw {
+    uint32_t w[(V * sizeof(T) + 3) / 4];
+
+    __device__ __forceinline__ void load(const T *p) {
+        const Pack<T, V> v = load_pack<T, V>(p);
+        w[0] = 0;
+        __builtin_memcpy(w, &v, sizeof(v));
+    }
+    __device__ __forceinline__ float operator[](int k) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+        else if constexpr (std::is_same_v<T, bf16>) return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+        else return (float)__builtin_bit_cast(f16, (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2]));
+    }
+    __device__ __forceinline__ void fill(uint32_t word) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+        for (uint32_t &one : w) one = word;
+    }
+    // The compiler takes them as new from here on, and in this order.  Without this it converts the rows of a whole run at
+    // once, and once for all passes, and spills what it cannot hold.
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (uint32_t &one : w) asm volatile("" : "+v"(one));
+    }
+};
+
+// sums and maxima over a wavefront's 64 lanes, in every lane
+// (by moves inside the vector unit: inside rows of 16 lanes, then from row to row; the last lane has them all)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float lane_move(float v, float none) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v += lane_move<0x111, 0xf>(v, 0.0f);     // row_shr 1, 2, 4, 8
+    v += lane_move<0x112, 0xf>(v, 0.0f);
+    v += lane_move<0x114, 0xf>(v, 0.0f);
+    v += lane_move<0x118, 0xf>(v, 0.0f);
+    v += lane_move<0x142, 0xa>(v, 0.0f);     // row_bcast 15, 31
+    v += lane_move<0x143, 0xc>(v, 0.0f);
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), kWave - 1));
 }
 
 __device__ __forceinline__ float wave_max(float v) {

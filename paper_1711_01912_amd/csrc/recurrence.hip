@@ -238,32 +238,6 @@ struct Place : Shape<T> {
     __device__ __forceinline__ uint64_t *word(const Scan &s, int64_t of) const { return s.words + ((of * s.strips + strip) * kLanes + lane) * V; }
 };
 
-// V values as the words they are loaded in.  (As values of 16 bits the compiler gives each a register of its own.)
-template <typename T, int V>
-struct Raw {
-    uint32_t w[(V * sizeof(T) + 3) / 4];
-
-    __device__ __forceinline__ void load(const T *p) {
-        const Pack<T, V> v = load_pack<T, V>(p);
-        w[0] = 0;
-        __builtin_memcpy(w, &v, sizeof(v));
-    }
-    __device__ __forceinline__ float operator[](int k) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
-        else if constexpr (std::is_same_v<T, bf16>) return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
-        else return (float)__builtin_bit_cast(f16, (uint16_t)(k & 1 ? w[k / 2] >> 16 : w[k / 2]));
-    }
-    __device__ __forceinline__ void fill(uint32_t word) {
-#pragma unroll
-        for (uint32_t &one : w) one = word;
-    }
-    // The compiler takes them as new from here on, and in this order.  Without this it converts the rows of a whole run at
-    // once, and once for all passes, and spills what it cannot hold.
-    __device__ __forceinline__ void renew() {
-#pragma unroll
-        for (uint32_t &one : w) asm volatile("" : "+v"(one));
-    }
-};
 template <typename T>
 constexpr uint32_t kInfinite = sizeof(T) == 4 ? 0x7f800000u : std::is_same_v<T, bf16> ? 0x7f807f80u : 0x7c007c00u;
 
