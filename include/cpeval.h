@@ -611,7 +611,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
  *                 logit, equal ones by rising place, and top_logp; -1 and -inf where fewer have a probability
  *   status_out    device int32, required: CP_STATUS_BAD_TOKEN after the stream has drained
  * A row with nothing allowed has entropy 0, logp -inf and no alternatives.  A NaN or +inf at an allowed
- * place makes its row's results NaN.
+ * place makes its row's results NaN; a NaN is no alternative.
  * Errors: CP_ERR_ARG (type, token_type, scale), CP_ERR_SIZE (rows, vocab, given, top, ld < vocab),
  * CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.
  */

@@ -399,7 +399,7 @@ struct Join {
 
 // One tile.  INSIDE: of the inside of a sequence, the common case; else its wavefronts look for sequences' ends and for rows
 // that are not there.
-template <typename T, int V, bool INSIDE>
+template <typename T, int V, bool STREAM, bool INSIDE>
 __device__ __forceinline__ void scan(const Scan &s, const Place<T, V> &p, T *h, int64_t ldh, float *last, float *carry) {
     constexpr int RUN = Shape<T>::kForwardRun;
     const Sequences &seq = s.seq;
@@ -461,20 +461,20 @@ __device__ __forceinline__ void scan(const Scan &s, const Place<T, V> &p, T *h, 
                 out.v[k] = (T)state[k];
             }
             if (p.live && i < rows) {
-                store_pack<T, V>(to.row(i), out);
+                store_pack<T, V>(to.row(i), out, STREAM);
                 if (last && lasts >> i & 1) put<V>(last, starts.ended_by(seq, i), s.width, c, state);
             }
         }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool STREAM>
 __global__ __launch_bounds__(kWaves *kWave, 4) void scan_kernel(Scan s, T *h, int64_t ldh, float *last, float *carry, int32_t *status) {
     constexpr int RUN = Shape<T>::kForwardRun, kRuns = Shape<T>::kRuns;
     Place<T, V> p;
     p.template take<RUN>(s, false);
     const Sequences &seq = s.seq;
-    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan<T, V, true>(s, p, h, ldh, last, carry);
-    else scan<T, V, false>(s, p, h, ldh, last, carry);
+    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan<T, V, STREAM, true>(s, p, h, ldh, last, carry);
+    else scan<T, V, STREAM, false>(s, p, h, ldh, last, carry);
     if (status && blockIdx.x == 0) check_sequences(seq, status);
     // a sequence without rows ends in the state that it begins with
     if (last && p.live && (seq.ptr || seq.each == 0)) {
@@ -496,7 +496,7 @@ struct Gradient {
     float *dbias_part, *dh0;
 };
 
-template <typename T, int V, bool INSIDE>
+template <typename T, int V, bool STREAM, bool INSIDE>
 __device__ __forceinline__ void scan_backward(const Scan &s, const Gradient<T> &g, const Place<T, V> &p, float (&sum)[V]) {
     constexpr int RUN = Shape<T>::kBackwardRun, kRuns = Shape<T>::kRuns;
     static_assert(kRuns * RUN % CP_RECURRENCE_CHUNK == 0, "a tile begins where a state was kept");
@@ -602,22 +602,22 @@ __device__ __forceinline__ void scan_backward(const Scan &s, const Gradient<T> &
                 u[k] = to - gz;
             }
             if (p.live && i < rows) {
-                store_pack<T, V>(to_x.row(i), ox);
-                store_pack<T, V>(to_f.row(i), of);
+                store_pack<T, V>(to_x.row(i), ox, STREAM);
+                store_pack<T, V>(to_f.row(i), of, STREAM);
                 if (g.dh0 && firsts >> i & 1) put<V>(g.dh0, starts.begun_by(seq, i), s.width, c, u);
             }
         }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool STREAM>
 __global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s, Gradient<T> g, int32_t *status) {
     constexpr int RUN = Shape<T>::kBackwardRun, kRuns = Shape<T>::kRuns, kLanes = Shape<T>::kLanes;
     Place<T, V> p;
     p.template take<RUN>(s, true);
     const Sequences &seq = s.seq;
     float sum[V];                        // of df over the lane's rows
-    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan_backward<T, V, true>(s, g, p, sum);
-    else scan_backward<T, V, false>(s, g, p, sum);
+    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan_backward<T, V, STREAM, true>(s, g, p, sum);
+    else scan_backward<T, V, STREAM, false>(s, g, p, sum);
     if (status && blockIdx.x == 0) check_sequences(seq, status);
     if (g.dbias_part) {
         __shared__ float lds[kWaves][V][kLanes];
@@ -782,9 +782,10 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
             constexpr int V = decltype(v)::value;
             constexpr int strip = Shape<T>::kLanes * V;
             split_over(s, false, strip, workspace);
+            auto *kernel = (size_t)rows * width * sizeof(T) > kStreamed ? scan_kernel<T, V, true> : scan_kernel<T, V, false>;
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
             if (s.ticket) clear_words(s, strip, st);
-            hipLaunchKernelGGL((scan_kernel<T, V>), dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
                                seq_ptr ? status_out : nullptr);
             return launched();
         };
@@ -819,9 +820,10 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
             constexpr int V = decltype(v)::value;
             constexpr int strip = Shape<T>::kLanes * V;
             split_over(s, true, strip, workspace);
+            auto *kernel = 2 * (size_t)rows * width * sizeof(T) > kStreamed ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>;
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
             if (s.ticket) clear_words(s, strip, st);
-            hipLaunchKernelGGL((scan_backward_kernel<T, V>), dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
                                Gradient<T>{(const T *)dh, lddh, dlast, carry, (T *)df, (T *)dx, lddf, lddx, part, dh0}, seq_ptr ? status_out : nullptr);
             if (dbias)
                 hipLaunchKernelGGL(column_sum_kernel, dim3((width + 15) / 16), dim3(1024), 0, st, part, s.tiles, width, dbias);

@@ -17,7 +17,7 @@ namespace cpeval {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr float kNone = -INFINITY;
 constexpr float kLift = 24.0f;
 constexpr float kFar = -1000.0f;         // 2^kFar is 0: keeps 0 * -inf out of sums
@@ -43,7 +43,15 @@ struct Tokens {
     }
 };
 
-// one slice's sums, of the places it holds
+// The larger of three, as one instruction (fmaxf makes each operand a quiet NaN first, by one of its own).  A NaN is passed
+// over, or makes the result one.
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+
+// sums over some of a row's places
 struct Part {
     float m, s, t;
 };
@@ -60,19 +68,22 @@ __device__ __forceinline__ Part joined(Part a, Part b, float unit) {
 __device__ __forceinline__ bool is_empty(Part a) { return a.m == kNone && a.s == 0.0f; }
 __device__ __forceinline__ float base_of(Part a) { return a.m == kNone ? 0.0f : a.m; }
 __device__ __forceinline__ float log2_of(Part a) { return is_empty(a) ? 0.0f : __builtin_amdgcn_logf(a.s); }
+__device__ __forceinline__ float entropy_of(Part a) { return is_empty(a) ? 0.0f : kLn2 * (log2_of(a) - a.t / a.s); }
 
-// Larger logits first, ties by the lower place; 0: not an alternative.  (NaN counts as the largest, as in torch's orders.)
+// Larger logits first, ties by the lower place; 0: not an alternative (-inf, a NaN)
+__device__ __forceinline__ uint32_t value_key(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
 __device__ __forceinline__ uint64_t rank_key(float x, int32_t v) {
-    if (x == kNone) return 0;
-    uint32_t b = __float_as_uint(x + 0.0f);
-    b = b & 0x80000000u ? ~b : b | 0x80000000u;
-    return (uint64_t)b << 32 | (0xffffffffu - (uint32_t)v);
+    return !(x > kNone) ? 0 : (uint64_t)value_key(x) << 32 | (0xffffffffu - (uint32_t)v);
 }
 __device__ __forceinline__ int32_t key_place(uint64_t key) { return (int32_t)(0xffffffffu - (uint32_t)key); }
 __device__ __forceinline__ float key_value(uint64_t key) {
     const uint32_t b = (uint32_t)(key >> 32);
     return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
+constexpr uint32_t kNoneKey = 0x007fffffu;       // value_key(-inf)
 
 // which of the places from v on may be taken, the lowest bit first: as many as v's word still holds.  (The word is read in
 // every case that has a mask, so that what depends on it is a choice between two values: hipcc has compiled a read behind
@@ -85,7 +96,6 @@ __device__ __forceinline__ uint64_t allowed_from(const Rows &r, int64_t row, int
 
 // log2 of the probability at a place, with the row's m and log2 s
 __device__ __forceinline__ float log2_p(float x, float m, float l2s, float unit) { return x == kNone ? kNone : (x - m) * unit - l2s; }
-
 // its natural logarithm (in these units the difference of two of a type's values fits the type)
 __device__ __forceinline__ float log_p(const Rows &r, float x, float m, float l2s) {
     return x == kNone ? kNone : fmaf(x - m, r.scale, -kLn2 * l2s);
@@ -97,31 +107,47 @@ __device__ __forceinline__ float logit(const Rows &r, int64_t row, int32_t v) {
     return allowed_from(r, row, v) & 1 ? x : kNone;
 }
 
-__device__ __forceinline__ uint64_t wave_most(uint64_t v) {
+// maxima and sums over groups of L neighbouring lanes, in all of them
+template <int L>
+__device__ __forceinline__ uint64_t most(uint64_t v) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
+    for (int off = L / 2; off > 0; off >>= 1) {
         const uint64_t o = __shfl_xor((unsigned long long)v, off);
         v = o > v ? o : v;
     }
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+    for (int off = L / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float group_add(float v) {
+#pragma unroll
+    for (int off = L / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
     return v;
 }
 
 struct Results {
     float *logp, *entropy, *stats, *top_logp;
     int32_t *top_idx, top, *status;
+    bool stream;             // logp goes past the caches
 };
 
-// what is written of a row once its sums are known, by a workgroup: stats, entropy, tokens
+__device__ __forceinline__ void write_sums(const Results &out, int64_t row, Part all) {
+    const float entropy = entropy_of(all);
+    out.entropy[row] = entropy;
+    out.stats[3 * row] = base_of(all);
+    out.stats[3 * row + 1] = log2_of(all);
+    out.stats[3 * row + 2] = entropy;
+}
+
+// a row's tokens, by a workgroup
 template <typename T>
-__device__ void write_row(const Rows &r, const Tokens &tok, const Results &out, int64_t row, Part all) {
+__device__ void write_tokens(const Rows &r, const Tokens &tok, const Results &out, int64_t row, Part all) {
     const float m = base_of(all), l2s = log2_of(all);
-    const float entropy = is_empty(all) ? 0.0f : kLn2 * (l2s - all.t / all.s);
-    if (threadIdx.x == 0) {
-        out.entropy[row] = entropy;
-        out.stats[3 * row] = m;
-        out.stats[3 * row + 1] = l2s;
-        out.stats[3 * row + 2] = entropy;
-    }
     for (int32_t g = threadIdx.x; g < tok.count; g += blockDim.x) {
         const int64_t v = tok.get(row, g);
         float lp = 0.0f;
@@ -131,105 +157,230 @@ __device__ void write_row(const Rows &r, const Tokens &tok, const Results &out, 
     }
 }
 
-__device__ void write_top(const Rows &r, const Results &out, int64_t row, int i, uint64_t key, float m, float l2s) {
+__device__ void write_top(const Rows &r, const Results &out, int64_t row, int i, uint64_t key, Part all) {
     out.top_idx[row * out.top + i] = key ? key_place(key) : -1;
-    out.top_logp[row * out.top + i] = key ? log_p(r, key_value(key), m, l2s) : kNone;
+    out.top_logp[row * out.top + i] = key ? log_p(r, key_value(key), base_of(all), log2_of(all)) : kNone;
 }
 
-// One slice of one row a workgroup, held in registers.  ONE: the slice is the whole row, and everything is written here;
-// else its sums and its best places go to the workspace.
-template <typename T, int V, int NV>
-__global__ __launch_bounds__(kThreads) void slice_kernel(Rows r, Tokens tok, Results out, int32_t slices, Part *parts, uint64_t *best) {
-    __shared__ float lds_m[4], lds_s[4], lds_t[4];
-    __shared__ uint64_t lds_key[2][4];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t row = blockIdx.x / slices;
-    const int32_t slice = blockIdx.x % slices, v0 = slice * (kThreads * V * NV);
-    const T *from = (const T *)r.logits + row * r.ld;
-    Pack<T, V> x[NV];
-    float m = kNone;
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int32_t v = v0 + (i * kThreads + threadIdx.x) * V;
-        if (v < r.vocab) {
-            x[i] = load_pack<T, V>(from + v);
-            const uint64_t bits = allowed_from(r, row, v);
-#pragma unroll
-            for (int k = 0; k < V; k++) x[i].v[k] = bits >> k & 1 ? x[i].v[k] : (T)kNone;
-        } else {
-#pragma unroll
-            for (int k = 0; k < V; k++) x[i].v[k] = (T)kNone;
-        }
-#pragma unroll
-        for (int k = 0; k < V; k++) m = fmaxf(m, (float)x[i].v[k]);
-    }
-    m = wave_max(m);
-    if (lane == 0) lds_m[wave] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(lds_m[0], lds_m[1]), fmaxf(lds_m[2], lds_m[3]));
-    float s = 0.0f, t = 0.0f;
-    const float base = m == kNone ? 0.0f : m;
-#pragma unroll
-    for (int i = 0; i < NV; i++)
-#pragma unroll
-        for (int k = 0; k < V; k++) {
-            const float d = ((float)x[i].v[k] - base) * r.unit, e = __builtin_amdgcn_exp2f(d);
-            s += e;
-            t = fmaf(e, fmaxf(d, kFar), t);
-        }
-    s = wave_sum(s);
-    t = wave_sum(t);
-    if (lane == 0) lds_s[wave] = s, lds_t[wave] = t;
-    __syncthreads();
-    const Part all = {m, (lds_s[0] + lds_s[1]) + (lds_s[2] + lds_s[3]), (lds_t[0] + lds_t[1]) + (lds_t[2] + lds_t[3])};
-    if (slices == 1) write_row<T>(r, tok, out, row, all);
-    else if (threadIdx.x == 0) parts[blockIdx.x] = all;
+// ---- rows of many places ----
+//
+// A workgroup takes a slice of a row into registers: exact maximum first, then the sums, with no rescaling on the way, and
+// the row is read once.  Rows are cut into as few slices as leave the chip enough workgroups; what they find is joined by a
+// second launch.
 
-    uint64_t last = ~0ull;
-    for (int q = 0; q < out.top; q++) {
-        uint64_t key = 0;
+// A slice's loads: NV vectors a thread.  The last vector of a row that is no multiple of V is the row's last V places, those
+// of them that belong to another vector counting as not there.
+template <typename T, int V, int NV>
+struct Slice {
+    Raw<T, V> x[NV];
+    int32_t v0;
+
+    __device__ __forceinline__ int32_t first(int i) const { return v0 + (i * kThreads + (int32_t)threadIdx.x) * V; }
+    __device__ __forceinline__ int32_t place(const Rows &r, int i) const { return min(first(i), r.vocab - V); }
+
+    __device__ __forceinline__ void load(const Rows &r, int64_t row, int32_t slice) {
+        v0 = slice * (kThreads * V * NV);
+        const T *from = (const T *)r.logits + row * r.ld;
 #pragma unroll
-        for (int i = 0; i < NV; i++)
+        for (int i = 0; i < NV; i++) x[i].load(from + max(place(r, i), 0));
+    }
+    // which of a vector's places count, the lowest bit first
+    __device__ __forceinline__ uint64_t counts(const Rows &r, int64_t row, int i) const {
+        const int32_t v = first(i);
+        const uint64_t own = v < r.vocab ? ~0ull << (v - place(r, i)) : 0;
+        const uint64_t may = allowed_from(r, row, min(v, r.vocab - 1));
+        return own & (may << (v < r.vocab ? v - place(r, i) : 0));
+    }
+    __device__ __forceinline__ void blank(const Rows &r, int64_t row) {
+        // (all of the places of most slices count)
+        if (!r.allow && v0 + kThreads * V * NV <= r.vocab) return;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const uint64_t bits = counts(r, row, i);
+#pragma unroll
+            for (int k = 0; k < V; k++) x[i].set_none(k, bits >> k & 1);
+        }
+    }
+};
+
+// The best places of a slice.  `own`: the thread's largest logit.  A fourth of K of the threads of each of the four wavefronts
+// have one at or above `bound`, so that K places do, and those that do, few more than K, are all that is put in order.
+// Where too many do (ties), the best are taken one by one, from memory.
+constexpr int kPool = 512;
+template <typename T, int V, int NV, typename F>
+__device__ __forceinline__ void slice_top(const Rows &r, int64_t row, Slice<T, V, NV> &in, float own, int top, F put) {
+    __shared__ uint64_t lds_pool[kPool], lds_key[2][kWaves];
+    __shared__ uint32_t lds_bound[kWaves];
+    __shared__ int lds_count;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, share = (top + kWaves - 1) / kWaves;
+    const uint32_t key = own > kNone ? value_key(own) : 0;
+    uint32_t bound = 0;                  // the share-th largest of the wavefront's: bit by bit, from the highest
+#pragma unroll
+    for (int bit = 31; bit >= 0; bit--) {
+        const uint32_t more = bound | 1u << bit;
+        bound = __popcll(__ballot(key >= more)) >= share ? more : bound;
+    }
+    if (lane == 0) lds_bound[wave] = bound;
+    if (threadIdx.x == 0) lds_count = 0;
+    __syncthreads();
+    bound = max(min(min(lds_bound[0], lds_bound[1]), min(lds_bound[2], lds_bound[3])), kNoneKey + 1);
+    if (key >= bound) {
+        const float low = key_value((uint64_t)bound << 32);
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            in.x[i].renew();
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                const uint64_t one = rank_key((float)x[i].v[k], v0 + (int32_t)((i * kThreads + threadIdx.x) * V) + k);
-                key = one < last && one > key ? one : key;
+                if (!(in.x[i][k] >= low)) continue;
+                const int at = atomicAdd(&lds_count, 1);
+                if (at < kPool) lds_pool[at] = rank_key(in.x[i][k], in.place(r, i) + k);
             }
-        key = wave_most(key);
+        }
+    }
+    __syncthreads();
+    const int count = lds_count;
+    if (count <= kPool) {
+        for (int i = threadIdx.x; i < count; i += kThreads) {
+            const uint64_t key = lds_pool[i];
+            int rank = 0;
+            for (int o = 0; o < count; o++) rank += lds_pool[o] > key;
+            if (rank < top) put(rank, key);
+        }
+        for (int i = count + threadIdx.x; i < top; i += kThreads) put(i, 0);
+        return;
+    }
+    uint64_t last = ~0ull;
+    for (int q = 0; q < top; q++) {
+        uint64_t key = 0;
+        for (int32_t v = in.v0 + threadIdx.x; v < min(in.v0 + kThreads * V * NV, r.vocab); v += kThreads) {
+            const uint64_t one = rank_key(logit<T>(r, row, v), v);
+            key = one < last && one > key ? one : key;
+        }
+        key = most<kWave>(key);
         if (lane == 0) lds_key[q & 1][wave] = key;
         __syncthreads();
-        for (int w = 0; w < 4; w++) key = lds_key[q & 1][w] > key ? lds_key[q & 1][w] : key;
-        if (threadIdx.x == 0) {
-            if (slices == 1) write_top(r, out, row, q, key, base, log2_of(all));
-            else best[(int64_t)blockIdx.x * out.top + q] = key;
-        }
+        for (int w = 0; w < kWaves; w++) key = lds_key[q & 1][w] > key ? lds_key[q & 1][w] : key;
+        if (threadIdx.x == 0) put(q, key);
         last = key;
     }
 }
 
-// a row's slices joined, in their order
-template <typename T>
-__global__ __launch_bounds__(kWave) void join_kernel(Rows r, Tokens tok, Results out, int32_t slices, const Part *parts, const uint64_t *best) {
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x;
-    Part all = {kNone, 0.0f, 0.0f};
-    for (int32_t i = lane; i < slices; i += kWave) all = joined(all, parts[row * slices + i], r.unit);
+// One slice of one row a workgroup.  One slice a row: everything is written here; else its sums and its best places go to the
+// workspace.
+template <typename T, int V, int NV, bool TOP>
+__global__ __launch_bounds__(kThreads, 4) void slice_kernel(Rows r, Tokens tok, Results out, int32_t slices, Part *parts, uint64_t *best) {
+    __shared__ float lds_m[kWaves], lds_s[kWaves], lds_t[kWaves];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t row = blockIdx.x / (uint32_t)slices;
+    Slice<T, V, NV> in;
+    in.load(r, row, (int32_t)(blockIdx.x - (uint32_t)row * (uint32_t)slices));
+    in.blank(r, row);
+    if (slices > 1 && blockIdx.x == 0 && threadIdx.x == 0) *out.status = CP_STATUS_OK;       // (tokens are looked at by the next launch)
+    float m = kNone;
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const Part o = {__shfl_xor(all.m, off), __shfl_xor(all.s, off), __shfl_xor(all.t, off)};
-        all = lane & off ? joined(o, all, r.unit) : joined(all, o, r.unit);
+    for (int i = 0; i < NV; i++) {
+        in.x[i].renew();
+#pragma unroll
+        for (int k = 0; k < V; k += 2) m = max_of(m, in.x[i][k], in.x[i][k + 1]);
     }
-    write_row<T>(r, tok, out, row, all);
-    const float m = base_of(all), l2s = log2_of(all);
+    const float own = m;
+    m = wave_max(m);
+    if (lane == 0) lds_m[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(lds_m[0], lds_m[1]), fmaxf(lds_m[2], lds_m[3]));
+    float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
+    const float base = m == kNone ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        in.x[i].renew();
+#pragma unroll
+        for (int k = 0; k < V; k++) {
+            const float d = (in.x[i][k] - base) * r.unit, e = __builtin_amdgcn_exp2f(d);
+            s[k & 1] += e;
+            t[k & 1] = fmaf(e, fmaxf(d, kFar), t[k & 1]);
+        }
+    }
+    s[0] = wave_sum(s[0] + s[1]);
+    t[0] = wave_sum(t[0] + t[1]);
+    if (lane == 0) lds_s[wave] = s[0], lds_t[wave] = t[0];
+    __syncthreads();
+    const Part all = {m, (lds_s[0] + lds_s[1]) + (lds_s[2] + lds_s[3]), (lds_t[0] + lds_t[1]) + (lds_t[2] + lds_t[3])};
+    if (slices == 1) {
+        if (threadIdx.x == 0) write_sums(out, row, all);
+        write_tokens<T>(r, tok, out, row, all);
+        if constexpr (TOP) slice_top<T, V, NV>(r, row, in, own, out.top, [&](int i, uint64_t key) { write_top(r, out, row, i, key, all); });
+    } else {
+        if (threadIdx.x == 0) parts[blockIdx.x] = all;
+        if constexpr (TOP) slice_top<T, V, NV>(r, row, in, own, out.top, [&](int i, uint64_t key) { best[(int64_t)blockIdx.x * out.top + i] = key; });
+    }
+}
+
+// A row's slices joined, in their order.  Of their best places those count that no slice's worst of its best lies above: the
+// worst of one slice's best is a bound for the row's.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_kernel(Rows r, Tokens tok, Results out, int32_t slices, const Part *parts, const uint64_t *best) {
+    __shared__ Part lds_part;
+    __shared__ uint64_t lds_pool[kPool], lds_key[kWaves];
+    __shared__ int lds_count;
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    if (wave == 0) {
+        Part all = {kNone, 0.0f, 0.0f};
+        for (int32_t i = lane; i < slices; i += kWave) all = joined(all, parts[row * slices + i], r.unit);
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const Part o = {__shfl_xor(all.m, off), __shfl_xor(all.s, off), __shfl_xor(all.t, off)};
+            all = lane & off ? joined(o, all, r.unit) : joined(all, o, r.unit);
+        }
+        if (lane == 0) {
+            lds_part = all;
+            lds_count = 0;
+            write_sums(out, row, all);
+        }
+    }
+    const int64_t count = (int64_t)slices * out.top;
+    const uint64_t *keys = best + row * count;
+    uint64_t bound = 0;
+    if (out.top) {
+        for (int32_t i = threadIdx.x; i < slices; i += kThreads) {
+            const uint64_t worst = keys[(int64_t)i * out.top + out.top - 1];
+            bound = worst > bound ? worst : bound;
+        }
+        bound = most<kWave>(bound);
+        if (lane == 0) lds_key[wave] = bound;
+    }
+    __syncthreads();
+    const Part all = lds_part;
+    write_tokens<T>(r, tok, out, row, all);
+    if (!out.top) return;
+    for (int w = 0; w < kWaves; w++) bound = lds_key[w] > bound ? lds_key[w] : bound;
+    for (int64_t i = threadIdx.x; i < count; i += kThreads) {
+        const uint64_t key = keys[i];
+        if (key == 0 || key < bound) continue;
+        const int at = atomicAdd(&lds_count, 1);
+        if (at < kPool) lds_pool[at] = key;
+    }
+    __syncthreads();
+    const int found = lds_count;
+    if (found <= kPool) {
+        for (int i = threadIdx.x; i < found; i += kThreads) {
+            int rank = 0;
+            for (int o = 0; o < found; o++) rank += lds_pool[o] > lds_pool[i];
+            if (rank < out.top) write_top(r, out, row, rank, lds_pool[i], all);
+        }
+        for (int i = found + threadIdx.x; i < out.top; i += kThreads) write_top(r, out, row, i, 0, all);
+        return;
+    }
     uint64_t last = ~0ull;
     for (int q = 0; q < out.top; q++) {
         uint64_t key = 0;
-        for (int64_t i = lane; i < (int64_t)slices * out.top; i += kWave) {
-            const uint64_t one = best[row * slices * out.top + i];
-            key = one < last && one > key ? one : key;
-        }
-        key = wave_most(key);
-        if (lane == 0) write_top(r, out, row, q, key, m, l2s);
+        for (int64_t i = threadIdx.x; i < count; i += kThreads) key = keys[i] < last && keys[i] > key ? keys[i] : key;
+        key = most<kWave>(key);
+        __syncthreads();
+        if (lane == 0) lds_key[wave] = key;
+        __syncthreads();
+        for (int w = 0; w < kWaves; w++) key = lds_key[w] > key ? lds_key[w] : key;
+        if (threadIdx.x == 0) write_top(r, out, row, q, key, all);
         last = key;
     }
 }
@@ -239,48 +390,82 @@ struct Grads {
     int64_t row_stride, stride;
     const float *dentropy;
     int64_t de_stride;
+    __device__ __forceinline__ float get(int64_t row, int32_t g) const { return dlogp[row * row_stride + g * stride]; }
 };
 
-// One row a workgroup: the softmax's part of every place, then what the tokens add at theirs.  A token's place is written
-// by its first holder in the row, whole.
-template <typename T, int V>
-__global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, float scale, T *out, int64_t ldo) {
-    __shared__ float lds[4];
+// A row's gradient, place by place: scale (hits + p (-sum - de (logp + entropy))) = scale (hits + p (flat + slope log2 p)).
+// p is lifted by 2^kLift: the hardware's exp gives 0 for what lies below the normal numbers, its product with the rest need
+// not.
+struct Slope {
+    float m, low, unit, slope, flat, down;
+    __device__ __forceinline__ Slope(const Rows &r, const float *stats, float de, float sum) {
+        const float l2s = stats[1];
+        m = stats[0];
+        unit = r.unit;
+        low = l2s - kLift;
+        slope = -de * kLn2;
+        flat = -sum - de * stats[2] - kLift * slope + 0.0f * l2s;        // (NaN where the row's sums are)
+        down = r.scale / exp2f(kLift);
+    }
+    __device__ __forceinline__ float at(float x, float hits) const {
+        const float l = log2_p(x, m, low, unit), p = __builtin_amdgcn_exp2f(l);
+        return down * fmaf(p, fmaf(fmaxf(l, kFar), slope, flat), hits * exp2f(kLift));
+    }
+};
+
+// One slice of one row a workgroup: the softmax's part of every place, then what the tokens add at theirs.  A token's place
+// is written by its first holder in the row, whole.
+template <typename T, int V, int NV>
+__global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int32_t slices, bool stream) {
+    __shared__ float lds[kWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t row = blockIdx.x;
-    const float m = stats[3 * row], l2s = stats[3 * row + 1], entropy = stats[3 * row + 2];
-    const float de = d.dentropy ? d.dentropy[row * d.de_stride] : 0.0f;
-    auto given = [&](int32_t g) {        // what token g's log probability passes on, and where
+    const int64_t row = blockIdx.x / (uint32_t)slices;
+    Slice<T, V, NV> in;
+    in.load(r, row, (int32_t)(blockIdx.x - (uint32_t)row * (uint32_t)slices));
+    auto given = [&](int32_t g) {        // what token g's log probability passes on
         const int64_t v = tok.get(row, g);
         const bool fine = v >= 0 && v < r.vocab && logit<T>(r, row, (int32_t)v) != kNone;
-        return fine ? d.dlogp[row * d.row_stride + g * d.stride] : 0.0f;
+        return fine ? d.get(row, g) : 0.0f;
     };
     float sum = 0.0f;
-    for (int32_t g = threadIdx.x; g < tok.count; g += kThreads) sum += given(g);
-    sum = wave_sum(sum);
-    if (lane == 0) lds[wave] = sum;
-    __syncthreads();
-    sum = (lds[0] + lds[1]) + (lds[2] + lds[3]);
-    // p (-sum - de (logp + entropy)) = p (flat + slope log2 p), with p lifted by 2^kLift: the hardware's exp gives 0 for what
-    // lies below the normal numbers, its product with the rest need not
-    const float slope = -de * kLn2, flat = -sum - de * entropy - kLift * slope + 0.0f * l2s;
-    const float lift = exp2f(kLift), down = scale / lift, low = l2s - kLift;
-    auto at = [&](float x, float hits) {
-        const float l = log2_p(x, m, low, r.unit), p = __builtin_amdgcn_exp2f(l);
-        return down * fmaf(p, fmaf(fmaxf(l, kFar), slope, flat), hits * lift);
-    };
-    for (int64_t v = (int64_t)threadIdx.x * V; v < r.vocab; v += kThreads * V) {
-        const Pack<T, V> x = load_pack<T, V>((const T *)r.logits + row * r.ld + v);
-        const uint64_t bits = allowed_from(r, row, (int32_t)v);
+    if (tok.count == 1) {
+        sum = given(0);
+    } else if (tok.count > 1) {
+        for (int32_t g = threadIdx.x; g < tok.count; g += kThreads) sum += given(g);
+        sum = wave_sum(sum);
+        if (lane == 0) lds[wave] = sum;
+        __syncthreads();
+        sum = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    }
+    const Slope slope(r, stats + 3 * row, d.dentropy ? d.dentropy[row * d.de_stride] : 0.0f, sum);
+    // (the places that do not count get what their owner gives them)
+    const int64_t only = tok.count == 1 ? tok.get(row, 0) : -1;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int32_t v = in.place(r, i);
+        if (in.first(i) >= r.vocab) continue;
+        uint64_t may = ~0ull;
+        if (r.allow) {
+            may = r.allow[row * r.words + (v >> 6)] >> (v & 63);
+            if ((v & 63) + V > 64) may |= r.allow[row * r.words + (v >> 6) + 1] << (64 - (v & 63));
+        }
         Pack<T, V> o;
 #pragma unroll
-        for (int k = 0; k < V; k++) o.v[k] = (T)at(bits >> k & 1 ? (float)x.v[k] : kNone, 0.0f);
-        store_pack<T, V>(out + row * ldo + v, o);
+        for (int k = 0; k < V; k++) o.v[k] = (T)slope.at(may >> k & 1 ? in.x[i][k] : kNone, 0.0f);
+        const int64_t to = only - v;
+        if (to >= 0 && to < V) {
+#pragma unroll
+            for (int k = 0; k < V; k++)
+                if (to == k && (may >> k & 1) && in.x[i][k] != kNone) o.v[k] = (T)slope.at(in.x[i][k], sum);
+        }
+        store_pack<T, V>(out + row * ldo + v, o, stream);
     }
+    if (tok.count < 2) return;
     __syncthreads();
+    const int32_t low = in.v0, high = min(in.v0 + kThreads * V * NV, r.vocab);
     for (int32_t g = threadIdx.x; g < tok.count; g += kThreads) {
         const int64_t v = tok.get(row, g);
-        if (v < 0 || v >= r.vocab) continue;
+        if (v < low || v >= high) continue;
         const float x = logit<T>(r, row, (int32_t)v);
         if (x == kNone) continue;
         bool mine = true;
@@ -288,31 +473,241 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, 
         if (!mine) continue;
         float hits = 0.0f;
         for (int32_t o = g; o < tok.count; o++)
-            if (tok.get(row, o) == v) hits += d.dlogp[row * d.row_stride + o * d.stride];
-        out[row * ldo + v] = (T)at(x, hits);
+            if (tok.get(row, o) == v) hits += d.get(row, o);
+        out[row * ldo + v] = (T)slope.at(x, hits);
+    }
+}
+
+// ---- rows of few places, such as devices ----
+//
+// Some neighbouring lanes a row, a place a lane (of more than 64 places: E), several rows a wavefront.  The row's log
+// probabilities are a table in LDS for its tokens, of which there may be as many as partitions were drawn.
+
+// Four tokens from g on, side by side or `stride` apart, -1 behind the last
+template <typename I>
+struct Four {
+    Pack<I, 4> v;
+    __device__ __forceinline__ void load(const Tokens &tok, int64_t row, int32_t g) {
+        const I *at = (const I *)tok.at + row * tok.row_stride;
+        if (tok.stride == 1 && g + 4 <= tok.count) v = load_pack<I, 4>(at + g);
+        else
+#pragma unroll
+            for (int j = 0; j < 4; j++) v.v[j] = at[(int64_t)min(g + j, tok.count - 1) * tok.stride];
+    }
+    // the place of the j-th, or -1 for one to be ignored; `bad`: it lies behind the last place
+    __device__ __forceinline__ int place(int j, int32_t vocab, bool &bad) const {
+        if constexpr (sizeof(I) == 8) {
+            bad |= v.v[j] >= vocab;
+            return v.v[j] >= 0 && v.v[j] < vocab ? (int)v.v[j] : -1;
+        } else {
+            bad |= (int32_t)v.v[j] >= vocab;
+            return (uint32_t)v.v[j] < (uint32_t)vocab ? (int)v.v[j] : -1;
+        }
+    }
+};
+constexpr int kAhead = 4;                // fours a lane loads before it looks at them
+
+// the logits of a row that a lane has, E of them S apart
+template <typename T, int S, int E>
+__device__ __forceinline__ void few_logits(float (&x)[E], const Rows &r, int64_t row, int place) {
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+        x[e] = logit<T>(r, row, min(e * S + place, r.vocab - 1));
+        x[e] = e * S + place < r.vocab ? x[e] : kNone;
+    }
+}
+
+// `lanes` (a multiple of S) lanes a row: S neighbours have its places, and where lanes are more than S, others the same again;
+// for its tokens each of them is another.
+template <typename T, typename I, int S, int E>
+__global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Results out, int lanes) {
+    __shared__ float lds[kWaves][kWave * E];
+    const int lane = threadIdx.x & (kWave - 1), here = lane & (lanes - 1), group = lane / lanes, place = lane & (S - 1);
+    float *table = lds[threadIdx.x / kWave] + group * (S * E);
+    bool bad = false;
+    const int side = kWave / lanes;
+    const int64_t step = (int64_t)gridDim.x * kWaves * side;
+    int64_t row0 = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * side;
+    float soon[E];
+    few_logits<T, S, E>(soon, r, min(row0 + group, r.rows - 1), place);
+    for (; row0 < r.rows; row0 += step) {
+        const int64_t row = min(row0 + group, r.rows - 1);
+        const bool live = row0 + group < r.rows;
+        // what memory has to give is asked for first: this row's tokens, the next row's logits
+        Four<I> four[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; a++)
+            if ((here + a * lanes) * 4 < tok.count) four[a].load(tok, row, (here + a * lanes) * 4);
+        float x[E], m = kNone;
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            x[e] = soon[e];
+            m = fmaxf(m, x[e]);
+        }
+        few_logits<T, S, E>(soon, r, min(row0 + step + group, r.rows - 1), place);
+        Part all = {group_max<S>(m), 0.0f, 0.0f};
+        const float base = base_of(all);
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const float d = (x[e] - base) * r.unit, p = __builtin_amdgcn_exp2f(d);
+            all.s += p;
+            all.t = fmaf(p, fmaxf(d, kFar), all.t);
+        }
+        all.s = group_add<S>(all.s);
+        all.t = group_add<S>(all.t);
+        const float l2s = log2_of(all);
+        if (live && here == 0) write_sums(out, row, all);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int e = 0; e < E; e++) table[e * S + place] = log_p(r, x[e], base, l2s);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * lanes * 4) {
+            if (g0 > here * 4) {
+#pragma unroll
+                for (int a = 0; a < kAhead; a++)
+                    if (g0 + a * lanes * 4 < tok.count) four[a].load(tok, row, g0 + a * lanes * 4);
+            }
+#pragma unroll
+            for (int a = 0; a < kAhead; a++) {
+                const int32_t g = g0 + a * lanes * 4;
+                if (g >= tok.count || !live) continue;
+                Pack<float, 4> lp;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const int v = four[a].place(j, r.vocab, bad);
+                    lp.v[j] = table[max(v, 0)];
+                    lp.v[j] = v >= 0 ? lp.v[j] : 0.0f;
+                }
+                float *to = out.logp + row * tok.count + g;
+                if (g + 4 <= tok.count) store_pack<float, 4>(to, lp, out.stream);
+                else
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        if (g + j < tok.count) to[j] = lp.v[j];
+            }
+        }
+        uint64_t last = ~0ull;
+        for (int q = 0; q < out.top; q++) {
+            uint64_t key = 0;
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const uint64_t one = rank_key(x[e], e * S + place);
+                key = one < last && one > key ? one : key;
+            }
+            key = most<S>(key);
+            if (live && here == 0) write_top(r, out, row, q, key, all);
+            last = key;
+        }
+    }
+    if (bad) atomicOr(out.status, CP_STATUS_BAD_TOKEN);
+}
+
+// COLUMNS: many tokens a row are summed by place in LDS, each lane in columns of its own (so that the order of the sums is
+// fixed), kSets of them, so that as many sums are under way at once, and the row's columns added up; else every lane looks
+// through all of the row's tokens for its own places.
+constexpr int kSets = 4;
+
+template <typename T, typename I, int L, int E, bool COLUMNS>
+__global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo) {
+    static_assert(!COLUMNS || E == 1, "a lane a place");
+    extern __shared__ float lds_columns[];       // COLUMNS: [kWaves][vocab][SETS][kWave + 1]
+    constexpr int SETS = L <= 16 ? kSets : 1;
+    const int lane = threadIdx.x & (kWave - 1), here = lane & (L - 1), group = lane / L;
+    float *columns = lds_columns + (threadIdx.x / kWave) * (r.vocab * SETS * (kWave + 1));
+    bool bad = false;
+    constexpr int kSide = kWave / L;
+    const int64_t step = (int64_t)gridDim.x * kWaves * kSide;
+    int64_t row0 = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kSide;
+    float soon[E];
+    few_logits<T, L, E>(soon, r, min(row0 + group, r.rows - 1), here);
+    for (; row0 < r.rows; row0 += step) {
+        const int64_t row = min(row0 + group, r.rows - 1);
+        const bool live = row0 + group < r.rows;
+        float x[E], hits[E];
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            x[e] = soon[e];
+            hits[e] = 0.0f;
+        }
+        few_logits<T, L, E>(soon, r, min(row0 + step + group, r.rows - 1), here);
+        if constexpr (COLUMNS) {
+            for (int v = 0; v < r.vocab * SETS; v++) columns[v * (kWave + 1) + lane] = 0.0f;
+            for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * L * 4) {
+                Four<I> four[kAhead];
+                Pack<float, 4> w[kAhead];
+#pragma unroll
+                for (int a = 0; a < kAhead; a++) {
+                    const int32_t g = g0 + a * L * 4;
+                    if (g >= tok.count) continue;
+                    four[a].load(tok, row, g);
+                    if (d.stride == 1 && g + 4 <= tok.count) w[a] = load_pack<float, 4>(d.dlogp + row * d.row_stride + g);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 4; j++) w[a].v[j] = g + j < tok.count ? d.get(row, g + j) : 0.0f;
+                }
+#pragma unroll
+                for (int a = 0; a < kAhead; a++) {
+                    if (g0 + a * L * 4 >= tok.count) continue;
+#pragma unroll
+                    for (int j = 0; j < 4; j += SETS) {
+                        float sum[SETS];
+                        int at[SETS];
+#pragma unroll
+                        for (int q = 0; q < SETS; q++) {
+                            const int v = four[a].place(j + q, r.vocab, bad);
+                            at[q] = (max(v, 0) * SETS + q) * (kWave + 1) + lane;
+                            sum[q] = columns[at[q]] + (v >= 0 ? w[a].v[j + q] : 0.0f);
+                        }
+#pragma unroll
+                        for (int q = 0; q < SETS; q++) columns[at[q]] = sum[q];
+                    }
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            const float *mine = columns + min(here, r.vocab - 1) * (SETS * (kWave + 1)) + group * L;
+#pragma unroll
+            for (int q = 0; q < SETS; q++)
+#pragma unroll
+                for (int j = 0; j < L; j++) hits[0] += mine[q * (kWave + 1) + j];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            for (int32_t g = 0; g < tok.count; g++) {
+                const int64_t v = ((const I *)tok.at)[row * tok.row_stride + (int64_t)g * tok.stride];
+                const float w = d.get(row, g);
+#pragma unroll
+                for (int e = 0; e < E; e++) hits[e] += v == e * L + here ? w : 0.0f;
+            }
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            hits[e] = x[e] == kNone ? 0.0f : hits[e];
+            sum += hits[e];
+        }
+        const Slope slope(r, stats + 3 * row, d.dentropy ? d.dentropy[row * d.de_stride] : 0.0f, group_add<L>(sum));
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            if (live && e * L + here < r.vocab) out[row * ldo + e * L + here] = (T)slope.at(x[e], hits[e]);
     }
 }
 
 __global__ void clear_status_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 
-// (sixteen bytes a lane where rows allow it)
-template <typename T>
-bool wide(int32_t vocab, std::initializer_list<const void *> at, std::initializer_list<int64_t> ld) {
-    constexpr int v = 16 / sizeof(T);
-    for (const void *p : at)
-        if ((uintptr_t)p % 16) return false;
-    for (int64_t l : ld)
-        if (l % v) return false;
-    return vocab % v == 0;
-}
-
-constexpr int kMostLoads = 8;
+constexpr int kMostLoads = 4;
+constexpr int32_t kFew = 256;            // up to so many places a row is some lanes'
+constexpr int32_t kColumns = 16;         // from so many tokens on they are summed in columns of LDS
 constexpr int32_t slice_places(int v, int nv) { return kThreads * v * nv; }
+int32_t slices_of(int32_t vocab, int v, int nv) { return (vocab + slice_places(v, nv) - 1) / slice_places(v, nv); }
 
 // loads a thread: as many as leave the chip two workgroups a compute unit, and no more than the row has
 int loads_of(int64_t rows, int32_t vocab, int v) {
     int nv = 1;
-    while (nv < kMostLoads && slice_places(v, nv) < vocab && rows * ((vocab + slice_places(v, 2 * nv) - 1) / slice_places(v, 2 * nv)) >= 512) nv *= 2;
+    while (nv < kMostLoads && slice_places(v, nv) < vocab && rows * slices_of(vocab, v, 2 * nv) >= 512) nv *= 2;
     return nv;
 }
 
@@ -324,10 +719,37 @@ int check_rows(int64_t rows, int32_t vocab, int type, int32_t given, int token_t
 
 // workgroups of the finest slicing that a call of these sizes can take
 int64_t most_slices(int64_t rows, int32_t vocab) {
-    const int64_t v1 = (vocab + slice_places(1, loads_of(rows, vocab, 1)) - 1) / slice_places(1, loads_of(rows, vocab, 1));
-    const int64_t v4 = (vocab + slice_places(4, loads_of(rows, vocab, 4)) - 1) / slice_places(4, loads_of(rows, vocab, 4));
-    const int64_t v8 = (vocab + slice_places(8, loads_of(rows, vocab, 8)) - 1) / slice_places(8, loads_of(rows, vocab, 8));
-    return rows * std::max(v1, std::max(v4, v8));
+    if (vocab <= kFew) return 0;
+    return rows * std::max(slices_of(vocab, 4, loads_of(rows, vocab, 4)), slices_of(vocab, 8, loads_of(rows, vocab, 8)));
+}
+
+// f(loads a thread)
+template <typename F>
+int by_loads(int nv, F f) {
+    if (nv == 1) return f(std::integral_constant<int, 1>{});
+    if (nv == 2) return f(std::integral_constant<int, 2>{});
+    if (nv == 4) return f(std::integral_constant<int, 4>{});
+    return f(std::integral_constant<int, 8>{});
+}
+
+// f(a value of the tokens' type, lanes a row, places a lane).  Lanes: as many as there are places, and with many tokens, of
+// which a lane writes 16 bytes at once, enough for a line of 128 bytes.
+template <typename F>
+int by_lanes(const Tokens &tok, int32_t vocab, int32_t least, F f) {
+    auto of = [&](auto i) {
+        using std::integral_constant;
+        auto go = [&](auto l, auto e) { return f(i, l, e); };
+        const int32_t want = std::max(vocab, least);
+        if (want <= 4) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+        if (want <= 8) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        if (want <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+        if (want <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+        if (want <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+        return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    };
+    if (tok.type == CP_TOKEN_U8) return of(uint8_t{});
+    if (tok.type == CP_TOKEN_I32) return of(int32_t{});
+    return of(int64_t{});
 }
 
 }  // namespace
@@ -362,34 +784,42 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
     if (need && !workspace) return CP_ERR_NULL;
     if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
     const hipStream_t st = (hipStream_t)stream;
-    hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_out);
-    if (rows == 0) return launched();
+    auto clear = [&] { hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_out); };
+    if (rows == 0) {
+        clear();
+        return launched();
+    }
     const Rows r{rows, vocab, logits, ld, scale, scale * kLog2e, allow, (vocab + 63) / 64};
     const Tokens tok{tokens, token_type, token_row_stride, token_stride, given};
-    const Results out{logp, entropy, stats, top_logp, top_idx, top, status_out};
+    const Results out{logp, entropy, stats, top_logp, top_idx, top, status_out, (size_t)rows * given * sizeof(float) > kStreamed};
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        auto go = [&](auto v) {
-            constexpr int V = decltype(v)::value;
-            const int nv = loads_of(rows, vocab, V);
-            const int32_t slices = (vocab + slice_places(V, nv) - 1) / slice_places(V, nv);
-            if (rows * slices > INT32_MAX) return (int)CP_ERR_SIZE;
-            Part *parts = (Part *)workspace;
-            uint64_t *best = (uint64_t *)((char *)workspace + align_up((size_t)rows * slices * sizeof(Part)));
-            auto run = [&](auto n) {
-                constexpr int NV = decltype(n)::value;
-                hipLaunchKernelGGL((slice_kernel<T, V, NV>), dim3((unsigned)(rows * slices)), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
-            };
-            if (nv == 1) run(std::integral_constant<int, 1>{});
-            else if (nv == 2) run(std::integral_constant<int, 2>{});
-            else if (nv == 4) run(std::integral_constant<int, 4>{});
-            else run(std::integral_constant<int, 8>{});
-            if (slices > 1) hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)rows), dim3(kWave), 0, st, r, tok, out, slices, parts, best);
-            return launched();
-        };
+        if (vocab <= kFew) {
+            clear();
+            return by_lanes(tok, vocab, 4, [&](auto i, auto l, auto e) {
+                constexpr int S = decltype(l)::value, E = decltype(e)::value;
+                // (four tokens a lane and load)
+                int lanes = S;
+                while (lanes < kWave && lanes * 4 < given) lanes *= 2;
+                const int side = kWaves * kWave / lanes;
+                hipLaunchKernelGGL((few_kernel<T, decltype(i), S, E>), dim3((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8)),
+                                   dim3(kThreads), 0, st, r, tok, out, lanes);
+                return launched();
+            });
+        }
         constexpr int V = 16 / sizeof(T);
-        if (wide<T>(vocab, {logits}, {ld})) return go(std::integral_constant<int, V>{});
-        return go(std::integral_constant<int, 1>{});
+        const int nv = loads_of(rows, vocab, V);
+        const int32_t slices = slices_of(vocab, V, nv);
+        if (rows * slices > INT32_MAX) return (int)CP_ERR_SIZE;
+        Part *parts = (Part *)workspace;
+        uint64_t *best = (uint64_t *)((char *)workspace + align_up((size_t)rows * slices * sizeof(Part)));
+        if (slices == 1) clear();
+        return by_loads(nv, [&](auto n) {
+            auto *kernel = top ? slice_kernel<T, V, decltype(n)::value, true> : slice_kernel<T, V, decltype(n)::value, false>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * slices)), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
+            if (slices > 1) hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)rows), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
+            return launched();
+        });
     });
 }
 
@@ -406,17 +836,34 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
     const Rows r{rows, vocab, logits, ld, scale, scale * kLog2e, allow, (vocab + 63) / 64};
     const Tokens tok{tokens, token_type, token_row_stride, token_stride, given};
     const Grads d{dlogp, dlogp_row_stride, dlogp_stride, dentropy, dentropy_stride};
+    const hipStream_t st = (hipStream_t)stream;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        auto go = [&](auto v) {
-            constexpr int V = decltype(v)::value;
-            hipLaunchKernelGGL((gradient_kernel<T, V>), dim3((unsigned)rows), dim3(kThreads), 0, (hipStream_t)stream, r, tok, stats, d, scale,
-                               (T *)dlogits, ldd);
-            return launched();
-        };
+        if (vocab <= kFew)
+            return by_lanes(tok, vocab, given >= 32 ? 8 : 4, [&](auto i, auto l, auto e) {
+                constexpr int L = decltype(l)::value, E = decltype(e)::value, side = kWaves * kWave / L;
+                const dim3 grid((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8));
+                if (E == 1 && given >= kColumns) {
+                    const size_t lds = (size_t)kWaves * vocab * (L <= 16 ? kSets : 1) * (kWave + 1) * sizeof(float);
+                    auto *kernel = few_gradient_kernel<T, decltype(i), L, E, E == 1>;
+                    if (lds > 48 * 1024 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+                        return (int)CP_ERR_HIP;
+                    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd);
+                } else {
+                    hipLaunchKernelGGL((few_gradient_kernel<T, decltype(i), L, E, false>), grid, dim3(kThreads), 0, st, r, tok, stats, d,
+                                       (T *)dlogits, ldd);
+                }
+                return launched();
+            });
         constexpr int V = 16 / sizeof(T);
-        if (wide<T>(vocab, {logits, dlogits}, {ld, ldd})) return go(std::integral_constant<int, V>{});
-        return go(std::integral_constant<int, 1>{});
+        const int nv = std::min(loads_of(rows, vocab, V), 4);
+        const int32_t slices = slices_of(vocab, V, nv);
+        if (rows * slices > INT32_MAX) return (int)CP_ERR_SIZE;
+        return by_loads(nv, [&](auto n) {
+            hipLaunchKernelGGL((gradient_kernel<T, V, decltype(n)::value>), dim3((unsigned)(rows * slices)), dim3(kThreads), 0, st, r, tok, stats, d,
+                               (T *)dlogits, ldd, slices, (size_t)rows * vocab * sizeof(T) > kStreamed);
+            return launched();
+        });
     });
 }
 
