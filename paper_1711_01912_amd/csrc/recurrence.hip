@@ -14,8 +14,8 @@
 //
 // Bound by memory, and laid out to read every input once: a workgroup takes a tile of rows x 128 bytes of channels (a cache
 // line of each row) into registers, two channels a lane.  It publishes what its tile does to a state, looks
-// back over the tiles before it until it meets a state that is known, publishes its own, and writes its rows.  Narrow and
-// long tiles keep what is read in looking back small beside a tile's own bytes, and the number of tiles that the chain of
+// at what the tiles of its group before it do, waits for the state that enters the group, and writes its rows.  Narrow and
+// long tiles keep what is read in looking back small beside a tile's own bytes, and the number of groups that the chain of
 // states has to pass.
 #include <hip/hip_runtime.h>
 
@@ -197,7 +197,7 @@ struct Scan {
     int64_t ldf, ldx;
     const float *bias, *h0;
     uint32_t *ticket;                    // the next tile to be taken; null: one tile a strip
-    uint64_t *words;                     // [tiles][strips][kLanes * V] effects
+    uint64_t *words;                     // [tiles][strips][kLanes * V] effects, then as many for the states that enter groups
 };
 
 // A lane's place: its channels and its run.  The last lane of a row that is no multiple of V takes its last V channels, some
@@ -313,74 +313,63 @@ struct Join {
         return all;
     }
 
-    // The state that enters the tile.  Each looking wavefront joins kSides tiles, the first one joins what they found.
+    // The state that enters the tile: that which enters its group of lookers * kSides tiles, and what the tiles of the group
+    // before it do to it.  Each looking wavefront joins kSides tiles, the first one joins what they found; a group's last
+    // tile tells the state that enters the next group.  What is joined with what goes by a tile's number alone, never by
+    // which state was known first, so that results are the same from call to call.
     __device__ __forceinline__ void behind(const Place<T, V> &p, const Scan &s, float (&state)[V]) {
         __shared__ Effect lds[kWaves][V][kLanes];
         __shared__ float lds_state[V][kLanes];
-        __shared__ int lds_known;
         const int64_t tile = BACK ? s.tiles - 1 - p.tile : p.tile;          // in the order of the chain
-        const bool tells = p.run == 0 && p.live && tile + 1 < s.tiles;
-        if (tells) {
+        const uint32_t size = (uint32_t)(s.lookers * kSides), group = (uint32_t)tile / size;
+        const int64_t first = (int64_t)group * size;
+        const bool tells = p.run == 0 && p.live && tile + 1 < s.tiles, ends = tile + 1 == first + size;
+        if (tells && !ends) {
 #pragma unroll
-            for (int k = 0; k < V; k++) {
-                const Effect all = whole(p, k);
-                publish(p.word(s, p.tile) + k, {tile ? all.A : -1.0f, all.H});
-            }
+            for (int k = 0; k < V; k++) publish(p.word(s, p.tile) + k, whole(p, k));
         }
         if (tile == 0) {
 #pragma unroll
             for (int k = 0; k < V; k++) state[k] = 0.0f;
             return;
         }
-        Effect all[V];                   // (the first wavefront's)
+        const bool asks = group > 0 && p.run == 0 && p.live;
+        uint64_t w_group[V];
 #pragma unroll
-        for (int k = 0; k < V; k++) all[k] = {1.0f, 0.0f};
-        for (int64_t near = tile - 1;; near -= s.lookers * kSides) {
-            if (p.wave < s.lookers) {
-                const int64_t of = near - p.run;
-                const bool there = of >= 0 && p.live;
-                const uint64_t *at = p.word(s, there ? BACK ? s.tiles - 1 - of : of : p.tile);
-                const int here = threadIdx.x & (kWave - 1);
-                uint64_t w[V];
+        for (int k = 0; k < V; k++) w_group[k] = asks ? look(p.word(s, s.tiles + group) + k) : 0;
+        if (p.wave < s.lookers) {
+            const int64_t of = tile - 1 - p.run;
+            const bool there = of >= first && p.live;
+            const uint64_t *at = p.word(s, there ? BACK ? s.tiles - 1 - of : of : p.tile);
+            const int here = threadIdx.x & (kWave - 1);
+            uint64_t w[V];
 #pragma unroll
-                for (int k = 0; k < V; k++) w[k] = there ? look(at + k) : 0;
+            for (int k = 0; k < V; k++) w[k] = there ? look(at + k) : 0;
 #pragma unroll
-                for (int k = 0; k < V; k++) {
-                    while (w[k] == kNotYet) w[k] = look(at + k);
-                    Effect e = there ? effect_of(w[k]) : Effect{-1.0f, 0.0f};
+            for (int k = 0; k < V; k++) {
+                while (w[k] == kNotYet) w[k] = look(at + k);
+                Effect e = there ? effect_of(w[k]) : Effect{1.0f, 0.0f};
 #pragma unroll
-                    for (int d = 1; d < kSides; d <<= 1) {
-                        const Effect o = {__shfl(e.A, here + d * kLanes), __shfl(e.H, here + d * kLanes)};
-                        e = then(o, e);          // (of side 0, in the end, all sides)
-                    }
-                    if (p.side == 0) lds[p.wave][k][p.lane] = e;
+                for (int d = 1; d < kSides; d <<= 1) {
+                    const Effect o = {__shfl(e.A, here + d * kLanes), __shfl(e.H, here + d * kLanes)};
+                    e = then(o, e);          // (of side 0, in the end, all sides)
                 }
+                if (p.side == 0) lds[p.wave][k][p.lane] = e;
             }
-            __syncthreads();
-            if (p.wave == 0) {
-                bool known = false;
-                for (int q = 0; q < s.lookers && !known; q++) {
-                    known = true;
-#pragma unroll
-                    for (int k = 0; k < V; k++) {
-                        all[k] = then(lds[q][k][p.lane], all[k]);
-                        known &= all[k].A < 0;
-                    }
-                    known = __all(known);
-                }
-                if (known && tells) {
-#pragma unroll
-                    for (int k = 0; k < V; k++) publish(p.word(s, p.tile) + k, {-1.0f, whole(p, k).of(all[k].H)});
-                }
-                if (p.side == 0) {
-#pragma unroll
-                    for (int k = 0; k < V; k++) lds_state[k][p.lane] = all[k].H;
-                }
-                if (threadIdx.x == 0) lds_known = known;
-            }
-            __syncthreads();
-            if (lds_known) break;
         }
+        __syncthreads();
+        if (p.run == 0) {
+#pragma unroll
+            for (int k = 0; k < V; k++) {
+                Effect all = {1.0f, 0.0f};
+                for (int q = 0; q < s.lookers; q++) all = then(lds[q][k][p.lane], all);
+                while (w_group[k] == kNotYet) w_group[k] = look(p.word(s, s.tiles + group) + k);
+                const float enters = asks ? all.of(effect_of(w_group[k]).H) : all.H;
+                if (tells && ends) publish(p.word(s, s.tiles + group + 1) + k, {-1.0f, whole(p, k).of(enters)});
+                lds_state[k][p.lane] = enters;
+            }
+        }
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < V; k++) state[k] = lds_state[k][p.lane];
     }
@@ -721,15 +710,17 @@ int64_t tiles_of(int64_t rows, bool backward) {
     return std::max<int64_t>(1, (rows + tile - 1) / tile);
 }
 
-// A ticket, and an effect for each tile and channel, channels counted up to whole strips of the narrower types' lanes
+// A ticket, and an effect for each tile and each group of two tiles or more, and channel, channels counted up to whole strips
+// of the narrower types' lanes
+int64_t words_of(int64_t tiles, int64_t group) { return tiles + (tiles + group - 1) / group; }
 size_t words_bytes(int64_t rows, int32_t width, bool backward) {
     constexpr size_t strip = Shape<bf16>::kLanes * kWide;
-    return kPolicyAlign + align_up(tiles_of(rows, backward) * ((width + strip - 1) / strip * strip) * sizeof(uint64_t));
+    return kPolicyAlign + align_up(words_of(tiles_of(rows, backward), 2) * ((width + strip - 1) / strip * strip) * sizeof(uint64_t));
 }
 size_t part_bytes(int64_t rows, int32_t width) { return align_up((size_t)tiles_of(rows, true) * width * sizeof(float)); }
 
-// Wavefronts that look back.  The chain of states passes as many tiles a round as are looked at; the fewer strips there are,
-// the more tiles of each are under way at once, and the faster it has to be.
+// Wavefronts that look back, kSides tiles each: a group.  The chain of states passes from group to group; the fewer strips
+// there are, the more tiles of each are under way at once, and the faster it has to be.
 int lookers_of(int32_t strips) { return std::max(1, std::min(kWaves, 32 / strips)); }
 
 void split_over(Scan &s, bool backward, int strip, void *workspace) {
@@ -740,8 +731,8 @@ void split_over(Scan &s, bool backward, int strip, void *workspace) {
     s.words = s.tiles > 1 ? (uint64_t *)((char *)workspace + kPolicyAlign) : nullptr;
 }
 
-void clear_words(const Scan &s, int strip, hipStream_t stream) {
-    const int64_t count = s.tiles * s.strips * strip;
+void clear_words(const Scan &s, int strip, int sides, hipStream_t stream) {
+    const int64_t count = words_of(s.tiles, s.lookers * sides) * s.strips * strip;
     hipLaunchKernelGGL(clear_words_kernel, dim3((unsigned)std::min<int64_t>((count + 255) / 256, 2048)), dim3(256), 0, stream, s.ticket, s.words, count);
 }
 
@@ -771,6 +762,7 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
         if (!workspace) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < words_bytes(rows, width, false)) return CP_ERR_WORKSPACE;
     }
+    if (rows < 2) ldf = ldx = ldh = width;         // (a single row is no distance from another)
     Scan s{};
     s.seq = {seq_ptr, rows, rows / num_seq, num_seq, reverse != 0};
     s.width = width;
@@ -784,7 +776,7 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
             split_over(s, false, strip, workspace);
             auto *kernel = (size_t)rows * width * sizeof(T) > kStreamed ? scan_kernel<T, V, true> : scan_kernel<T, V, false>;
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
-            if (s.ticket) clear_words(s, strip, st);
+            if (s.ticket) clear_words(s, strip, Shape<T>::kSides, st);
             hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
                                seq_ptr ? status_out : nullptr);
             return launched();
@@ -808,6 +800,7 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
         if (!workspace) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < words_bytes(rows, width, true) + part_bytes(rows, width)) return CP_ERR_WORKSPACE;
     }
+    if (rows < 2) lddh = ldf = ldx = lddf = lddx = width;
     float *part = dbias ? (float *)((char *)workspace + words_bytes(rows, width, true)) : nullptr;
     Scan s{};
     s.seq = {seq_ptr, rows, rows / num_seq, num_seq, reverse != 0};
@@ -822,7 +815,7 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
             split_over(s, true, strip, workspace);
             auto *kernel = 2 * (size_t)rows * width * sizeof(T) > kStreamed ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>;
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
-            if (s.ticket) clear_words(s, strip, st);
+            if (s.ticket) clear_words(s, strip, Shape<T>::kSides, st);
             hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
                                Gradient<T>{(const T *)dh, lddh, dlast, carry, (T *)df, (T *)dx, lddf, lddx, part, dh0}, seq_ptr ? status_out : nullptr);
             if (dbias)

@@ -728,8 +728,7 @@ template <typename F>
 int by_loads(int nv, F f) {
     if (nv == 1) return f(std::integral_constant<int, 1>{});
     if (nv == 2) return f(std::integral_constant<int, 2>{});
-    if (nv == 4) return f(std::integral_constant<int, 4>{});
-    return f(std::integral_constant<int, 8>{});
+    return f(std::integral_constant<int, kMostLoads>{});
 }
 
 // f(a value of the tokens' type, lanes a row, places a lane).  Lanes: as many as there are places, and with many tokens, of
@@ -856,7 +855,7 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
                 return launched();
             });
         constexpr int V = 16 / sizeof(T);
-        const int nv = std::min(loads_of(rows, vocab, V), 4);
+        const int nv = loads_of(rows, vocab, V);
         const int32_t slices = slices_of(vocab, V, nv);
         if (rows * slices > INT32_MAX) return (int)CP_ERR_SIZE;
         return by_loads(nv, [&](auto n) {

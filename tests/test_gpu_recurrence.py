@@ -224,3 +224,23 @@ def test_on_another_stream_and_in_a_graph():
         assert torch.equal(a["h"], e["h"]) and torch.equal(b["df"], eb["df"]) and torch.equal(b["dbias"], eb["dbias"])
         if turn % 2 == 0:
             assert torch.equal(e["h"], want["h"]) and torch.equal(eb["dbias"], grad["dbias"])
+
+
+@pytest.mark.parametrize("rows,width,kind,reverse", [(20011, 34, "bf16", False), (9999, 7, "fp32", True), (16384, 1, "fp16", False)])
+def test_sequences_of_many_tiles(rows, width, kind, reverse):
+    # (more tiles than a group of them has)
+    cuts = [0, rows // 2 + 3, rows // 2 + 3, rows - 5, rows]
+    compare(make(rows, width, kind, seqs=4), cuts, reverse, True, kind, f"{rows} x {width} {kind}, four sequences")
+    compare(make(rows, width, kind, seed=1), [0, rows], reverse, False, kind, f"{rows} x {width} {kind}, one sequence")
+
+
+def test_results_do_not_depend_on_the_order_of_workgroups():
+    d = make(150000, 96, "fp32", h0=False)
+    kw = dict(bias=d["bias"], want_carry=True, want_last=True)
+    one = cpe.cp_recurrence(d["f"], d["x"], **kw)
+    grad = cpe.cp_recurrence_backward(d["dh"], d["f"], d["x"], one["carry"], bias=d["bias"])
+    for _ in range(5):
+        again = cpe.cp_recurrence(d["f"], d["x"], **kw)
+        assert all(torch.equal(again[k], one[k]) for k in ("h", "last", "carry"))
+        back = cpe.cp_recurrence_backward(d["dh"], d["f"], d["x"], again["carry"], bias=d["bias"])
+        assert all(torch.equal(back[k], grad[k]) for k in ("df", "dx", "dbias"))
