@@ -33,6 +33,16 @@ struct Joint {
     float *stats;            // [2][rows]: 1 / rms of y and of r
 };
 
+// Rows: NT threads take one at a time.  Of NT below a wavefront's 64 lanes several rows lie side by side in a workgroup, which
+// is one wavefront: 405303 rows of 70 fp16 values, 9 of 64 lanes having some, took 397 us forward and backward.
+template <int NT>
+struct Sharing {
+    static constexpr int kSide = NT < kWave ? kWave / NT : 1, kThreads = NT < kWave ? kWave : NT;
+    static __device__ __forceinline__ int thread() { return NT < kWave ? threadIdx.x & (NT - 1) : threadIdx.x; }
+    static __device__ __forceinline__ int64_t first() { return NT < kWave ? (int64_t)blockIdx.x * kSide + threadIdx.x / NT : blockIdx.x; }
+    static __device__ __forceinline__ int64_t step() { return (int64_t)gridDim.x * kSide; }
+};
+
 // Where a thread's values lie: NV vectors of V.  The last vector of a row that is no multiple of V is the row's last V
 // values; those that are another vector's are `skip`ped in sums (and written twice, to the same).
 template <int NT, int V, int NV>
@@ -42,7 +52,7 @@ struct Columns {
     __device__ __forceinline__ Columns(int32_t width) {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int32_t first = (i * NT + (int32_t)threadIdx.x) * V;
+            const int32_t first = (i * NT + Sharing<NT>::thread()) * V;
             live[i] = first < width;
             c[i] = live[i] ? min(first, width - V) : 0;
             skip[i] = live[i] ? first - c[i] : V;
@@ -64,10 +74,15 @@ __device__ __forceinline__ void load_weights(float (&to)[V], const void *w, int 
     else from(f16{});
 }
 
-// Sum over a workgroup, in every thread.  `slot`: no two sums between which no other lies may have the same (a slow wavefront
+// Sum over a row's threads, in every one of them.  `slot`: no two sums between which no other lies may have the same (a slow wavefront
 // may still read what the last one left).
 template <int NT>
 __device__ __forceinline__ float group_sum(float v, int slot) {
+    if constexpr (NT < kWave) {
+#pragma unroll
+        for (int off = NT / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
+        return v;
+    }
     v = wave_sum(v);
     if constexpr (NT > kWave) {
         __shared__ float lds[4][NT / kWave];
@@ -94,7 +109,7 @@ __device__ __forceinline__ void gate_of(float g, int act, float &value, float &s
 
 // TS: the stream's type (x, r, dx, dr), TB: the block's (y, gate, z and their gradients)
 template <typename TS, typename TB, int NT, int V, int NV>
-__global__ __launch_bounds__(NT) void joint_kernel(Joint j, TS *r_out, int64_t ldr, TB *z_out, int64_t ldz) {
+__global__ __launch_bounds__(Sharing<NT>::kThreads) void joint_kernel(Joint j, TS *r_out, int64_t ldr, TB *z_out, int64_t ldz) {
     const Columns<NT, V, NV> at(j.width);
     const float inv = 1.0f / j.width;
     float w_pre[NV][V], w_post[NV][V];
@@ -107,7 +122,7 @@ __global__ __launch_bounds__(NT) void joint_kernel(Joint j, TS *r_out, int64_t l
             for (int k = 0; k < V; k++) w_post[i][k] = 1.0f;
     }
     int slot = 0;
-    for (int64_t row = blockIdx.x; row < j.rows; row += gridDim.x, slot ^= 2) {
+    for (int64_t row = Sharing<NT>::first(); row < j.rows; row += Sharing<NT>::step(), slot ^= 2) {
         Raw<TS, V> x[NV];
         Raw<TB, V> y[NV], g[NV];
 #pragma unroll
@@ -150,7 +165,7 @@ __global__ __launch_bounds__(NT) void joint_kernel(Joint j, TS *r_out, int64_t l
             for (int k = 0; k < V; k++) out.v[k] = (TB)(r[i][k] * rr * w_pre[i][k]);
             if (at.live[i]) store_pack<TB, V>(z_out + row * ldz + at.c[i], out);
         }
-        if (j.stats && threadIdx.x == 0) {
+        if (j.stats && Sharing<NT>::thread() == 0) {
             j.stats[row] = ry;
             j.stats[j.rows + row] = rr;
         }
@@ -168,7 +183,7 @@ struct JointGrad {
 };
 
 template <typename TS, typename TB, int NT, int V, int NV>
-__global__ __launch_bounds__(NT) void joint_backward_kernel(Joint j, JointGrad<TS, TB> b) {
+__global__ __launch_bounds__(Sharing<NT>::kThreads) void joint_backward_kernel(Joint j, JointGrad<TS, TB> b) {
     const Columns<NT, V, NV> at(j.width);
     const float inv = 1.0f / j.width;
     // (the longest rows leave no registers for weights and sums: these are kept in LDS, those loaded again for every row)
@@ -191,7 +206,7 @@ __global__ __launch_bounds__(NT) void joint_backward_kernel(Joint j, JointGrad<T
         for (int k = 0; k < V; k++) pre(i, k) = post(i, k) = 0.0f;
     }
     int slot = 0;
-    for (int64_t row = blockIdx.x; row < j.rows; row += gridDim.x, slot ^= 2) {
+    for (int64_t row = Sharing<NT>::first(); row < j.rows; row += Sharing<NT>::step(), slot ^= 2) {
         const float ry = j.w_post ? j.stats[row] : 1.0f, rr = j.stats[j.rows + row];
         Raw<TS, V> x[NV], d[NV];
         Raw<TB, V> y[NV], g[NV], e[NV];
@@ -257,6 +272,16 @@ __global__ __launch_bounds__(NT) void joint_backward_kernel(Joint j, JointGrad<T
             if (at.live[i]) store_pack<TB, V>(b.dy + row * b.lddy + at.c[i], oy);
         }
     }
+    if constexpr (NT < kWave) {          // the rows side by side
+#pragma unroll
+        for (int k = 0; k < V; k++)
+#pragma unroll
+            for (int off = NT; off < kWave; off <<= 1) {
+                pre(0, k) += __shfl_xor(pre(0, k), off);
+                post(0, k) += __shfl_xor(post(0, k), off);
+            }
+        if (threadIdx.x >= NT) return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
         if (!at.live[i]) continue;
@@ -296,37 +321,40 @@ __global__ __launch_bounds__(1024) void weight_sum_kernel(WeightSum pre, WeightS
 
 constexpr int kMostWaves = 16 * 256;         // that go over rows at once: what registers leave room for on 256 compute units
 
-// Calls f(threads, values a load, loads a thread) for the smallest workgroup that holds a row.  16 bytes a load, of the wider
+// Calls f(threads, values a load, loads a thread) for the fewest threads that hold a row.  16 bytes a load, of the wider
 // of the two types; a thread holds at most 16 values, so that a workgroup's registers leave room for others.
 template <int WIDE, typename F>
 int by_shape(int32_t width, F f) {
-    auto of = [&](auto v) {
-        constexpr int V = decltype(v)::value, MOST = V == 1 ? 1 : 16 / V;
-        using std::integral_constant;
-        auto go = [&](auto nt, auto nv) { return f(nt, v, nv); };
-        if (width <= 64 * V) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-        if constexpr (V > 1) {
-            if (width <= 128 * V) return go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
-            if (width <= 256 * V) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-            if (width <= 512 * V) return go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
-            if (width <= 1024 * V) return go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
-            if (width <= 2048 * V) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-            return go(integral_constant<int, 1024>{}, integral_constant<int, MOST>{});
-        }
-        return (int)CP_ERR_SIZE;
-    };
-    if (width >= WIDE) return of(std::integral_constant<int, WIDE>{});
-    return of(std::integral_constant<int, 1>{});
+    using std::integral_constant;
+    if (width < WIDE) return f(integral_constant<int, 8>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    auto go = [&](auto nt, auto nv) { return f(nt, integral_constant<int, WIDE>{}, nv); };
+    auto one = integral_constant<int, 1>{};
+    if (width <= 8 * WIDE) return go(integral_constant<int, 8>{}, one);
+    if (width <= 16 * WIDE) return go(integral_constant<int, 16>{}, one);
+    if (width <= 32 * WIDE) return go(integral_constant<int, 32>{}, one);
+    if (width <= 64 * WIDE) return go(integral_constant<int, 64>{}, one);
+    if (width <= 128 * WIDE) return go(integral_constant<int, 128>{}, one);
+    if (width <= 256 * WIDE) return go(integral_constant<int, 256>{}, one);
+    if (width <= 512 * WIDE) return go(integral_constant<int, 512>{}, one);
+    if (width <= 1024 * WIDE) return go(integral_constant<int, 1024>{}, one);
+    if (width <= 2048 * WIDE) return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    if constexpr (2048 * WIDE < CP_NORM_MAX_WIDTH) return go(integral_constant<int, 1024>{}, integral_constant<int, 16 / WIDE>{});
+    return (int)CP_ERR_SIZE;
 }
 static_assert(1024 * 16 >= CP_NORM_MAX_WIDTH, "the largest workgroup holds the longest row");
 
-// threads of the workgroup that by_shape takes
-int shape_threads(int wide, int32_t width) {
-    int nt = 64;
+// Workgroups that go over rows.  (Threads of a row: as by_shape takes them.)
+int groups_of(int64_t rows, int32_t width, int wide) {
+    int nt = 8;
     while (nt < 1024 && width > nt * wide) nt *= 2;
-    return nt;
+    if (nt < kWave) return (int)std::min<int64_t>((rows + kWave / nt - 1) / (kWave / nt), kMostWaves);
+    return (int)std::min<int64_t>(rows, kMostWaves / (nt / kWave));
 }
-int groups_of(int64_t rows, int32_t width, int wide) { return (int)std::min<int64_t>(rows, kMostWaves / (shape_threads(wide, width) / kWave)); }
+
+// a workspace's half: the sums of as many workgroups as any pair of types makes
+size_t part_bytes(int64_t rows, int32_t width) {
+    return align_up((size_t)std::max(groups_of(rows, width, 8), groups_of(rows, width, 4)) * width * sizeof(float));
+}
 
 int check_joint(int64_t rows, int32_t width, int stream_type, int type, int weight_type, int act) {
     if (!known_type(stream_type) || !known_type(type) || !known_type(weight_type)) return CP_ERR_ARG;
@@ -367,8 +395,9 @@ int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int wei
         using TB = decltype(tb);
         return by_shape<16 / sizeof(TS)>(width, [&](auto nt, auto v, auto nv) {
             constexpr int NT = decltype(nt)::value, V = decltype(v)::value, NV = decltype(nv)::value;
+            constexpr int side = Sharing<NT>::kSide;
             const int groups = groups_of(rows, width, 16 / sizeof(TS)) * 2;
-            hipLaunchKernelGGL((joint_kernel<TS, TB, NT, V, NV>), dim3((unsigned)std::min<int64_t>(rows, groups)), dim3(NT), 0,
+            hipLaunchKernelGGL((joint_kernel<TS, TB, NT, V, NV>), dim3((unsigned)std::min<int64_t>((rows + side - 1) / side, groups)), dim3(Sharing<NT>::kThreads), 0,
                                (hipStream_t)stream, j, (TS *)r, ldr, (TB *)z, ldz);
             return launched();
         });
@@ -378,7 +407,7 @@ int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int wei
 int cp_norm_gate_backward_workspace_bytes(int64_t rows, int32_t width, size_t *out_bytes) {
     if (!out_bytes) return CP_ERR_NULL;
     if (rows < 0 || width < 1 || width > CP_NORM_MAX_WIDTH) return CP_ERR_SIZE;
-    *out_bytes = 2 * align_up((size_t)groups_of(rows, width, 8) * width * sizeof(float));
+    *out_bytes = 2 * part_bytes(rows, width);
     return CP_OK;
 }
 
@@ -395,7 +424,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
     if (rows > 1 && ((dr && lddr < width) || lddz < width || ldx < width || (y && (ldy < width || lddy < width)) || (gate && ldg < width) ||
                      (dgate && lddg < width) || lddx < width))
         return CP_ERR_SIZE;
-    const size_t one = align_up((size_t)groups_of(rows, width, 8) * width * sizeof(float));
+    const size_t one = part_bytes(rows, width);
     if (dw_pre || dw_post) {
         if (!workspace && rows > 0) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < 2 * one) return CP_ERR_WORKSPACE;
@@ -418,7 +447,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
                 auto *kernel = joint_backward_kernel<TS, TB, NT, V, NV>;
                 if (lds && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
                     return (int)CP_ERR_HIP;
-                hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(NT), lds, st, j, b);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(Sharing<NT>::kThreads), lds, st, j, b);
                 return launched();
             });
         });

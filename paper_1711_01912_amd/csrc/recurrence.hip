@@ -801,7 +801,9 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < words_bytes(rows, width, true) + part_bytes(rows, width)) return CP_ERR_WORKSPACE;
     }
     if (rows < 2) lddh = ldf = ldx = lddf = lddx = width;
-    float *part = dbias ? (float *)((char *)workspace + words_bytes(rows, width, true)) : nullptr;
+    // (the sums of a single tile are the whole sums)
+    const bool alone = tiles_of(rows, true) == 1;
+    float *part = !dbias || alone ? dbias : (float *)((char *)workspace + words_bytes(rows, width, true));
     Scan s{};
     s.seq = {seq_ptr, rows, rows / num_seq, num_seq, reverse != 0};
     s.width = width;
@@ -818,7 +820,7 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
             if (s.ticket) clear_words(s, strip, Shape<T>::kSides, st);
             hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
                                Gradient<T>{(const T *)dh, lddh, dlast, carry, (T *)df, (T *)dx, lddf, lddx, part, dh0}, seq_ptr ? status_out : nullptr);
-            if (dbias)
+            if (dbias && !alone)
                 hipLaunchKernelGGL(column_sum_kernel, dim3((width + 15) / 16), dim3(1024), 0, st, part, s.tiles, width, dbias);
             return launched();
         };

@@ -203,27 +203,37 @@ struct Slice {
     }
 };
 
-// The best places of a slice.  `own`: the thread's largest logit.  A fourth of K of the threads of each of the four wavefronts
-// have one at or above `bound`, so that K places do, and those that do, few more than K, are all that is put in order.
-// Where too many do (ties), the best are taken one by one, from memory.
-constexpr int kPool = 512;
-template <typename T, int V, int NV, typename F>
-__device__ __forceinline__ void slice_top(const Rows &r, int64_t row, Slice<T, V, NV> &in, float own, int top, F put) {
-    __shared__ uint64_t lds_pool[kPool], lds_key[2][kWaves];
-    __shared__ uint32_t lds_bound[kWaves];
-    __shared__ int lds_count;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, share = (top + kWaves - 1) / kWaves;
-    const uint32_t key = own > kNone ? value_key(own) : 0;
-    uint32_t bound = 0;                  // the share-th largest of the wavefront's: bit by bit, from the highest
+// A bound that at least `top` of a workgroup's value keys reach, and few more: `key` is the largest of each thread's.  Of each
+// wavefront whose threads all have some, a share of `top` (together: `top`) reach the share-th largest of theirs, found bit
+// by bit, and the lowest of these counts.  (A wavefront without any would leave no bound: 5250 rows of 1401 bf16, the 20 best
+// of each, took 146 us so.)  `threads`: so many have some.
+__device__ __forceinline__ uint32_t bound_of(uint32_t key, int top, int threads) {
+    __shared__ uint32_t lds[kWaves];
+    const int full = max(1, min(kWaves, threads / kWave)), share = (top + full - 1) / full;
+    uint32_t bound = 0;
 #pragma unroll
     for (int bit = 31; bit >= 0; bit--) {
         const uint32_t more = bound | 1u << bit;
         bound = __popcll(__ballot(key >= more)) >= share ? more : bound;
     }
-    if (lane == 0) lds_bound[wave] = bound;
-    if (threadIdx.x == 0) lds_count = 0;
+    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = bound;
     __syncthreads();
-    bound = max(min(min(lds_bound[0], lds_bound[1]), min(lds_bound[2], lds_bound[3])), kNoneKey + 1);
+    bound = lds[0];
+    for (int w = 1; w < full; w++) bound = min(bound, lds[w]);
+    return max(bound, kNoneKey + 1);
+}
+
+// The best places of a slice.  `own`: the thread's largest logit.  Those at or above the bound are all that is put in order.
+// Where too many are (ties), the best are taken one by one, from memory.
+constexpr int kPool = 512;
+template <typename T, int V, int NV, typename F>
+__device__ __forceinline__ void slice_top(const Rows &r, int64_t row, Slice<T, V, NV> &in, float own, int top, F put) {
+    __shared__ uint64_t lds_pool[kPool], lds_key[2][kWaves];
+    __shared__ int lds_count;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const uint32_t key = own > kNone ? value_key(own) : 0;
+    if (threadIdx.x == 0) lds_count = 0;
+    const uint32_t bound = bound_of(key, top, (r.vocab - in.v0) / V);
     if (key >= bound) {
         const float low = key_value((uint64_t)bound << 32);
 #pragma unroll
@@ -315,8 +325,7 @@ __global__ __launch_bounds__(kThreads, 4) void slice_kernel(Rows r, Tokens tok, 
     }
 }
 
-// A row's slices joined, in their order.  Of their best places those count that no slice's worst of its best lies above: the
-// worst of one slice's best is a bound for the row's.
+// A row's slices joined, in their order, and the best of their best places.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void join_kernel(Rows r, Tokens tok, Results out, int32_t slices, const Part *parts, const uint64_t *best) {
     __shared__ Part lds_part;
@@ -340,23 +349,18 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Rows r, Tokens tok, Resu
     }
     const int64_t count = (int64_t)slices * out.top;
     const uint64_t *keys = best + row * count;
-    uint64_t bound = 0;
+    uint32_t bound = 0;
     if (out.top) {
-        for (int32_t i = threadIdx.x; i < slices; i += kThreads) {
-            const uint64_t worst = keys[(int64_t)i * out.top + out.top - 1];
-            bound = worst > bound ? worst : bound;
-        }
-        bound = most<kWave>(bound);
-        if (lane == 0) lds_key[wave] = bound;
+        for (int64_t i = threadIdx.x; i < count; i += kThreads) bound = max(bound, (uint32_t)(keys[i] >> 32));
+        bound = bound_of(bound, out.top, (int)min(count, (int64_t)kThreads));
     }
     __syncthreads();
     const Part all = lds_part;
     write_tokens<T>(r, tok, out, row, all);
     if (!out.top) return;
-    for (int w = 0; w < kWaves; w++) bound = lds_key[w] > bound ? lds_key[w] : bound;
     for (int64_t i = threadIdx.x; i < count; i += kThreads) {
         const uint64_t key = keys[i];
-        if (key == 0 || key < bound) continue;
+        if ((uint32_t)(key >> 32) < bound) continue;
         const int at = atomicAdd(&lds_count, 1);
         if (at < kPool) lds_pool[at] = key;
     }
@@ -606,11 +610,12 @@ __global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Re
 
 // COLUMNS: many tokens a row are summed by place in LDS, each lane in columns of its own (so that the order of the sums is
 // fixed), kSets of them, so that as many sums are under way at once, and the row's columns added up; else every lane looks
-// through all of the row's tokens for its own places.
+// through all of the row's tokens for its own places.  `used` (a power of two): of the row's L lanes those that have
+// tokens; only their columns are cleared and added up.
 constexpr int kSets = 4;
 
 template <typename T, typename I, int L, int E, bool COLUMNS>
-__global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo) {
+__global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int used) {
     static_assert(!COLUMNS || E == 1, "a lane a place");
     extern __shared__ float lds_columns[];       // COLUMNS: [kWaves][vocab][SETS][kWave + 1]
     constexpr int SETS = L <= 16 ? kSets : 1;
@@ -633,7 +638,11 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
         }
         few_logits<T, L, E>(soon, r, min(row0 + step + group, r.rows - 1), here);
         if constexpr (COLUMNS) {
-            for (int v = 0; v < r.vocab * SETS; v++) columns[v * (kWave + 1) + lane] = 0.0f;
+            const int log_used = __builtin_ctz(used);
+            for (int i = here; i < r.vocab * SETS * used; i += L) columns[(i >> log_used) * (kWave + 1) + group * L + (i & (used - 1))] = 0.0f;
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * L * 4) {
                 Four<I> four[kAhead];
                 Pack<float, 4> w[kAhead];
@@ -670,9 +679,15 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             const float *mine = columns + min(here, r.vocab - 1) * (SETS * (kWave + 1)) + group * L;
 #pragma unroll
-            for (int q = 0; q < SETS; q++)
+            for (int q = 0; q < SETS; q++) {
+                if (used == L) {
 #pragma unroll
-                for (int j = 0; j < L; j++) hits[0] += mine[q * (kWave + 1) + j];
+                    for (int j = 0; j < L; j++) hits[0] += mine[q * (kWave + 1) + j];
+                } else {
+#pragma unroll 4
+                    for (int j = 0; j < used; j++) hits[0] += mine[q * (kWave + 1) + j];
+                }
+            }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
         } else {
@@ -842,15 +857,17 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
             return by_lanes(tok, vocab, given >= 32 ? 8 : 4, [&](auto i, auto l, auto e) {
                 constexpr int L = decltype(l)::value, E = decltype(e)::value, side = kWaves * kWave / L;
                 const dim3 grid((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8));
+                int used = 1;
+                while (used < L && used * 4 < given) used *= 2;
                 if (E == 1 && given >= kColumns) {
                     const size_t lds = (size_t)kWaves * vocab * (L <= 16 ? kSets : 1) * (kWave + 1) * sizeof(float);
                     auto *kernel = few_gradient_kernel<T, decltype(i), L, E, E == 1>;
                     if (lds > 48 * 1024 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
                         return (int)CP_ERR_HIP;
-                    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd);
+                    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd, used);
                 } else {
                     hipLaunchKernelGGL((few_gradient_kernel<T, decltype(i), L, E, false>), grid, dim3(kThreads), 0, st, r, tok, stats, d,
-                                       (T *)dlogits, ldd);
+                                       (T *)dlogits, ldd, used);
                 }
                 return launched();
             });

@@ -9,7 +9,7 @@ Matrices may be views whose rows are further apart than their length (slices of 
 projection), as long as a row's elements are contiguous.  ``out`` may carry preallocated outputs
 under the keys of the result, ``workspace`` a preallocated uint8 tensor.
 
-``autograd`` has the same operators as differentiable functions.
+The submodule ``autograd`` has the same operators as differentiable functions.
 """
 from __future__ import annotations
 
@@ -43,13 +43,14 @@ def _matrix(t, name, rows, width, dtype, device):
     """The distance between the rows of a [rows][width] (or [batch][rows / batch][width]) tensor."""
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype}, not {t.dtype}")
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
     if shape[-1] != width or t.numel() != rows * width:
         raise ValueError(f"{name}: shape {tuple(shape)} does not fit {rows} rows of {width}")
-    if t.numel() == 0:
+    if t.is_contiguous():
         return width
+    stride = t.stride()
     if width > 1 and stride[-1] != 1:
         raise ValueError(f"{name}: the elements of a row have to be contiguous (strides {tuple(stride)})")
     if len(shape) == 3 and shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
@@ -68,10 +69,10 @@ def _vector(t, name, shape, dtype, device):
         return None
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype}, not {t.dtype}")
-    if tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous tensor of shape {shape}, not {tuple(t.shape)}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor of shape {tuple(shape)}, not {tuple(t.shape)}")
     return t.data_ptr()
 
 
@@ -88,16 +89,44 @@ def _other(device, stream):
         yield
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _place(device, stream):
     """What to allocate and launch under, and the stream's handle."""
     import torch
     if stream is None and device.index == torch.cuda.current_device():
-        return contextlib.nullcontext(), torch.cuda.current_stream().cuda_stream
+        # (the handle alone: a stream object takes 3 us, as long as the launch of a step)
+        return _HERE, torch._C._cuda_getCurrentRawStream(device.index)
     if stream is None:
         stream = torch.cuda.current_stream(device)
     elif stream.device != device:
         raise ValueError(f"the stream is {stream.device}'s, the tensors are on {device}")
     return _other(device, stream), stream.cuda_stream
+
+
+def _rows_out(out, key, like, device, dtype=None):
+    """out[key], rows as `like`'s of its type or that, made if it is not there: its address and the rows' distance."""
+    import torch
+    t = out.get(key)
+    if t is not None:
+        return t.data_ptr(), _matrix(t, key, like.numel() // max(like.shape[-1], 1), like.shape[-1], dtype or like.dtype, device)
+    if dtype is None and like.is_contiguous():
+        t = torch.empty_like(like)
+    else:
+        t = torch.empty(like.shape, dtype=dtype or like.dtype, device=device)
+    out[key] = t
+    return t.data_ptr(), like.shape[-1]
+
+
+def _vector_out(out, key, shape, dtype, device):
+    """out[key], contiguous, made if it is not there: its address."""
+    import torch
+    t = out.get(key)
+    if t is not None:
+        return _vector(t, key, shape, dtype, device)
+    t = out[key] = torch.empty(shape, dtype=dtype, device=device)
+    return t.data_ptr()
 
 
 @functools.lru_cache(maxsize=4096)
@@ -109,17 +138,17 @@ def _need(entry, *sizes):
     return int(out.value)
 
 
-def _work(workspace, need, device):
+def _room(workspace, need, device):
+    """(the workspace or a new one, which has to live until the call is made; its address and size)"""
     import torch
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=device) if need else None
+        if not need:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), need
     if workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace: a contiguous uint8 tensor on the device of the inputs")
-    return workspace
-
-
-def _room(work):
-    return (None, 0) if work is None else (work.data_ptr(), work.numel())
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
 def _check(status, flag, text, device):
@@ -168,20 +197,14 @@ def cp_recurrence(f, x, *, bias=None, seq_ptr=None, h0=None, reverse=False, want
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        if "h" not in out:
-            out["h"] = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        if want_last and "last" not in out:
-            out["last"] = torch.empty((count, width), dtype=f32, device=dev)
-        if want_carry and "carry" not in out:
-            out["carry"] = torch.empty((-(-rows // RECURRENCE_CHUNK), width), dtype=f32, device=dev)
-        if ptr is not None and "status" not in out:
-            out["status"] = torch.empty(1, dtype=torch.int32, device=dev)
-        work = _work(workspace, _need("cp_recurrence_workspace_bytes", rows, width, 0) if rows > RECURRENCE_CHUNK else 0, dev)
-        ldh = _matrix(out["h"], "h", rows, width, f.dtype, dev)
+        h_at, ldh = _rows_out(out, "h", x, dev)
+        last_at = _vector_out(out, "last", (count, width), f32, dev) if want_last or "last" in out else None
+        carry_at = _vector_out(out, "carry", (-(-rows // RECURRENCE_CHUNK), width), f32, dev) if want_carry or "carry" in out else None
+        status_at = _vector_out(out, "status", (1,), torch.int32, dev) if ptr is not None else None
+        need = _need("cp_recurrence_workspace_bytes", rows, width, 0) if rows > RECURRENCE_CHUNK else 0
+        work, work_at, room = _room(workspace, need, dev)
         rc = lib.cp_recurrence(rows, width, count, ptr, kind, int(bool(reverse)), f.data_ptr(), ldf, x.data_ptr(), ldx, bias_at,
-                               h0_at, out["h"].data_ptr(), ldh, _vector(out.get("last"), "last", (count, width), f32, dev),
-                               _vector(out.get("carry"), "carry", (-(-rows // RECURRENCE_CHUNK), width), f32, dev), *_room(work),
-                               handle, _vector(out.get("status"), "status", (1,), torch.int32, dev))
+                               h0_at, h_at, ldh, last_at, carry_at, work_at, room, handle, status_at)
     if rc:
         raise CpError(rc, "cp_recurrence")
     if check_status and ptr is not None:
@@ -198,30 +221,24 @@ def cp_recurrence_backward(dh, f, x, carry, *, dlast=None, bias=None, seq_ptr=No
     dev = _on_gpu(f, "f")
     rows, width, count, ptr = _sequences(f, seq_ptr, dev)
     kind, f32 = _type(f, "f"), torch.float32
-    lds = [_matrix(t, n, rows, width, f.dtype, dev) for t, n in ((dh, "dh"), (f, "f"), (x, "x"))]
+    lddh, ldf, ldx = (_matrix(dh, "dh", rows, width, f.dtype, dev), _matrix(f, "f", rows, width, f.dtype, dev),
+                      _matrix(x, "x", rows, width, f.dtype, dev))
     bias_at, h0_at = _vector(bias, "bias", (width,), f32, dev), _vector(h0, "h0", (count, width), f32, dev)
     dlast_at = _vector(dlast, "dlast", (count, width), f32, dev)
     carry_at = _vector(carry, "carry", (-(-rows // RECURRENCE_CHUNK), width), f32, dev)
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        for key, like in (("df", f), ("dx", x)):
-            if key not in out:
-                out[key] = torch.empty(like.shape, dtype=like.dtype, device=dev)
-        if bias is not None and "dbias" not in out:
-            out["dbias"] = torch.empty(width, dtype=f32, device=dev)
-        if h0 is not None and "dh0" not in out:
-            out["dh0"] = torch.empty((count, width), dtype=f32, device=dev)
-        if ptr is not None and "status" not in out:
-            out["status"] = torch.empty(1, dtype=torch.int32, device=dev)
-        work = _work(workspace, _need("cp_recurrence_workspace_bytes", rows, width, 1), dev)
-        lddf, lddx = (_matrix(out[k], k, rows, width, f.dtype, dev) for k in ("df", "dx"))
-        rc = lib.cp_recurrence_backward(rows, width, count, ptr, kind, int(bool(reverse)), dh.data_ptr(), lds[0], dlast_at,
-                                        f.data_ptr(), lds[1], x.data_ptr(), lds[2], bias_at, h0_at, carry_at,
-                                        out["df"].data_ptr(), lddf, out["dx"].data_ptr(), lddx,
-                                        _vector(out.get("dbias"), "dbias", (width,), f32, dev),
-                                        _vector(out.get("dh0"), "dh0", (count, width), f32, dev), *_room(work), handle,
-                                        _vector(out.get("status"), "status", (1,), torch.int32, dev))
+        df_at, lddf = _rows_out(out, "df", f, dev)
+        dx_at, lddx = _rows_out(out, "dx", x, dev)
+        dbias_at = _vector_out(out, "dbias", (width,), f32, dev) if bias is not None or "dbias" in out else None
+        dh0_at = _vector_out(out, "dh0", (count, width), f32, dev) if h0 is not None or "dh0" in out else None
+        status_at = _vector_out(out, "status", (1,), torch.int32, dev) if ptr is not None else None
+        need = _need("cp_recurrence_workspace_bytes", rows, width, 1) if rows > RECURRENCE_CHUNK or dbias_at is not None else 0
+        work, work_at, room = _room(workspace, need, dev)
+        rc = lib.cp_recurrence_backward(rows, width, count, ptr, kind, int(bool(reverse)), dh.data_ptr(), lddh, dlast_at,
+                                        f.data_ptr(), ldf, x.data_ptr(), ldx, bias_at, h0_at, carry_at, df_at, lddf, dx_at, lddx,
+                                        dbias_at, dh0_at, work_at, room, handle, status_at)
     if rc:
         raise CpError(rc, "cp_recurrence_backward")
     if check_status and ptr is not None:
@@ -238,22 +255,18 @@ def cp_recurrence_step(f, x, state, *, bias=None, slots=None, out=None, stream=N
     dev = _on_gpu(f, "f")
     if f.dim() != 2 or state.dim() != 2:
         raise ValueError("f: [sequences][width], state: [slots][width]")
-    count, width = int(f.shape[0]), int(f.shape[1])
+    (count, width), num_slots = f.shape, state.shape[0]
     kind, f32, i32 = _type(f, "f"), torch.float32, torch.int32
     ldf, ldx = _matrix(f, "f", count, width, f.dtype, dev), _matrix(x, "x", count, width, f.dtype, dev)
-    num_slots = int(state.shape[0])
     state_at = _vector(state, "state", (num_slots, width), f32, dev)
     bias_at, slots_at = _vector(bias, "bias", (width,), f32, dev), _vector(slots, "slots", (count,), i32, dev)
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        if "h" not in out:
-            out["h"] = torch.empty((count, width), dtype=f.dtype, device=dev)
-        if slots is not None and "status" not in out:
-            out["status"] = torch.empty(1, dtype=i32, device=dev)
-        ldh = _matrix(out["h"], "h", count, width, f.dtype, dev)
+        h_at, ldh = _rows_out(out, "h", x, dev)
+        status_at = _vector_out(out, "status", (1,), i32, dev) if slots is not None else None
         rc = lib.cp_recurrence_step(count, width, kind, f.data_ptr(), ldf, x.data_ptr(), ldx, bias_at, state_at, num_slots, slots_at,
-                                    out["h"].data_ptr(), ldh, handle, _vector(out.get("status"), "status", (1,), i32, dev))
+                                    h_at, ldh, handle, status_at)
     if rc:
         raise CpError(rc, "cp_recurrence_step")
     if check_status and slots is not None:
@@ -272,7 +285,7 @@ def _joint(x, y, gate, w_pre, w_post, gate_act):
         raise ValueError(f"gate_act: one of {sorted(GATES)}, not {gate_act!r}")
     if y is None and (gate is not None or w_post is not None):
         raise ValueError("gate and w_post belong to y")
-    return dev, int(x.shape[0]), int(x.shape[1]), GATES[gate_act]
+    return dev, x.shape, GATES[gate_act]
 
 
 def cp_norm_gate(x, y=None, gate=None, *, w_pre, w_post=None, gate_act="sigmoid", scale=1.0, eps=1e-6, z_dtype=None,
@@ -285,28 +298,20 @@ def cp_norm_gate(x, y=None, gate=None, *, w_pre, w_post=None, gate_act="sigmoid"
     Returns a dict: ``r`` (with ``y``), ``z`` and, if wanted, ``stats`` for the backward pass."""
     import torch
     lib = load_library()
-    dev, rows, width, act = _joint(x, y, gate, w_pre, w_post, gate_act)
+    dev, (rows, width), act = _joint(x, y, gate, w_pre, w_post, gate_act)
     block = y.dtype if y is not None else z_dtype or x.dtype
     ldx = _matrix(x, "x", rows, width, x.dtype, dev)
-    ldy = _matrix(y, "y", rows, width, block, dev) if y is not None else 0
-    ldg = _matrix(gate, "gate", rows, width, block, dev) if gate is not None else 0
+    y_at, ldy = (y.data_ptr(), _matrix(y, "y", rows, width, block, dev)) if y is not None else (None, 0)
+    gate_at, ldg = (gate.data_ptr(), _matrix(gate, "gate", rows, width, block, dev)) if gate is not None else (None, 0)
     pre_at, post_at = _vector(w_pre, "w_pre", (width,), w_pre.dtype, dev), _vector(w_post, "w_post", (width,), w_pre.dtype, dev)
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        if y is not None and "r" not in out:
-            out["r"] = torch.empty((rows, width), dtype=x.dtype, device=dev)
-        if "z" not in out:
-            out["z"] = torch.empty((rows, width), dtype=block, device=dev)
-        if want_stats and "stats" not in out:
-            out["stats"] = torch.empty((2, rows), dtype=torch.float32, device=dev)
-        r, z = out.get("r"), out["z"]
-        ldr = _matrix(r, "r", rows, width, x.dtype, dev) if r is not None else 0
-        rc = lib.cp_norm_gate(rows, width, _type(x, "x"), _type(z, "z"), _type(w_pre, "w_pre"), act, x.data_ptr(), ldx,
-                              y.data_ptr() if y is not None else None, ldy, gate.data_ptr() if gate is not None else None, ldg,
-                              pre_at, post_at, scale, eps, r.data_ptr() if r is not None else None, ldr, z.data_ptr(),
-                              _matrix(z, "z", rows, width, block, dev),
-                              _vector(out.get("stats"), "stats", (2, rows), torch.float32, dev), handle)
+        r_at, ldr = _rows_out(out, "r", x, dev) if y is not None else (None, 0)
+        z_at, ldz = _rows_out(out, "z", y, dev) if y is not None else _rows_out(out, "z", x, dev, block)
+        stats_at = _vector_out(out, "stats", (2, rows), torch.float32, dev) if want_stats or "stats" in out else None
+        rc = lib.cp_norm_gate(rows, width, _type(x, "x"), _type(out["z"], "z"), _type(w_pre, "w_pre"), act, x.data_ptr(), ldx, y_at,
+                              ldy, gate_at, ldg, pre_at, post_at, scale, eps, r_at, ldr, z_at, ldz, stats_at, handle)
     if rc:
         raise CpError(rc, "cp_norm_gate")
     return out
@@ -318,34 +323,26 @@ def cp_norm_gate_backward(dr, dz, x, y=None, gate=None, *, w_pre, w_post=None, g
     dict: ``dx``, ``dw_pre`` and, as there are such inputs, ``dy``, ``dgate``, ``dw_post``, each of its input's type."""
     import torch
     lib = load_library()
-    dev, rows, width, act = _joint(x, y, gate, w_pre, w_post, gate_act)
-    block = y.dtype if y is not None else dz.dtype
-    ldx = _matrix(x, "x", rows, width, x.dtype, dev)
-    ldy = _matrix(y, "y", rows, width, block, dev) if y is not None else 0
-    ldg = _matrix(gate, "gate", rows, width, block, dev) if gate is not None else 0
-    lddr = _matrix(dr, "dr", rows, width, x.dtype, dev) if dr is not None else 0
-    lddz = _matrix(dz, "dz", rows, width, block, dev)
-    pre_at, post_at = _vector(w_pre, "w_pre", (width,), w_pre.dtype, dev), _vector(w_post, "w_post", (width,), w_pre.dtype, dev)
+    dev, (rows, width), act = _joint(x, y, gate, w_pre, w_post, gate_act)
+    block, weight = y.dtype if y is not None else dz.dtype, w_pre.dtype
+    ldx, lddz = _matrix(x, "x", rows, width, x.dtype, dev), _matrix(dz, "dz", rows, width, block, dev)
+    y_at, ldy = (y.data_ptr(), _matrix(y, "y", rows, width, block, dev)) if y is not None else (None, 0)
+    gate_at, ldg = (gate.data_ptr(), _matrix(gate, "gate", rows, width, block, dev)) if gate is not None else (None, 0)
+    dr_at, lddr = (dr.data_ptr(), _matrix(dr, "dr", rows, width, x.dtype, dev)) if dr is not None else (None, 0)
+    pre_at, post_at = _vector(w_pre, "w_pre", (width,), weight, dev), _vector(w_post, "w_post", (width,), weight, dev)
     stats_at = _vector(stats, "stats", (2, rows), torch.float32, dev)
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        for key, like in (("dx", x), ("dy", y), ("dgate", gate)):
-            if like is not None and key not in out:
-                out[key] = torch.empty((rows, width), dtype=like.dtype, device=dev)
-        for key, like in (("dw_pre", w_pre), ("dw_post", w_post)):
-            if like is not None and key not in out:
-                out[key] = torch.empty(width, dtype=like.dtype, device=dev)
-        work = _work(workspace, _need("cp_norm_gate_backward_workspace_bytes", rows, width), dev)
-        at = lambda key: out[key].data_ptr() if key in out else None  # noqa: E731
-        ld = lambda key, like: _matrix(out[key], key, rows, width, like.dtype, dev) if like is not None else 0  # noqa: E731
-        rc = lib.cp_norm_gate_backward(rows, width, _type(x, "x"), _type(dz, "dz"), _type(w_pre, "w_pre"), act,
-                                       dr.data_ptr() if dr is not None else None, lddr, dz.data_ptr(), lddz, x.data_ptr(), ldx,
-                                       y.data_ptr() if y is not None else None, ldy,
-                                       gate.data_ptr() if gate is not None else None, ldg, pre_at, post_at, scale, stats_at,
-                                       at("dx"), ld("dx", x), at("dy"), ld("dy", y), at("dgate"), ld("dgate", gate),
-                                       _vector(out["dw_pre"], "dw_pre", (width,), w_pre.dtype, dev),
-                                       _vector(out.get("dw_post"), "dw_post", (width,), w_pre.dtype, dev), *_room(work), handle)
+        dx_at, lddx = _rows_out(out, "dx", x, dev)
+        dy_at, lddy = _rows_out(out, "dy", y, dev) if y is not None else (None, 0)
+        dg_at, lddg = _rows_out(out, "dgate", gate, dev) if gate is not None else (None, 0)
+        dw_pre_at = _vector_out(out, "dw_pre", (width,), weight, dev)
+        dw_post_at = _vector_out(out, "dw_post", (width,), weight, dev) if w_post is not None else None
+        work, work_at, room = _room(workspace, _need("cp_norm_gate_backward_workspace_bytes", rows, width), dev)
+        rc = lib.cp_norm_gate_backward(rows, width, _type(x, "x"), _type(dz, "dz"), _type(w_pre, "w_pre"), act, dr_at, lddr,
+                                       dz.data_ptr(), lddz, x.data_ptr(), ldx, y_at, ldy, gate_at, ldg, pre_at, post_at, scale,
+                                       stats_at, dx_at, lddx, dy_at, lddy, dg_at, lddg, dw_pre_at, dw_post_at, work_at, room, handle)
     if rc:
         raise CpError(rc, "cp_norm_gate_backward")
     return out
@@ -354,7 +351,12 @@ def cp_norm_gate_backward(dr, dz, x, y=None, gate=None, *, w_pre, w_post=None, g
 # ---- log probabilities of given tokens -------------------------------------------------------------
 
 _ANY_TOKEN = 4        # the type of no tokens
-_TOKEN_BYTES = {"torch.uint8": 1, "torch.int32": 4, "torch.int64": 8}
+
+
+@functools.lru_cache(maxsize=1)
+def _token_types():
+    import torch
+    return {torch.uint8: 1, torch.int32: 4, torch.int64: 8}
 
 
 def _rows_of(logits, tokens, allow):
@@ -362,19 +364,20 @@ def _rows_of(logits, tokens, allow):
     dev = _on_gpu(logits, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits: [rows][vocab], not {tuple(logits.shape)}")
-    rows, vocab = int(logits.shape[0]), int(logits.shape[1])
+    rows, vocab = logits.shape
     ld = _matrix(logits, "logits", rows, vocab, logits.dtype, dev)
     allow_at = _vector(allow, "allow", (rows, -(-vocab // 64)), torch.int64, dev)
     if tokens is None:
         return dev, rows, vocab, ld, allow_at, (0, None, _ANY_TOKEN, 0, 0)
-    size = _TOKEN_BYTES.get(str(tokens.dtype))
+    size = _token_types().get(tokens.dtype)
     if size is None:
         raise TypeError(f"tokens: uint8, int32 or int64, not {tokens.dtype}")
-    if tokens.device != dev or tokens.dim() not in (1, 2) or int(tokens.shape[0]) != rows:
+    shape, stride = tokens.shape, tokens.stride()
+    if tokens.device != dev or len(shape) not in (1, 2) or shape[0] != rows:
         raise ValueError("tokens: [rows] or [rows][given], on the device of the logits")
-    given = 1 if tokens.dim() == 1 else int(tokens.shape[1])
-    stride = tokens.stride()
-    return dev, rows, vocab, ld, allow_at, (given, tokens.data_ptr(), size, stride[0], stride[1] if tokens.dim() == 2 else 0)
+    if len(shape) == 1:
+        return dev, rows, vocab, ld, allow_at, (1, tokens.data_ptr(), size, stride[0], 0)
+    return dev, rows, vocab, ld, allow_at, (shape[1], tokens.data_ptr(), size, *stride)
 
 
 def cp_token_logprobs(logits, tokens=None, *, scale=1.0, allow=None, top=0, out=None, workspace=None, stream=None,
@@ -394,27 +397,14 @@ def cp_token_logprobs(logits, tokens=None, *, scale=1.0, allow=None, top=0, out=
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        if tokens is not None and "logp" not in out:
-            out["logp"] = torch.empty(tokens.shape, dtype=f32, device=dev)
-        if "entropy" not in out:
-            out["entropy"] = torch.empty(rows, dtype=f32, device=dev)
-        if "stats" not in out:
-            out["stats"] = torch.empty((rows, 3), dtype=f32, device=dev)
-        if "status" not in out:
-            out["status"] = torch.empty(1, dtype=torch.int32, device=dev)
-        if top:
-            if "top_logp" not in out:
-                out["top_logp"] = torch.empty((rows, top), dtype=f32, device=dev)
-            if "top_idx" not in out:
-                out["top_idx"] = torch.empty((rows, top), dtype=torch.int32, device=dev)
-        work = _work(workspace, _need("cp_token_logprobs_workspace_bytes", rows, vocab, top), dev)
-        rc = lib.cp_token_logprobs(rows, vocab, _type(logits, "logits"), logits.data_ptr(), ld, scale, allow_at, *tok,
-                                   _vector(out.get("logp"), "logp", tuple(tokens.shape) if tokens is not None else (), f32, dev),
-                                   _vector(out["entropy"], "entropy", (rows,), f32, dev),
-                                   _vector(out["stats"], "stats", (rows, 3), f32, dev), int(top),
-                                   _vector(out["top_logp"], "top_logp", (rows, top), f32, dev) if top else None,
-                                   _vector(out["top_idx"], "top_idx", (rows, top), torch.int32, dev) if top else None,
-                                   *_room(work), handle, _vector(out["status"], "status", (1,), torch.int32, dev))
+        logp_at = _vector_out(out, "logp", tokens.shape, f32, dev) if tokens is not None else None
+        entropy_at, stats_at = _vector_out(out, "entropy", (rows,), f32, dev), _vector_out(out, "stats", (rows, 3), f32, dev)
+        status_at = _vector_out(out, "status", (1,), torch.int32, dev)
+        top_at, idx_at = (_vector_out(out, "top_logp", (rows, top), f32, dev),
+                          _vector_out(out, "top_idx", (rows, top), torch.int32, dev)) if top else (None, None)
+        work, work_at, room = _room(workspace, _need("cp_token_logprobs_workspace_bytes", rows, vocab, top), dev)
+        rc = lib.cp_token_logprobs(rows, vocab, _type(logits, "logits"), logits.data_ptr(), ld, scale, allow_at, *tok, logp_at,
+                                   entropy_at, stats_at, top, top_at, idx_at, work_at, room, handle, status_at)
     if rc:
         raise CpError(rc, "cp_token_logprobs")
     if check_status:
@@ -432,22 +422,23 @@ def cp_token_logprobs_backward(logits, tokens, stats, dlogp, *, dentropy=None, s
     lib = load_library()
     dev, rows, vocab, ld, allow_at, tok = _rows_of(logits, tokens, allow)
     stats_at = _vector(stats, "stats", (rows, 3), torch.float32, dev)
-    for name, t, shape in (("dlogp", dlogp, None if tokens is None else tuple(tokens.shape)), ("dentropy", dentropy, (rows,))):
-        if t is not None and (t.device != dev or t.dtype != torch.float32 or tuple(t.shape) != shape):
-            raise ValueError(f"{name}: a float32 tensor of shape {shape} on the device of the logits")
-    if tokens is not None and dlogp is None:
-        raise ValueError("dlogp is missing")
-    ds = dlogp.stride() if dlogp is not None else (0,)
+    if (dlogp is None) != (tokens is None):
+        raise ValueError("dlogp belongs to tokens")
+    dlogp_at, row_stride, stride, de_at, de_stride = None, 0, 0, None, 0
+    if dlogp is not None:
+        if dlogp.device != dev or dlogp.dtype is not torch.float32 or dlogp.shape != tokens.shape:
+            raise ValueError(f"dlogp: a float32 tensor of shape {tuple(tokens.shape)} on the device of the logits")
+        dlogp_at, row_stride, stride = dlogp.data_ptr(), dlogp.stride(0), dlogp.stride(1) if dlogp.dim() == 2 else 0
+    if dentropy is not None:
+        if dentropy.device != dev or dentropy.dtype is not torch.float32 or dentropy.shape != (rows,):
+            raise ValueError(f"dentropy: a float32 tensor of shape {(rows,)} on the device of the logits")
+        de_at, de_stride = dentropy.data_ptr(), dentropy.stride(0)
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:
-        if "dlogits" not in out:
-            out["dlogits"] = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
+        to, ldd = _rows_out(out, "dlogits", logits, dev)
         rc = lib.cp_token_logprobs_backward(rows, vocab, _type(logits, "logits"), logits.data_ptr(), ld, scale, allow_at, *tok,
-                                            stats_at, dlogp.data_ptr() if dlogp is not None else None, ds[0],
-                                            ds[1] if len(ds) > 1 else 0, dentropy.data_ptr() if dentropy is not None else None,
-                                            dentropy.stride(0) if dentropy is not None else 0, out["dlogits"].data_ptr(),
-                                            _matrix(out["dlogits"], "dlogits", rows, vocab, logits.dtype, dev), handle)
+                                            stats_at, dlogp_at, row_stride, stride, de_at, de_stride, to, ldd, handle)
     if rc:
         raise CpError(rc, "cp_token_logprobs_backward")
     return out

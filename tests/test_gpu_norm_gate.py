@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_1711_01912_amd as cpe
+from paper_1711_01912_amd import policy
 from policy_util import TYPES, half_step, joint, near, wide
 
 pytestmark = pytest.mark.gpu
@@ -156,3 +157,23 @@ def test_in_a_graph():
         e = cpe.cp_norm_gate(x, d["y"], d["gate"], want_stats=True, **kw)
         eb = cpe.cp_norm_gate_backward(d["dr"], d["dz"], x, d["y"], d["gate"], stats=e["stats"], **kw)
         assert torch.equal(a["z"], e["z"]) and torch.equal(b["dx"], eb["dx"]) and torch.equal(b["dw_pre"], eb["dw_pre"])
+
+
+@pytest.mark.parametrize("block,stream", [("bf16", "bf16"), ("fp16", "fp32"), ("fp32", "fp32")])
+@pytest.mark.parametrize("rows,width", [(9, 3), (1001, 7), (517, 31), (77, 65), (131, 127), (40000, 33)])
+def test_rows_side_by_side(rows, width, block, stream):
+    compare(make(rows, width, block, stream, weights="fp32", seed=width), f"{rows}x{width} {block} {stream}")
+
+
+@pytest.mark.parametrize("width", [5, 64, 72, 200, 1000])
+def test_the_workspace_is_as_large_as_said(width):
+    for block, stream in (("bf16", "bf16"), ("bf16", "fp32")):
+        d = make(70000, width, block, stream, weights="fp32")
+        kw = dict(w_pre=d["w_pre"], w_post=d["w_post"])
+        fwd = cpe.cp_norm_gate(d["x"], d["y"], d["gate"], want_stats=True, **kw)
+        need = policy._need("cp_norm_gate_backward_workspace_bytes", 70000, width)
+        room = torch.full((need + 4096,), 7, dtype=torch.uint8, device=DEV)
+        one = cpe.cp_norm_gate_backward(None, d["dz"], d["x"], d["y"], d["gate"], stats=fwd["stats"], workspace=room[:need], **kw)
+        assert (room[need:] == 7).all()
+        two = cpe.cp_norm_gate_backward(None, d["dz"], d["x"], d["y"], d["gate"], stats=fwd["stats"], **kw)
+        assert torch.equal(one["dw_pre"], two["dw_pre"]) and torch.equal(one["dw_post"], two["dw_post"])

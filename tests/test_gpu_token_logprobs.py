@@ -193,3 +193,14 @@ def test_in_a_graph():
             e = cpe.cp_token_logprobs(x, d["tokens"], top=4)
             eb = cpe.cp_token_logprobs_backward(x, d["tokens"], e["stats"], d["dlogp"], dentropy=d["dentropy"])
             assert torch.equal(a["logp"], e["logp"]) and torch.equal(a["top_idx"], e["top_idx"]) and torch.equal(b["dlogits"], eb["dlogits"])
+
+
+@pytest.mark.parametrize("vocab,top", [(257, 64), (363, 1), (520, 64), (1401, 20), (2049, 33), (6000, 64), (66000, 20)])
+@pytest.mark.parametrize("kind,mask", [("bf16", False), ("fp32", False), ("fp32", True)])
+def test_alternatives_of_rows_that_do_not_fill_a_workgroup(vocab, top, kind, mask):
+    compare(make(3, vocab, kind, 1, seed=vocab, mask=mask), f"{vocab} {top} {kind} {mask}", top=top)
+
+
+@pytest.mark.parametrize("rows,vocab,given", [(70, 45, 113), (9, 64, 16), (35, 33, 20), (50, 12, 17), (50, 8, 33), (3, 64, 300), (11, 2, 1024)])
+def test_columns_of_few_tokens(rows, vocab, given):
+    compare(make(rows, vocab, "fp32", given, seed=given, mask=True), f"{rows} {vocab} {given}")
