@@ -29,14 +29,20 @@ namespace cpeval {
 namespace {
 
 constexpr int kWaves = 8;
+constexpr int kLooks = 2;                               // tiles that a lane looks at
 constexpr int kWide = 2;                                // channels of a lane (of a width of one: one)
-constexpr int kForwardSpan = 64, kBackwardSpan = 32;    // rows of a wavefront
+// Rows of a wavefront.  Forward, of 16-bit types, short spans need half the registers and long ones half the groups that the
+// chain of states passes: 65536 x 1024 bf16 take 103 us with 32 and 118 with 64, 300000 x 75 fp16 74 and 86, a million x 256
+// 413 and 357.  Floats, of which a lane has half as many rows, take long ones.
+constexpr int kShortSpan = 32, kLongSpan = 64, kBackwardSpan = 32;
+constexpr int64_t kLongChain = 500000;                  // rows from which on spans are long
+constexpr int forward_span(int64_t rows, size_t bytes) { return bytes == 2 && rows < kLongChain ? kShortSpan : kLongSpan; }
 
 // How a wavefront's lanes share its rows: 128 bytes of each, kSides runs of them side by side, held in registers
 template <typename T>
 struct Shape {
     static constexpr int kLanes = 128 / (kWide * (int)sizeof(T)), kSides = kWave / kLanes, kRuns = kWaves * kSides;
-    static constexpr int kForwardRun = kForwardSpan / kSides, kBackwardRun = kBackwardSpan / kSides;
+    static constexpr int kBackwardRun = kBackwardSpan / kSides;
 };
 
 // Where sequences begin, in positions
@@ -313,15 +319,15 @@ struct Join {
         return all;
     }
 
-    // The state that enters the tile: that which enters its group of lookers * kSides tiles, and what the tiles of the group
-    // before it do to it.  Each looking wavefront joins kSides tiles, the first one joins what they found; a group's last
+    // The state that enters the tile: that which enters its group of tiles, and what the tiles of the group
+    // before it do to it.  Each looking wavefront joins kLooks * kSides tiles, the first one joins what they found; a group's last
     // tile tells the state that enters the next group.  What is joined with what goes by a tile's number alone, never by
     // which state was known first, so that results are the same from call to call.
     __device__ __forceinline__ void behind(const Place<T, V> &p, const Scan &s, float (&state)[V]) {
         __shared__ Effect lds[kWaves][V][kLanes];
         __shared__ float lds_state[V][kLanes];
         const int64_t tile = BACK ? s.tiles - 1 - p.tile : p.tile;          // in the order of the chain
-        const uint32_t size = (uint32_t)(s.lookers * kSides), group = (uint32_t)tile / size;
+        const uint32_t size = (uint32_t)(s.lookers * kSides * kLooks), group = (uint32_t)tile / size;
         const int64_t first = (int64_t)group * size;
         const bool tells = p.run == 0 && p.live && tile + 1 < s.tiles, ends = tile + 1 == first + size;
         if (tells && !ends) {
@@ -338,17 +344,26 @@ struct Join {
 #pragma unroll
         for (int k = 0; k < V; k++) w_group[k] = asks ? look(p.word(s, s.tiles + group) + k) : 0;
         if (p.wave < s.lookers) {
-            const int64_t of = tile - 1 - p.run;
-            const bool there = of >= first && p.live;
-            const uint64_t *at = p.word(s, there ? BACK ? s.tiles - 1 - of : of : p.tile);
             const int here = threadIdx.x & (kWave - 1);
-            uint64_t w[V];
+            const uint64_t *at[kLooks];
+            bool there[kLooks];
+            uint64_t w[kLooks][V];
 #pragma unroll
-            for (int k = 0; k < V; k++) w[k] = there ? look(at + k) : 0;
+            for (int m = 0; m < kLooks; m++) {
+                const int64_t of = tile - 1 - (p.run * kLooks + m);
+                there[m] = of >= first && p.live;
+                at[m] = p.word(s, there[m] ? BACK ? s.tiles - 1 - of : of : p.tile);
+#pragma unroll
+                for (int k = 0; k < V; k++) w[m][k] = there[m] ? look(at[m] + k) : 0;
+            }
 #pragma unroll
             for (int k = 0; k < V; k++) {
-                while (w[k] == kNotYet) w[k] = look(at + k);
-                Effect e = there ? effect_of(w[k]) : Effect{1.0f, 0.0f};
+                Effect e = {1.0f, 0.0f};
+#pragma unroll
+                for (int m = 0; m < kLooks; m++) {
+                    while (w[m][k] == kNotYet) w[m][k] = look(at[m] + k);
+                    if (there[m]) e = then(effect_of(w[m][k]), e);
+                }
 #pragma unroll
                 for (int d = 1; d < kSides; d <<= 1) {
                     const Effect o = {__shfl(e.A, here + d * kLanes), __shfl(e.H, here + d * kLanes)};
@@ -388,9 +403,9 @@ struct Join {
 
 // One tile.  INSIDE: of the inside of a sequence, the common case; else its wavefronts look for sequences' ends and for rows
 // that are not there.
-template <typename T, int V, bool STREAM, bool INSIDE>
+template <typename T, int V, int SPAN, bool STREAM, bool INSIDE>
 __device__ __forceinline__ void scan(const Scan &s, const Place<T, V> &p, T *h, int64_t ldh, float *last, float *carry) {
-    constexpr int RUN = Shape<T>::kForwardRun;
+    constexpr int RUN = SPAN / Shape<T>::kSides;
     const Sequences &seq = s.seq;
     const int32_t c = p.c;
     const int64_t left = seq.rows - p.p0;
@@ -456,14 +471,14 @@ __device__ __forceinline__ void scan(const Scan &s, const Place<T, V> &p, T *h, 
         }
 }
 
-template <typename T, int V, bool STREAM>
+template <typename T, int V, int SPAN, bool STREAM>
 __global__ __launch_bounds__(kWaves *kWave, 4) void scan_kernel(Scan s, T *h, int64_t ldh, float *last, float *carry, int32_t *status) {
-    constexpr int RUN = Shape<T>::kForwardRun, kRuns = Shape<T>::kRuns;
+    constexpr int RUN = SPAN / Shape<T>::kSides, kRuns = Shape<T>::kRuns;
     Place<T, V> p;
     p.template take<RUN>(s, false);
     const Sequences &seq = s.seq;
-    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan<T, V, STREAM, true>(s, p, h, ldh, last, carry);
-    else scan<T, V, STREAM, false>(s, p, h, ldh, last, carry);
+    if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan<T, V, SPAN, STREAM, true>(s, p, h, ldh, last, carry);
+    else scan<T, V, SPAN, STREAM, false>(s, p, h, ldh, last, carry);
     if (status && blockIdx.x == 0) check_sequences(seq, status);
     // a sequence without rows ends in the state that it begins with
     if (last && p.live && (seq.ptr || seq.each == 0)) {
@@ -705,8 +720,8 @@ int check_scan(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_
     return CP_OK;
 }
 
-int64_t tiles_of(int64_t rows, bool backward) {
-    const int64_t tile = kWaves * (backward ? kBackwardSpan : kForwardSpan);
+int64_t tiles_of(int64_t rows, int span) {
+    const int64_t tile = kWaves * span;
     return std::max<int64_t>(1, (rows + tile - 1) / tile);
 }
 
@@ -715,24 +730,30 @@ int64_t tiles_of(int64_t rows, bool backward) {
 int64_t words_of(int64_t tiles, int64_t group) { return tiles + (tiles + group - 1) / group; }
 size_t words_bytes(int64_t rows, int32_t width, bool backward) {
     constexpr size_t strip = Shape<bf16>::kLanes * kWide;
-    return kPolicyAlign + align_up(words_of(tiles_of(rows, backward), 2) * ((width + strip - 1) / strip * strip) * sizeof(uint64_t));
+    return kPolicyAlign + align_up(words_of(tiles_of(rows, backward ? kBackwardSpan : forward_span(rows, 2)), 2) * ((width + strip - 1) / strip * strip) * sizeof(uint64_t));
 }
-size_t part_bytes(int64_t rows, int32_t width) { return align_up((size_t)tiles_of(rows, true) * width * sizeof(float)); }
+size_t part_bytes(int64_t rows, int32_t width) { return align_up((size_t)tiles_of(rows, kBackwardSpan) * width * sizeof(float)); }
 
-// Wavefronts that look back, kSides tiles each: a group.  The chain of states passes from group to group; the fewer strips
+// Wavefronts that look back, kLooks * kSides tiles each: a group.  The chain of states passes from group to group; the fewer strips
 // there are, the more tiles of each are under way at once, and the faster it has to be.
 int lookers_of(int32_t strips) { return std::max(1, std::min(kWaves, 32 / strips)); }
 
-void split_over(Scan &s, bool backward, int strip, void *workspace) {
+// Results that fill the caches go past them, unless neighbouring strips write parts of the same 32 bytes: 234037 x 411 bf16
+// forward and backward take 597 us past the caches and 569 through them, 74241 x 1016 float 583 and 600.
+bool past_caches(int64_t rows, int32_t width, size_t bytes, int results) {
+    return results * (size_t)rows * width * bytes > kStreamed && width * bytes % 32 == 0;
+}
+
+void split_over(Scan &s, int span, int strip, void *workspace) {
     s.strips = (s.width + strip - 1) / strip;
-    s.tiles = tiles_of(s.seq.rows, backward);
+    s.tiles = tiles_of(s.seq.rows, span);
     s.lookers = lookers_of(s.strips);
     s.ticket = s.tiles > 1 ? (uint32_t *)workspace : nullptr;
     s.words = s.tiles > 1 ? (uint64_t *)((char *)workspace + kPolicyAlign) : nullptr;
 }
 
-void clear_words(const Scan &s, int strip, int sides, hipStream_t stream) {
-    const int64_t count = words_of(s.tiles, s.lookers * sides) * s.strips * strip;
+void clear_words(const Scan &s, int strip, int each, hipStream_t stream) {
+    const int64_t count = words_of(s.tiles, s.lookers * each) * s.strips * strip;
     hipLaunchKernelGGL(clear_words_kernel, dim3((unsigned)std::min<int64_t>((count + 255) / 256, 2048)), dim3(256), 0, stream, s.ticket, s.words, count);
 }
 
@@ -773,10 +794,15 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
         auto go = [&](auto v) {
             constexpr int V = decltype(v)::value;
             constexpr int strip = Shape<T>::kLanes * V;
-            split_over(s, false, strip, workspace);
-            auto *kernel = (size_t)rows * width * sizeof(T) > kStreamed ? scan_kernel<T, V, true> : scan_kernel<T, V, false>;
+            split_over(s, forward_span(rows, sizeof(T)), strip, workspace);
+            const bool past = past_caches(rows, width, sizeof(T), 1);
+            auto *kernel = past ? scan_kernel<T, V, kLongSpan, true> : scan_kernel<T, V, kLongSpan, false>;
+            if constexpr (sizeof(T) == 2) {
+                if (forward_span(rows, sizeof(T)) == kShortSpan)
+                    kernel = past ? scan_kernel<T, V, kShortSpan, true> : scan_kernel<T, V, kShortSpan, false>;
+            }
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
-            if (s.ticket) clear_words(s, strip, Shape<T>::kSides, st);
+            if (s.ticket) clear_words(s, strip, kLooks * Shape<T>::kSides, st);
             hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
                                seq_ptr ? status_out : nullptr);
             return launched();
@@ -802,7 +828,7 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
     }
     if (rows < 2) lddh = ldf = ldx = lddf = lddx = width;
     // (the sums of a single tile are the whole sums)
-    const bool alone = tiles_of(rows, true) == 1;
+    const bool alone = tiles_of(rows, kBackwardSpan) == 1;
     float *part = !dbias || alone ? dbias : (float *)((char *)workspace + words_bytes(rows, width, true));
     Scan s{};
     s.seq = {seq_ptr, rows, rows / num_seq, num_seq, reverse != 0};
@@ -814,10 +840,10 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
         auto go = [&](auto v) {
             constexpr int V = decltype(v)::value;
             constexpr int strip = Shape<T>::kLanes * V;
-            split_over(s, true, strip, workspace);
-            auto *kernel = 2 * (size_t)rows * width * sizeof(T) > kStreamed ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>;
+            split_over(s, kBackwardSpan, strip, workspace);
+            auto *kernel = past_caches(rows, width, sizeof(T), 2) ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>;
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
-            if (s.ticket) clear_words(s, strip, Shape<T>::kSides, st);
+            if (s.ticket) clear_words(s, strip, kLooks * Shape<T>::kSides, st);
             hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
                                Gradient<T>{(const T *)dh, lddh, dlast, carry, (T *)df, (T *)dx, lddf, lddx, part, dh0}, seq_ptr ? status_out : nullptr);
             if (dbias && !alone)

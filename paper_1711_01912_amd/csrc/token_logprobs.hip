@@ -484,8 +484,10 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, 
 
 // ---- rows of few places, such as devices ----
 //
-// Some neighbouring lanes a row, a place a lane (of more than 64 places: E), several rows a wavefront.  The row's log
-// probabilities are a table in LDS for its tokens, of which there may be as many as partitions were drawn.
+// Some neighbouring lanes a row, kEach of its places a lane, several rows a wavefront, so that what is done once a row is done
+// for many at once.  (A place a lane, a wavefront took 362 us for a million rows of 64 bf16 logits and four tokens, most of it
+// for moving sums from lane to lane.)  The row's log probabilities are a table in LDS for its tokens, of which there may be as
+// many as partitions were drawn.
 
 // Four tokens from g on, side by side or `stride` apart, -1 behind the last
 template <typename I>
@@ -511,29 +513,64 @@ struct Four {
 };
 constexpr int kAhead = 4;                // fours a lane loads before it looks at them
 
-// the logits of a row that a lane has, E of them S apart
-template <typename T, int S, int E>
-__device__ __forceinline__ void few_logits(float (&x)[E], const Rows &r, int64_t row, int place) {
-#pragma unroll
-    for (int e = 0; e < E; e++) {
-        x[e] = logit<T>(r, row, min(e * S + place, r.vocab - 1));
-        x[e] = e * S + place < r.vocab ? x[e] : kNone;
+constexpr int kEach = 8;
+
+// The places of a row that a lane has: kEach from `at` on, the last of them the row's last (of shorter rows: all), so that
+// some may be its neighbour's, which counts them.
+struct Few {
+    int32_t at;
+    uint32_t here, mine;                 // bit e: at + e is a place of the row; and it is counted by this lane
+    __device__ __forceinline__ Few(int32_t vocab, int part) {
+        const int32_t first = part * kEach, behind = first < vocab ? min(vocab - first, kEach) : 0;
+        at = max(min(first, vocab - kEach), 0);
+        here = (1u << min(vocab, kEach)) - 1;
+        mine = ((1u << behind) - 1) << (behind ? first - at : 0);
     }
+    // their logits, -inf where not allowed
+    template <typename T>
+    __device__ __forceinline__ void load(float (&x)[kEach], const Rows &r, int64_t row) const {
+        const T *from = (const T *)r.logits + row * r.ld + at;
+        if (r.vocab >= kEach) {
+            Raw<T, kEach> raw;
+            raw.load(from);
+#pragma unroll
+            for (int e = 0; e < kEach; e++) x[e] = raw[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; e++) x[e] = (float)from[min(e, r.vocab - 1)];
+        }
+        if (r.allow) {
+            const uint64_t *word = r.allow + row * r.words + (at >> 6);
+            uint64_t may = word[0] >> (at & 63);
+            if ((at & 63) + kEach > 64) may |= word[1] << (64 - (at & 63));
+#pragma unroll
+            for (int e = 0; e < kEach; e++) x[e] = may >> e & 1 ? x[e] : kNone;
+        }
+    }
+};
+
+// what a wavefront's lanes have written to LDS is there for all of them
+__device__ __forceinline__ void lds_ready() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // `lanes` (a multiple of S) lanes a row: S neighbours have its places, and where lanes are more than S, others the same again;
 // for its tokens each of them is another.
-template <typename T, typename I, int S, int E>
-__global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Results out, int lanes) {
-    __shared__ float lds[kWaves][kWave * E];
-    const int lane = threadIdx.x & (kWave - 1), here = lane & (lanes - 1), group = lane / lanes, place = lane & (S - 1);
-    float *table = lds[threadIdx.x / kWave] + group * (S * E);
+template <typename T, typename I, int S>
+__global__ __launch_bounds__(kThreads, 4) void few_kernel(Rows r, Tokens tok, Results out, int lanes) {
+    constexpr int kPitch = S * kEach + 1;
+    __shared__ float lds[kWaves][kWave / S * kPitch];
+    const int lane = threadIdx.x & (kWave - 1), here = lane & (lanes - 1), group = lane / lanes;
+    float *table = lds[threadIdx.x / kWave] + group * kPitch;
+    const Few few(r.vocab, lane & (S - 1));
     bool bad = false;
     const int side = kWave / lanes;
     const int64_t step = (int64_t)gridDim.x * kWaves * side;
     int64_t row0 = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * side;
-    float soon[E];
-    few_logits<T, S, E>(soon, r, min(row0 + group, r.rows - 1), place);
+    float soon[kEach];
+    few.load<T>(soon, r, min(row0 + group, r.rows - 1));
     for (; row0 < r.rows; row0 += step) {
         const int64_t row = min(row0 + group, r.rows - 1);
         const bool live = row0 + group < r.rows;
@@ -542,17 +579,17 @@ __global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Re
 #pragma unroll
         for (int a = 0; a < kAhead; a++)
             if ((here + a * lanes) * 4 < tok.count) four[a].load(tok, row, (here + a * lanes) * 4);
-        float x[E], m = kNone;
+        float x[kEach], m = kNone;
 #pragma unroll
-        for (int e = 0; e < E; e++) {
-            x[e] = soon[e];
+        for (int e = 0; e < kEach; e++) {
+            x[e] = few.mine >> e & 1 ? soon[e] : kNone;
             m = fmaxf(m, x[e]);
         }
-        few_logits<T, S, E>(soon, r, min(row0 + step + group, r.rows - 1), place);
+        few.load<T>(soon, r, min(row0 + step + group, r.rows - 1));
         Part all = {group_max<S>(m), 0.0f, 0.0f};
         const float base = base_of(all);
 #pragma unroll
-        for (int e = 0; e < E; e++) {
+        for (int e = 0; e < kEach; e++) {
             const float d = (x[e] - base) * r.unit, p = __builtin_amdgcn_exp2f(d);
             all.s += p;
             all.t = fmaf(p, fmaxf(d, kFar), all.t);
@@ -563,10 +600,9 @@ __global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Re
         if (live && here == 0) write_sums(out, row, all);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int e = 0; e < E; e++) table[e * S + place] = log_p(r, x[e], base, l2s);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int e = 0; e < kEach; e++)
+            if (few.mine >> e & 1) table[few.at + e] = log_p(r, x[e], base, l2s);
+        lds_ready();
         for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * lanes * 4) {
             if (g0 > here * 4) {
 #pragma unroll
@@ -596,8 +632,8 @@ __global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Re
         for (int q = 0; q < out.top; q++) {
             uint64_t key = 0;
 #pragma unroll
-            for (int e = 0; e < E; e++) {
-                const uint64_t one = rank_key(x[e], e * S + place);
+            for (int e = 0; e < kEach; e++) {
+                const uint64_t one = rank_key(x[e], few.at + e);
                 key = one < last && one > key ? one : key;
             }
             key = most<S>(key);
@@ -608,47 +644,41 @@ __global__ __launch_bounds__(kThreads, 6) void few_kernel(Rows r, Tokens tok, Re
     if (bad) atomicOr(out.status, CP_STATUS_BAD_TOKEN);
 }
 
-// COLUMNS: many tokens a row are summed by place in LDS, each lane in columns of its own (so that the order of the sums is
-// fixed), kSets of them, so that as many sums are under way at once, and the row's columns added up; else every lane looks
-// through all of the row's tokens for its own places.  `used` (a power of two): of the row's L lanes those that have
-// tokens; only their columns are cleared and added up.
-constexpr int kSets = 4;
-
-template <typename T, typename I, int L, int E, bool COLUMNS>
-__global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int used) {
-    static_assert(!COLUMNS || E == 1, "a lane a place");
-    extern __shared__ float lds_columns[];       // COLUMNS: [kWaves][vocab][SETS][kWave + 1]
-    constexpr int SETS = L <= 16 ? kSets : 1;
-    const int lane = threadIdx.x & (kWave - 1), here = lane & (L - 1), group = lane / L;
-    float *columns = lds_columns + (threadIdx.x / kWave) * (r.vocab * SETS * (kWave + 1));
+// SETS > 0: many tokens a row are summed by place in LDS, each of `lanes` lanes in columns of its own (so that the order of the
+// sums is fixed), SETS of them, so that as many sums are under way at once, and the row's columns added up; 0: every lane
+// looks through all of the row's tokens for its own places.  `used` (a power of two): of a row's lanes those that have
+// tokens; only these have columns.
+template <typename T, typename I, int S, int SETS>
+__global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int lanes, int used) {
+    extern __shared__ float lds_columns[];       // [kWaves][vocab][SETS][side * used + 1]
+    const int lane = threadIdx.x & (kWave - 1), here = lane & (lanes - 1), group = lane / lanes, side = kWave / lanes;
+    const int pitch = side * used + 1, column = group * used + here, log_used = __builtin_ctz(used);
+    float *columns = lds_columns + (threadIdx.x / kWave) * (r.vocab * SETS * pitch);
+    const Few few(r.vocab, lane & (S - 1));
     bool bad = false;
-    constexpr int kSide = kWave / L;
-    const int64_t step = (int64_t)gridDim.x * kWaves * kSide;
-    int64_t row0 = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kSide;
-    float soon[E];
-    few_logits<T, L, E>(soon, r, min(row0 + group, r.rows - 1), here);
+    const int64_t step = (int64_t)gridDim.x * kWaves * side;
+    int64_t row0 = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * side;
+    float soon[kEach];
+    few.load<T>(soon, r, min(row0 + group, r.rows - 1));
     for (; row0 < r.rows; row0 += step) {
         const int64_t row = min(row0 + group, r.rows - 1);
         const bool live = row0 + group < r.rows;
-        float x[E], hits[E];
+        float x[kEach], hits[kEach];
 #pragma unroll
-        for (int e = 0; e < E; e++) {
+        for (int e = 0; e < kEach; e++) {
             x[e] = soon[e];
             hits[e] = 0.0f;
         }
-        few_logits<T, L, E>(soon, r, min(row0 + step + group, r.rows - 1), here);
-        if constexpr (COLUMNS) {
-            const int log_used = __builtin_ctz(used);
-            for (int i = here; i < r.vocab * SETS * used; i += L) columns[(i >> log_used) * (kWave + 1) + group * L + (i & (used - 1))] = 0.0f;
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * L * 4) {
+        few.load<T>(soon, r, min(row0 + step + group, r.rows - 1));
+        if constexpr (SETS > 0) {
+            for (int i = here; i < r.vocab * SETS * used; i += lanes) columns[(i >> log_used) * pitch + group * used + (i & (used - 1))] = 0.0f;
+            lds_ready();
+            for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * lanes * 4) {
                 Four<I> four[kAhead];
                 Pack<float, 4> w[kAhead];
 #pragma unroll
                 for (int a = 0; a < kAhead; a++) {
-                    const int32_t g = g0 + a * L * 4;
+                    const int32_t g = g0 + a * lanes * 4;
                     if (g >= tok.count) continue;
                     four[a].load(tok, row, g);
                     if (d.stride == 1 && g + 4 <= tok.count) w[a] = load_pack<float, 4>(d.dlogp + row * d.row_stride + g);
@@ -658,7 +688,7 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
                 }
 #pragma unroll
                 for (int a = 0; a < kAhead; a++) {
-                    if (g0 + a * L * 4 >= tok.count) continue;
+                    if (g0 + a * lanes * 4 >= tok.count) continue;
 #pragma unroll
                     for (int j = 0; j < 4; j += SETS) {
                         float sum[SETS];
@@ -666,7 +696,7 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
 #pragma unroll
                         for (int q = 0; q < SETS; q++) {
                             const int v = four[a].place(j + q, r.vocab, bad);
-                            at[q] = (max(v, 0) * SETS + q) * (kWave + 1) + lane;
+                            at[q] = (max(v, 0) * SETS + q) * pitch + column;
                             sum[q] = columns[at[q]] + (v >= 0 ? w[a].v[j + q] : 0.0f);
                         }
 #pragma unroll
@@ -674,20 +704,19 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
                     }
                 }
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            const float *mine = columns + min(here, r.vocab - 1) * (SETS * (kWave + 1)) + group * L;
+            lds_ready();
+            // (a place's sum goes where its first column was, which no other lane has read)
+            for (int v = here; v < r.vocab; v += lanes) {
+                float *from = columns + v * (SETS * pitch) + group * used, sum = 0.0f;
 #pragma unroll
-            for (int q = 0; q < SETS; q++) {
-                if (used == L) {
-#pragma unroll
-                    for (int j = 0; j < L; j++) hits[0] += mine[q * (kWave + 1) + j];
-                } else {
-#pragma unroll 4
-                    for (int j = 0; j < used; j++) hits[0] += mine[q * (kWave + 1) + j];
-                }
+                for (int q = 0; q < SETS; q++)
+#pragma unroll 8
+                    for (int j = 0; j < used; j++) sum += from[q * pitch + j];
+                from[0] = sum;
             }
+            lds_ready();
+#pragma unroll
+            for (int e = 0; e < kEach; e++) hits[e] = columns[min(few.at + e, r.vocab - 1) * (SETS * pitch) + group * used];
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
         } else {
@@ -695,19 +724,26 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
                 const int64_t v = ((const I *)tok.at)[row * tok.row_stride + (int64_t)g * tok.stride];
                 const float w = d.get(row, g);
 #pragma unroll
-                for (int e = 0; e < E; e++) hits[e] += v == e * L + here ? w : 0.0f;
+                for (int e = 0; e < kEach; e++) hits[e] += v == few.at + e ? w : 0.0f;
             }
         }
         float sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; e++) {
+        for (int e = 0; e < kEach; e++) {
             hits[e] = x[e] == kNone ? 0.0f : hits[e];
-            sum += hits[e];
+            sum += few.mine >> e & 1 ? hits[e] : 0.0f;
         }
-        const Slope slope(r, stats + 3 * row, d.dentropy ? d.dentropy[row * d.de_stride] : 0.0f, group_add<L>(sum));
+        const Slope slope(r, stats + 3 * row, d.dentropy ? d.dentropy[row * d.de_stride] : 0.0f, group_add<S>(sum));
+        if (!live || here >= S || few.mine == 0) continue;
+        Pack<T, kEach> o;
 #pragma unroll
-        for (int e = 0; e < E; e++)
-            if (live && e * L + here < r.vocab) out[row * ldo + e * L + here] = (T)slope.at(x[e], hits[e]);
+        for (int e = 0; e < kEach; e++) o.v[e] = (T)slope.at(x[e], hits[e]);
+        T *to = out + row * ldo + few.at;
+        if (r.vocab >= kEach) store_pack<T, kEach>(to, o);
+        else
+#pragma unroll
+            for (int e = 0; e < kEach; e++)
+                if (few.here >> e & 1) to[e] = o.v[e];
     }
 }
 
@@ -715,7 +751,8 @@ __global__ void clear_status_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 
 constexpr int kMostLoads = 4;
 constexpr int32_t kFew = 256;            // up to so many places a row is some lanes'
-constexpr int32_t kColumns = 16;         // from so many tokens on they are summed in columns of LDS
+constexpr int32_t kMostColumns = 128;    // places whose columns LDS has room for (128 KiB)
+constexpr int kSets = 4;
 constexpr int32_t slice_places(int v, int nv) { return kThreads * v * nv; }
 int32_t slices_of(int32_t vocab, int v, int nv) { return (vocab + slice_places(v, nv) - 1) / slice_places(v, nv); }
 
@@ -746,24 +783,29 @@ int by_loads(int nv, F f) {
     return f(std::integral_constant<int, kMostLoads>{});
 }
 
-// f(a value of the tokens' type, lanes a row, places a lane).  Lanes: as many as there are places, and with many tokens, of
-// which a lane writes 16 bytes at once, enough for a line of 128 bytes.
+// f(a value of the tokens' type, lanes that have a row's places)
 template <typename F>
-int by_lanes(const Tokens &tok, int32_t vocab, int32_t least, F f) {
+int by_lanes(const Tokens &tok, int32_t vocab, F f) {
     auto of = [&](auto i) {
         using std::integral_constant;
-        auto go = [&](auto l, auto e) { return f(i, l, e); };
-        const int32_t want = std::max(vocab, least);
-        if (want <= 4) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-        if (want <= 8) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-        if (want <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-        if (want <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-        if (want <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-        return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+        if (vocab <= kEach) return f(i, integral_constant<int, 1>{});
+        if (vocab <= 2 * kEach) return f(i, integral_constant<int, 2>{});
+        if (vocab <= 4 * kEach) return f(i, integral_constant<int, 4>{});
+        if (vocab <= 8 * kEach) return f(i, integral_constant<int, 8>{});
+        if (vocab <= 16 * kEach) return f(i, integral_constant<int, 16>{});
+        return f(i, integral_constant<int, 32>{});
     };
     if (tok.type == CP_TOKEN_U8) return of(uint8_t{});
     if (tok.type == CP_TOKEN_I32) return of(int32_t{});
     return of(int64_t{});
+}
+static_assert(kFew <= 32 * kEach, "the most lanes have a row's places");
+
+// Lanes of a row with `given` tokens, of which a lane takes four at once: no more than `most`, unless rows do not fill the chip.
+int lanes_of(int64_t rows, int32_t given, int least, int most) {
+    int lanes = least;
+    while (lanes < kWave && lanes * 4 < given && (lanes < most || rows * lanes < (1 << 19))) lanes *= 2;
+    return lanes;
 }
 
 }  // namespace
@@ -810,13 +852,13 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
         using T = decltype(t);
         if (vocab <= kFew) {
             clear();
-            return by_lanes(tok, vocab, 4, [&](auto i, auto l, auto e) {
-                constexpr int S = decltype(l)::value, E = decltype(e)::value;
-                // (four tokens a lane and load)
-                int lanes = S;
-                while (lanes < kWave && lanes * 4 < given) lanes *= 2;
-                const int side = kWaves * kWave / lanes;
-                hipLaunchKernelGGL((few_kernel<T, decltype(i), S, E>), dim3((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8)),
+            return by_lanes(tok, vocab, [&](auto i, auto l) {
+                constexpr int S = decltype(l)::value;
+                // (eight lanes write a line of 128 bytes, and many rows share what is done once a row: 646087 rows of 25 with 94
+                // tokens take 189 us so, 218 with lanes for all tokens; 200000 rows of 16 with 200 tokens 85 and 103.  Of more
+                // tokens the results are written faster line behind line: 200000 rows with 1000 tokens 446 and 186 us.)
+                const int lanes = lanes_of(rows, given, S, given < 256 ? 8 : kWave), side = kWaves * kWave / lanes;
+                hipLaunchKernelGGL((few_kernel<T, decltype(i), S>), dim3((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8)),
                                    dim3(kThreads), 0, st, r, tok, out, lanes);
                 return launched();
             });
@@ -854,22 +896,28 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         if (vocab <= kFew)
-            return by_lanes(tok, vocab, given >= 32 ? 8 : 4, [&](auto i, auto l, auto e) {
-                constexpr int L = decltype(l)::value, E = decltype(e)::value, side = kWaves * kWave / L;
+            return by_lanes(tok, vocab, [&](auto i, auto l) {
+                constexpr int S = decltype(l)::value;
+                using I = decltype(i);
+                const bool sums = given >= (S <= 2 ? 16 : 48) && vocab <= kMostColumns;
+                const int lanes = sums ? lanes_of(rows, given, S, 8) : S, side = kWaves * kWave / lanes;
                 const dim3 grid((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8));
                 int used = 1;
-                while (used < L && used * 4 < given) used *= 2;
-                if (E == 1 && given >= kColumns) {
-                    const size_t lds = (size_t)kWaves * vocab * (L <= 16 ? kSets : 1) * (kWave + 1) * sizeof(float);
-                    auto *kernel = few_gradient_kernel<T, decltype(i), L, E, E == 1>;
+                while (used < lanes && used * 4 < given) used *= 2;
+                auto go = [&](auto n) {
+                    constexpr int SETS = decltype(n)::value;
+                    const size_t lds = (size_t)kWaves * vocab * SETS * (kWave / lanes * used + 1) * sizeof(float);
+                    auto *kernel = few_gradient_kernel<T, I, S, SETS>;
                     if (lds > 48 * 1024 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
                         return (int)CP_ERR_HIP;
-                    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd, used);
-                } else {
-                    hipLaunchKernelGGL((few_gradient_kernel<T, decltype(i), L, E, false>), grid, dim3(kThreads), 0, st, r, tok, stats, d,
-                                       (T *)dlogits, ldd, used);
-                }
-                return launched();
+                    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd, lanes, used);
+                    return launched();
+                };
+                if (!sums) return go(std::integral_constant<int, 0>{});
+                // (where a lane has few tokens, clearing and adding up more columns costs more than waiting for the last sum)
+                if constexpr (S <= 2)
+                    if (given >= 64 * lanes) return go(std::integral_constant<int, kSets>{});
+                return go(std::integral_constant<int, 1>{});
             });
         constexpr int V = 16 / sizeof(T);
         const int nv = loads_of(rows, vocab, V);

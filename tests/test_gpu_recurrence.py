@@ -244,3 +244,7 @@ def test_results_do_not_depend_on_the_order_of_workgroups():
         assert all(torch.equal(again[k], one[k]) for k in ("h", "last", "carry"))
         back = cpe.cp_recurrence_backward(d["dh"], d["f"], d["x"], again["carry"], bias=d["bias"])
         assert all(torch.equal(back[k], grad[k]) for k in ("df", "dx", "dbias"))
+
+
+def test_a_long_chain():
+    compare(make(500003, 3, "bf16", seqs=3), [0, 7, 300001, 500003], True, True, "bf16", "half a million rows")
