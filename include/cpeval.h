@@ -519,7 +519,8 @@ int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *s
  *                 drained where seq_ptr is not what it has to be (no access leaves the arrays)
  * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, width, num_seq < 1, rows no
  * multiple of num_seq without seq_ptr, a distance below width or above CP_RECURRENCE_MAX_DISTANCE), CP_ERR_NULL,
- * CP_ERR_WORKSPACE, CP_ERR_HIP.  h may not overlap f or x.
+ * CP_ERR_WORKSPACE, CP_ERR_HIP.  h may not overlap f or x.  An infinite x or state makes its channel NaN from the next
+ * row to the sequence's end; nothing passes from one sequence or channel to another.
  */
 int cp_recurrence_workspace_bytes(int64_t rows, int32_t width, int backward, size_t *out_bytes);
 int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_ptr, int type, int reverse,

@@ -6,6 +6,11 @@
 //
 // Differences from the maximum are formed before they are scaled, and m and log2 s are kept apart, so that rows of a type's
 // lowest value keep their probabilities.  A place that is not allowed counts as -inf whatever it holds.  Sums are floats.
+//
+// Bound by memory where rows are long: 8192 x 65536 bf16 take 208 us forward (5.1 TB/s, the rate of a copy) and 365 us backward
+// (5.9 TB/s, some of it from the caches).  Rows of few places with many tokens: 200000 x 8 with 1024 tokens of a byte 265 us
+// forward (3.8 TB/s read and written; 166 us where the tokens are still in the caches), 125 backward, where each token is a
+// read and a write of a sum in LDS.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -646,7 +651,7 @@ __global__ __launch_bounds__(kThreads, 4) void few_kernel(Rows r, Tokens tok, Re
 
 // SETS > 0: many tokens a row are summed by place in LDS, each of `lanes` lanes in columns of its own (so that the order of the
 // sums is fixed), SETS of them, so that as many sums are under way at once, and the row's columns added up; 0: every lane
-// looks through all of the row's tokens for its own places.  `used` (a power of two): of a row's lanes those that have
+// looks through all of the row's tokens for its own places.  `used` (a power of two): of a row's lanes those that take
 // tokens; only these have columns.
 template <typename T, typename I, int S, int SETS>
 __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int lanes, int used) {
@@ -673,12 +678,12 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
         if constexpr (SETS > 0) {
             for (int i = here; i < r.vocab * SETS * used; i += lanes) columns[(i >> log_used) * pitch + group * used + (i & (used - 1))] = 0.0f;
             lds_ready();
-            for (int32_t g0 = here * 4; g0 < tok.count; g0 += kAhead * lanes * 4) {
+            for (int32_t g0 = here < used ? here * 4 : tok.count; g0 < tok.count; g0 += kAhead * used * 4) {
                 Four<I> four[kAhead];
                 Pack<float, 4> w[kAhead];
 #pragma unroll
                 for (int a = 0; a < kAhead; a++) {
-                    const int32_t g = g0 + a * lanes * 4;
+                    const int32_t g = g0 + a * used * 4;
                     if (g >= tok.count) continue;
                     four[a].load(tok, row, g);
                     if (d.stride == 1 && g + 4 <= tok.count) w[a] = load_pack<float, 4>(d.dlogp + row * d.row_stride + g);
@@ -688,7 +693,7 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
                 }
 #pragma unroll
                 for (int a = 0; a < kAhead; a++) {
-                    if (g0 + a * lanes * 4 >= tok.count) continue;
+                    if (g0 + a * used * 4 >= tok.count) continue;
 #pragma unroll
                     for (int j = 0; j < 4; j += SETS) {
                         float sum[SETS];
@@ -751,7 +756,7 @@ __global__ void clear_status_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 
 constexpr int kMostLoads = 4;
 constexpr int32_t kFew = 256;            // up to so many places a row is some lanes'
-constexpr int32_t kMostColumns = 128;    // places whose columns LDS has room for (128 KiB)
+constexpr size_t kColumnBytes = 72u << 10;   // of LDS for a workgroup's columns: two of them on a compute unit
 constexpr int kSets = 4;
 constexpr int32_t slice_places(int v, int nv) { return kThreads * v * nv; }
 int32_t slices_of(int32_t vocab, int v, int nv) { return (vocab + slice_places(v, nv) - 1) / slice_places(v, nv); }
@@ -856,7 +861,7 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
                 constexpr int S = decltype(l)::value;
                 // (eight lanes write a line of 128 bytes, and many rows share what is done once a row: 646087 rows of 25 with 94
                 // tokens take 189 us so, 218 with lanes for all tokens; 200000 rows of 16 with 200 tokens 85 and 103.  Of more
-                // tokens the results are written faster line behind line: 200000 rows with 1000 tokens 446 and 186 us.)
+                // tokens the results are written faster line behind line: 200000 rows with 1000 tokens 446 and 186 us, tokens in the caches.)
                 const int lanes = lanes_of(rows, given, S, given < 256 ? 8 : kWave), side = kWaves * kWave / lanes;
                 hipLaunchKernelGGL((few_kernel<T, decltype(i), S>), dim3((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8)),
                                    dim3(kThreads), 0, st, r, tok, out, lanes);
@@ -899,14 +904,18 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
             return by_lanes(tok, vocab, [&](auto i, auto l) {
                 constexpr int S = decltype(l)::value;
                 using I = decltype(i);
-                const bool sums = given >= (S <= 2 ? 16 : 48) && vocab <= kMostColumns;
+                // (a lane's places are more to clear and add up, the more there are: a million rows of 64 with 30 tokens 412 us in
+                // columns and 301 without; 66695 rows of 45 with 113 tokens 28 in columns)
+                const bool sums = given >= (S <= 2 ? 16 : 48);
                 const int lanes = sums ? lanes_of(rows, given, S, 8) : S, side = kWaves * kWave / lanes;
                 const dim3 grid((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8));
                 int used = 1;
                 while (used < lanes && used * 4 < given) used *= 2;
                 auto go = [&](auto n) {
                     constexpr int SETS = decltype(n)::value;
-                    const size_t lds = (size_t)kWaves * vocab * SETS * (kWave / lanes * used + 1) * sizeof(float);
+                    auto bytes = [&] { return (size_t)kWaves * vocab * SETS * (kWave / lanes * used + 1) * sizeof(float); };
+                    while (used > 1 && bytes() > kColumnBytes) used /= 2;
+                    const size_t lds = bytes();
                     auto *kernel = few_gradient_kernel<T, I, S, SETS>;
                     if (lds > 48 * 1024 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
                         return (int)CP_ERR_HIP;

@@ -4,7 +4,7 @@
 ``cp_token_logprobs`` (with ``_backward``) follow the C entry points of the same names.  As in
 ``binding``, nothing is computed here: arguments are checked, outputs and workspaces allocated, and
 the library's kernels called on ``stream`` (default: the current one).  Outputs and workspaces are
-allocated for that stream; inputs that another stream still writes are the caller's to wait for.
+allocated for that stream; inputs of another stream are the caller's to wait for and to keep (``record_stream``).
 Matrices may be views whose rows are further apart than their length (slices of a fused
 projection), as long as a row's elements are contiguous.  ``out`` may carry preallocated outputs
 under the keys of the result, ``workspace`` a preallocated uint8 tensor.

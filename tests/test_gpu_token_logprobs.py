@@ -201,6 +201,7 @@ def test_alternatives_of_rows_that_do_not_fill_a_workgroup(vocab, top, kind, mas
     compare(make(3, vocab, kind, 1, seed=vocab, mask=mask), f"{vocab} {top} {kind} {mask}", top=top)
 
 
-@pytest.mark.parametrize("rows,vocab,given", [(70, 45, 113), (9, 64, 16), (35, 33, 20), (50, 12, 17), (50, 8, 33), (3, 64, 300), (11, 2, 1024)])
+@pytest.mark.parametrize("rows,vocab,given", [(70, 45, 113), (9, 64, 16), (35, 33, 20), (50, 12, 17), (50, 8, 33), (3, 64, 300), (11, 2, 1024), (9, 200, 300),
+                                              (5, 256, 1000), (70, 128, 64), (20, 255, 50)])
 def test_columns_of_few_tokens(rows, vocab, given):
     compare(make(rows, vocab, "fp32", given, seed=given, mask=True), f"{rows} {vocab} {given}")
