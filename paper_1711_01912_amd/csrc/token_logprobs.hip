@@ -423,7 +423,8 @@ struct Slope {
 };
 
 // One slice of one row a workgroup: the softmax's part of every place, then what the tokens add at theirs.  A token's place
-// is written by its first holder in the row, whole.
+// is written by its first holder in the row, whole.  No place is written by two workgroups: the last vector of a row, moved
+// back to end with it, may begin in the slice before, whose workgroup adds the tokens there.
 template <typename T, int V, int NV>
 __global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int32_t slices, bool stream) {
     __shared__ float lds[kWaves];
@@ -467,7 +468,14 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, 
             for (int k = 0; k < V; k++)
                 if (to == k && (may >> k & 1) && in.x[i][k] != kNone) o.v[k] = (T)slope.at(in.x[i][k], sum);
         }
-        store_pack<T, V>(out + row * ldo + v, o, stream);
+        T *to_v = out + row * ldo + v;
+        if (i == 0 && v < in.v0) {           // (a slice of fewer than V places: its first vector is the row's last)
+#pragma unroll
+            for (int k = 0; k < V; k++)
+                if (v + k >= in.v0) to_v[k] = o.v[k];
+        } else {
+            store_pack<T, V>(to_v, o, stream);
+        }
     }
     if (tok.count < 2) return;
     __syncthreads();

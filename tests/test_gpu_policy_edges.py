@@ -1,0 +1,31 @@
+"""The operators of a learned placement policy at the borders of what their kernels divide among workgroups."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1711_01912_amd as cpe
+import test_gpu_token_logprobs as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("given", [2, 3, 40])
+@pytest.mark.parametrize("rows,vocab,kind", [
+    (100, 1025, "fp32"), (9, 1027, "fp32"), (300, 2051, "fp32"), (5, 4097, "fp32"), (100, 2049, "bf16"), (100, 2049, "fp16"), (9, 2055, "fp16"),
+    (300, 4097, "bf16"), (600, 8193, "bf16"), (3, 65537, "bf16"), (2, 65537, "fp32"),
+    (4200, 8193, "bf16"),                    # (results past the caches)
+])
+def test_tokens_at_places_that_begin_a_row_s_last_vector(rows, vocab, kind, given, mask):
+    # the last slice of a row has fewer places than a vector: the places in front of it are those of another workgroup,
+    # which adds what the tokens pass on
+    d = L.make(rows, vocab, kind, given, seed=vocab, mask=mask)
+    g = torch.Generator().manual_seed(given)
+    d["tokens"][:, :2] = torch.randint(vocab - 8, vocab, (rows, 2), generator=g).to(DEV)
+    d["tokens"][0, :2] = vocab - 4
+    fwd, bwd = L.compare(d, f"{rows}x{vocab} {kind} {given} {mask}")
+    allow = L.pack_mask(d["allowed"]).to(DEV) if mask else None
+    for _ in range(3):
+        again = cpe.cp_token_logprobs_backward(d["logits"], d["tokens"], fwd["stats"], d["dlogp"], dentropy=d["dentropy"], scale=0.8, allow=allow)
+        assert torch.equal(again["dlogits"], bwd["dlogits"])
