@@ -120,6 +120,14 @@ __device__ __forceinline__ float wave_max(float v) {
 __device__ __forceinline__ float fast_exp(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 __device__ __forceinline__ float fast_rcp(float v) { return __builtin_amdgcn_rcpf(v); }
 
+// A grid of `groups` workgroups of up to 512 threads, and a workgroup's number in it.  HIP takes fewer than 2^32 threads in a
+// dimension; those that the first has no room for go into the second, whose last row may have some too many.
+constexpr uint32_t kGridX = 1u << 22;
+inline dim3 grid_of(int64_t groups) {
+    return dim3((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)((groups + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ uint32_t group_number() { return blockIdx.y * kGridX + blockIdx.x; }
+
 inline size_t type_bytes(int type) { return type == CP_TYPE_F32 ? 4 : 2; }
 inline bool known_type(int type) { return type == CP_TYPE_F32 || type == CP_TYPE_BF16 || type == CP_TYPE_F16; }
 inline size_t align_up(size_t v) { return (v + kPolicyAlign - 1) / kPolicyAlign * kPolicyAlign; }

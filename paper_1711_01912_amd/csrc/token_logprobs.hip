@@ -286,11 +286,13 @@ template <typename T, int V, int NV, bool TOP>
 __global__ __launch_bounds__(kThreads, 4) void slice_kernel(Rows r, Tokens tok, Results out, int32_t slices, Part *parts, uint64_t *best) {
     __shared__ float lds_m[kWaves], lds_s[kWaves], lds_t[kWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t row = blockIdx.x / (uint32_t)slices;
+    const uint32_t number = group_number();
+    const int64_t row = number / (uint32_t)slices;
+    if (row >= r.rows) return;
     Slice<T, V, NV> in;
-    in.load(r, row, (int32_t)(blockIdx.x - (uint32_t)row * (uint32_t)slices));
+    in.load(r, row, (int32_t)(number - (uint32_t)row * (uint32_t)slices));
     in.blank(r, row);
-    if (slices > 1 && blockIdx.x == 0 && threadIdx.x == 0) *out.status = CP_STATUS_OK;       // (tokens are looked at by the next launch)
+    if (slices > 1 && number == 0 && threadIdx.x == 0) *out.status = CP_STATUS_OK;       // (tokens are looked at by the next launch)
     float m = kNone;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
@@ -325,8 +327,8 @@ __global__ __launch_bounds__(kThreads, 4) void slice_kernel(Rows r, Tokens tok, 
         write_tokens<T>(r, tok, out, row, all);
         if constexpr (TOP) slice_top<T, V, NV>(r, row, in, own, out.top, [&](int i, uint64_t key) { write_top(r, out, row, i, key, all); });
     } else {
-        if (threadIdx.x == 0) parts[blockIdx.x] = all;
-        if constexpr (TOP) slice_top<T, V, NV>(r, row, in, own, out.top, [&](int i, uint64_t key) { best[(int64_t)blockIdx.x * out.top + i] = key; });
+        if (threadIdx.x == 0) parts[number] = all;
+        if constexpr (TOP) slice_top<T, V, NV>(r, row, in, own, out.top, [&](int i, uint64_t key) { best[(int64_t)number * out.top + i] = key; });
     }
 }
 
@@ -336,7 +338,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Rows r, Tokens tok, Resu
     __shared__ Part lds_part;
     __shared__ uint64_t lds_pool[kPool], lds_key[kWaves];
     __shared__ int lds_count;
-    const int64_t row = blockIdx.x;
+    const int64_t row = group_number();
+    if (row >= r.rows) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     if (wave == 0) {
         Part all = {kNone, 0.0f, 0.0f};
@@ -429,9 +432,11 @@ template <typename T, int V, int NV>
 __global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int32_t slices, bool stream) {
     __shared__ float lds[kWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t row = blockIdx.x / (uint32_t)slices;
+    const uint32_t number = group_number();
+    const int64_t row = number / (uint32_t)slices;
+    if (row >= r.rows) return;
     Slice<T, V, NV> in;
-    in.load(r, row, (int32_t)(blockIdx.x - (uint32_t)row * (uint32_t)slices));
+    in.load(r, row, (int32_t)(number - (uint32_t)row * (uint32_t)slices));
     auto given = [&](int32_t g) {        // what token g's log probability passes on
         const int64_t v = tok.get(row, g);
         const bool fine = v >= 0 && v < r.vocab && logit<T>(r, row, (int32_t)v) != kNone;
@@ -885,8 +890,8 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
         if (slices == 1) clear();
         return by_loads(nv, [&](auto n) {
             auto *kernel = top ? slice_kernel<T, V, decltype(n)::value, true> : slice_kernel<T, V, decltype(n)::value, false>;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * slices)), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
-            if (slices > 1) hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)rows), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
+            hipLaunchKernelGGL(kernel, grid_of(rows * slices), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
+            if (slices > 1) hipLaunchKernelGGL((join_kernel<T>), grid_of(rows), dim3(kThreads), 0, st, r, tok, out, slices, parts, best);
             return launched();
         });
     });
@@ -941,7 +946,7 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
         const int32_t slices = slices_of(vocab, V, nv);
         if (rows * slices > INT32_MAX) return (int)CP_ERR_SIZE;
         return by_loads(nv, [&](auto n) {
-            hipLaunchKernelGGL((gradient_kernel<T, V, decltype(n)::value>), dim3((unsigned)(rows * slices)), dim3(kThreads), 0, st, r, tok, stats, d,
+            hipLaunchKernelGGL((gradient_kernel<T, V, decltype(n)::value>), grid_of(rows * slices), dim3(kThreads), 0, st, r, tok, stats, d,
                                (T *)dlogits, ldd, slices, (size_t)rows * vocab * sizeof(T) > kStreamed);
             return launched();
         });

@@ -29,3 +29,17 @@ def test_tokens_at_places_that_begin_a_row_s_last_vector(rows, vocab, kind, give
     for _ in range(3):
         again = cpe.cp_token_logprobs_backward(d["logits"], d["tokens"], fwd["stats"], d["dlogp"], dentropy=d["dentropy"], scale=0.8, allow=allow)
         assert torch.equal(again["dlogits"], bwd["dlogits"])
+
+
+def test_more_rows_than_a_grid_s_first_dimension_has_threads_for():
+    rows, vocab = 2 ** 24 + 3, 257          # a workgroup of 256 threads each: 2^32 threads and more
+    g = torch.Generator(device=DEV).manual_seed(5)
+    x = torch.empty(rows, vocab, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    tok = torch.randint(0, vocab, (rows, 2), generator=g, device=DEV, dtype=torch.int32)
+    dlogp = torch.ones(1, 2, device=DEV).expand(rows, 2)
+    fwd = cpe.cp_token_logprobs(x, tok, top=2)
+    grad = cpe.cp_token_logprobs_backward(x, tok, fwd["stats"], dlogp)["dlogits"]
+    for lo, hi in ((0, 3), (2 ** 22 - 2, 2 ** 22 + 2), (2 ** 23 - 2, 2 ** 23 + 2), (2 ** 24 - 2, rows)):
+        one = cpe.cp_token_logprobs(x[lo:hi], tok[lo:hi], top=2)
+        assert all(torch.equal(fwd[k][lo:hi], one[k]) for k in ("logp", "entropy", "stats", "top_logp", "top_idx")), lo
+        assert torch.equal(grad[lo:hi], cpe.cp_token_logprobs_backward(x[lo:hi], tok[lo:hi], one["stats"], dlogp[lo:hi])["dlogits"]), lo
