@@ -219,14 +219,15 @@ struct Place : Shape<T> {
     int lane, side, wave, run;
     bool live;
 
+    // (false: there is nothing for this workgroup, which is one of those that round a grid up)
     template <int RUN>
-    __device__ __forceinline__ void take(const Scan &s, bool backward) {
+    __device__ __forceinline__ bool take(const Scan &s, bool backward) {
         __shared__ uint32_t ticket;
         lane = threadIdx.x & (kLanes - 1);
         side = threadIdx.x / kLanes & (kSides - 1);
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         run = wave * kSides + side;
-        uint32_t n = blockIdx.x;
+        uint32_t n = group_number();
         if (s.ticket) {
             // in the order in which workgroups come to life: one waits for none but those that live already
             if (threadIdx.x == 0) ticket = atomicAdd(s.ticket, 1u);
@@ -235,12 +236,14 @@ struct Place : Shape<T> {
         }
         tile = n / (uint32_t)s.strips;
         strip = (int32_t)(n - (uint32_t)tile * (uint32_t)s.strips);
+        if (tile >= s.tiles) return false;
         if (backward) tile = s.tiles - 1 - tile;
         wave0 = tile * (kRuns * RUN) + wave * (kSides * RUN);
         p0 = wave0 + side * RUN;
         c = (strip * kLanes + lane) * V;
         live = c < s.width;
         c = live ? min(c, s.width - V) : 0;
+        return true;
     }
     __device__ __forceinline__ uint64_t *word(const Scan &s, int64_t of) const { return s.words + ((of * s.strips + strip) * kLanes + lane) * V; }
 };
@@ -476,11 +479,11 @@ template <typename T, int V, int SPAN, bool STREAM>
 __global__ __launch_bounds__(kWaves *kWave, 4) void scan_kernel(Scan s, T *h, int64_t ldh, float *last, float *carry, int32_t *status) {
     constexpr int RUN = SPAN / Shape<T>::kSides, kRuns = Shape<T>::kRuns;
     Place<T, V> p;
-    p.template take<RUN>(s, false);
+    if (!p.template take<RUN>(s, false)) return;
     const Sequences &seq = s.seq;
     if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan<T, V, SPAN, STREAM, true>(s, p, h, ldh, last, carry);
     else scan<T, V, SPAN, STREAM, false>(s, p, h, ldh, last, carry);
-    if (status && blockIdx.x == 0) check_sequences(seq, status);
+    if (status && p.tile == 0 && p.strip == 0) check_sequences(seq, status);
     // a sequence without rows ends in the state that it begins with
     if (last && p.live && (seq.ptr || seq.each == 0)) {
         for (int64_t j = p.tile * kRuns + p.run; j < seq.count; j += s.tiles * kRuns) {
@@ -618,12 +621,12 @@ template <typename T, int V, bool STREAM>
 __global__ __launch_bounds__(kWaves *kWave, 4) void scan_backward_kernel(Scan s, Gradient<T> g, int32_t *status) {
     constexpr int RUN = Shape<T>::kBackwardRun, kRuns = Shape<T>::kRuns, kLanes = Shape<T>::kLanes;
     Place<T, V> p;
-    p.template take<RUN>(s, true);
+    if (!p.template take<RUN>(s, true)) return;
     const Sequences &seq = s.seq;
     float sum[V];                        // of df over the lane's rows
     if (is_inside(seq, p.tile * (kRuns * RUN), kRuns * RUN)) scan_backward<T, V, STREAM, true>(s, g, p, sum);
     else scan_backward<T, V, STREAM, false>(s, g, p, sum);
-    if (status && blockIdx.x == 0) check_sequences(seq, status);
+    if (status && p.tile == s.tiles - 1 && p.strip == 0) check_sequences(seq, status);
     if (g.dbias_part) {
         __shared__ float lds[kWaves][V][kLanes];
 #pragma unroll
@@ -804,7 +807,7 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
             }
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
             if (s.ticket) clear_words(s, strip, kLooks * Shape<T>::kSides, st);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
+            hipLaunchKernelGGL(kernel, grid_of(s.tiles * s.strips), dim3(kWaves * kWave), 0, st, s, (T *)h, ldh, last, carry,
                                seq_ptr ? status_out : nullptr);
             return launched();
         };
@@ -845,7 +848,7 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
             auto *kernel = past_caches(rows, width, sizeof(T), 2) ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>;
             if (s.tiles * s.strips > INT32_MAX) return (int)CP_ERR_SIZE;
             if (s.ticket) clear_words(s, strip, kLooks * Shape<T>::kSides, st);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(s.tiles * s.strips)), dim3(kWaves * kWave), 0, st, s,
+            hipLaunchKernelGGL(kernel, grid_of(s.tiles * s.strips), dim3(kWaves * kWave), 0, st, s,
                                Gradient<T>{(const T *)dh, lddh, dlast, carry, (T *)df, (T *)dx, lddf, lddx, part, dh0}, seq_ptr ? status_out : nullptr);
             if (dbias && !alone)
                 hipLaunchKernelGGL(column_sum_kernel, dim3((width + 15) / 16), dim3(1024), 0, st, part, s.tiles, width, dbias);

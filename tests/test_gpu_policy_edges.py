@@ -1,10 +1,10 @@
 """The operators of a learned placement policy at the borders of what their kernels divide among workgroups."""
-import numpy as np
 import pytest
 import torch
 
 import paper_1711_01912_amd as cpe
 import test_gpu_token_logprobs as L
+from policy_util import half_step, near, recurrence
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -43,3 +43,23 @@ def test_more_rows_than_a_grid_s_first_dimension_has_threads_for():
         one = cpe.cp_token_logprobs(x[lo:hi], tok[lo:hi], top=2)
         assert all(torch.equal(fwd[k][lo:hi], one[k]) for k in ("logp", "entropy", "stats", "top_logp", "top_idx")), lo
         assert torch.equal(grad[lo:hi], cpe.cp_token_logprobs_backward(x[lo:hi], tok[lo:hi], one["stats"], dlogp[lo:hi])["dlogits"]), lo
+
+
+def test_the_gradient_of_as_many_rows_as_there_may_be():
+    # 2^23 tiles of 512 threads: as many threads as a dimension of a grid may not have
+    rows = 2 ** 31 - 1
+    g = torch.Generator(device=DEV).manual_seed(6)
+    f, x, dh = (torch.empty(rows, 1, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(3))
+    cuts = [0, 700, rows - 900, rows]
+    ptr = torch.tensor(cuts, dtype=torch.int32, device=DEV)
+    dlast = torch.randn(3, 1, generator=g, device=DEV)
+    fwd = cpe.cp_recurrence(f, x, seq_ptr=ptr, want_last=True, want_carry=True)
+    bwd = cpe.cp_recurrence_backward(dh, f, x, fwd["carry"], seq_ptr=ptr, dlast=dlast)
+    got = {"h": fwd["h"], "df": bwd["df"], "dx": bwd["dx"]}
+    for i, (lo, hi) in enumerate(((0, 700), (0, 0), (rows - 900, rows))):
+        if lo == hi:
+            continue
+        ref, tol = recurrence(f[lo:hi], x[lo:hi], [0, hi - lo], dh=dh[lo:hi], dlast=dlast[i:i + 1])
+        for key, t in got.items():
+            near(t[lo:hi], ref[key], tol[key] + half_step(t.dtype, ref[key]), f"rows from {lo} {key}")
+        near(fwd["last"][i], ref["last"][0], tol["last"][0] + half_step(torch.float32, ref["last"][0]), f"last {i}")
