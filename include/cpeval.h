@@ -500,6 +500,7 @@ int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *s
 #define CP_RECURRENCE_CHUNK      128
 #define CP_RECURRENCE_MAX_WIDTH  65536
 #define CP_RECURRENCE_MAX_DISTANCE (1 << 24)   /* elements from a row to the next */
+#define CP_RECURRENCE_MAX_PACKED 0x7ffffc00    /* sequences that seq_ptr can cut the rows into */
 
 /*
  * Gated linear recurrence along `rows` rows of `width` channels, for each channel on its own:
@@ -517,9 +518,9 @@ int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *s
  *   carry         [ceil(rows / CP_RECURRENCE_CHUNK)][width] for the backward pass, or NULL
  *   status_out    device int32, required with seq_ptr: CP_STATUS_BAD_SEQUENCE after the stream has
  *                 drained where seq_ptr is not what it has to be (no access leaves the arrays)
- * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, width, num_seq < 1, rows no
- * multiple of num_seq without seq_ptr, a distance below width or above CP_RECURRENCE_MAX_DISTANCE), CP_ERR_NULL,
- * CP_ERR_WORKSPACE, CP_ERR_HIP.  h may not overlap f or x.  An infinite x or state makes its channel NaN from the next
+ * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, width, num_seq < 1 or, with
+ * seq_ptr, above CP_RECURRENCE_MAX_PACKED, rows no multiple of num_seq without seq_ptr, a distance below
+ * width or above CP_RECURRENCE_MAX_DISTANCE), CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.  h may not overlap f or x.  An infinite x or state makes its channel NaN from the next
  * row to the sequence's end; nothing passes from one sequence or channel to another.
  */
 int cp_recurrence_workspace_bytes(int64_t rows, int32_t width, int backward, size_t *out_bytes);
@@ -594,6 +595,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
 #define CP_TOKEN_I64 8
 #define CP_LOGPROBS_MAX_VOCAB (1 << 26)
 #define CP_LOGPROBS_MAX_TOP   64
+#define CP_LOGPROBS_MAX_GIVEN 0x7ffffc00   /* tokens of a row */
 
 /*
  * Log probabilities of given tokens, with the rows' entropy and their best alternatives, under
@@ -602,7 +604,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
  *   logits        [rows][vocab] of `type`; scale > 0 (1 / temperature)
  *   allow         uint64 [rows][ceil(vocab / 64)], bit i of word w = place 64 w + i may be taken, or NULL
  *                 (all).  What lies at a place that may not is not looked at.
- *   given, tokens `given` tokens of each row: token g of row i at i * token_row_stride + g * token_stride, of
+ *   given, tokens `given` tokens of each row, at most CP_LOGPROBS_MAX_GIVEN: token g of row i at i * token_row_stride + g * token_stride, of
  *                 CP_TOKEN_*.  cp_eval's assignments of a batch of partitions are such tokens, in either
  *                 layout.  A negative token is ignored: its logp is 0 and it has no gradient.
  *   logp          [rows][given]; -inf at a place that is not allowed

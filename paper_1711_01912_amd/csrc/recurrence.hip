@@ -101,7 +101,7 @@ struct Starts {
         const int32_t lo = wave0 > 0 ? s.begun(wave0 - 1) : 0;
         bool some = false;
         for (int32_t j = lo; j < s.count; j += kWave) {
-            const int64_t p = j + lane < s.count ? s.start(j + lane) : INT64_MAX;
+            const int64_t p = lane < s.count - j ? s.start(j + lane) : INT64_MAX;
             const bool in = p >= wave0 && p <= wave0 + kSpan && p <= s.rows;
             if (__ballot(in)) {
                 if (!some) {
@@ -720,7 +720,8 @@ bool distances(int32_t width, std::initializer_list<int64_t> ld) {
 int check_scan(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_ptr, int type, int reverse) {
     if (!known_type(type) || (reverse != 0 && reverse != 1)) return CP_ERR_ARG;
     if (rows < 0 || rows > INT32_MAX || width < 1 || width > CP_RECURRENCE_MAX_WIDTH || num_seq < 1) return CP_ERR_SIZE;
-    if (!seq_ptr && rows % num_seq) return CP_ERR_SIZE;
+    // (a workgroup's loops over the pointers count on by its threads, in 32 bits)
+    if (seq_ptr ? num_seq > CP_RECURRENCE_MAX_PACKED : rows % num_seq != 0) return CP_ERR_SIZE;
     return CP_OK;
 }
 

@@ -783,7 +783,9 @@ int loads_of(int64_t rows, int32_t vocab, int v) {
 
 int check_rows(int64_t rows, int32_t vocab, int type, int32_t given, int token_type) {
     if (!known_type(type) || (given > 0 && token_type != CP_TOKEN_U8 && token_type != CP_TOKEN_I32 && token_type != CP_TOKEN_I64)) return CP_ERR_ARG;
-    if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > CP_LOGPROBS_MAX_VOCAB || given < 0) return CP_ERR_SIZE;
+    // (a row's lanes go on by up to kAhead fours each, together 1,024 tokens, and count them in 32 bits)
+    static_assert(CP_LOGPROBS_MAX_GIVEN - 1ll + kAhead * 4 * kWave <= INT32_MAX, "the last step ends behind the last token");
+    if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > CP_LOGPROBS_MAX_VOCAB || given < 0 || given > CP_LOGPROBS_MAX_GIVEN) return CP_ERR_SIZE;
     return CP_OK;
 }
 

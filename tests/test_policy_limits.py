@@ -1,0 +1,19 @@
+"""Limits of the policy operators' entry points, on the CPU: every call here returns before anything is launched (the
+addresses are made up)."""
+import torch
+
+from test_policy_refusals import LOGP, LOGP_BACK, P, SCAN, SCAN_BACK, SIZE, lib, with_  # noqa: F401
+
+NO_GPU = not torch.cuda.is_available()       # (elsewhere a call with made-up addresses would be launched)
+
+
+def test_counts_that_end_near_the_largest_number(lib):
+    # a kernel's counter goes on by up to 1,024 from the last of them, and would not pass the end but begin again below zero
+    most = 0x7ffffc00
+    assert lib.cp_recurrence(*with_(SCAN, ptr=P, status=P, num_seq=most + 1)) == SIZE
+    assert lib.cp_recurrence_backward(*with_(SCAN_BACK, ptr=P, status=P, num_seq=most + 1)) == SIZE
+    assert lib.cp_token_logprobs(*with_(LOGP, vocab=8, given=most + 1)) == SIZE
+    assert lib.cp_token_logprobs_backward(*with_(LOGP_BACK, vocab=8, given=most + 1)) == SIZE
+    if NO_GPU:
+        assert lib.cp_recurrence(*with_(SCAN, ptr=P, status=P, num_seq=most)) != SIZE
+        assert lib.cp_token_logprobs(*with_(LOGP, vocab=8, given=most)) != SIZE
