@@ -601,7 +601,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
  * Log probabilities of given tokens, with the rows' entropy and their best alternatives, under
  * softmax(scale * logits) over the allowed places of each row.
  *
- *   logits        [rows][vocab] of `type`; scale > 0 (1 / temperature)
+ *   logits        [rows][vocab] of `type`; scale > 0 (1 / temperature), so that scale / ln 2 is a finite float
  *   allow         uint64 [rows][ceil(vocab / 64)], bit i of word w = place 64 w + i may be taken, or NULL
  *                 (all).  What lies at a place that may not is not looked at.
  *   given, tokens `given` tokens of each row, at most CP_LOGPROBS_MAX_GIVEN: token g of row i at i * token_row_stride + g * token_stride, of

@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 
 #include "policy.hpp"
@@ -789,6 +790,9 @@ int check_rows(int64_t rows, int32_t vocab, int type, int32_t given, int token_t
     return CP_OK;
 }
 
+// (in units of ln 2 a scale above 2.358e38 is infinite, and a row's largest logit, 0 units from itself, a NaN)
+bool scale_fits(float scale) { return scale > 0.0f && scale * kLog2e <= FLT_MAX; }
+
 // workgroups of the finest slicing that a call of these sizes can take
 int64_t most_slices(int64_t rows, int32_t vocab) {
     if (vocab <= kFew) return 0;
@@ -851,7 +855,7 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
     int rc = check_rows(rows, vocab, type, given, token_type);
     if (rc) return rc;
     if (top < 0 || top > CP_LOGPROBS_MAX_TOP) return CP_ERR_SIZE;
-    if (!(scale > 0.0f) || scale > 3.0e38f) return CP_ERR_ARG;
+    if (!scale_fits(scale)) return CP_ERR_ARG;
     if (!status_out) return CP_ERR_NULL;
     if (rows > 0 && (!logits || !entropy || !stats || (given && (!tokens || !logp)) || (top && (!top_logp || !top_idx)))) return CP_ERR_NULL;
     if (rows > 1 && ld < vocab) return CP_ERR_SIZE;
@@ -905,7 +909,7 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
                                const float *dentropy, int64_t dentropy_stride, void *dlogits, int64_t ldd, void *stream) {
     int rc = check_rows(rows, vocab, type, given, token_type);
     if (rc) return rc;
-    if (!(scale > 0.0f) || scale > 3.0e38f) return CP_ERR_ARG;
+    if (!scale_fits(scale)) return CP_ERR_ARG;
     if (rows > 0 && (!logits || !stats || !dlogits || (given && (!tokens || !dlogp)))) return CP_ERR_NULL;
     if (rows > 1 && (ld < vocab || ldd < vocab)) return CP_ERR_SIZE;
     if (rows == 0) return CP_OK;

@@ -63,3 +63,9 @@ def test_the_gradient_of_as_many_rows_as_there_may_be():
         for key, t in got.items():
             near(t[lo:hi], ref[key], tol[key] + half_step(t.dtype, ref[key]), f"rows from {lo} {key}")
         near(fwd["last"][i], ref["last"][0], tol["last"][0] + half_step(torch.float32, ref["last"][0]), f"last {i}")
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e30, 2.3e38])
+def test_scales_from_end_to_end(scale):
+    for vocab in (9, 4000):
+        L.compare(L.make(4, vocab, "fp32", 3, seed=vocab), f"{vocab} {scale}", scale=scale, top=3)
