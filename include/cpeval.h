@@ -570,6 +570,7 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
  *   y             NULL: no block yet, z is the norm of x (gate, w_post NULL; r may be)
  *   gate          NULL: 1;   w_post NULL: u = y
  *   stats         [2][rows] for the backward pass (1 / rms of y and of r), or NULL
+ * r and z may each take the place of an input whose elements are as wide (its address and distance).
  * Errors: CP_ERR_ARG, CP_ERR_SIZE (rows < 0, width, a distance below width), CP_ERR_NULL, CP_ERR_HIP.
  */
 int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int weight_type, int gate_act,
@@ -581,6 +582,7 @@ int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int wei
  * Gradient of cp_norm_gate: dr (of r, or NULL: 0) and dz (of z) in; dx, dy, dgate, dw_pre, dw_post out,
  * each of the type of what it is the gradient of; dy is required with y, the last three may be
  * NULL.  The inputs and stats are those of the forward call; workspace is needed for dw_pre and dw_post.
+ * dx, dy and dgate may each take the place of an input, as cp_norm_gate's r and z.
  */
 int cp_norm_gate_backward_workspace_bytes(int64_t rows, int32_t width, size_t *out_bytes);
 int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type, int weight_type, int gate_act,

@@ -122,6 +122,9 @@ __global__ __launch_bounds__(Sharing<NT>::kThreads) void joint_kernel(Joint j, T
 #pragma unroll
             for (int k = 0; k < V; k++) w_post[i][k] = 1.0f;
     }
+    // r in the place of an input: the row's last vector, moved back, reads what its neighbour is to write (z comes after a sum over
+    // the row's threads, and so does r where there is one of y's)
+    const bool over = r_out && (r_out == j.x || (const void *)r_out == j.y || (const void *)r_out == j.gate);
     int slot = 0;
     for (int64_t row = Sharing<NT>::first(); row < j.rows; row += Sharing<NT>::step(), slot ^= 2) {
         Raw<TS, V> x[NV];
@@ -140,6 +143,8 @@ __global__ __launch_bounds__(Sharing<NT>::kThreads) void joint_kernel(Joint j, T
 #pragma unroll
                 for (int k = 0; k < V; k++) sum = k >= at.skip[i] ? fmaf(y[i][k], y[i][k], sum) : sum;
             ry = 1.0f / sqrtf(group_sum<NT>(sum, slot) * inv + j.eps);
+        } else if (NT > kWave && over) {
+            __syncthreads();
         }
         float r[NV][V], sum = 0.0f;
 #pragma unroll

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_1711_01912_amd as cpe
+import test_gpu_norm_gate as N
 import test_gpu_token_logprobs as L
 from policy_util import half_step, near, recurrence
 
@@ -69,3 +70,21 @@ def test_the_gradient_of_as_many_rows_as_there_may_be():
 def test_scales_from_end_to_end(scale):
     for vocab in (9, 4000):
         L.compare(L.make(4, vocab, "fp32", 3, seed=vocab), f"{vocab} {scale}", scale=scale, top=3)
+
+
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("rows,width,kind", [(700, 1111, "fp16"), (300, 4101, "bf16"), (40, 5003, "fp32"), (9, 16381, "bf16"), (1000, 70, "bf16"), (200, 301, "fp16"), (50, 5, "fp32")])
+def test_outputs_of_a_joint_in_the_place_of_its_inputs(rows, width, kind, post):
+    d = N.make(rows, width, kind, kind, seed=width)
+    kw = dict(w_pre=d["w_pre"], w_post=d["w_post"] if post else None, scale=0.5)
+    fwd = cpe.cp_norm_gate(d["x"], d["y"], d["gate"], want_stats=True, **kw)
+    bwd = cpe.cp_norm_gate_backward(d["dr"], d["dz"], d["x"], d["y"], d["gate"], stats=fwd["stats"], **kw)
+    for r, z in (("x", "y"), ("y", "gate"), ("gate", "x"), ("x", None), (None, "x")):
+        c = {k: d[k].clone() for k in ("x", "y", "gate")}
+        got = cpe.cp_norm_gate(c["x"], c["y"], c["gate"], out={k: c[v] for k, v in (("r", r), ("z", z)) if v}, **kw)
+        assert torch.equal(got["r"], fwd["r"]) and torch.equal(got["z"], fwd["z"]), (r, z)
+    for dx, dy, dgate in (("x", "y", "gate"), ("dr", "dz", "x"), ("y", "x", "dr")):
+        c = {k: d[k].clone() for k in ("x", "y", "gate", "dr", "dz")}
+        got = cpe.cp_norm_gate_backward(c["dr"], c["dz"], c["x"], c["y"], c["gate"], stats=fwd["stats"],
+                                        out={"dx": c[dx], "dy": c[dy], "dgate": c[dgate]}, **kw)
+        assert all(torch.equal(got[k], bwd[k]) for k in bwd), (dx, dy, dgate)
