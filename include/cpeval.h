@@ -488,10 +488,11 @@ int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *s
  * a distance ld between rows, in elements, at least the row's length.  Element types are
  * CP_TYPE_*; vectors of parameters, states and statistics are float where nothing else is said.
  * States, sums and statistics are formed in 32 bits or more and a result is rounded once, to its
- * type.  The calls only enqueue work on `stream`, allocate nothing and record no memset or copy,
- * so that they may be captured into a graph; results do not depend on the order in which
- * workgroups run.  Workspaces are scratch, 256-byte aligned; two calls that may overlap in time
- * need distinct ones.
+ * type.  Results share no memory with inputs or with each other (CP_ERR_ARG) except where it is
+ * said; the rows of slices of one buffer may lie between each other.  The calls only enqueue work
+ * on `stream`, allocate nothing and record no memset or copy, so that they may be captured into a
+ * graph; results do not depend on the order in which workgroups run.  Workspaces are scratch,
+ * 256-byte aligned; two calls that may overlap in time need distinct ones.
  */
 #define CP_TYPE_F32  0
 #define CP_TYPE_BF16 1
@@ -520,8 +521,9 @@ int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *s
  *                 drained where seq_ptr is not what it has to be (no access leaves the arrays)
  * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, width, num_seq < 1 or, with
  * seq_ptr, above CP_RECURRENCE_MAX_PACKED, rows no multiple of num_seq without seq_ptr, a distance below
- * width or above CP_RECURRENCE_MAX_DISTANCE), CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.  h may not overlap f or x.  An infinite x or state makes its channel NaN from the next
- * row to the sequence's end; nothing passes from one sequence or channel to another.
+ * width or above CP_RECURRENCE_MAX_DISTANCE), CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.  An infinite
+ * x or state makes its channel NaN from the next row to the sequence's end; nothing passes from one sequence
+ * or channel to another.
  */
 int cp_recurrence_workspace_bytes(int64_t rows, int32_t width, int backward, size_t *out_bytes);
 int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_ptr, int type, int reverse,
@@ -546,6 +548,7 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
  * One more row of each of num_seq sequences: state [num_slots][width] is updated in place and
  * h [num_seq][width] gets the new states.  slots int32 [num_seq]: the state row of each sequence, all
  * different, or NULL (row i for sequence i); a negative slot leaves its sequence out (its h is 0).
+ * h may take the place of f or x.
  * status_out: device int32, required with slots (CP_STATUS_BAD_SLOT).  Errors as cp_recurrence's.
  */
 int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, int64_t ldf, const void *x, int64_t ldx,
@@ -597,6 +600,7 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
 #define CP_TOKEN_I64 8
 #define CP_LOGPROBS_MAX_VOCAB (1 << 26)
 #define CP_LOGPROBS_MAX_TOP   64
+#define CP_LOGPROBS_IN_PLACE  256
 #define CP_LOGPROBS_MAX_GIVEN 0x7ffffc00   /* tokens of a row */
 
 /*
@@ -632,7 +636,8 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
  * gradient of logp, at i * dlogp_row_stride + g * dlogp_stride (a stride of 0: the same for all rows or
  * tokens), dentropy that of entropy at i * dentropy_stride, or NULL; stats are the forward call's.  Tokens
  * that are ignored, out of range or without a probability pass nothing on; places that are not allowed
- * and rows with nothing allowed get 0.  The alternatives have no gradient.
+ * and rows with nothing allowed get 0.  The alternatives have no gradient.  Of up to CP_LOGPROBS_IN_PLACE
+ * places a row, dlogits may take the place of the logits.
  */
 int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, float scale,
                                const uint64_t *allow, int32_t given, const void *tokens, int token_type,

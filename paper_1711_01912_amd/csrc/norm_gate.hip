@@ -394,6 +394,12 @@ int cp_norm_gate(int64_t rows, int32_t width, int stream_type, int type, int wei
     if (rows > 0 && !y && (gate || w_post)) return CP_ERR_ARG;      // (tensors without rows have no address)
     if (!w_pre || (rows > 0 && (!x || !z || (y && !r)))) return CP_ERR_NULL;
     if (rows > 1 && (ldx < width || ldz < width || (y && ldy < width) || (gate && ldg < width) || (r && ldr < width))) return CP_ERR_SIZE;
+    const auto of = [&](const void *at, int64_t ld, int t) { return matrix_at(at, rows, width, ld, t); };
+    const Extent sums = vector_at(stats, 2 * rows);
+    if (in_the_way({of(x, ldx, stream_type), of(y, ldy, type), of(gate, ldg, type)}, {of(r, ldr, stream_type), of(z, ldz, type), sums}, true) ||
+        in_the_way({vector_at(w_pre, width, type_bytes(weight_type)), vector_at(w_post, width, type_bytes(weight_type))},
+                   {of(r, ldr, stream_type), of(z, ldz, type), sums}))
+        return CP_ERR_ARG;
     if (rows == 0) return CP_OK;
     const Joint j{rows, width, x, y, gate, ldx, ldy, ldg, w_pre, w_post, weight_type, gate_act, scale, eps, stats};
     return by_types(stream_type, type, [&](auto ts, auto tb) {
@@ -435,6 +441,14 @@ int cp_norm_gate_backward(int64_t rows, int32_t width, int stream_type, int type
         if (!workspace && rows > 0) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < 2 * one) return CP_ERR_WORKSPACE;
     }
+    const auto of = [&](const void *at, int64_t ld, int t) { return matrix_at(at, rows, width, ld, t); };
+    const auto weight = [&](const void *at) { return vector_at(at, width, type_bytes(weight_type)); };
+    const Extent e_dr = of(dr, lddr, stream_type), e_dz = of(dz, lddz, type), e_x = of(x, ldx, stream_type), e_y = of(y, ldy, type),
+                 e_gate = of(gate, ldg, type), e_dx = of(dx, lddx, stream_type), e_dy = of(dy, lddy, type), e_dgate = of(dgate, lddg, type);
+    if (in_the_way({e_dr, e_dz, e_x, e_y, e_gate}, {e_dx, e_dy, e_dgate}, true) ||
+        in_the_way({vector_at(stats, 2 * rows), weight(w_pre), weight(w_post)}, {e_dx, e_dy, e_dgate}) ||
+        in_the_way({e_dr, e_dz, e_x, e_y, e_gate, vector_at(stats, 2 * rows), e_dx, e_dy, e_dgate}, {weight(dw_pre), weight(dw_post)}))
+        return CP_ERR_ARG;
     float *part_pre = dw_pre ? (float *)workspace : nullptr;
     float *part_post = dw_post ? (float *)((char *)workspace + one) : nullptr;
     const Joint j{rows, width, x, y, gate, ldx, ldy, ldg, w_pre, w_post, weight_type, gate_act, scale, 0.0f, (float *)stats};

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 #include <type_traits>
 
 #include "../../include/cpeval.h"
@@ -132,6 +133,48 @@ inline size_t type_bytes(int type) { return type == CP_TYPE_F32 ? 4 : 2; }
 inline bool known_type(int type) { return type == CP_TYPE_F32 || type == CP_TYPE_BF16 || type == CP_TYPE_F16; }
 inline size_t align_up(size_t v) { return (v + kPolicyAlign - 1) / kPolicyAlign * kPolicyAlign; }
 inline int launched() { return hipGetLastError() == hipSuccess ? CP_OK : CP_ERR_HIP; }
+
+// An array of rows in memory (of a vector: one row), for whether a result lies where something else does.  at: null, if there is
+// none
+struct Extent {
+    const void *at;
+    int64_t rows, bytes, pitch;          // of a row; from a row to the next
+    size_t each;                         // of an element
+};
+inline Extent matrix_at(const void *at, int64_t rows, int32_t width, int64_t ld, int type) {
+    const int64_t each = (int64_t)type_bytes(type);
+    return {at, rows, width * each, (rows > 1 ? ld : width) * each, (size_t)each};
+}
+inline Extent vector_at(const void *at, int64_t count, size_t each = sizeof(float)) { return {at, 1, count * (int64_t)each, count * (int64_t)each, each}; }
+
+// whether they share any byte (the rows of two slices of one buffer lie between each other and share none)
+inline bool share(const Extent &a, const Extent &b) {
+    if (!a.at || !b.at || a.rows < 1 || b.rows < 1 || a.bytes < 1 || b.bytes < 1) return false;
+    const int64_t pa = (int64_t)(uintptr_t)a.at, pb = (int64_t)(uintptr_t)b.at;
+    if (pa + (a.rows - 1) * a.pitch + a.bytes <= pb || pb + (b.rows - 1) * b.pitch + b.bytes <= pa) return false;
+    const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if ((a.rows == 1 && b.rows == 1) || pitch < a.bytes || pitch < b.bytes || (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch)) return true;
+    // b's first row begins `off` bytes behind the start of a's row number `row`, if a had rows without end both ways
+    int64_t row = (pb - pa) / pitch, off = (pb - pa) % pitch;
+    if (off < 0) row--, off += pitch;
+    auto meet = [&](int64_t first) { return first < a.rows && first + b.rows > 0; };
+    return (off < a.bytes && meet(row)) || (off + b.bytes > pitch && meet(row + 1));
+}
+// whether they are one and the same, element upon element
+inline bool same(const Extent &a, const Extent &b) {
+    return a.at == b.at && a.rows == b.rows && a.bytes == b.bytes && a.pitch == b.pitch && a.each == b.each;
+}
+
+// Whether a result shares memory with another result or with an input; `in_place`: it may be one of the inputs
+inline bool in_the_way(std::initializer_list<Extent> in, std::initializer_list<Extent> out, bool in_place = false) {
+    for (const Extent *o = out.begin(); o != out.end(); o++) {
+        for (const Extent &i : in)
+            if (share(i, *o) && !(in_place && same(i, *o))) return true;
+        for (const Extent *p = out.begin(); p != o; p++)
+            if (share(*p, *o)) return true;
+    }
+    return false;
+}
 
 // calls f with a value of the element type that `type` names
 template <typename F>

@@ -725,6 +725,8 @@ int check_scan(int64_t rows, int32_t width, int32_t num_seq, const int32_t *seq_
     return CP_OK;
 }
 
+int64_t chunks_of(int64_t rows) { return (rows + CP_RECURRENCE_CHUNK - 1) / CP_RECURRENCE_CHUNK; }
+
 int64_t tiles_of(int64_t rows, int span) {
     const int64_t tile = kWaves * span;
     return std::max<int64_t>(1, (rows + tile - 1) / tile);
@@ -788,6 +790,13 @@ int cp_recurrence(int64_t rows, int32_t width, int32_t num_seq, const int32_t *s
         if (!workspace) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < words_bytes(rows, width, false)) return CP_ERR_WORKSPACE;
     }
+    // (h in the place of an input is not possible: a strip of channels may read one of its neighbour's.  Nor is last in h0's: a sequence's
+    // end may be known before its first tile has read its start a second time.)
+    const auto matrix = [&](const void *at, int64_t ld) { return matrix_at(at, rows, width, ld, type); };
+    const auto states = [&](const void *at) { return vector_at(at, (int64_t)num_seq * width); };
+    if (in_the_way({matrix(f, ldf), matrix(x, ldx), vector_at(bias, width), states(h0)},
+                   {matrix(h, ldh), states(last), vector_at(carry, chunks_of(rows) * width)}))
+        return CP_ERR_ARG;
     if (rows < 2) ldf = ldx = ldh = width;         // (a single row is no distance from another)
     Scan s{};
     s.seq = {seq_ptr, rows, rows / num_seq, num_seq, reverse != 0};
@@ -831,6 +840,12 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
         if (!workspace) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < words_bytes(rows, width, true) + part_bytes(rows, width)) return CP_ERR_WORKSPACE;
     }
+    const auto matrix = [&](const void *at, int64_t ld) { return matrix_at(at, rows, width, ld, type); };
+    const auto states = [&](const void *at) { return vector_at(at, (int64_t)num_seq * width); };
+    if (in_the_way({matrix(dh, lddh), matrix(f, ldf), matrix(x, ldx), states(dlast), states(h0), vector_at(bias, width),
+                    vector_at(carry, chunks_of(rows) * width)},
+                   {matrix(df, lddf), matrix(dx, lddx), states(dh0), vector_at(dbias, width)}))
+        return CP_ERR_ARG;
     if (rows < 2) lddh = ldf = ldx = lddf = lddx = width;
     // (the sums of a single tile are the whole sums)
     const bool alone = tiles_of(rows, kBackwardSpan) == 1;
@@ -867,6 +882,12 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
     if (num_seq < 0 || num_slots < 1 || width < 1 || width > CP_RECURRENCE_MAX_WIDTH || (!slots && num_seq > num_slots)) return CP_ERR_SIZE;
     if ((num_seq > 0 && (!f || !x || !h)) || !state || (slots && !status_out)) return CP_ERR_NULL;
     if (num_seq > 1 && !distances(width, {ldf, ldx, ldh})) return CP_ERR_SIZE;
+    const auto matrix = [&](const void *at, int64_t ld) { return matrix_at(at, num_seq, width, ld, type); };
+    const Extent states = vector_at(state, (int64_t)num_slots * width);
+    if (in_the_way({matrix(f, ldf), matrix(x, ldx)}, {matrix(h, ldh)}, true) ||
+        in_the_way({matrix(f, ldf), matrix(x, ldx), vector_at(bias, width), vector_at(slots, num_seq, sizeof(int32_t))}, {states}) ||
+        in_the_way({states, vector_at(bias, width), vector_at(slots, num_seq, sizeof(int32_t))}, {matrix(h, ldh)}))
+        return CP_ERR_ARG;
     const hipStream_t st = (hipStream_t)stream;
     if (slots) hipLaunchKernelGGL(set_status_kernel, dim3(1), dim3(1), 0, st, status_out, CP_STATUS_OK);
     if (num_seq == 0) return launched();

@@ -769,7 +769,7 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
 __global__ void clear_status_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 
 constexpr int kMostLoads = 4;
-constexpr int32_t kFew = 256;            // up to so many places a row is some lanes'
+constexpr int32_t kFew = CP_LOGPROBS_IN_PLACE;       // up to so many places a row is some lanes'
 constexpr size_t kColumnBytes = 72u << 10;   // of LDS for a workgroup's columns: two of them on a compute unit
 constexpr int kSets = 4;
 constexpr int32_t slice_places(int v, int nv) { return kThreads * v * nv; }
@@ -863,6 +863,10 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
     cp_token_logprobs_workspace_bytes(rows, vocab, top, &need);
     if (need && !workspace) return CP_ERR_NULL;
     if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
+    const Extent in = matrix_at(logits, rows, vocab, ld, type);
+    if (in_the_way({in}, {vector_at(logp, rows * given), vector_at(entropy, rows), vector_at(stats, 3 * rows), vector_at(top ? top_logp : nullptr, rows * top),
+                          vector_at(top ? top_idx : nullptr, rows * top, sizeof(int32_t))}))
+        return CP_ERR_ARG;
     const hipStream_t st = (hipStream_t)stream;
     auto clear = [&] { hipLaunchKernelGGL(clear_status_kernel, dim3(1), dim3(1), 0, st, status_out); };
     if (rows == 0) {
@@ -912,6 +916,10 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
     if (!scale_fits(scale)) return CP_ERR_ARG;
     if (rows > 0 && (!logits || !stats || !dlogits || (given && (!tokens || !dlogp)))) return CP_ERR_NULL;
     if (rows > 1 && (ld < vocab || ldd < vocab)) return CP_ERR_SIZE;
+    // (a row of few places is read and written by one group of lanes; of many, by workgroups that each read the logits of all its tokens)
+    if (in_the_way({matrix_at(logits, rows, vocab, ld, type)}, {matrix_at(dlogits, rows, vocab, ldd, type)}, vocab <= kFew) ||
+        in_the_way({vector_at(stats, 3 * rows)}, {matrix_at(dlogits, rows, vocab, ldd, type)}))
+        return CP_ERR_ARG;
     if (rows == 0) return CP_OK;
     const Rows r{rows, vocab, logits, ld, scale, scale * kLog2e, allow, (vocab + 63) / 64};
     const Tokens tok{tokens, token_type, token_row_stride, token_stride, given};

@@ -7,7 +7,9 @@ the library's kernels called on ``stream`` (default: the current one).  Outputs 
 allocated for that stream; inputs of another stream are the caller's to wait for and to keep (``record_stream``).
 Matrices may be views whose rows are further apart than their length (slices of a fused
 projection), as long as a row's elements are contiguous.  ``out`` may carry preallocated outputs
-under the keys of the result, ``workspace`` a preallocated uint8 tensor.
+under the keys of the result, ``workspace`` a preallocated uint8 tensor.  An output lies apart from the inputs
+(``CpError`` otherwise), but cp_norm_gate's and its gradient's may be an input of as wide elements, ``h`` of
+cp_recurrence_step ``f`` or ``x``, and ``dlogits`` the logits of at most 256 places a row.
 
 The submodule ``autograd`` has the same operators as differentiable functions.
 """

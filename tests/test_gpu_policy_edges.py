@@ -88,3 +88,40 @@ def test_outputs_of_a_joint_in_the_place_of_its_inputs(rows, width, kind, post):
         got = cpe.cp_norm_gate_backward(c["dr"], c["dz"], c["x"], c["y"], c["gate"], stats=fwd["stats"],
                                         out={"dx": c[dx], "dy": c[dy], "dgate": c[dgate]}, **kw)
         assert all(torch.equal(got[k], bwd[k]) for k in bwd), (dx, dy, dgate)
+
+
+def test_a_step_in_the_place_of_its_input():
+    for width in (64, 67):
+        g = torch.Generator().manual_seed(width)
+        f, x, state = (torch.randn(50, width, generator=g).to(DEV) for _ in range(3))
+        want_state = state.clone()
+        want = cpe.cp_recurrence_step(f, x, want_state)["h"]
+        for over in (0, 1):
+            st, fx = state.clone(), [f.clone(), x.clone()]
+            assert torch.equal(cpe.cp_recurrence_step(*fx, st, out={"h": fx[over]})["h"], want) and torch.equal(st, want_state)
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,given", [(3000, 5, 9), (3000, 13, 100), (1000, 64, 30), (777, 200, 300), (300, 256, 1)])
+def test_a_gradient_in_the_place_of_few_logits(rows, vocab, given, kind):
+    d = L.make(rows, vocab, kind, given, seed=vocab, mask=True)
+    allow = L.pack_mask(d["allowed"]).to(DEV)
+    stats = cpe.cp_token_logprobs(d["logits"], d["tokens"], allow=allow)["stats"]
+    want = cpe.cp_token_logprobs_backward(d["logits"], d["tokens"], stats, d["dlogp"], dentropy=d["dentropy"], allow=allow)["dlogits"]
+    x = d["logits"].clone()
+    cpe.cp_token_logprobs_backward(x, d["tokens"], stats, d["dlogp"], dentropy=d["dentropy"], allow=allow, out={"dlogits": x})
+    assert torch.equal(x, want)
+
+
+def test_results_over_inputs_that_are_read_again_are_refused():
+    x = torch.randn(300, 300, device=DEV)
+    with pytest.raises(cpe.CpError):
+        cpe.cp_recurrence(x, x.clone(), out={"h": x})
+    fwd = cpe.cp_recurrence(x, x, want_last=True, want_carry=True)
+    with pytest.raises(cpe.CpError):
+        cpe.cp_recurrence_backward(x.clone(), x, x, fwd["carry"], out={"df": x})
+    with pytest.raises(cpe.CpError):
+        cpe.cp_recurrence(x, x, h0=fwd["last"], want_last=True, out={"last": fwd["last"]})
+    got = cpe.cp_token_logprobs(x)
+    with pytest.raises(cpe.CpError):
+        cpe.cp_token_logprobs_backward(x, None, got["stats"], None, dentropy=got["entropy"], out={"dlogits": x})
