@@ -153,10 +153,10 @@ def _room(workspace, need, device):
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
-def _check(status, flag, text, device):
-    import torch
-    torch.cuda.synchronize(device)
-    if int(status.item()) & flag:
+def _check(status, flag, text, stream):
+    if stream is not None:
+        stream.synchronize()
+    if int(status.item()) & flag:        # (waits for the current stream)
         raise ValueError(text)
 
 
@@ -210,7 +210,7 @@ def cp_recurrence(f, x, *, bias=None, seq_ptr=None, h0=None, reverse=False, want
     if rc:
         raise CpError(rc, "cp_recurrence")
     if check_status and ptr is not None:
-        _check(out["status"], STATUS_BAD_SEQUENCE, "seq_ptr does not rise from 0 to the number of rows", dev)
+        _check(out["status"], STATUS_BAD_SEQUENCE, "seq_ptr does not rise from 0 to the number of rows", stream)
     return out
 
 
@@ -244,7 +244,7 @@ def cp_recurrence_backward(dh, f, x, carry, *, dlast=None, bias=None, seq_ptr=No
     if rc:
         raise CpError(rc, "cp_recurrence_backward")
     if check_status and ptr is not None:
-        _check(out["status"], STATUS_BAD_SEQUENCE, "seq_ptr does not rise from 0 to the number of rows", dev)
+        _check(out["status"], STATUS_BAD_SEQUENCE, "seq_ptr does not rise from 0 to the number of rows", stream)
     return out
 
 
@@ -272,7 +272,7 @@ def cp_recurrence_step(f, x, state, *, bias=None, slots=None, out=None, stream=N
     if rc:
         raise CpError(rc, "cp_recurrence_step")
     if check_status and slots is not None:
-        _check(out["status"], STATUS_BAD_SLOT, "a slot lies behind the last state", dev)
+        _check(out["status"], STATUS_BAD_SLOT, "a slot lies behind the last state", stream)
     return out
 
 
@@ -410,7 +410,7 @@ def cp_token_logprobs(logits, tokens=None, *, scale=1.0, allow=None, top=0, out=
     if rc:
         raise CpError(rc, "cp_token_logprobs")
     if check_status:
-        _check(out["status"], STATUS_BAD_TOKEN, "tokens holds a place >= vocab", dev)
+        _check(out["status"], STATUS_BAD_TOKEN, "tokens holds a place >= vocab", stream)
     return out
 
 

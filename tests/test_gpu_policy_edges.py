@@ -125,3 +125,21 @@ def test_results_over_inputs_that_are_read_again_are_refused():
     got = cpe.cp_token_logprobs(x)
     with pytest.raises(cpe.CpError):
         cpe.cp_token_logprobs_backward(x, None, got["stats"], None, dentropy=got["entropy"], out={"dlogits": x})
+
+
+def test_checked_calls_on_the_current_and_on_another_stream():
+    x = torch.randn(64, 8, device=DEV)
+    tok, ptr = torch.full((64, 3), 2, device=DEV), torch.tensor([0, 9, 64], dtype=torch.int32, device=DEV)
+    state, slots = torch.zeros(64, 8, device=DEV), torch.arange(64, dtype=torch.int32, device=DEV)
+    bad_tok, bad_ptr, bad_slots = torch.full_like(tok, 8), torch.flip(ptr, [0]), slots + 1
+    torch.cuda.synchronize()
+    for stream in (None, torch.cuda.Stream(), None):
+        for _ in range(20):
+            cpe.cp_token_logprobs(x, tok, stream=stream)
+            cpe.cp_recurrence(x, x, seq_ptr=ptr, stream=stream)
+            cpe.cp_recurrence_step(x, x, state, slots=slots, stream=stream)
+            for call in (lambda: cpe.cp_token_logprobs(x, bad_tok, stream=stream), lambda: cpe.cp_recurrence(x, x, seq_ptr=bad_ptr, stream=stream),
+                         lambda: cpe.cp_recurrence_step(x, x, state, slots=bad_slots, stream=stream)):
+                with pytest.raises(ValueError):
+                    call()
+        torch.cuda.synchronize()

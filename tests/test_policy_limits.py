@@ -3,6 +3,7 @@ addresses are made up)."""
 import pytest
 import torch
 
+from paper_1711_01912_amd import policy
 from test_policy_refusals import ARG, LOGP, LOGP_BACK, NORM, NORM_BACK, P, SCAN, SCAN_BACK, SIZE, STEP, lib, with_  # noqa: F401
 
 NO_GPU = not torch.cuda.is_available()       # (elsewhere a call with made-up addresses would be launched)
@@ -106,3 +107,25 @@ def test_places_of_other_types_and_of_few_logits(lib):
         assert lib.cp_token_logprobs_backward(*with_(grad, vocab=256, dlogits=grad["logits"])) != ARG
     assert lib.cp_token_logprobs_backward(*with_(grad, vocab=257, dlogits=grad["logits"])) == ARG
     assert lib.cp_token_logprobs_backward(*with_(grad, vocab=256, dlogits=grad["logits"], ldd=299)) == ARG
+
+
+# ---- the binding ----------------------------------------------------------------------------------------
+
+
+def test_a_status_is_waited_for_on_its_stream_alone(monkeypatch):
+    def never(*args):
+        raise AssertionError("waits for every stream of the device")
+
+    class Stream:
+        waits = 0
+
+        def synchronize(self):
+            self.waits += 1
+
+    monkeypatch.setattr(torch.cuda, "synchronize", never)
+    stream, told, fine = Stream(), torch.tensor([32], dtype=torch.int32), torch.tensor([64], dtype=torch.int32)
+    with pytest.raises(ValueError, match="bad"):
+        policy._check(told, policy.STATUS_BAD_TOKEN, "bad", stream)
+    policy._check(fine, policy.STATUS_BAD_TOKEN, "bad", stream)
+    policy._check(fine, policy.STATUS_BAD_TOKEN, "bad", None)
+    assert stream.waits == 2
