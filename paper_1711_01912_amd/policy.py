@@ -42,7 +42,8 @@ def _type(t, name):
 
 
 def _matrix(t, name, rows, width, dtype, device):
-    """The distance between the rows of a [rows][width] (or [batch][rows / batch][width]) tensor."""
+    """The distance between the rows of a [rows][width] tensor; ``rows`` may be several axes, as long as they are equally far
+    apart throughout."""
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
     if t.dtype is not dtype:
@@ -55,11 +56,17 @@ def _matrix(t, name, rows, width, dtype, device):
     stride = t.stride()
     if width > 1 and stride[-1] != 1:
         raise ValueError(f"{name}: the elements of a row have to be contiguous (strides {tuple(stride)})")
-    if len(shape) == 3 and shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
-        raise ValueError(f"{name}: all rows have to be equally far apart (strides {tuple(stride)})")
     if rows == 1:
         return width
-    ld = stride[0] if len(shape) == 2 or shape[1] == 1 else stride[1]
+    ld, inner = None, 1          # rows of the axes from the last but one on that have been looked at
+    for size, step in zip(shape[-2::-1], stride[-2::-1]):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = step
+        elif step != ld * inner:
+            raise ValueError(f"{name}: all rows have to be equally far apart (strides {tuple(stride)})")
+        inner *= size
     if ld < width:
         raise ValueError(f"{name}: rows overlap (strides {tuple(stride)})")
     return ld

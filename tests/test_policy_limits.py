@@ -129,3 +129,17 @@ def test_a_status_is_waited_for_on_its_stream_alone(monkeypatch):
     policy._check(fine, policy.STATUS_BAD_TOKEN, "bad", stream)
     policy._check(fine, policy.STATUS_BAD_TOKEN, "bad", None)
     assert stream.waits == 2
+
+
+def test_rows_of_several_axes_are_equally_far_apart():
+    m = lambda t, rows, width: policy._matrix(t, "t", rows, width, torch.float32, t.device)  # noqa: E731
+    t = torch.zeros(2, 3, 5, 20)
+    assert m(t, 30, 20) == 20 and m(t[..., 3:11], 30, 8) == 20
+    assert m(t[:1, :, :, :8], 15, 8) == 20 and m(t[:1, :1, :, :8], 5, 8) == 20
+    assert m(t[:, :, 2:3, :8], 6, 8) == 100 and m(t[:, 1:2, 2:3, :8], 2, 8) == 300 and m(t[1:, 1:2, 2:3, :8], 1, 8) == 8
+    assert m(torch.zeros(4, 1, 7, 6)[..., :4], 28, 4) == 6
+    for bad, rows, width in ((t[:, :2], 20, 20), (t[:, :, :4], 24, 20), (t[:, :2, :, :8], 20, 8), (t.transpose(0, 1), 30, 20),
+                             (t.transpose(1, 2)[..., :8], 30, 8), (t[:, :, ::2, :8], 18, 8), (torch.zeros(3, 5, 20).expand(2, 3, 5, 20), 30, 20),
+                             (torch.zeros(2, 3, 1, 8).expand(2, 3, 5, 8), 30, 8)):
+        with pytest.raises(ValueError):
+            m(bad, rows, width)
