@@ -49,8 +49,8 @@ struct Tokens {
     }
 };
 
-// The larger of three, as one instruction (fmaxf makes each operand a quiet NaN first, by one of its own).  A NaN is passed
-// over, or makes the result one.
+// The larger of three, as one instruction (fmaxf makes each operand a quiet NaN first, by one of its own).  A quiet NaN is
+// passed over, a signalling one makes the result a quiet NaN, which hides what was in front of it.
 __device__ __forceinline__ float max_of(float a, float b, float c) {
     float m;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kThreads, 4) void slice_kernel(Rows r, Tokens tok, 
 #pragma unroll
         for (int k = 0; k < V; k += 2) m = max_of(m, in.x[i][k], in.x[i][k + 1]);
     }
-    const float own = m;
+    float own = m;
     m = wave_max(m);
     if (lane == 0) lds_m[wave] = m;
     __syncthreads();
@@ -323,6 +323,15 @@ __global__ __launch_bounds__(kThreads, 4) void slice_kernel(Rows r, Tokens tok, 
     if (lane == 0) lds_s[wave] = s[0], lds_t[wave] = t[0];
     __syncthreads();
     const Part all = {m, (lds_s[0] + lds_s[1]) + (lds_s[2] + lds_s[3]), (lds_t[0] + lds_t[1]) + (lds_t[2] + lds_t[3])};
+    if (TOP && !(all.s == all.s)) {          // (with a NaN about, which is no alternative but may have hidden some)
+        own = kNone;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            in.x[i].renew();
+#pragma unroll
+            for (int k = 0; k < V; k++) own = in.x[i][k] > own ? in.x[i][k] : own;
+        }
+    }
     if (slices == 1) {
         if (threadIdx.x == 0) write_sums(out, row, all);
         write_tokens<T>(r, tok, out, row, all);

@@ -5,7 +5,7 @@ import torch
 import paper_1711_01912_amd as cpe
 import test_gpu_norm_gate as N
 import test_gpu_token_logprobs as L
-from policy_util import half_step, near, recurrence
+from policy_util import TYPES, half_step, near, recurrence
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -143,3 +143,26 @@ def test_checked_calls_on_the_current_and_on_another_stream():
                 with pytest.raises(ValueError):
                     call()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [9, 64, 200, 300, 1401, 2100, 4000, 40000])
+def test_a_nan_is_no_alternative_and_hides_none(vocab, kind):
+    # quiet and signalling, beside the best places of their vectors, in front of and behind them
+    top = min(vocab, 20)
+    g = torch.Generator().manual_seed(vocab)
+    dt = TYPES[kind]
+    bits = torch.int32 if kind == "fp32" else torch.int16
+    quiet, signalling = {"fp32": (0x7fc00000, 0x7f800001), "bf16": (0x7fc0, 0x7f81), "fp16": (0x7e00, 0x7c01)}[kind]
+    x = (torch.randn(6, vocab, generator=g) * 2.5).to(dt)
+    best = torch.sort(x, dim=-1, descending=True, stable=True).indices
+    for row, (word, step) in enumerate(((quiet, 1), (quiet, -1), (signalling, 1), (signalling, -1), (quiet, 3), (signalling, 2))):
+        at = (best[row, [0, 1, 3]] + step) % vocab
+        x[row].view(bits)[at] = word if word < 2 ** 15 or kind == "fp32" else word - 2 ** 16
+    got = cpe.cp_token_logprobs(x.to(DEV), top=top)
+    assert got["entropy"].isnan().all() and got["top_logp"][got["top_idx"] >= 0].isnan().all()
+    for row in range(6):
+        order = torch.where(x[row].isnan(), float("-inf"), x[row].float())
+        want = torch.sort(order, dim=-1, descending=True, stable=True).indices[:top]
+        want = torch.where(order[want] == float("-inf"), -1, want)
+        assert got["top_idx"][row].tolist() == want.tolist(), row
