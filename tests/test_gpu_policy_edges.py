@@ -166,3 +166,17 @@ def test_a_nan_is_no_alternative_and_hides_none(vocab, kind):
         want = torch.sort(order, dim=-1, descending=True, stable=True).indices[:top]
         want = torch.where(order[want] == float("-inf"), -1, want)
         assert got["top_idx"][row].tolist() == want.tolist(), row
+
+
+@pytest.mark.parametrize("width", [8193, 9001, 16383, 16384])
+@pytest.mark.parametrize("block,stream", [("fp32", "fp32"), ("fp16", "fp16"), ("fp16", "fp32")])
+def test_the_widest_rows_of_a_joint(width, block, stream):
+    N.compare(N.make(300, width, block, stream, seed=width), f"{width} {block} {stream}")
+    N.compare(N.make(3, width, block, stream, weights="fp32", seed=3), f"{width} {block} {stream}, without", gate=False, post=False, dr=False)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,vocab,given,ints", [(40, 8, 64, torch.uint8), (33, 16, 257, torch.int32), (7, 50, 1000, torch.int64), (300, 4, 12, torch.uint8),
+                                                   (11, 2, 1024, torch.int32), (70, 45, 113, torch.uint8), (9, 200, 300, torch.int64), (5, 256, 1000, torch.uint8)])
+def test_many_tokens_of_few_places_in_16_bits(rows, vocab, given, ints, kind):
+    L.compare(L.make(rows, vocab, kind, given, seed=given, ints=ints, mask=True), f"{rows} {vocab} {given} {kind}")
