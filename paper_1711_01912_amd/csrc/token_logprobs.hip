@@ -672,16 +672,15 @@ __global__ __launch_bounds__(kThreads, 4) void few_kernel(Rows r, Tokens tok, Re
     if (bad) atomicOr(out.status, CP_STATUS_BAD_TOKEN);
 }
 
-// SETS > 0: many tokens a row are summed by place in LDS, each of `lanes` lanes in columns of its own (so that the order of the
-// sums is fixed), SETS of them, so that as many sums are under way at once, and the row's columns added up; 0: every lane
-// looks through all of the row's tokens for its own places.  `used` (a power of two): of a row's lanes those that take
-// tokens; only these have columns.
-template <typename T, typename I, int S, int SETS>
+// COLUMNS: many tokens a row are summed by place in LDS, each of `lanes` lanes in a column of its own (so that the order of the
+// sums is fixed), and the row's columns added up; else every lane looks through all of the row's tokens for its own places.
+// `used` (a power of two): of a row's lanes those that take tokens; only these have columns.
+template <typename T, typename I, int S, bool COLUMNS>
 __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens tok, const float *stats, Grads d, T *out, int64_t ldo, int lanes, int used) {
-    extern __shared__ float lds_columns[];       // [kWaves][vocab][SETS][side * used + 1]
+    extern __shared__ float lds_columns[];       // [kWaves][vocab][side * used + 1]
     const int lane = threadIdx.x & (kWave - 1), here = lane & (lanes - 1), group = lane / lanes, side = kWave / lanes;
     const int pitch = side * used + 1, column = group * used + here, log_used = __builtin_ctz(used);
-    float *columns = lds_columns + (threadIdx.x / kWave) * (r.vocab * SETS * pitch);
+    float *columns = lds_columns + (threadIdx.x / kWave) * (r.vocab * pitch);
     const Few few(r.vocab, lane & (S - 1));
     bool bad = false;
     const int64_t step = (int64_t)gridDim.x * kWaves * side;
@@ -698,8 +697,8 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
             hits[e] = 0.0f;
         }
         few.load<T>(soon, r, min(row0 + step + group, r.rows - 1));
-        if constexpr (SETS > 0) {
-            for (int i = here; i < r.vocab * SETS * used; i += lanes) columns[(i >> log_used) * pitch + group * used + (i & (used - 1))] = 0.0f;
+        if constexpr (COLUMNS) {
+            for (int i = here; i < r.vocab * used; i += lanes) columns[(i >> log_used) * pitch + group * used + (i & (used - 1))] = 0.0f;
             lds_ready();
             for (int32_t g0 = here < used ? here * 4 : tok.count; g0 < tok.count; g0 += kAhead * used * 4) {
                 Four<I> four[kAhead];
@@ -718,33 +717,23 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
                 for (int a = 0; a < kAhead; a++) {
                     if (g0 + a * used * 4 >= tok.count) continue;
 #pragma unroll
-                    for (int j = 0; j < 4; j += SETS) {
-                        float sum[SETS];
-                        int at[SETS];
-#pragma unroll
-                        for (int q = 0; q < SETS; q++) {
-                            const int v = four[a].place(j + q, r.vocab, bad);
-                            at[q] = (max(v, 0) * SETS + q) * pitch + column;
-                            sum[q] = columns[at[q]] + (v >= 0 ? w[a].v[j + q] : 0.0f);
-                        }
-#pragma unroll
-                        for (int q = 0; q < SETS; q++) columns[at[q]] = sum[q];
+                    for (int j = 0; j < 4; j++) {
+                        const int v = four[a].place(j, r.vocab, bad);
+                        columns[max(v, 0) * pitch + column] += v >= 0 ? w[a].v[j] : 0.0f;
                     }
                 }
             }
             lds_ready();
             // (a place's sum goes where its first column was, which no other lane has read)
             for (int v = here; v < r.vocab; v += lanes) {
-                float *from = columns + v * (SETS * pitch) + group * used, sum = 0.0f;
-#pragma unroll
-                for (int q = 0; q < SETS; q++)
+                float *from = columns + v * pitch + group * used, sum = 0.0f;
 #pragma unroll 8
-                    for (int j = 0; j < used; j++) sum += from[q * pitch + j];
+                for (int j = 0; j < used; j++) sum += from[j];
                 from[0] = sum;
             }
             lds_ready();
 #pragma unroll
-            for (int e = 0; e < kEach; e++) hits[e] = columns[min(few.at + e, r.vocab - 1) * (SETS * pitch) + group * used];
+            for (int e = 0; e < kEach; e++) hits[e] = columns[min(few.at + e, r.vocab - 1) * pitch + group * used];
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
         } else {
@@ -780,7 +769,6 @@ __global__ void clear_status_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 constexpr int kMostLoads = 4;
 constexpr int32_t kFew = CP_LOGPROBS_IN_PLACE;       // up to so many places a row is some lanes'
 constexpr size_t kColumnBytes = 72u << 10;   // of LDS for a workgroup's columns: two of them on a compute unit
-constexpr int kSets = 4;
 constexpr int32_t slice_places(int v, int nv) { return kThreads * v * nv; }
 int32_t slices_of(int32_t vocab, int v, int nv) { return (vocab + slice_places(v, nv) - 1) / slice_places(v, nv); }
 
@@ -947,22 +935,14 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
                 const dim3 grid((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8));
                 int used = 1;
                 while (used < lanes && used * 4 < given) used *= 2;
-                auto go = [&](auto n) {
-                    constexpr int SETS = decltype(n)::value;
-                    auto bytes = [&] { return (size_t)kWaves * vocab * SETS * (kWave / lanes * used + 1) * sizeof(float); };
-                    while (used > 1 && bytes() > kColumnBytes) used /= 2;
-                    const size_t lds = bytes();
-                    auto *kernel = few_gradient_kernel<T, I, S, SETS>;
-                    if (lds > 48 * 1024 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
-                        return (int)CP_ERR_HIP;
-                    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd, lanes, used);
-                    return launched();
-                };
-                if (!sums) return go(std::integral_constant<int, 0>{});
-                // (where a lane has few tokens, clearing and adding up more columns costs more than waiting for the last sum)
-                if constexpr (S <= 2)
-                    if (given >= 64 * lanes) return go(std::integral_constant<int, kSets>{});
-                return go(std::integral_constant<int, 1>{});
+                auto bytes = [&] { return sums ? (size_t)kWaves * vocab * (kWave / lanes * used + 1) * sizeof(float) : 0; };
+                while (used > 1 && bytes() > kColumnBytes) used /= 2;
+                const size_t lds = bytes();
+                auto *kernel = sums ? few_gradient_kernel<T, I, S, true> : few_gradient_kernel<T, I, S, false>;
+                if (lds > 48 * 1024 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+                    return (int)CP_ERR_HIP;
+                hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, r, tok, stats, d, (T *)dlogits, ldd, lanes, used);
+                return launched();
             });
         constexpr int V = 16 / sizeof(T);
         const int nv = loads_of(rows, vocab, V);
