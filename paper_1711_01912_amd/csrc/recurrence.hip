@@ -8,16 +8,19 @@
 //
 //   g_t = dh_t + u_{t+1},  dx_t = z_t g_t,  df_t = g_t (h_{t-1} - x_t) a_t z_t,  u_t = a_t g_t
 //
-// the same kind of recurrence from the last row to the first; h_{t-1} is computed again from states kept by the forward pass.
+// the same kind of recurrence from the last row to the first; h_{t-1} is computed again from states kept by the forward pass:
+// one per 128 rows, of which a tile's first, every second, is read.
 // Rows are counted in the direction of the scan throughout ("position"): of a reversed scan, position 0 is the last row.
-// States, products and sums are floats; a row's result is rounded once, to the element type.
+// States, products and sums are floats, and a result is rounded once, to the element type; dbias is summed in floats over a
+// tile's 256 rows and in 64 bits over tiles, which leaves it off by less than its terms are.
 //
 // Bound by memory, and laid out to read every input once: a workgroup takes a tile of rows x 128 bytes of channels (a cache
 // line of each row) into registers, two channels a lane.  It publishes what its tile does to a state, looks
 // at what the tiles of its group before it do, waits for the state that enters the group, and writes its rows.  Narrow and
 // long tiles keep what is read in looking back small beside a tile's own bytes, and the number of groups that the chain of
 // states has to pass.  A million rows of 256 bf16 channels: 358 us forward and 605 backward, 4.2 TB/s both, where a copy reaches
-// 5.1; 65536 x 1024 forward 103 us (3.9 TB/s), where a tile's wait for the state of its group shows.
+// 5.1 (the forward kernel keeps 28 of its registers in scratch memory); 65536 x 1024 forward 103 us (3.9 TB/s), where a tile's wait
+// for the state of its group shows, with two workgroups on a compute unit at 84 registers a lane.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,9 +35,15 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kLooks = 2;                               // tiles that a lane looks at
 constexpr int kWide = 2;                                // channels of a lane (of a width of one: one)
-// Rows of a wavefront.  Forward, of 16-bit types, short spans need half the registers and long ones half the groups that the
-// chain of states passes: 65536 x 1024 bf16 take 103 us with 32 and 118 with 64, 300000 x 75 fp16 74 and 86, a million x 256
-// 413 and 357.  Floats, of which a lane has half as many rows, take long ones.
+// Rows of a wavefront.  Forward, of 16-bit types, short spans need two thirds of the registers and long ones half the groups that
+// the chain of states passes.  us a call with 32 and with 64 rows, bf16:
+//   rows         65536      300000     400000     500000     700000     1000000
+//   x 64       21 / 29    58 / 65    75 / 77    91 / 87   117 / 106    161 / 132
+//   x 256      39 / 42   128 / 136  163 / 163  202 / 194  276 / 252    390 / 340
+//   x 1024    100 / 121  402 / 378  533 / 486  661 / 596  920 / 817   1320 / 1157
+// and 300000 x 75 fp16 76 and 90.  (At 1,024 channels the two meet below 300,000 rows: the line is 6 to 9 % off from there on.)
+// Floats, of which a lane has half as many rows, take long ones: 65536 x 1024 149 us (short: 163), 500000 x 256 275 (329), a
+// million x 64 161 (201), 300000 x 75 99 (107); 52710 x 333 74 (72) as one sequence, 65 (68) as 37.
 constexpr int kShortSpan = 32, kLongSpan = 64, kBackwardSpan = 32;
 constexpr int64_t kLongChain = 500000;                  // rows from which on spans are long
 constexpr int forward_span(int64_t rows, size_t bytes) { return bytes == 2 && rows < kLongChain ? kShortSpan : kLongSpan; }
@@ -900,7 +909,7 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
                                num_slots, slots, (T *)h, ldh, status_out);
             return launched();
         };
-        // (no two lanes may share a channel here: its state is read and written)
+        // (no two lanes may share a channel here: its state is read and written.  4096 x 2048 bf16 18.4 us, x 2047 25.9; float 27.2, 32.8)
         if (width % 4 == 0) return go(std::integral_constant<int, 4>{});
         return go(std::integral_constant<int, 1>{});
     });

@@ -5,12 +5,13 @@
 //   dlogits_v = scale (sum_{g: token_g = v} dlogp_g - p_v sum_g dlogp_g - dentropy p_v (logp_v + entropy))
 //
 // Differences from the maximum are formed before they are scaled, and m and log2 s are kept apart, so that rows of a type's
-// lowest value keep their probabilities.  A place that is not allowed counts as -inf whatever it holds.  Sums are floats.
+// lowest value keep their probabilities.  A place that is not allowed counts as -inf whatever it holds.  Sums are floats, also
+// those over a row's tokens: a gradient of 1,024 tokens a row is off by 1.3e-7 of its size, one with these sums in 64 bits by 6e-8.
 //
 // Bound by memory where rows are long: 8192 x 65536 bf16 take 208 us forward (5.1 TB/s, the rate of a copy) and 365 us backward
 // (5.9 TB/s, some of it from the caches).  Rows of few places with many tokens: 200000 x 8 with 1024 tokens of a byte 265 us
-// forward (3.8 TB/s read and written; 166 us where the tokens are still in the caches), 125 backward, where each token is a
-// read and a write of a sum in LDS.
+// forward (3.8 TB/s read and written; 166 us where the tokens are still in the caches), 113 backward, where each token is a
+// read and a write of a sum in LDS, and lanes whose tokens differ meet in the same banks: 64 % of the LDS's busy cycles.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -517,7 +518,8 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(Rows r, Tokens tok, 
 // for moving sums from lane to lane.)  The row's log probabilities are a table in LDS for its tokens, of which there may be as
 // many as partitions were drawn.
 
-// Four tokens from g on, side by side or `stride` apart, -1 behind the last
+// Four tokens from g on, side by side or `stride` apart; behind the last, the last again (whose results go nowhere, and whose
+// weights are 0)
 template <typename I>
 struct Four {
     Pack<I, 4> v;
@@ -767,7 +769,9 @@ __global__ __launch_bounds__(kThreads) void few_gradient_kernel(Rows r, Tokens t
 __global__ void clear_status_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 
 constexpr int kMostLoads = 4;
-constexpr int32_t kFew = CP_LOGPROBS_IN_PLACE;       // up to so many places a row is some lanes'
+// Up to so many places a row is some lanes', as many as 32 have room for: 300000 bf16 rows of 200 with one token 101 us forward and
+// 96 backward, 350 and 302 in slices of a workgroup each; of 256 111 and 103 (367, 333); 20000 of 256 19 and 11 (29, 23).
+constexpr int32_t kFew = CP_LOGPROBS_IN_PLACE;
 constexpr size_t kColumnBytes = 72u << 10;   // of LDS for a workgroup's columns: two of them on a compute unit
 constexpr int32_t slice_places(int v, int nv) { return kThreads * v * nv; }
 int32_t slices_of(int32_t vocab, int v, int nv) { return (vocab + slice_places(v, nv) - 1) / slice_places(v, nv); }
@@ -928,8 +932,10 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
             return by_lanes(tok, vocab, [&](auto i, auto l) {
                 constexpr int S = decltype(l)::value;
                 using I = decltype(i);
-                // (a lane's places are more to clear and add up, the more there are: a million rows of 64 with 30 tokens 412 us in
-                // columns and 301 without; 66695 rows of 45 with 113 tokens 28 in columns)
+                // (Columns have to be cleared and added up; without them each of S lanes reads all tokens.  us in columns and without,
+                // 300000 rows: of 8 places with 16 tokens of a byte 20 and 12, with 32 31 and 26, with 64 33 and 45; with 16 of eight
+                // bytes 21 and 30, with 32 34 and 66.  Of 25 places with 24 tokens of a byte 45 and 39, with 48 48 and 59; of 64 with 48
+                // 125 and 117, with 96 135 and 193.)
                 const bool sums = given >= (S <= 2 ? 16 : 48);
                 const int lanes = sums ? lanes_of(rows, given, S, 8) : S, side = kWaves * kWave / lanes;
                 const dim3 grid((unsigned)std::min<int64_t>((rows + side - 1) / side, 256 * 8));
