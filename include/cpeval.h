@@ -636,7 +636,7 @@ int cp_token_logprobs(int64_t rows, int32_t vocab, int type, const void *logits,
  * gradient of logp, at i * dlogp_row_stride + g * dlogp_stride (a stride of 0: the same for all rows or
  * tokens), dentropy that of entropy at i * dentropy_stride, or NULL; stats are the forward call's.  Tokens
  * that are ignored, out of range or without a probability pass nothing on; places that are not allowed
- * and rows with nothing allowed get 0.  The alternatives have no gradient.  Of up to CP_LOGPROBS_IN_PLACE
+ * or hold -inf and rows with nothing allowed get 0, whatever flows in.  The alternatives have no gradient.  Of up to CP_LOGPROBS_IN_PLACE
  * places a row, dlogits may take the place of the logits.
  */
 int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, float scale,

@@ -418,7 +418,7 @@ struct Grads {
 
 // A row's gradient, place by place: scale (hits + p (-sum - de (logp + entropy))) = scale (hits + p (flat + slope log2 p)).
 // p is lifted by 2^kLift: the hardware's exp gives 0 for what lies below the normal numbers, its product with the rest need
-// not.
+// not.  A place without a probability gets 0 itself, since what its row passes on may be infinite, and 0 times that a NaN.
 struct Slope {
     float m, low, unit, slope, flat, down;
     __device__ __forceinline__ Slope(const Rows &r, const float *stats, float de, float sum) {
@@ -432,7 +432,8 @@ struct Slope {
     }
     __device__ __forceinline__ float at(float x, float hits) const {
         const float l = log2_p(x, m, low, unit), p = __builtin_amdgcn_exp2f(l);
-        return down * fmaf(p, fmaf(fmaxf(l, kFar), slope, flat), hits * exp2f(kLift));
+        const float all = down * fmaf(p, fmaf(fmaxf(l, kFar), slope, flat), hits * exp2f(kLift));
+        return x == kNone ? 0.0f : all;
     }
 };
 

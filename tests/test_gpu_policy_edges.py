@@ -180,3 +180,25 @@ def test_the_widest_rows_of_a_joint(width, block, stream):
                                                    (11, 2, 1024, torch.int32), (70, 45, 113, torch.uint8), (9, 200, 300, torch.int64), (5, 256, 1000, torch.uint8)])
 def test_many_tokens_of_few_places_in_16_bits(rows, vocab, given, ints, kind):
     L.compare(L.make(rows, vocab, kind, given, seed=given, ints=ints, mask=True), f"{rows} {vocab} {given} {kind}")
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab,given", [(9, 3), (9, 40), (64, 3), (200, 100), (300, 1), (300, 3), (4000, 2), (20001, 1)])
+def test_what_has_no_probability_gets_no_gradient(vocab, given, kind):
+    # whatever flows into its row: a row without a place has an entropy of 0, by which a loss may have divided
+    d = L.make(8, vocab, kind, given, seed=vocab, mask=True)
+    d["allowed"][3] = False
+    d["allowed"][7] = True
+    allow, open_ = L.pack_mask(d["allowed"]).to(DEV), torch.from_numpy(d["allowed"]).to(DEV)
+    x, dlogp, de = d["logits"].clone(), d["dlogp"].clone(), d["dentropy"].clone()
+    x[7, 1::2] = float("-inf")
+    d["tokens"][5:8, 0] = torch.from_numpy(d["allowed"][5:8].argmax(1)).to(DEV)
+    de[3], de[4], de[6] = float("inf"), float("nan"), float("-inf")         # rows 3 and 4 have no place
+    dlogp[5, 0], dlogp[7, 0] = float("inf"), float("nan")
+    x[2, int(d["allowed"][2].argmax())] = float("nan")
+    stats = cpe.cp_token_logprobs(x, d["tokens"], allow=allow)["stats"]
+    g = cpe.cp_token_logprobs_backward(x, d["tokens"], stats, dlogp, dentropy=de, allow=allow)["dlogits"]
+    none = ~open_ | (x == float("-inf"))
+    assert (g[none] == 0).all()
+    assert g[2][~none[2]].isnan().all() and g[7][~none[7]].isnan().all() and not g[5][~none[5]].isfinite().all()
+    assert g[[0, 1]].isfinite().all() and not (~none[[3, 4]]).any()
