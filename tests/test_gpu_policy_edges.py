@@ -202,3 +202,42 @@ def test_what_has_no_probability_gets_no_gradient(vocab, given, kind):
     assert (g[none] == 0).all()
     assert g[2][~none[2]].isnan().all() and g[7][~none[7]].isnan().all() and not g[5][~none[5]].isfinite().all()
     assert g[[0, 1]].isfinite().all() and not (~none[[3, 4]]).any()
+
+
+def test_rows_that_lie_beyond_2_to_the_31_elements():
+    rows, ld, width = 270000, 8200, 72
+    buf = torch.zeros(rows, ld, dtype=torch.bfloat16, device=DEV)        # 2.2e9 elements
+    g = torch.Generator(device=DEV).manual_seed(9)
+    v = {k: torch.randn(rows, width, generator=g, device=DEV).bfloat16() for k in ("f", "x", "dh")}
+    cut = {k: buf[:, 1 + 100 * i:1 + 100 * i + width] for i, k in enumerate(("f", "x", "dh", "h", "df", "dx", "dgate", "gone"))}
+    for key, t in v.items():
+        cut[key].copy_(t)
+    bias, w = torch.linspace(0, 4, width, device=DEV), torch.ones(width, dtype=torch.bfloat16, device=DEV)
+    tok = torch.randint(0, width, (rows, 1), generator=g, device=DEV, dtype=torch.int32)
+    for reverse in (False, True):
+        a = cpe.cp_recurrence(v["f"], v["x"], bias=bias, reverse=reverse, want_carry=True, want_last=True)
+        b = cpe.cp_recurrence(cut["f"], cut["x"], bias=bias, reverse=reverse, want_carry=True, want_last=True, out={"h": cut["h"]})
+        assert torch.equal(a["h"], b["h"]) and torch.equal(a["last"], b["last"]) and torch.equal(a["carry"], b["carry"])
+        c = cpe.cp_recurrence_backward(v["dh"], v["f"], v["x"], a["carry"], bias=bias, reverse=reverse)
+        d = cpe.cp_recurrence_backward(cut["dh"], cut["f"], cut["x"], a["carry"], bias=bias, reverse=reverse, out={k: cut[k] for k in ("df", "dx")})
+        assert all(torch.equal(c[k], d[k]) for k in ("df", "dx", "dbias"))
+    a = cpe.cp_norm_gate(v["x"], v["f"], v["dh"], w_pre=w, w_post=w, want_stats=True)
+    b = cpe.cp_norm_gate(cut["x"], cut["f"], cut["dh"], w_pre=w, w_post=w, want_stats=True, out={"r": cut["df"], "z": cut["dx"]})
+    assert all(torch.equal(a[k], b[k]) for k in ("r", "z", "stats"))
+    c = cpe.cp_norm_gate_backward(None, v["dh"], v["x"], v["f"], v["dh"], w_pre=w, w_post=w, stats=a["stats"])
+    d = cpe.cp_norm_gate_backward(None, cut["dh"], cut["x"], cut["f"], cut["dh"], w_pre=w, w_post=w, stats=a["stats"],
+                                  out={"dx": cut["dx"], "dy": cut["df"], "dgate": cut["dgate"]})
+    assert all(torch.equal(c[k], d[k]) for k in c)
+    a, b = cpe.cp_token_logprobs(v["x"], tok, top=3), cpe.cp_token_logprobs(cut["x"], tok, top=3)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+    c = cpe.cp_token_logprobs_backward(v["x"], tok, a["stats"], a["logp"], dentropy=a["entropy"])["dlogits"]
+    d = cpe.cp_token_logprobs_backward(cut["x"], tok, a["stats"], a["logp"], dentropy=a["entropy"], out={"dlogits": cut["h"]})["dlogits"]
+    assert torch.equal(c, d) and not cut["gone"].any()
+    x = torch.randn(rows, 1000, generator=g, device=DEV).bfloat16()
+    wide, tok = buf[:, 3:1003], tok * 13
+    wide.copy_(x)
+    a, b = cpe.cp_token_logprobs(x, tok, top=3), cpe.cp_token_logprobs(wide, tok, top=3)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+    c = cpe.cp_token_logprobs_backward(x, tok, a["stats"], a["logp"], dentropy=a["entropy"])["dlogits"]
+    d = cpe.cp_token_logprobs_backward(wide, tok, a["stats"], a["logp"], dentropy=a["entropy"], out={"dlogits": buf[:, 2001:3001]})["dlogits"]
+    assert torch.equal(c, d) and not buf[:, 3001:].any()
