@@ -67,6 +67,7 @@ extern "C" {
 #define CP_STATUS_BAD_TOKEN      32  /* cp_token_logprobs: a token >= vocab; it counts as one that is to be ignored */
 #define CP_STATUS_BAD_SEQUENCE   64  /* cp_recurrence: seq_ptr does not rise from 0 to rows: the outputs are meaningless */
 #define CP_STATUS_BAD_SLOT       128 /* cp_recurrence_step: a slot >= num_slots; its row was left out */
+#define CP_STATUS_BAD_SAMPLING   256 /* cp_token_sample: a row's own setting is out of range: the row got no tokens */
 
 /* ---- enums ---- */
 #define CP_TICK_I32  4   /* b-level / t-level stored as int32 (only if the graph's bound allows) */
@@ -554,6 +555,67 @@ int cp_recurrence_backward(int64_t rows, int32_t width, int32_t num_seq, const i
 int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, int64_t ldf, const void *x, int64_t ldx,
                        const float *bias, float *state, int32_t num_slots, const int32_t *slots, void *h, int64_t ldh,
                        void *stream, int32_t *status_out);
+
+#define CP_ATTENTION_MAX_WIDTH 256
+#define CP_ATTENTION_MAX_HEADS 1024
+#define CP_ATTENTION_MAX_DISTANCE (1 << 28)            /* elements from a row to the next */
+#define CP_ATTENTION_MAX_HEAD_DISTANCE (1ll << 40)     /* from a head to the next */
+
+/*
+ * Linear attention with a decay for each head, along `rows` rows of `heads` heads: the recurrence whose state
+ * is a width_k x width_v matrix a head,
+ *     S_t = exp(log_decay) S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t
+ *
+ *   num_seq, seq_ptr   as cp_recurrence's, but seq_ptr may end before rows: the rows behind the last sequence
+ *                 are not looked at and their results left as they were
+ *   heads, kv_heads   k and v have kv_heads heads, heads / kv_heads neighbouring heads share one
+ *   type          CP_TYPE_* of q, k, v and o
+ *   reverse       as cp_recurrence's
+ *   q, k          [rows][heads or kv_heads][width_k], ldq (ldk) elements from row to row and hdq (hdk) from head to head, in
+ *                 either order of rows and heads; of inputs either may be 0 (one row or head for all)
+ *   v, o          [rows][kv_heads or heads][width_v]
+ *   log_decay     [heads], at most 0 (above it, or NaN, its head becomes NaN), or NULL (0: no decay)
+ *   h0            [num_seq][heads][width_k][width_v], the state that each sequence begins with, or NULL (0)
+ *   last          as h0, the state that each sequence ends in (h0's where it is empty), or NULL
+ *   carry         [cp_linear_attention_carry_states][heads][width_k][width_v] for the backward pass, or NULL
+ *   status_out    device int32, required with seq_ptr: CP_STATUS_BAD_SEQUENCE where seq_ptr does not rise from 0 to at most
+ *                 rows (no access leaves the arrays)
+ * 16-bit products are exact and summed in 32 bits; states and scores go into them as the sum of two bf16, off by at most 2^-16.  An
+ * infinity or a NaN makes results from its row to its sequence's end infinite or NaN, of its head alone.
+ * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, widths, heads, num_seq < 1, num_seq * heads of equal
+ * parts above 2^28, rows no multiple of num_seq without seq_ptr, distances; results whose rows or heads overlap),
+ * CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.
+ */
+int cp_linear_attention_workspace_bytes(int64_t rows, int32_t num_seq, int packed, int32_t heads, int32_t kv_heads, int32_t width_k,
+                                        int32_t width_v, int backward, size_t *out_bytes);
+int cp_linear_attention_carry_states(int64_t rows, int32_t num_seq, int packed, int32_t heads, int64_t *out_states);
+int cp_linear_attention(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, int32_t heads, int32_t kv_heads, int32_t width_k,
+                        int32_t width_v, int type, int reverse, const void *q, int64_t ldq, int64_t hdq, const void *k, int64_t ldk,
+                        int64_t hdk, const void *v, int64_t ldv, int64_t hdv, const float *log_decay, float scale, const float *h0, void *o,
+                        int64_t ldo, int64_t hdo, float *last, float *carry, void *workspace, size_t workspace_bytes, void *stream,
+                        int32_t *status_out);
+
+/*
+ * Gradient of cp_linear_attention: d_o (of o) and dlast (of last, or NULL) in; dq, dk, dv of the element type out, each with
+ * its own distances; dlog_decay [heads] and dh0 (as h0) float, or NULL.  The inputs and carry are those of the forward call; carry is
+ * required where cp_linear_attention_carry_states is above 0.  Gradients of shared heads are summed in 32 bits; those
+ * of inputs given with a distance of 0 are not (the results have rows and heads of their own).
+ */
+int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, int32_t heads, int32_t kv_heads, int32_t width_k,
+                                 int32_t width_v, int type, int reverse, const void *d_o, int64_t lddo, int64_t hddo, const float *dlast,
+                                 const void *q, int64_t ldq, int64_t hdq, const void *k, int64_t ldk, int64_t hdk, const void *v, int64_t ldv,
+                                 int64_t hdv, const float *log_decay, float scale, const float *h0, const float *carry, void *dq, int64_t lddq,
+                                 int64_t hddq, void *dk, int64_t lddk, int64_t hddk, void *dv, int64_t lddv, int64_t hddv, float *dlog_decay,
+                                 float *dh0, void *workspace, size_t workspace_bytes, void *stream, int32_t *status_out);
+
+/*
+ * One more row of each of num_seq sequences: state [num_slots][heads][width_k][width_v] is updated in place and o gets the new rows.
+ * slots as cp_recurrence_step's; o of a sequence that is left out is 0.
+ */
+int cp_linear_attention_step(int32_t num_seq, int32_t heads, int32_t kv_heads, int32_t width_k, int32_t width_v, int type, const void *q,
+                             int64_t ldq, int64_t hdq, const void *k, int64_t ldk, int64_t hdk, const void *v, int64_t ldv, int64_t hdv,
+                             const float *log_decay, float scale, float *state, int32_t num_slots, const int32_t *slots, void *o, int64_t ldo,
+                             int64_t hdo, void *stream, int32_t *status_out);
 
 #define CP_GATE_NONE     0   /* the gate as it is */
 #define CP_GATE_SIGMOID  1

@@ -36,6 +36,11 @@ from .binding import (  # noqa: F401
     error_string,
     load_library,
 )
+from .attention import (  # noqa: F401
+    cp_linear_attention,
+    cp_linear_attention_backward,
+    cp_linear_attention_step,
+)
 from .policy import (  # noqa: F401
     cp_norm_gate,
     cp_norm_gate_backward,

@@ -38,6 +38,8 @@ EXPORTS = (
     "cp_recurrence_workspace_bytes", "cp_recurrence", "cp_recurrence_backward", "cp_recurrence_step",
     "cp_norm_gate", "cp_norm_gate_backward_workspace_bytes", "cp_norm_gate_backward",
     "cp_token_logprobs_workspace_bytes", "cp_token_logprobs", "cp_token_logprobs_backward",
+    "cp_linear_attention_workspace_bytes", "cp_linear_attention_carry_states", "cp_linear_attention", "cp_linear_attention_backward",
+    "cp_linear_attention_step",
 )
 
 
@@ -171,6 +173,15 @@ def load_library():
                                       vp, vp, vp, C.c_size_t, vp, vp]
     lib.cp_token_logprobs_backward.argtypes = [i64, i32, C.c_int, vp, i64, C.c_float, vp, i32, vp, C.c_int, i64, i64, vp, vp,
                                                i64, i64, vp, i64, vp, i64, vp]
+    heads = [vp, i64, i64]
+    lib.cp_linear_attention_workspace_bytes.argtypes = [i64, i32, C.c_int, i32, i32, i32, i32, C.c_int, szp]
+    lib.cp_linear_attention_carry_states.argtypes = [i64, i32, C.c_int, i32, C.POINTER(i64)]
+    lib.cp_linear_attention.argtypes = [i64, i32, vp, i32, i32, i32, i32, C.c_int, C.c_int, *heads, *heads, *heads, vp, C.c_float, vp,
+                                        *heads, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.cp_linear_attention_backward.argtypes = [i64, i32, vp, i32, i32, i32, i32, C.c_int, C.c_int, *heads, vp, *heads, *heads, *heads,
+                                                 vp, C.c_float, vp, vp, *heads, *heads, *heads, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.cp_linear_attention_step.argtypes = [i32, i32, i32, i32, i32, C.c_int, *heads, *heads, *heads, vp, C.c_float, vp, i32, vp,
+                                             *heads, vp, vp]
     _lib = lib
     return lib
 

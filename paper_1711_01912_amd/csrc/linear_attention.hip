@@ -1,0 +1,806 @@
+// Linear attention with a decay for each head: a recurrence whose state is a matrix,
+//
+//   S_t = gamma S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t,   gamma = exp(log_decay) of the head
+//
+// in chunks of 64 rows, which makes it matrix products: with S the state that enters a chunk and i, j its rows,
+//
+//   o_i = scale (gamma^(i+1) q_i S + sum_{j <= i} gamma^(i-j) (q_i . k_j) v_j)
+//   S'  = gamma^n S + sum_j gamma^(n-1-j) k_j^T v_j
+//
+// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS.  All products of
+// a column stay in its wavefront: the scores are computed by each, and only the tiles on and below the diagonal.
+//
+// The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
+//   dq_t = scale do_t S_t^T (the pass with do, v, k in the places of q, k, v),   dv_t = k_t D_t and dk_t = v_t D_t^T (from the last
+//   row on, with k, q, do and v, do, q),   dlog_decay = sum_t <D_t, gamma S_{t-1}> = sum_i scale do_i . do_i/dlog(gamma),
+// the last by carrying R = dS / dlog(gamma) along with S.
+//
+// Where sequences and heads do not fill the chip, the rows are cut into segments: each segment's effect on the state first, then the
+// states that enter them, segment by segment, then the outputs.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "linear_attention.hpp"
+
+namespace cpeval {
+namespace attention {
+
+namespace {
+
+// up to 4 neighbouring results, rounded once
+template <typename T>
+__device__ __forceinline__ void put(T *to, f32x4 o, float scale, int count) {
+    Pack<T, 4> v;
+#pragma unroll
+    for (int e = 0; e < 4; e++) v.v[e] = (T)(o[e] * scale);
+    if (count >= 4) store_pack<T, 4>(to, v);
+    else {
+#pragma unroll
+        for (int e = 0; e < 3; e++)
+            if (e < count) to[e] = v.v[e];
+    }
+}
+
+// ---- the pass ----------------------------------------------------------------------------------------
+
+// kOut: outputs; kEffect: a segment's effect on the state alone; kDecay: the decays' gradient
+enum Kind { kOut, kEffect, kDecay };
+
+template <int KB, int NT>
+struct State {
+    f32x4 at[2 * KB][NT];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+            for (int n = 0; n < NT; n++) at[k][n] = f32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void load(const Pass &p, const float *from, int64_t index, int32_t head, int col, int g) {
+#pragma unroll
+        for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int row = 16 * k + 4 * g + e, c = col + 16 * n;
+                    at[k][n][e] = row < p.wa && c < p.wb ? from[state_at(p, index, head, row, c)] : 0.0f;
+                }
+    }
+    __device__ __forceinline__ void store(const Pass &p, float *to, int64_t index, int32_t head, int col, int g) const {
+#pragma unroll
+        for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int row = 16 * k + 4 * g + e, c = col + 16 * n;
+                    if (row < p.wa && c < p.wb) to[state_at(p, index, head, row, c)] = at[k][n][e];
+                }
+    }
+    __device__ __forceinline__ double dot(const Pass &p, const float *with, int64_t index, int32_t head, int col, int g) const {
+        double sum = 0;
+#pragma unroll
+        for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int row = 16 * k + 4 * g + e, c = col + 16 * n;
+                    if (row < p.wa && c < p.wb) sum += (double)(at[k][n][e] * with[state_at(p, index, head, row, c)]);
+                }
+        return sum;
+    }
+};
+
+template <typename T, int KB, int NT, Kind kind>
+__global__ __launch_bounds__(kThreads) void pass_kernel(Pass p, float *effect, float *gain) {
+    using E = typename Form<T>::E;
+    constexpr int P = Form<T>::kPlanes, PS = Form<T>::kSplit, kWide = 16 * NT * kWaves;
+    __shared__ Tile<E, P, 32 * KB> b_tile;
+    __shared__ Tile<E, P, kWide> x_tile;
+    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB> a_tile;
+    __shared__ int odd[2];
+
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane % 16, g = lane / 16;
+    const uint32_t group = group_number();
+    const int32_t slice = group % p.slices, head = group / p.slices % p.heads, seg = group / p.slices / p.heads;
+    if (seg >= p.segments) return;                     // (the whole workgroup)
+    const int c0 = slice * kWide, mine = c0 + wave * 16 * NT, col = mine + l;
+    const float lg = lg_of(p.log_decay ? p.log_decay[head] : 0.0f);
+
+    // the decay between rows i and j of the diagonal's tiles and of those right below it, of lane l's i and 4 places of j
+    float near_[2][4];
+#pragma unroll
+    for (int d = 0; d < 2; d++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int apart = 16 * d + l - 4 * g - e;
+            near_[d][e] = apart < 0 ? 0.0f : power(lg, apart) * p.s_in;
+        }
+    const float by16 = power(lg, 16);
+
+    int64_t lo, hi;
+    segment_of(p, seg, lo, hi);
+    if (threadIdx.x == 0) odd[0] = odd[1] = 0;
+    double decay_sum = 0;
+    int turn = 0;
+    State<KB, NT> s, r;
+    bool whole = true;
+    if constexpr (kind == kEffect) {
+        // only the sequence that goes on behind the segment
+        s.zero();
+        bool ends = true;
+        if (lo < hi) {
+            int64_t from = lo, to = hi;
+            // (the last piece in the order of the pass: the one at that end, seen from the other direction)
+            Pass turned = p;
+            turned.back = !p.back;
+            const Piece last = piece_at(turned, lo, hi);
+            from = last.lo, to = last.hi;
+            ends = last.starts;                        // (its end, seen from there)
+            whole = !last.ends;
+            lo = from, hi = to;
+        }
+        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = lo < hi && whole && !ends ? power(lg, (int)(hi - lo)) : 0.0f;
+        if (ends) lo = hi;
+    }
+    while (lo < hi) {
+        const Piece piece = piece_at(p, lo, hi);
+        if (piece.starts && p.init) s.load(p, p.init, piece.seq, head, col, g);
+        else if (kind != kEffect && !piece.starts && p.enter) s.load(p, p.enter, seg, head, col, g);
+        else s.zero();
+        if constexpr (kind == kDecay) r.zero();
+        int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
+        int most = kRows;
+        while (left > 0) {
+            const int n = (int)min((int64_t)most, left);
+            __syncthreads();
+            bool found = stage<T>(x_tile, p.x, head, row, p.back, n, c0, p.wb);
+            stage<T>(b_tile, p.b, head, row, p.back, n, 0, p.wa);
+            if constexpr (kind != kEffect) {
+                stage<T>(a_tile, p.a, head, row, p.back, n, 0, p.wa);
+                if (found) odd[turn] = 1;
+            }
+            __syncthreads();
+            if constexpr (kind != kEffect) {
+                // An infinity or a NaN in x would pass, times a score of 0, to the rows before its own: such chunks go row by row
+                const bool bad = __builtin_amdgcn_readfirstlane(odd[turn]);
+                turn ^= 1;
+                if (threadIdx.x == 0) odd[turn] = 0;
+                if (bad && n > 1) {
+                    most = 1;
+                    continue;
+                }
+                most = kRows;
+            }
+
+            // outputs
+            if constexpr (kind != kEffect) {
+                Frag<E, PS> sf[KB][NT], rf[kind == kDecay ? KB : 1][NT];
+#pragma unroll
+                for (int k = 0; k < KB; k++)
+#pragma unroll
+                    for (int t = 0; t < NT; t++) {
+                        split(s.at[2 * k][t], s.at[2 * k + 1][t], sf[k][t]);
+                        if constexpr (kind == kDecay) split(r.at[2 * k][t], r.at[2 * k + 1][t], rf[k][t]);
+                    }
+#pragma unroll
+                for (int it = 0; it < kRows / 16; it++) {
+                    if (16 * it >= n) break;
+                    const int i = 16 * it + l;
+                    Frag<E, P> af[KB];
+#pragma unroll
+                    for (int k = 0; k < KB; k++) af[k] = a_tile.along(16 * it, k, lane);
+                    // scores of rows i (lanes) and j (places), with the decay between them
+                    f32x4 score[4] = {};
+                    float far_ = 1.0f;
+#pragma unroll
+                    for (int jt = it; jt >= 0; jt--) {
+                        f32x4 c = {0, 0, 0, 0};
+#pragma unroll
+                        for (int k = 0; k < KB; k++) c = product(b_tile.along(16 * jt, k, lane), af[k], c);
+                        if (it - jt > 1) far_ *= by16;
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const float by = near_[it - jt > 0][e] * far_;
+                            // (the diagonal's tile: what lies above it is not looked at)
+                            score[jt][e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * by;
+                        }
+                    }
+                    const float in = power(lg, i + 1 - p.shift);
+#pragma unroll
+                    for (int t = 0; t < NT; t++) {
+                        f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+                        for (int k = 0; k < KB; k++) o = product(sf[k][t], af[k], o);
+                        if constexpr (kind == kDecay) {
+                            f32x4 more = {0, 0, 0, 0};
+#pragma unroll
+                            for (int k = 0; k < KB; k++) more = product(rf[k][t], af[k], more);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) o[e] = more[e] + (float)(i + 1) * o[e];
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; e++) o[e] *= in;
+#pragma unroll
+                        for (int jb = 0; jb <= it / 2; jb++) {
+                            f32x4 u = score[2 * jb], v = score[2 * jb + 1];
+                            if constexpr (kind == kDecay) {
+#pragma unroll
+                                for (int e = 0; e < 4; e++) {
+                                    u[e] *= (float)(i - (32 * jb + 4 * g + e));
+                                    v[e] *= (float)(i - (32 * jb + 16 + 4 * g + e));
+                                }
+                            }
+                            Frag<E, PS> sc;
+                            split(u, v, sc);
+                            o = product(x_tile.across(wave * 16 * NT + 16 * t, jb, lane), sc, o);
+                        }
+                        // lane l has row i, columns 4 g + 0..3
+                        const int c = mine + 16 * t + 4 * g;
+                        if (i < n) {
+                            const int64_t at = row + (p.back ? -i : i);
+                            if constexpr (kind == kOut) {
+                                const int64_t to = at * p.ldo + head * p.hdo + c;
+                                if (p.wide) put((float *)p.o + to, o, p.s_out, p.wb - c);
+                                else put((T *)p.o + to, o, p.s_out, p.wb - c);
+                            } else {
+                                const T *from = (const T *)p.d.at + at * p.d.ld + (head / p.d.group) * p.d.hd + c;
+                                float sum = 0;
+#pragma unroll
+                                for (int e = 0; e < 4; e++)
+                                    if (c + e < p.wb) sum += (float)from[e] * o[e];
+                                decay_sum += (double)(sum * p.s_out);
+                            }
+                        }
+                    }
+                }
+            }
+
+            // the state behind the chunk
+            const float wane = power_less_one(lg, n);
+            if constexpr (kind == kDecay) {
+                const float far_ = power(lg, n) * (float)n;
+#pragma unroll
+                for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+                    for (int t = 0; t < NT; t++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) r.at[k][t][e] = fmaf(r.at[k][t][e], wane, r.at[k][t][e]) + far_ * s.at[k][t][e];
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) s.at[k][t][e] = fmaf(s.at[k][t][e], wane, s.at[k][t][e]);
+#pragma unroll
+            for (int jb = 0; jb < kRows / 32; jb++) {
+                if (32 * jb >= n) break;
+                float w[8];
+                int behind[8];
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    behind[e] = max(n - 1 - (32 * jb + 16 * (e / 4) + 4 * g + e % 4), 0);       // (rows behind the chunk's are zeros)
+                    w[e] = power(lg, behind[e] + p.shift) * p.s_in;
+                }
+                Frag<E, PS> xf[NT], yf[kind == kDecay ? NT : 1];
+#pragma unroll
+                for (int t = 0; t < NT; t++) {
+                    float v[8];
+                    values(x_tile.across(wave * 16 * NT + 16 * t, jb, lane), v);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] *= w[e];
+                    split(v, xf[t]);
+                    if constexpr (kind == kDecay) {
+#pragma unroll
+                        for (int e = 0; e < 8; e++) v[e] *= (float)behind[e];
+                        split(v, yf[t]);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2 * KB; k++) {
+                    const Frag<E, P> bf = b_tile.across(16 * k, jb, lane);
+#pragma unroll
+                    for (int t = 0; t < NT; t++) {
+                        s.at[k][t] = product(bf, xf[t], s.at[k][t]);
+                        if constexpr (kind == kDecay) r.at[k][t] = product(bf, yf[t], r.at[k][t]);
+                    }
+                }
+            }
+            left -= n;
+            row += p.back ? -n : n;
+        }
+        if constexpr (kind == kOut) {
+            if (piece.ends && p.last) s.store(p, p.last, piece.seq, head, col, g);
+        }
+        if constexpr (kind == kDecay) {
+            if (piece.ends) {
+                if (p.dlast) decay_sum += r.dot(p, p.dlast, piece.seq, head, col, g);
+            } else if (p.denter) decay_sum += r.dot(p, p.denter, seg, head, col, g);
+        }
+        if (p.back) hi = piece.lo;
+        else lo = piece.hi;
+    }
+    if constexpr (kind == kEffect) s.store(p, effect, seg, head, col, g);
+    if constexpr (kind == kDecay) {
+        __shared__ double sums[kWaves];
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) decay_sum += __shfl_xor(decay_sum, off);
+        if (lane == 0) sums[wave] = decay_sum;
+        __syncthreads();
+        if (threadIdx.x == 0) p.part[(int64_t)head * p.segments * p.slices + seg * p.slices + slice] = sums[0] + sums[1] + sums[2] + sums[3];
+    }
+}
+
+// States that enter the segments, from their effects, in place and in the order of the pass: E' = gain E + U.  A gain of 0 drops
+// the state before it (a sequence began), whatever it holds.
+template <int V>
+__global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float *gain, int32_t segments, int32_t heads, int32_t size, bool back) {
+    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * V;
+    if (i >= size) return;
+    const int32_t head = blockIdx.y;
+    Pack<float, V> e;
+#pragma unroll
+    for (int k = 0; k < V; k++) e.v[k] = 0.0f;
+#pragma unroll 8
+    for (int32_t n = 0; n < segments; n++) {
+        const int32_t s = back ? segments - 1 - n : n;
+        float *here = at + ((int64_t)s * heads + head) * size + i;
+        const Pack<float, V> u = load_pack<float, V>(here);
+        const float by = gain[(int64_t)s * heads + head];
+        store_pack<float, V>(here, e);
+#pragma unroll
+        for (int k = 0; k < V; k++) e.v[k] = by == 0.0f ? u.v[k] : fmaf(by, e.v[k], u.v[k]);
+    }
+}
+
+// Pointers that do not rise from 0, or beyond the rows
+__global__ __launch_bounds__(kThreads) void check_kernel(const int32_t *ptr, int32_t num_seq, int64_t rows, int32_t *status) {
+    __shared__ int bad;
+    if (threadIdx.x == 0) bad = ptr[0] != 0 || ptr[num_seq] > rows;
+    __syncthreads();
+    bool mine = false;
+    for (int64_t s = threadIdx.x; s < num_seq; s += kThreads) mine |= ptr[s + 1] < ptr[s];
+    if (mine) bad = 1;
+    __syncthreads();
+    if (threadIdx.x == 0) *status = bad ? CP_STATUS_BAD_SEQUENCE : CP_STATUS_OK;
+}
+
+// A sequence without rows ends in the state that it begins with
+__global__ __launch_bounds__(kThreads) void empty_kernel(const int32_t *ptr, int64_t len, int32_t num_seq, int64_t state, const float *from, float *to) {
+    for (int64_t s = blockIdx.x; s < num_seq; s += gridDim.x) {
+        if (ptr ? ptr[s + 1] > ptr[s] : len > 0) continue;
+        for (int64_t i = threadIdx.x; i < state; i += kThreads) to[s * state + i] = from ? from[s * state + i] : 0.0f;
+    }
+}
+
+// Gradients of a head's keys or values from those of the heads that share it, in their order
+template <typename T>
+__global__ __launch_bounds__(kThreads) void share_kernel(const float *part, const int32_t *ptr, int32_t num_seq, int64_t rows, int32_t heads, int32_t group,
+                                                         int32_t width, T *to, int64_t ld, int64_t hd) {
+    const int64_t total = ptr ? min((int64_t)max(ptr[num_seq], 0), rows) : rows;
+    const int32_t kv = heads / group, line = kv * width;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total * line; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / line;
+        const int32_t h = (int32_t)(i % line) / width, c = (int32_t)(i % line) % width;
+        const float *from = part + (row * heads + (int64_t)h * group) * width + c;
+        float sum = 0;
+        for (int32_t k = 0; k < group; k++) sum += from[(int64_t)k * width];
+        to[row * ld + h * hd + c] = (T)sum;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void decay_kernel(const double *part, int64_t each, float *to) {
+    __shared__ double sums[kThreads];
+    double sum = 0;
+    for (int64_t i = threadIdx.x; i < each; i += kThreads) sum += part[blockIdx.x * each + i];
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kThreads; i++) sum += sums[i];
+        to[blockIdx.x] = (float)sum;
+    }
+}
+
+// ---- one more row of every sequence --------------------------------------------------------------------
+
+struct Step {
+    int32_t count, heads, wk, wv, num_slots;
+    Operand q, k, v;
+    const float *log_decay;
+    float scale;
+    float *state;
+    const int32_t *slots;
+    void *o;
+    int64_t ldo, hdo;
+    int32_t *status;
+};
+
+// A workgroup has the state of one head of one sequence; a thread V neighbouring columns of every few rows.  It is read once and written
+// once, which is all there is to it.
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void step_kernel(Step p) {
+    __shared__ float sums[kThreads * V], kq[2][256];
+    const int64_t unit = group_number();
+    const int32_t head = (int32_t)(unit % p.heads);
+    const int64_t seq = unit / p.heads;
+    if (seq >= p.count) return;
+    const int32_t slot = p.slots ? p.slots[seq] : (int32_t)seq;
+    const bool bad = slot >= p.num_slots;
+    if (bad && p.slots && threadIdx.x == 0 && head == 0) atomicOr(p.status, CP_STATUS_BAD_SLOT);
+    T *o = (T *)p.o + seq * p.ldo + head * p.hdo;
+    if (slot < 0 || bad) {
+        for (int c = threadIdx.x; c < p.wv; c += kThreads) o[c] = (T)0.0f;
+        return;
+    }
+    const T *q = (const T *)p.q.at + seq * p.q.ld + (head / p.q.group) * p.q.hd;
+    const T *k = (const T *)p.k.at + seq * p.k.ld + (head / p.k.group) * p.k.hd;
+    const T *v = (const T *)p.v.at + seq * p.v.ld + (head / p.v.group) * p.v.hd;
+    for (int c = threadIdx.x; c < p.wk; c += kThreads) kq[0][c] = (float)k[c], kq[1][c] = (float)q[c];
+    const float by = power(lg_of(p.log_decay ? p.log_decay[head] : 0.0f), 1);
+    const int lanes = (p.wv + V - 1) / V, side = kThreads / lanes;      // (wv is a multiple of V; lanes <= 256)
+    const int mine = threadIdx.x % lanes, first = threadIdx.x / lanes;
+    float *state = p.state + ((int64_t)slot * p.heads + head) * ((int64_t)p.wk * p.wv) + mine * V;
+    float value[V], sum[V];
+#pragma unroll
+    for (int e = 0; e < V; e++) value[e] = (float)v[mine * V + e], sum[e] = 0.0f;
+    __syncthreads();
+    if (first < side) {
+#pragma unroll 8
+        for (int row = first; row < p.wk; row += side) {
+            Pack<float, V> s = load_pack<float, V>(state + (int64_t)row * p.wv);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                s.v[e] = fmaf(by, s.v[e], kq[0][row] * value[e]);
+                sum[e] = fmaf(kq[1][row], s.v[e], sum[e]);
+            }
+            store_pack<float, V>(state + (int64_t)row * p.wv, s);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; e++) sums[threadIdx.x * V + e] = sum[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.wv; c += kThreads) {
+        float all = 0.0f;
+        for (int i = 0; i < side; i++) all += sums[i * lanes * V + c];
+        o[c] = (T)(all * p.scale);
+    }
+}
+
+__global__ void set_status_kernel(int32_t *status, int32_t value) { *status = value; }
+
+// ---- host --------------------------------------------------------------------------------------------
+
+constexpr int kMaxWidth = CP_ATTENTION_MAX_WIDTH, kMaxHeads = CP_ATTENTION_MAX_HEADS;
+
+// Segments: workgroups enough for the chip (two a compute unit), of 128 rows at least.  The same for all types and for both
+// directions, since the backward pass reads the states that the forward call kept.
+struct Cut {
+    int64_t seg_rows;
+    int32_t parts, segments;
+    bool split;                          // whether a sequence may be cut
+};
+constexpr int64_t kWanted = 512, kLeast = 128;
+
+Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads) {
+    const int64_t len = packed ? rows : rows / num_seq;
+    const int64_t units = (int64_t)heads * (packed ? 1 : num_seq);
+    int64_t parts = std::max<int64_t>(1, std::min((kWanted + units - 1) / units, len / kLeast));
+    Cut c;
+    c.seg_rows = std::max<int64_t>((len + parts - 1) / parts, 1);
+    c.seg_rows = (c.seg_rows + kRows - 1) / kRows * kRows;
+    parts = std::max<int64_t>(1, (len + c.seg_rows - 1) / c.seg_rows);
+    c.parts = (int32_t)parts;
+    c.segments = (int32_t)(packed ? parts : parts * num_seq);
+    c.split = parts > 1;
+    return c;
+}
+
+// columns that a workgroup takes: 64, or 128 where there are more and registers hold them
+int tiles_of(int32_t wa, int32_t wb) { return wb > 64 && wa <= 128 ? 2 : 1; }
+int32_t slices_of(int32_t wa, int32_t wb) { return (wb + 64 * tiles_of(wa, wb) - 1) / (64 * tiles_of(wa, wb)); }
+
+template <typename T, int KB, int NT>
+int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t st) {
+    auto *kernel = kind == kOut ? pass_kernel<T, KB, NT, kOut> : kind == kEffect ? pass_kernel<T, KB, NT, kEffect> : pass_kernel<T, KB, NT, kDecay>;
+    hipLaunchKernelGGL(kernel, grid_of((int64_t)p.segments * p.heads * p.slices), dim3(kThreads), 0, st, p, effect, gain);
+    return launched();
+}
+
+int run(Kind kind, int type, Pass p, float *effect, float *gain, hipStream_t st) {
+    p.slices = slices_of(p.wa, p.wb);
+    const int tiles = tiles_of(p.wa, p.wb);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        if (p.wa > 128) return run_sized<T, 8, 1>(kind, p, effect, gain, st);
+        if (p.wa > 64) return tiles == 2 ? run_sized<T, 4, 2>(kind, p, effect, gain, st) : run_sized<T, 4, 1>(kind, p, effect, gain, st);
+        return tiles == 2 ? run_sized<T, 2, 2>(kind, p, effect, gain, st) : run_sized<T, 2, 1>(kind, p, effect, gain, st);
+    });
+}
+
+// the states that enter the pass's segments, into `at`
+int run_enter(int type, const Pass &p, float *at, float *gain, hipStream_t st) {
+    const int rc = run(kEffect, type, p, at, gain, st);
+    if (rc) return rc;
+    const int32_t size = p.wa * p.wb;
+    const int per = size % 4 == 0 ? 4 : 1;
+    const dim3 grid((unsigned)((size + kThreads * per - 1) / (kThreads * per)), (unsigned)p.heads);
+    hipLaunchKernelGGL(per == 4 ? enter_kernel<4> : enter_kernel<1>, grid, dim3(kThreads), 0, st, at, gain, p.segments, p.heads, size, p.back);
+    return launched();
+}
+
+struct Shape {
+    int64_t rows;
+    int32_t num_seq;
+    const int32_t *ptr;
+    int32_t heads, kv_heads, wk, wv;
+    int type;
+};
+
+int check(const Shape &s, int reverse) {
+    if (!known_type(s.type) || (reverse != 0 && reverse != 1)) return CP_ERR_ARG;
+    if (s.rows < 0 || s.rows > INT32_MAX || s.num_seq < 1 || s.heads < 1 || s.heads > kMaxHeads || s.kv_heads < 1 || s.heads % s.kv_heads != 0 ||
+        s.wk < 1 || s.wk > kMaxWidth || s.wv < 1 || s.wv > kMaxWidth)
+        return CP_ERR_SIZE;
+    // (workgroups are counted in 32 bits)
+    if (s.ptr ? s.num_seq == INT32_MAX : s.rows % s.num_seq != 0 || (int64_t)s.num_seq * s.heads > INT32_MAX / 8) return CP_ERR_SIZE;
+    return CP_OK;
+}
+
+size_t state_floats(const Shape &s) { return (size_t)s.heads * s.wk * s.wv; }
+// of the states that enter segments, and of their gains
+size_t enter_bytes(const Shape &s, const Cut &c) { return c.split ? align_up(c.segments * state_floats(s) * sizeof(float)) : 0; }
+size_t gain_bytes(const Shape &s, const Cut &c) { return c.split ? align_up((size_t)c.segments * s.heads * sizeof(float)) : 0; }
+size_t part_bytes(const Shape &s, const Cut &c) { return align_up((size_t)s.heads * c.segments * slices_of(s.wk, s.wv) * sizeof(double)); }
+size_t share_bytes(const Shape &s) { return s.heads == s.kv_heads ? 0 : align_up((size_t)s.rows * s.heads * std::max(s.wk, s.wv) * sizeof(float)); }
+
+size_t need_of(const Shape &s, bool backward) {
+    const Cut c = cut_of(s.rows, s.num_seq, s.ptr != nullptr, s.heads);
+    return enter_bytes(s, c) + gain_bytes(s, c) + (backward ? part_bytes(s, c) + share_bytes(s) : 0);
+}
+
+// rows of `heads` heads of `width` values, a distance ld from row to row and hd from head to head (0: one head for all, of inputs)
+struct Heads {
+    const void *at;
+    int64_t ld, hd;
+    int32_t heads, width;
+    bool result;
+};
+
+// Elements of one row's heads may lie between those of another's (heads in front of rows); rows or heads of a result may not overlap
+bool fits(const Heads &m, int64_t rows) {
+    if (m.ld < 0 || m.hd < 0 || m.ld > CP_ATTENTION_MAX_DISTANCE || m.hd > CP_ATTENTION_MAX_HEAD_DISTANCE) return false;
+    if (!m.result) return true;
+    if (m.heads > 1 && m.hd < m.width) return false;
+    if (rows > 1 && m.ld < m.width) return false;
+    if (m.heads > 1 && rows > 1) {
+        const bool inside = m.ld >= (m.heads - 1) * m.hd + m.width, outside = m.hd >= (rows - 1) * m.ld + m.width;
+        return inside || outside;
+    }
+    return true;
+}
+
+// Where it lies: as equally distant rows where it can be put so, else all from its first element to its last
+Extent extent(const Heads &m, int64_t rows, int type) {
+    const int64_t each = (int64_t)type_bytes(type);
+    if (!m.at || rows < 1) return {nullptr, 0, 0, 0, (size_t)each};
+    const int64_t ld = rows > 1 ? m.ld : 0, hd = m.heads > 1 ? m.hd : 0;
+    if (m.heads == 1 || hd == 0) return {m.at, ld ? rows : 1, m.width * each, (ld ? ld : m.width) * each, (size_t)each};
+    if (rows == 1 || ld == 0) return {m.at, m.heads, m.width * each, hd * each, (size_t)each};
+    if (hd == m.width && ld >= (int64_t)m.heads * hd) return {m.at, rows, m.heads * hd * each, ld * each, (size_t)each};
+    if (ld == m.heads * hd) return {m.at, rows * m.heads, m.width * each, hd * each, (size_t)each};
+    if (hd == rows * ld) return {m.at, rows * m.heads, m.width * each, ld * each, (size_t)each};
+    const int64_t all = ((rows - 1) * ld + (m.heads - 1) * hd + m.width) * each;
+    return {m.at, 1, all, all, (size_t)each};
+}
+
+}  // namespace
+}  // namespace attention
+}  // namespace cpeval
+
+using namespace cpeval;
+using namespace cpeval::attention;
+
+extern "C" {
+
+int cp_linear_attention_workspace_bytes(int64_t rows, int32_t num_seq, int packed, int32_t heads, int32_t kv_heads, int32_t width_k,
+                                        int32_t width_v, int backward, size_t *out_bytes) {
+    if (!out_bytes) return CP_ERR_NULL;
+    const int32_t some = 0;
+    const Shape s{rows, num_seq, packed ? &some : nullptr, heads, kv_heads, width_k, width_v, CP_TYPE_F32};
+    const int rc = check(s, 0);
+    if (rc) return rc;
+    *out_bytes = need_of(s, backward != 0);
+    return CP_OK;
+}
+
+int cp_linear_attention_carry_states(int64_t rows, int32_t num_seq, int packed, int32_t heads, int64_t *out_states) {
+    if (!out_states) return CP_ERR_NULL;
+    const int32_t some = 0;
+    const int rc = check({rows, num_seq, packed ? &some : nullptr, heads, heads, 1, 1, CP_TYPE_F32}, 0);
+    if (rc) return rc;
+    const Cut c = cut_of(rows, num_seq, packed != 0, heads);
+    *out_states = c.split ? c.segments : 0;
+    return CP_OK;
+}
+
+int cp_linear_attention(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, int32_t heads, int32_t kv_heads, int32_t width_k,
+                        int32_t width_v, int type, int reverse, const void *q, int64_t ldq, int64_t hdq, const void *k, int64_t ldk,
+                        int64_t hdk, const void *v, int64_t ldv, int64_t hdv, const float *log_decay, float scale, const float *h0, void *o,
+                        int64_t ldo, int64_t hdo, float *last, float *carry, void *workspace, size_t workspace_bytes, void *stream,
+                        int32_t *status_out) {
+    const Shape s{rows, num_seq, seq_ptr, heads, kv_heads, width_k, width_v, type};
+    int rc = check(s, reverse);
+    if (rc) return rc;
+    if ((rows > 0 && (!q || !k || !v || !o)) || (seq_ptr && !status_out)) return CP_ERR_NULL;
+    const Heads mq{q, ldq, hdq, heads, width_k, false}, mk{k, ldk, hdk, kv_heads, width_k, false}, mv{v, ldv, hdv, kv_heads, width_v, false},
+        mo{o, ldo, hdo, heads, width_v, true};
+    if (rows > 0 && (!fits(mq, rows) || !fits(mk, rows) || !fits(mv, rows) || !fits(mo, rows))) return CP_ERR_SIZE;
+    const Cut c = cut_of(rows, num_seq, seq_ptr != nullptr, heads);
+    const size_t enter = enter_bytes(s, c), need = gain_bytes(s, c) + (carry ? 0 : enter);
+    if (need) {
+        if (!workspace) return CP_ERR_NULL;
+        if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
+    }
+    const auto states = [&](const void *at) { return vector_at(at, (int64_t)num_seq * state_floats(s)); };
+    if (in_the_way({extent(mq, rows, type), extent(mk, rows, type), extent(mv, rows, type), vector_at(log_decay, heads), states(h0),
+                    vector_at(seq_ptr, (int64_t)num_seq + 1, sizeof(int32_t))},
+                   {extent(mo, rows, type), states(last), vector_at(c.split ? carry : nullptr, c.segments * (int64_t)state_floats(s)),
+                    vector_at(seq_ptr ? status_out : nullptr, 1, sizeof(int32_t)), vector_at(need ? workspace : nullptr, (int64_t)need, 1)}))
+        return CP_ERR_ARG;
+    const hipStream_t st = (hipStream_t)stream;
+    if (seq_ptr) hipLaunchKernelGGL(check_kernel, dim3(1), dim3(kThreads), 0, st, seq_ptr, num_seq, rows, status_out);
+    if (last && (seq_ptr || rows == 0))
+        hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096)), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
+                           (int64_t)state_floats(s), h0, last);
+    if (rows == 0) return launched();
+    Pass p{};
+    p.rows = rows, p.len = rows / num_seq, p.ptr = seq_ptr, p.num_seq = num_seq;
+    p.segments = c.segments, p.parts = c.parts, p.seg_rows = c.seg_rows;
+    p.heads = heads, p.wa = width_k, p.wb = width_v, p.back = reverse != 0;
+    p.s_in = 1.0f, p.s_out = scale, p.log_decay = log_decay;
+    p.a = {q, ldq, hdq, 1}, p.b = {k, ldk, hdk, heads / kv_heads}, p.x = {v, ldv, hdv, heads / kv_heads};
+    p.init = h0, p.last = last, p.o = o, p.ldo = ldo, p.hdo = hdo;
+    if (c.split) {
+        float *gain = (float *)workspace, *at = carry ? carry : (float *)((char *)workspace + gain_bytes(s, c));
+        rc = run_enter(type, p, at, gain, st);
+        if (rc) return rc;
+        p.enter = at;
+    }
+    return run(kOut, type, p, nullptr, nullptr, st);
+}
+
+int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, int32_t heads, int32_t kv_heads, int32_t width_k,
+                                 int32_t width_v, int type, int reverse, const void *d_o, int64_t lddo, int64_t hddo, const float *dlast,
+                                 const void *q, int64_t ldq, int64_t hdq, const void *k, int64_t ldk, int64_t hdk, const void *v, int64_t ldv,
+                                 int64_t hdv, const float *log_decay, float scale, const float *h0, const float *carry, void *dq, int64_t lddq,
+                                 int64_t hddq, void *dk, int64_t lddk, int64_t hddk, void *dv, int64_t lddv, int64_t hddv, float *dlog_decay,
+                                 float *dh0, void *workspace, size_t workspace_bytes, void *stream, int32_t *status_out) {
+    const Shape s{rows, num_seq, seq_ptr, heads, kv_heads, width_k, width_v, type};
+    int rc = check(s, reverse);
+    if (rc) return rc;
+    const Cut c = cut_of(rows, num_seq, seq_ptr != nullptr, heads);
+    if ((rows > 0 && (!d_o || !q || !k || !v || !dq || !dk || !dv || (c.split && !carry))) || (seq_ptr && !status_out)) return CP_ERR_NULL;
+    const Heads mo{d_o, lddo, hddo, heads, width_v, false}, mq{q, ldq, hdq, heads, width_k, false}, mk{k, ldk, hdk, kv_heads, width_k, false},
+        mv{v, ldv, hdv, kv_heads, width_v, false}, nq{dq, lddq, hddq, heads, width_k, true}, nk{dk, lddk, hddk, kv_heads, width_k, true},
+        nv{dv, lddv, hddv, kv_heads, width_v, true};
+    if (rows > 0)
+        for (const Heads *m : {&mo, &mq, &mk, &mv, &nq, &nk, &nv})
+            if (!fits(*m, rows)) return CP_ERR_SIZE;
+    const size_t need = need_of(s, true);
+    if (rows > 0 || dlog_decay) {
+        if (!workspace) return CP_ERR_NULL;
+        if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
+    }
+    const auto states = [&](const void *at) { return vector_at(at, (int64_t)num_seq * state_floats(s)); };
+    const auto at = [&](const Heads &m) { return extent(m, rows, type); };
+    if (in_the_way({at(mo), at(mq), at(mk), at(mv), vector_at(log_decay, heads), states(h0), states(dlast),
+                    vector_at(c.split ? carry : nullptr, c.segments * (int64_t)state_floats(s)),
+                    vector_at(seq_ptr, (int64_t)num_seq + 1, sizeof(int32_t))},
+                   {at(nq), at(nk), at(nv), vector_at(dlog_decay, heads), states(dh0), vector_at(seq_ptr ? status_out : nullptr, 1, sizeof(int32_t)),
+                    vector_at(rows > 0 || dlog_decay ? workspace : nullptr, (int64_t)need, 1)}))
+        return CP_ERR_ARG;
+    const hipStream_t st = (hipStream_t)stream;
+    if (seq_ptr) hipLaunchKernelGGL(check_kernel, dim3(1), dim3(kThreads), 0, st, seq_ptr, num_seq, rows, status_out);
+    if (dh0 && (seq_ptr || rows == 0))
+        hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096)), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
+                           (int64_t)state_floats(s), dlast, dh0);
+    char *room = (char *)workspace;
+    float *gain = (float *)room, *denter = (float *)(room + gain_bytes(s, c));
+    double *part = (double *)(room + gain_bytes(s, c) + enter_bytes(s, c));
+    float *share = (float *)((char *)part + part_bytes(s, c));
+    const int32_t group = heads / kv_heads;
+    if (rows == 0) {
+        if (dlog_decay) hipLaunchKernelGGL(decay_kernel, dim3((unsigned)heads), dim3(kThreads), 0, st, part, (int64_t)0, dlog_decay);
+        return launched();
+    }
+    const Operand in_do{d_o, lddo, hddo, 1}, in_q{q, ldq, hdq, 1}, in_k{k, ldk, hdk, group}, in_v{v, ldv, hdv, group};
+    Pass p{};
+    p.rows = rows, p.len = rows / num_seq, p.ptr = seq_ptr, p.num_seq = num_seq;
+    p.segments = c.segments, p.parts = c.parts, p.seg_rows = c.seg_rows;
+    p.heads = heads, p.log_decay = log_decay;
+
+    // dv: keys read the gradient of the state
+    Pass b = p;
+    b.wa = width_k, b.wb = width_v, b.back = reverse == 0, b.shift = 1, b.s_in = scale, b.s_out = 1.0f;
+    b.a = in_k, b.b = in_q, b.x = in_do, b.init = dlast, b.last = dh0;
+    if (c.split) {
+        rc = run_enter(type, b, denter, gain, st);
+        if (rc) return rc;
+        b.enter = denter;
+    }
+    // (heads that share keys and values: their gradients apart first, in 32 bits)
+    const auto gradient = [&](Pass pass, void *to, int64_t ld, int64_t hd) {
+        if (group == 1) {
+            pass.o = to, pass.ldo = ld, pass.hdo = hd;
+            return run(kOut, type, pass, nullptr, nullptr, st);
+        }
+        pass.o = share, pass.hdo = pass.wb, pass.ldo = (int64_t)heads * pass.wb, pass.wide = true;
+        const int code = run(kOut, type, pass, nullptr, nullptr, st);
+        if (code) return code;
+        const int64_t blocks = (rows * kv_heads * pass.wb + kThreads - 1) / kThreads;
+        return by_type(type, [&](auto t) {
+            using T = decltype(t);
+            hipLaunchKernelGGL(share_kernel<T>, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(kThreads), 0, st, share, seq_ptr, num_seq, rows, heads,
+                               group, pass.wb, (T *)to, ld, hd);
+            return launched();
+        });
+    };
+    rc = gradient(b, dv, lddv, hddv);
+    if (rc) return rc;
+    // dk: values read it, transposed
+    b.wa = width_v, b.wb = width_k, b.transposed = true, b.last = nullptr;
+    b.a = in_v, b.b = in_do, b.x = in_q;
+    rc = gradient(b, dk, lddk, hddk);
+    if (rc) return rc;
+    // dq: the gradients of the outputs read the state, transposed
+    Pass a = p;
+    a.wa = width_v, a.wb = width_k, a.transposed = true, a.back = reverse != 0, a.s_in = 1.0f, a.s_out = scale;
+    a.a = in_do, a.b = in_v, a.x = in_k, a.init = h0, a.enter = c.split ? carry : nullptr;
+    a.o = dq, a.ldo = lddq, a.hdo = hddq;
+    rc = run(kOut, type, a, nullptr, nullptr, st);
+    if (rc || !dlog_decay) return rc;
+    Pass e = p;
+    e.wa = width_k, e.wb = width_v, e.back = reverse != 0, e.s_in = 1.0f, e.s_out = scale;
+    e.a = in_q, e.b = in_k, e.x = in_v, e.d = in_do, e.init = h0, e.enter = c.split ? carry : nullptr;
+    e.dlast = dlast, e.denter = c.split ? denter : nullptr, e.part = part;
+    rc = run(kDecay, type, e, nullptr, nullptr, st);
+    if (rc) return rc;
+    hipLaunchKernelGGL(decay_kernel, dim3((unsigned)heads), dim3(kThreads), 0, st, part, (int64_t)c.segments * slices_of(width_k, width_v), dlog_decay);
+    return launched();
+}
+
+int cp_linear_attention_step(int32_t num_seq, int32_t heads, int32_t kv_heads, int32_t width_k, int32_t width_v, int type, const void *q,
+                             int64_t ldq, int64_t hdq, const void *k, int64_t ldk, int64_t hdk, const void *v, int64_t ldv, int64_t hdv,
+                             const float *log_decay, float scale, float *state, int32_t num_slots, const int32_t *slots, void *o, int64_t ldo,
+                             int64_t hdo, void *stream, int32_t *status_out) {
+    if (!known_type(type)) return CP_ERR_ARG;
+    if (num_seq < 0 || num_slots < 1 || (!slots && num_seq > num_slots)) return CP_ERR_SIZE;
+    const Shape s{num_seq, 1, nullptr, heads, kv_heads, width_k, width_v, type};
+    const int rc = check(s, 0);
+    if (rc) return rc;
+    if ((int64_t)num_seq * heads > INT32_MAX) return CP_ERR_SIZE;
+    if ((num_seq > 0 && (!q || !k || !v || !o)) || !state || (slots && !status_out)) return CP_ERR_NULL;
+    const Heads mq{q, ldq, hdq, heads, width_k, false}, mk{k, ldk, hdk, kv_heads, width_k, false}, mv{v, ldv, hdv, kv_heads, width_v, false},
+        mo{o, ldo, hdo, heads, width_v, true};
+    if (num_seq > 0 && (!fits(mq, num_seq) || !fits(mk, num_seq) || !fits(mv, num_seq) || !fits(mo, num_seq))) return CP_ERR_SIZE;
+    if (in_the_way({extent(mq, num_seq, type), extent(mk, num_seq, type), extent(mv, num_seq, type), vector_at(log_decay, heads),
+                    vector_at(slots, num_seq, sizeof(int32_t))},
+                   {extent(mo, num_seq, type), vector_at(state, (int64_t)num_slots * state_floats(s)),
+                    vector_at(slots ? status_out : nullptr, 1, sizeof(int32_t))}))
+        return CP_ERR_ARG;
+    const hipStream_t st = (hipStream_t)stream;
+    if (slots) hipLaunchKernelGGL(set_status_kernel, dim3(1), dim3(1), 0, st, status_out, CP_STATUS_OK);
+    if (num_seq == 0) return launched();
+    const Step p{num_seq, heads, width_k, width_v, num_slots, {q, ldq, hdq, 1}, {k, ldk, hdk, heads / kv_heads}, {v, ldv, hdv, heads / kv_heads},
+                 log_decay, scale, state, slots, o, ldo, hdo, status_out};
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        hipLaunchKernelGGL((width_v % 4 == 0 ? step_kernel<T, 4> : step_kernel<T, 1>), grid_of((int64_t)num_seq * heads), dim3(kThreads), 0, st, p);
+        return launched();
+    });
+}
+
+}  // extern "C"

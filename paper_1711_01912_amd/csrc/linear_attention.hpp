@@ -1,0 +1,280 @@
+// What the kernels of cp_linear_attention share: the pass over rows with a matrix a head as its state, its operands, the cutting
+// of rows into segments, sequences and chunks, and the fragments that the matrix instructions take.
+#pragma once
+
+#include <climits>
+
+#include "policy.hpp"
+
+namespace cpeval {
+namespace attention {
+
+constexpr int kRows = 64;                // of a chunk
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+
+// rows [rows][heads][width]: element c of head h of row r at r * ld + (h / group) * hd + c
+struct Operand {
+    const void *at;
+    int64_t ld, hd;
+    int32_t group;
+};
+
+// One pass: S_t = gamma S_{t-1} + s_in b_t^T x_t and o_t = s_out a_t S_t along the rows of each sequence, S of wa x wb.  The forward call
+// is one (a, b, x = q, k, v), dq one with (do, v, k), and, from the last row on, dv one with (k, q, do) and dk with (v, do, q).
+// There the state is the gradient of S: it takes part in its own row undecayed (shift 1: gamma^0 for the first row after it).
+struct Pass {
+    int64_t rows, len;                   // len: of a sequence, without ptr
+    const int32_t *ptr;                  // [num_seq + 1], or null
+    int32_t num_seq, segments, parts;    // parts: segments of a sequence, without ptr
+    int64_t seg_rows;
+    int32_t heads, wa, wb, slices;       // slices: workgroups side by side along wb
+    bool back, transposed;               // back: from the last row to the first; transposed: states lie in memory as [wb][wa]
+    int32_t shift;
+    float s_in, s_out;
+    const float *log_decay;
+    Operand a, b, x;
+    const float *init;                   // [num_seq][heads][..] or null
+    const float *enter;                  // [segments][heads][..], states that enter segments, or null (no sequence is cut)
+    float *last;                         // [num_seq][heads][..] or null
+    void *o;                             // rows as a's heads
+    int64_t ldo, hdo;
+    bool wide;                           // o in floats, whatever the type
+    // of the pass for the decays' gradient
+    Operand d;                           // do
+    const float *dlast, *denter;         // gradients of the states behind sequences and segments, or null
+    double *part;                        // [heads][segments * slices]
+};
+
+// ---- sequences ---------------------------------------------------------------------------------------
+
+// rows [lo, hi) of a segment
+__device__ __forceinline__ void segment_of(const Pass &p, int32_t s, int64_t &lo, int64_t &hi) {
+    if (p.ptr) {
+        const int64_t total = min((int64_t)max(p.ptr[p.num_seq], 0), p.rows);
+        lo = min(s * p.seg_rows, total), hi = min(lo + p.seg_rows, total);
+    } else {
+        const int64_t seq = s / p.parts, from = seq * p.len;
+        lo = from + (s % p.parts) * p.seg_rows, hi = min(lo + p.seg_rows, from + p.len);
+    }
+}
+
+// The rows of one sequence inside a segment, in the order of the pass.  (Whatever ptr holds, pieces lie inside the segment and
+// hold a row at least.)
+struct Piece {
+    int64_t lo, hi;
+    int32_t seq;
+    bool starts, ends;                   // whether the sequence does, in the order of the pass
+};
+
+__device__ __forceinline__ Piece piece_at(const Pass &p, int64_t lo, int64_t hi) {
+    const int64_t row = p.back ? hi - 1 : lo;
+    Piece a;
+    int64_t from, to;
+    if (p.ptr) {
+        int32_t l = 0, r = p.num_seq;    // the last sequence that begins at or before the row
+        while (r - l > 1) {
+            const int32_t m = l + (r - l) / 2;
+            if (p.ptr[m] <= row) l = m;
+            else r = m;
+        }
+        a.seq = l;
+        from = p.ptr[l], to = p.ptr[l + 1];
+    } else {
+        a.seq = (int32_t)(row / p.len);
+        from = a.seq * p.len, to = from + p.len;
+    }
+    if (p.back) {
+        a.hi = hi, a.lo = max(lo, min(from, hi - 1));
+        a.starts = to <= hi, a.ends = from >= lo;
+    } else {
+        a.lo = lo, a.hi = min(hi, max(to, lo + 1));
+        a.starts = from >= lo, a.ends = to <= hi;
+    }
+    return a;
+}
+
+// ---- decays ------------------------------------------------------------------------------------------
+
+// Powers of a head's decay: lg = log2 gamma.  So far below one that any power is 0, it is as good as that: 0 * inf does not come up.
+// Above 0, or NaN: NaN.
+__device__ __forceinline__ float lg_of(float log_decay) { return log_decay <= 0.0f ? fmaxf(log_decay * kLog2e, -1000.0f) : __uint_as_float(0x7fc00000u); }
+__device__ __forceinline__ float power(float lg, int n) { return __builtin_amdgcn_exp2f(lg * (float)n); }
+// gamma^n - 1: states are decayed as S + S (gamma^n - 1), which is off by half a step of S where the rounding of a gamma^n close to one
+// would add up along a head's whole memory
+__device__ __forceinline__ float power_less_one(float lg, int n) { return expm1f(lg * (float)n * kLn2); }
+
+// ---- fragments ---------------------------------------------------------------------------------------
+
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Elements as the matrix instructions take them.  bf16 as it is; fp16 as the sum of two bf16, which is exact; what is computed in 32
+// bits (states, scores) as the sum of two bf16, off by at most 2^-16; float as it is, through the float instructions.
+template <typename T>
+struct Form {
+    using E = bf16;
+    static constexpr int kPlanes = 1, kSplit = 2;
+};
+template <>
+struct Form<f16> {
+    using E = bf16;
+    static constexpr int kPlanes = 2, kSplit = 2;
+};
+template <>
+struct Form<float> {
+    using E = float;
+    static constexpr int kPlanes = 1, kSplit = 1;
+};
+
+// 16 x 32 of a matrix in a wavefront: lane l holds, of row (or column) l % 16, places 4 (l / 16) + 0..3 and 16 + 4 (l / 16) + 0..3.
+// That is a result tile's own layout (4 of 16 rows a lane, two tiles), so that states and scores go from results to operands where they are;
+// the order of places in a product does not matter as long as both operands have the same.
+template <typename E, int P>
+struct Frag {
+    bf16x8 p[P];
+};
+template <>
+struct Frag<float, 1> {
+    float v[8];
+};
+
+template <int PA, int PB>
+__device__ __forceinline__ f32x4 product(const Frag<bf16, PA> &a, const Frag<bf16, PB> &b, f32x4 c) {
+#pragma unroll
+    for (int s = 1; s >= 0; s--)
+#pragma unroll
+        for (int i = 0; i < PA; i++) {
+            const int j = s - i;
+            if (j >= 0 && j < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c, 0, 0, 0);
+        }
+    return c;
+}
+__device__ __forceinline__ f32x4 product(const Frag<float, 1> &a, const Frag<float, 1> &b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
+    return c;
+}
+
+__device__ __forceinline__ void split(const float (&v)[8], Frag<float, 1> &f) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) f.v[e] = v[e];
+}
+__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16, 2> &f) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const bf16 hi = (bf16)v[e];
+        f.p[0][e] = hi;
+        f.p[1][e] = (bf16)(v[e] - (float)hi);
+    }
+}
+template <typename E, int P>
+__device__ __forceinline__ void split(f32x4 a, f32x4 b, Frag<E, P> &f) {
+    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    split(v, f);
+}
+__device__ __forceinline__ void values(const Frag<float, 1> &f, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = f.v[e];
+}
+template <int P>
+__device__ __forceinline__ void values(const Frag<bf16, P> &f, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        v[e] = (float)f.p[0][e];
+        if constexpr (P > 1) v[e] += (float)f.p[1][e];
+    }
+}
+
+// Rows of a chunk in LDS; 16 bytes more from row to row than they hold, so that 16 rows' same places lie in different banks.
+template <typename E, int P, int W>
+struct Tile {
+    static constexpr int kPitch = W + 16 / (int)sizeof(E);
+    E at[P][kRows][kPitch];
+
+    // rows r0 + 0..15, places 32 kb + 0..31
+    __device__ __forceinline__ Frag<E, P> along(int r0, int kb, int lane) const {
+        Frag<E, P> f;
+        const int row = r0 + lane % 16, c = 32 * kb + 4 * (lane / 16);
+        if constexpr (sizeof(E) == 4) {
+            const f32x4 a = *(const f32x4 *)&at[0][row][c], b = *(const f32x4 *)&at[0][row][c + 16];
+#pragma unroll
+            for (int e = 0; e < 4; e++) f.v[e] = a[e], f.v[4 + e] = b[e];
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                const bf16x4 a = *(const bf16x4 *)&at[i][row][c], b = *(const bf16x4 *)&at[i][row][c + 16];
+                f.p[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+        }
+        return f;
+    }
+    // columns c0 + 0..15, rows 32 jb + 0..31 as places (16 bits: transposed as they are read, 4 rows of 16 places by 16 lanes)
+    __device__ __forceinline__ Frag<E, P> across(int c0, int jb, int lane) const {
+        Frag<E, P> f;
+        const int i = lane % 16, row = 32 * jb + 4 * (lane / 16);
+        if constexpr (sizeof(E) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) f.v[e] = at[0][row + e][c0 + i], f.v[4 + e] = at[0][row + 16 + e][c0 + i];
+        } else {
+            typedef __attribute__((address_space(3))) bf16x4 *Lds;
+#pragma unroll
+            for (int k = 0; k < P; k++) {
+                const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)&at[k][row + i / 4][c0 + 4 * (i % 4)]);
+                const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((Lds)&at[k][row + 16 + i / 4][c0 + 4 * (i % 4)]);
+                f.p[k] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+        }
+        return f;
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ bool endless(T v) {       // an infinity or a NaN
+    return !(fabsf((float)v) < INFINITY);
+}
+
+// Rows of a chunk from memory to a tile: `count` rows from `row` on (upwards or downwards), places c0 .. c0 + W - 1 of `width`; zeros for the rest.
+// True where a value is an infinity or a NaN.
+template <typename T, typename E, int P, int W>
+__device__ __forceinline__ bool stage(Tile<E, P, W> &tile, const Operand &m, int32_t head, int64_t row, bool down, int count, int c0, int width) {
+    const T *base = (const T *)m.at + row * m.ld + (head / m.group) * m.hd + c0;
+    const int64_t step = down ? -m.ld : m.ld;
+    bool odd = false;
+    constexpr int kPer = W / 8;
+#pragma unroll
+    for (int k = 0; k < kRows * kPer / kThreads; k++) {
+        const int at = k * kThreads + (int)threadIdx.x, r = at / kPer, c = at % kPer * 8;
+        Pack<T, 8> v;
+        const T *from = base + r * step + c;
+        if (r < count && c0 + c + 8 <= width) v = load_pack<T, 8>(from);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v.v[e] = r < count && c0 + c + e < width ? from[e] : (T)0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) odd |= endless(v.v[e]);
+        if constexpr (std::is_same_v<T, E>) *(Pack<T, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = v;
+        else {
+            Pack<E, 8> hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                hi.v[e] = (E)(float)v.v[e];
+                lo.v[e] = (E)((float)v.v[e] - (float)hi.v[e]);
+            }
+            *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = hi;
+            *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[1][r][c], 16) = lo;
+        }
+    }
+    return odd;
+}
+
+// ---- states ------------------------------------------------------------------------------------------
+
+// element (row, col) of a state in memory
+__device__ __forceinline__ int64_t state_at(const Pass &p, int64_t index, int32_t head, int row, int col) {
+    return (index * p.heads + head) * ((int64_t)p.wa * p.wb) + (p.transposed ? (int64_t)col * p.wa + row : (int64_t)row * p.wb + col);
+}
+
+}  // namespace attention
+}  // namespace cpeval
