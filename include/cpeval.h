@@ -708,6 +708,33 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
                                const float *dentropy, int64_t dentropy_stride, void *dlogits, int64_t ldd, void *stream);
 
 /*
+ * Tokens drawn from softmax(scale * logits) over what top_k, top_p and min_p leave of each row's allowed places, by given random
+ * numbers.  With p_v the probabilities in units of the best place's, and the places in the order of falling logit (equal ones by rising
+ * place), what is kept is of the first top_k places those in front of which less than top_p of these places' mass lies (the first
+ * in any case), and of them those with p_v >= min_p.  A token is the first kept place, by place, up to and with which more than u of
+ * the kept mass lies.
+ *
+ *   logits, allow as cp_token_logprobs's
+ *   scale, top_k, top_p, min_p   for all rows: scale > 0 and finite (1 / temperature), top_k >= 0 (0: all), top_p and
+ *                 min_p from 0 to 1; or for each row from scales, top_ks, top_ps, min_ps ([rows] on the device, or NULL).  A row whose
+ *                 own setting is none of these gets no tokens, and CP_STATUS_BAD_SAMPLING
+ *   given, u      random numbers of each row, number g of row i at i * u_row_stride + g * u_stride, from 0 to 1 (below 0 and NaN
+ *                 count as 0, from 1 on as the last number below 1)
+ *   tokens        of CP_TOKEN_* (CP_TOKEN_U8 for at most 255 places), token g of row i at i * token_row_stride + g *
+ *                 token_stride: in either layout such as cp_eval takes as a batch of assignments
+ *   logp          [rows][given], the logarithm of the token's share of the kept mass, or NULL
+ *   status_out    device int32, required where a row has settings of its own
+ * A row with nothing allowed, or with a NaN or +inf at an allowed place, gets tokens -1 (255 of CP_TOKEN_U8) and logp 0.
+ * Probabilities and sums are formed in 64 bits.  Errors: as cp_token_logprobs's; CP_ERR_SIZE where strides put two tokens in one place.
+ */
+int cp_token_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t given, size_t *out_bytes);
+int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, double scale, const float *scales,
+                    const uint64_t *allow, int32_t top_k, const int32_t *top_ks, double top_p, const float *top_ps, double min_p,
+                    const float *min_ps, int32_t given, const float *u, int64_t u_row_stride, int64_t u_stride, void *tokens, int token_type,
+                    int64_t token_row_stride, int64_t token_stride, float *logp, void *workspace, size_t workspace_bytes, void *stream,
+                    int32_t *status_out);
+
+/*
  * Stage timing with HIP events recorded on the stream the kernels run on.
  * A profile holds `slots` sets of CP_NUM_STAGES+1 events; every cp_eval call that
  * is given the profile fills the next slot (CP_ERR_STATE when full).

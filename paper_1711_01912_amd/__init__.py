@@ -49,4 +49,5 @@ from .policy import (  # noqa: F401
     cp_recurrence_step,
     cp_token_logprobs,
     cp_token_logprobs_backward,
+    cp_token_sample,
 )

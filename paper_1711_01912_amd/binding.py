@@ -39,7 +39,7 @@ EXPORTS = (
     "cp_norm_gate", "cp_norm_gate_backward_workspace_bytes", "cp_norm_gate_backward",
     "cp_token_logprobs_workspace_bytes", "cp_token_logprobs", "cp_token_logprobs_backward",
     "cp_linear_attention_workspace_bytes", "cp_linear_attention_carry_states", "cp_linear_attention", "cp_linear_attention_backward",
-    "cp_linear_attention_step",
+    "cp_linear_attention_step", "cp_token_sample_workspace_bytes", "cp_token_sample",
 )
 
 
@@ -182,6 +182,9 @@ def load_library():
                                                  vp, C.c_float, vp, vp, *heads, *heads, *heads, vp, vp, vp, C.c_size_t, vp, vp]
     lib.cp_linear_attention_step.argtypes = [i32, i32, i32, i32, i32, C.c_int, *heads, *heads, *heads, vp, C.c_float, vp, i32, vp,
                                              *heads, vp, vp]
+    lib.cp_token_sample_workspace_bytes.argtypes = [i64, i32, i32, szp]
+    lib.cp_token_sample.argtypes = [i64, i32, C.c_int, vp, i64, C.c_double, vp, vp, i32, vp, C.c_double, vp, C.c_double, vp, i32, vp, i64, i64,
+                                    vp, C.c_int, i64, i64, vp, vp, C.c_size_t, vp, vp]
     _lib = lib
     return lib
 

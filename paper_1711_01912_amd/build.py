@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcpeval.so")
 SOURCES = ["graph.cpp", "cost.cpp", "api.hip", "kernels.hip", "window_shared.hip", "window_stream.hip", "window_lanes.hip", "chain_sweep.hip", "whole_sweep.hip", "column_slice.hip", "pct_order.hip", "constraints.hip", "search.hip", "simulate.hip",
-           "recurrence.hip", "norm_gate.hip", "token_logprobs.hip", "linear_attention.hip"]
+           "recurrence.hip", "norm_gate.hip", "token_logprobs.hip", "token_sample.hip", "linear_attention.hip"]
 HEADERS = ["cpeval_internal.hpp", "launch.hpp", "device_math.hpp", "policy.hpp", "linear_attention.hpp", os.path.join("..", "..", "include", "cpeval.h")]
 
 

@@ -1,7 +1,7 @@
 """The operators of a learned placement policy on torch tensors (see ``include/cpeval.h``).
 
-``cp_recurrence`` (with ``_backward`` and ``_step``), ``cp_norm_gate`` (with ``_backward``) and
-``cp_token_logprobs`` (with ``_backward``) follow the C entry points of the same names.  As in
+``cp_recurrence`` (with ``_backward`` and ``_step``), ``cp_norm_gate`` (with ``_backward``),
+``cp_token_logprobs`` (with ``_backward``) and ``cp_token_sample`` follow the C entry points of the same names.  As in
 ``binding``, nothing is computed here: arguments are checked, outputs and workspaces allocated, and
 the library's kernels called on ``stream`` (default: the current one).  Outputs and workspaces are
 allocated for that stream; inputs of another stream are the caller's to wait for and to keep (``record_stream``).
@@ -24,7 +24,7 @@ from .binding import CpError, load_library
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
 GATE_NONE, GATE_SIGMOID, GATE_SILU = 0, 1, 2
 GATES = {"none": GATE_NONE, "sigmoid": GATE_SIGMOID, "silu": GATE_SILU}
-STATUS_BAD_TOKEN, STATUS_BAD_SEQUENCE, STATUS_BAD_SLOT = 32, 64, 128
+STATUS_BAD_TOKEN, STATUS_BAD_SEQUENCE, STATUS_BAD_SLOT, STATUS_BAD_SAMPLING = 32, 64, 128, 256
 RECURRENCE_CHUNK = 128
 
 
@@ -450,4 +450,69 @@ def cp_token_logprobs_backward(logits, tokens, stats, dlogp, *, dentropy=None, s
                                             stats_at, dlogp_at, row_stride, stride, de_at, de_stride, to, ldd, handle)
     if rc:
         raise CpError(rc, "cp_token_logprobs_backward")
+    return out
+
+
+# ---- tokens from given random numbers --------------------------------------------------------------
+
+
+def _setting(value, name, rows, dtype, device):
+    """(the number for all rows, the address of the rows' own)"""
+    import torch
+    if not isinstance(value, torch.Tensor):
+        return value, None
+    return 1, _vector(value, name, (rows,), dtype, device)
+
+
+def cp_token_sample(logits, u, *, scale=1.0, allow=None, top_k=0, top_p=1.0, min_p=0.0, dtype=None, want_logp=False, out=None,
+                    workspace=None, stream=None, check_status=True):
+    """Tokens drawn from softmax(scale * logits) over what ``top_k``, ``top_p`` and ``min_p`` leave of the places that ``allow``
+    leaves, one for each random number of ``u``.
+
+    ``logits`` [rows][vocab] and ``allow`` as cp_token_logprobs's; ``u`` float32 [rows] or [rows][given], any strides, from 0 to 1.
+    ``scale``, ``top_k`` (0: all), ``top_p``, ``min_p``: numbers, or contiguous tensors [rows] (float32, ``top_k`` int32).  Returns a
+    dict: ``tokens`` as ``u``, of ``dtype`` (uint8, int32 or int64, the default), which ``out`` may bring with any strides, the
+    transposed view of partition-major assignments among them; ``logp`` float32 as ``u`` if wanted; ``status`` with settings a row.
+    A row from which nothing can be drawn gets -1 (255 in uint8).  With ``check_status`` and settings a row the stream is
+    synchronised and settings out of range raise."""
+    import torch
+    lib = load_library()
+    dev = _on_gpu(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError(f"logits: [rows][vocab], not {tuple(logits.shape)}")
+    rows, vocab = logits.shape
+    f32, i32 = torch.float32, torch.int32
+    ld = _matrix(logits, "logits", rows, vocab, logits.dtype, dev)
+    allow_at = _vector(allow, "allow", (rows, -(-vocab // 64)), torch.int64, dev)
+    if u.device != dev or u.dtype is not f32 or u.dim() not in (1, 2) or u.shape[0] != rows:
+        raise ValueError("u: float32 [rows] or [rows][given], on the device of the logits")
+    given = 1 if u.dim() == 1 else int(u.shape[1])
+    (scale, scales), (top_p, top_ps), (min_p, min_ps) = (_setting(v, n, rows, f32, dev) for v, n in
+                                                         ((scale, "scale"), (top_p, "top_p"), (min_p, "min_p")))
+    top_k, top_ks = _setting(top_k, "top_k", rows, i32, dev)
+    if not 0 <= top_k < 1 << 31:
+        raise ValueError(f"top_k: from 0 to 2^31 - 1, not {top_k}")
+    own = not (scales is None and top_ks is None and top_ps is None and min_ps is None)
+    out = dict(out) if out else {}
+    place, handle = _place(dev, stream)
+    with place:
+        tokens = out.get("tokens")
+        if tokens is None:
+            tokens = out["tokens"] = torch.empty(u.shape, dtype=dtype or torch.int64, device=dev)
+        elif tokens.device != dev or tokens.shape != u.shape or (dtype is not None and tokens.dtype is not dtype):
+            raise ValueError(f"tokens: {dtype or 'of'} shape {tuple(u.shape)} on the device of the logits")
+        size = _token_types().get(tokens.dtype)
+        if size is None:
+            raise TypeError(f"tokens: uint8, int32 or int64, not {tokens.dtype}")
+        u_stride, t_stride = u.stride(), tokens.stride()
+        logp_at = _vector_out(out, "logp", u.shape, f32, dev) if want_logp or "logp" in out else None
+        status_at = _vector_out(out, "status", (1,), i32, dev) if own else None
+        work, work_at, room = _room(workspace, _need("cp_token_sample_workspace_bytes", rows, vocab, given), dev)
+        rc = lib.cp_token_sample(rows, vocab, _type(logits, "logits"), logits.data_ptr(), ld, scale, scales, allow_at, top_k, top_ks, top_p, top_ps,
+                                 min_p, min_ps, given, u.data_ptr(), u_stride[0], u_stride[1] if len(u_stride) == 2 else 0, tokens.data_ptr(), size,
+                                 t_stride[0], t_stride[1] if len(t_stride) == 2 else 1, logp_at, work_at, room, handle, status_at)
+    if rc:
+        raise CpError(rc, "cp_token_sample")
+    if check_status and own:
+        _check(out["status"], STATUS_BAD_SAMPLING, "scale, top_k, top_p or min_p of a row is out of range", stream)
     return out
