@@ -7,8 +7,8 @@
 //   o_i = scale (gamma^(i+1) q_i S + sum_{j <= i} gamma^(i-j) (q_i . k_j) v_j)
 //   S'  = gamma^n S + sum_j gamma^(n-1-j) k_j^T v_j
 //
-// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS.  All products of
-// a column stay in its wavefront: the scores are computed by each, and only the tiles on and below the diagonal.
+// A wavefront owns 16 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS, the next chunk is on its
+// way in registers.  The scores, of which only the tiles on and below the diagonal are computed, are shared out among the wavefronts.
 //
 // The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
 //   dq_t = scale do_t S_t^T (the pass with do, v, k in the places of q, k, v),   dv_t = k_t D_t and dk_t = v_t D_t^T (from the last
@@ -47,119 +47,106 @@ __device__ __forceinline__ void put(T *to, f32x4 o, float scale, int count) {
 // kOut: outputs; kEffect: a segment's effect on the state alone; kDecay: the decays' gradient
 enum Kind { kOut, kEffect, kDecay };
 
-template <int KB, int NT>
+// 16 columns of a state, all of its rows, in a wavefront's registers: lane l has column l % 16, rows 16 k + 4 (l / 16) + 0..3
+template <int KB>
 struct State {
-    f32x4 at[2 * KB][NT];
+    f32x4 at[2 * KB];
     __device__ __forceinline__ void zero() {
 #pragma unroll
+        for (int k = 0; k < 2 * KB; k++) at[k] = f32x4{0, 0, 0, 0};
+    }
+    // (where the lane's first element lies is hidden from the compiler, which else keeps the addresses of all of them, and whether they
+    // are there, in registers throughout the pass)
+    template <typename F>
+    __device__ __forceinline__ void each(const Pass &p, int64_t index, int32_t head, int col, int g, F f) {
+        int row0 = 4 * g;
+        asm volatile("" : "+v"(row0));
+        const int64_t base = (index * p.heads + head) * ((int64_t)p.wa * p.wb);
+        const int across = p.transposed ? p.wa : 1, down = p.transposed ? 1 : p.wb;
+        const int at0 = col * across;
+#pragma unroll
         for (int k = 0; k < 2 * KB; k++)
 #pragma unroll
-            for (int n = 0; n < NT; n++) at[k][n] = f32x4{0, 0, 0, 0};
+            for (int e = 0; e < 4; e++) {
+                const int row = row0 + 16 * k + e;
+                if (row < p.wa && col < p.wb) at[k][e] = f(at[k][e], base + (at0 + row * down));
+            }
     }
     __device__ __forceinline__ void load(const Pass &p, const float *from, int64_t index, int32_t head, int col, int g) {
-#pragma unroll
-        for (int k = 0; k < 2 * KB; k++)
-#pragma unroll
-            for (int n = 0; n < NT; n++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int row = 16 * k + 4 * g + e, c = col + 16 * n;
-                    at[k][n][e] = row < p.wa && c < p.wb ? from[state_at(p, index, head, row, c)] : 0.0f;
-                }
+        zero();
+        each(p, index, head, col, g, [&](float, int64_t i) { return from[i]; });
     }
-    __device__ __forceinline__ void store(const Pass &p, float *to, int64_t index, int32_t head, int col, int g) const {
-#pragma unroll
-        for (int k = 0; k < 2 * KB; k++)
-#pragma unroll
-            for (int n = 0; n < NT; n++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int row = 16 * k + 4 * g + e, c = col + 16 * n;
-                    if (row < p.wa && c < p.wb) to[state_at(p, index, head, row, c)] = at[k][n][e];
-                }
+    __device__ __forceinline__ void store(const Pass &p, float *to, int64_t index, int32_t head, int col, int g) {
+        each(p, index, head, col, g, [&](float v, int64_t i) { return to[i] = v; });
     }
-    __device__ __forceinline__ double dot(const Pass &p, const float *with, int64_t index, int32_t head, int col, int g) const {
+    __device__ __forceinline__ double dot(const Pass &p, const float *with, int64_t index, int32_t head, int col, int g) {
         double sum = 0;
-#pragma unroll
-        for (int k = 0; k < 2 * KB; k++)
-#pragma unroll
-            for (int n = 0; n < NT; n++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int row = 16 * k + 4 * g + e, c = col + 16 * n;
-                    if (row < p.wa && c < p.wb) sum += (double)(at[k][n][e] * with[state_at(p, index, head, row, c)]);
-                }
+        each(p, index, head, col, g, [&](float v, int64_t i) { return sum += (double)(v * with[i]), v; });
         return sum;
     }
 };
 
-template <typename T, int KB, int NT, Kind kind>
-__global__ __launch_bounds__(kThreads) void pass_kernel(Pass p, float *effect, float *gain) {
-    using E = typename Form<T>::E;
-    constexpr int P = Form<T>::kPlanes, PS = Form<T>::kSplit, kWide = 16 * NT * kWaves;
-    __shared__ Tile<E, P, 32 * KB> b_tile;
-    __shared__ Tile<E, P, kWide> x_tile;
-    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB> a_tile;
+// KB: blocks of 32 that the state's rows fill; WAVES: of a workgroup, 16 columns each; R: rows of a chunk
+template <typename T, int KB, int WAVES, int R, Kind kind>
+__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel(Pass p, float *effect, float *gain) {
+    using F = Form<T>;
+    using E = typename F::E;
+    constexpr int P = F::kPlanes, PS = kind == kDecay ? F::kFine : F::kSplit, PU = F::kFine;
+    constexpr int kThreadsHere = WAVES * kWave, kWide = 16 * WAVES, IT = R / 16, JB = R / 32;
+    __shared__ Tile<E, P, 32 * KB, R> b_tile;
+    __shared__ Tile<E, P, kWide, R> x_tile;
+    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R> a_tile;
+    __shared__ Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R> s_tile;       // scores [row][place]
     __shared__ int odd[2];
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane % 16, g = lane / 16;
     const uint32_t group = group_number();
     const int32_t slice = group % p.slices, head = group / p.slices % p.heads, seg = group / p.slices / p.heads;
     if (seg >= p.segments) return;                     // (the whole workgroup)
-    const int c0 = slice * kWide, mine = c0 + wave * 16 * NT, col = mine + l;
+    const int c0 = slice * kWide, col = c0 + 16 * wave + l;
     const float lg = lg_of(p.log_decay ? p.log_decay[head] : 0.0f);
-
-    // the decay between rows i and j of the diagonal's tiles and of those right below it, of lane l's i and 4 places of j
-    float near_[2][4];
-#pragma unroll
-    for (int d = 0; d < 2; d++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int apart = 16 * d + l - 4 * g - e;
-            near_[d][e] = apart < 0 ? 0.0f : power(lg, apart) * p.s_in;
-        }
-    const float by16 = power(lg, 16);
 
     int64_t lo, hi;
     segment_of(p, seg, lo, hi);
     if (threadIdx.x == 0) odd[0] = odd[1] = 0;
     double decay_sum = 0;
     int turn = 0;
-    State<KB, NT> s, r;
-    bool whole = true;
+    State<KB> s, r;
     if constexpr (kind == kEffect) {
-        // only the sequence that goes on behind the segment
+        // only the sequence that goes on behind the segment: the last piece in the order of the pass, which is the first one seen from there
         s.zero();
-        bool ends = true;
+        bool ends = true, whole = false;
         if (lo < hi) {
-            int64_t from = lo, to = hi;
-            // (the last piece in the order of the pass: the one at that end, seen from the other direction)
             Pass turned = p;
             turned.back = !p.back;
             const Piece last = piece_at(turned, lo, hi);
-            from = last.lo, to = last.hi;
-            ends = last.starts;                        // (its end, seen from there)
-            whole = !last.ends;
-            lo = from, hi = to;
+            ends = last.starts, whole = !last.ends;    // (its end and its start, seen from there)
+            lo = last.lo, hi = last.hi;
         }
-        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = lo < hi && whole && !ends ? power(lg, (int)(hi - lo)) : 0.0f;
+        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = whole && !ends ? power(lg, (int)(hi - lo)) : 0.0f;
         if (ends) lo = hi;
     }
+    Rows<T, 32 * KB, R, kThreadsHere> a_rows, b_rows;
+    Rows<T, kWide, R, kThreadsHere> x_rows;
     while (lo < hi) {
         const Piece piece = piece_at(p, lo, hi);
+        int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
+        const auto fetch = [&](int count) {
+            x_rows.load(p.x, head, row, p.back, count, c0, p.wb);
+            b_rows.load(p.b, head, row, p.back, count, 0, p.wa);
+            if constexpr (kind != kEffect) a_rows.load(p.a, head, row, p.back, count, 0, p.wa);
+        };
+        int n = (int)min((int64_t)R, left);
+        fetch(n);
         if (piece.starts && p.init) s.load(p, p.init, piece.seq, head, col, g);
         else if (kind != kEffect && !piece.starts && p.enter) s.load(p, p.enter, seg, head, col, g);
         else s.zero();
         if constexpr (kind == kDecay) r.zero();
-        int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
-        int most = kRows;
         while (left > 0) {
-            const int n = (int)min((int64_t)most, left);
-            __syncthreads();
-            bool found = stage<T>(x_tile, p.x, head, row, p.back, n, c0, p.wb);
-            stage<T>(b_tile, p.b, head, row, p.back, n, 0, p.wa);
+            const bool found = x_rows.store(x_tile, n);
+            b_rows.store(b_tile, n);
             if constexpr (kind != kEffect) {
-                stage<T>(a_tile, p.a, head, row, p.back, n, 0, p.wa);
+                a_rows.store(a_tile, n);
                 if (found) odd[turn] = 1;
             }
             __syncthreads();
@@ -169,148 +156,133 @@ __global__ __launch_bounds__(kThreads) void pass_kernel(Pass p, float *effect, f
                 turn ^= 1;
                 if (threadIdx.x == 0) odd[turn] = 0;
                 if (bad && n > 1) {
-                    most = 1;
-                    continue;
+                    n = 1;
+                    __syncthreads();
+                    continue;                          // (the registers still hold the rows)
                 }
-                most = kRows;
             }
+            // the next chunk is on its way while this one is computed
+            const int64_t here = row;
+            const int count = n;
+            left -= n;
+            row += p.back ? -n : n;
+            n = (int)min((int64_t)R, left);
+            if (left > 0) fetch(n);
 
-            // outputs
+            f32x4 o[IT];
             if constexpr (kind != kEffect) {
-                Frag<E, PS> sf[KB][NT], rf[kind == kDecay ? KB : 1][NT];
+                // scores of rows i (lanes) and j (places), with the decay between them: the tiles on and below the diagonal, shared out
 #pragma unroll
-                for (int k = 0; k < KB; k++)
+                for (int k0 = 0; k0 < (IT * (IT + 1) / 2 + WAVES - 1) / WAVES; k0++) {
+                    const int tile = wave + k0 * WAVES;
+                    int it = 0;
 #pragma unroll
-                    for (int t = 0; t < NT; t++) {
-                        split(s.at[2 * k][t], s.at[2 * k + 1][t], sf[k][t]);
-                        if constexpr (kind == kDecay) split(r.at[2 * k][t], r.at[2 * k + 1][t], rf[k][t]);
+                    for (int k = 1; k < IT; k++) it += tile >= k * (k + 1) / 2;
+                    const int jt = tile - it * (it + 1) / 2;
+                    if (tile >= IT * (IT + 1) / 2 || 16 * it >= count) continue;
+                    f32x4 c = {0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < KB; k++) c = product<true>(b_tile.along(16 * jt, k, lane), a_tile.along(16 * it, k, lane), c);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int apart = 16 * (it - jt) + l - 4 * g - e;
+                        // (what lies above the diagonal is not looked at)
+                        c[e] = apart < 0 ? 0.0f : c[e] * (power(lg, apart) * p.s_in);
+                        if constexpr (kind == kDecay) c[e] *= (float)max(apart, 0);
                     }
+                    s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
+                    // (the tile right of the diagonal shares its block of 32)
+                    if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
+                }
+                // what the state that enters gives
+                Frag<E, PS> sf[KB], rf[kind == kDecay ? KB : 1];
 #pragma unroll
-                for (int it = 0; it < kRows / 16; it++) {
-                    if (16 * it >= n) break;
+                for (int k = 0; k < KB; k++) {
+                    split(s.at[2 * k], s.at[2 * k + 1], sf[k]);
+                    if constexpr (kind == kDecay) split(r.at[2 * k], r.at[2 * k + 1], rf[k]);
+                }
+#pragma unroll
+                for (int it = 0; it < IT; it++) {
+                    if (16 * it >= count) break;
                     const int i = 16 * it + l;
-                    Frag<E, P> af[KB];
+                    f32x4 from_s = {0, 0, 0, 0}, from_r = {0, 0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < KB; k++) af[k] = a_tile.along(16 * it, k, lane);
-                    // scores of rows i (lanes) and j (places), with the decay between them
-                    f32x4 score[4] = {};
-                    float far_ = 1.0f;
-#pragma unroll
-                    for (int jt = it; jt >= 0; jt--) {
-                        f32x4 c = {0, 0, 0, 0};
-#pragma unroll
-                        for (int k = 0; k < KB; k++) c = product(b_tile.along(16 * jt, k, lane), af[k], c);
-                        if (it - jt > 1) far_ *= by16;
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const float by = near_[it - jt > 0][e] * far_;
-                            // (the diagonal's tile: what lies above it is not looked at)
-                            score[jt][e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * by;
-                        }
+                    for (int k = 0; k < KB; k++) {
+                        const Frag<E, P> af = a_tile.along(16 * it, k, lane);
+                        from_s = product(sf[k], af, from_s);
+                        if constexpr (kind == kDecay) from_r = product(rf[k], af, from_r);
                     }
                     const float in = power(lg, i + 1 - p.shift);
 #pragma unroll
-                    for (int t = 0; t < NT; t++) {
-                        f32x4 o = {0, 0, 0, 0};
+                    for (int e = 0; e < 4; e++) o[it][e] = (kind == kDecay ? from_r[e] + (float)(i + 1) * from_s[e] : from_s[e]) * in;
+                }
+                __syncthreads();
+            }
+            Frag<E, P> xf[JB];
 #pragma unroll
-                        for (int k = 0; k < KB; k++) o = product(sf[k][t], af[k], o);
-                        if constexpr (kind == kDecay) {
-                            f32x4 more = {0, 0, 0, 0};
+            for (int jb = 0; jb < JB; jb++) xf[jb] = x_tile.across(16 * wave, jb, lane);
+            if constexpr (kind != kEffect) {
+                // and what its own rows give; lane l has row i, columns 4 g + 0..3
+                const int c = c0 + 16 * wave + 4 * g;
 #pragma unroll
-                            for (int k = 0; k < KB; k++) more = product(rf[k][t], af[k], more);
+                for (int it = 0; it < IT; it++) {
+                    if (16 * it >= count) break;
+                    const int i = 16 * it + l;
 #pragma unroll
-                            for (int e = 0; e < 4; e++) o[e] = more[e] + (float)(i + 1) * o[e];
-                        }
+                    for (int jb = 0; jb <= it / 2; jb++) o[it] = product(xf[jb], s_tile.along(16 * it, jb, lane), o[it]);
+                    if (i < count) {
+                        const int64_t at = here + (p.back ? -i : i);
+                        if constexpr (kind == kOut) {
+                            const int64_t to = at * p.ldo + head * p.hdo + c;
+                            if (p.wide) put((float *)p.o + to, o[it], p.s_out, p.wb - c);
+                            else put((T *)p.o + to, o[it], p.s_out, p.wb - c);
+                        } else {
+                            const T *from = (const T *)p.d.at + at * p.d.ld + (head / p.d.group) * p.d.hd + c;
+                            float sum = 0;
 #pragma unroll
-                        for (int e = 0; e < 4; e++) o[e] *= in;
-#pragma unroll
-                        for (int jb = 0; jb <= it / 2; jb++) {
-                            f32x4 u = score[2 * jb], v = score[2 * jb + 1];
-                            if constexpr (kind == kDecay) {
-#pragma unroll
-                                for (int e = 0; e < 4; e++) {
-                                    u[e] *= (float)(i - (32 * jb + 4 * g + e));
-                                    v[e] *= (float)(i - (32 * jb + 16 + 4 * g + e));
-                                }
-                            }
-                            Frag<E, PS> sc;
-                            split(u, v, sc);
-                            o = product(x_tile.across(wave * 16 * NT + 16 * t, jb, lane), sc, o);
-                        }
-                        // lane l has row i, columns 4 g + 0..3
-                        const int c = mine + 16 * t + 4 * g;
-                        if (i < n) {
-                            const int64_t at = row + (p.back ? -i : i);
-                            if constexpr (kind == kOut) {
-                                const int64_t to = at * p.ldo + head * p.hdo + c;
-                                if (p.wide) put((float *)p.o + to, o, p.s_out, p.wb - c);
-                                else put((T *)p.o + to, o, p.s_out, p.wb - c);
-                            } else {
-                                const T *from = (const T *)p.d.at + at * p.d.ld + (head / p.d.group) * p.d.hd + c;
-                                float sum = 0;
-#pragma unroll
-                                for (int e = 0; e < 4; e++)
-                                    if (c + e < p.wb) sum += (float)from[e] * o[e];
-                                decay_sum += (double)(sum * p.s_out);
-                            }
+                            for (int e = 0; e < 4; e++)
+                                if (c + e < p.wb) sum += (float)from[e] * o[it][e];
+                            decay_sum += (double)(sum * p.s_out);
                         }
                     }
                 }
             }
 
             // the state behind the chunk
-            const float wane = power_less_one(lg, n);
+            const float wane = power_less_one(lg, count);
             if constexpr (kind == kDecay) {
-                const float far_ = power(lg, n) * (float)n;
+                const float far_ = power(lg, count) * (float)count;
 #pragma unroll
                 for (int k = 0; k < 2 * KB; k++)
 #pragma unroll
-                    for (int t = 0; t < NT; t++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) r.at[k][t][e] = fmaf(r.at[k][t][e], wane, r.at[k][t][e]) + far_ * s.at[k][t][e];
+                    for (int e = 0; e < 4; e++) r.at[k][e] = fmaf(r.at[k][e], wane, r.at[k][e]) + far_ * s.at[k][e];
             }
 #pragma unroll
             for (int k = 0; k < 2 * KB; k++)
 #pragma unroll
-                for (int t = 0; t < NT; t++)
+                for (int e = 0; e < 4; e++) s.at[k][e] = fmaf(s.at[k][e], wane, s.at[k][e]);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) s.at[k][t][e] = fmaf(s.at[k][t][e], wane, s.at[k][t][e]);
-#pragma unroll
-            for (int jb = 0; jb < kRows / 32; jb++) {
-                if (32 * jb >= n) break;
-                float w[8];
-                int behind[8];
+            for (int jb = 0; jb < JB; jb++) {
+                if (32 * jb >= count) break;
+                float v[8], w[8];
+                values(xf[jb], v);
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    behind[e] = max(n - 1 - (32 * jb + 16 * (e / 4) + 4 * g + e % 4), 0);       // (rows behind the chunk's are zeros)
-                    w[e] = power(lg, behind[e] + p.shift) * p.s_in;
+                    const int behind = max(count - 1 - (32 * jb + 16 * (e / 4) + 4 * g + e % 4), 0);       // (rows behind the chunk's are zeros)
+                    v[e] *= power(lg, behind + p.shift) * p.s_in;
+                    w[e] = v[e] * (float)behind;
                 }
-                Frag<E, PS> xf[NT], yf[kind == kDecay ? NT : 1];
-#pragma unroll
-                for (int t = 0; t < NT; t++) {
-                    float v[8];
-                    values(x_tile.across(wave * 16 * NT + 16 * t, jb, lane), v);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] *= w[e];
-                    split(v, xf[t]);
-                    if constexpr (kind == kDecay) {
-#pragma unroll
-                        for (int e = 0; e < 8; e++) v[e] *= (float)behind[e];
-                        split(v, yf[t]);
-                    }
-                }
+                Frag<E, PU> vf, wf;
+                split(v, vf);
+                if constexpr (kind == kDecay) split(w, wf);
 #pragma unroll
                 for (int k = 0; k < 2 * KB; k++) {
                     const Frag<E, P> bf = b_tile.across(16 * k, jb, lane);
-#pragma unroll
-                    for (int t = 0; t < NT; t++) {
-                        s.at[k][t] = product(bf, xf[t], s.at[k][t]);
-                        if constexpr (kind == kDecay) r.at[k][t] = product(bf, yf[t], r.at[k][t]);
-                    }
+                    s.at[k] = product(bf, vf, s.at[k]);
+                    if constexpr (kind == kDecay) r.at[k] = product(bf, wf, r.at[k]);
                 }
             }
-            left -= n;
-            row += p.back ? -n : n;
+            __syncthreads();
         }
         if constexpr (kind == kOut) {
             if (piece.ends && p.last) s.store(p, p.last, piece.seq, head, col, g);
@@ -325,12 +297,15 @@ __global__ __launch_bounds__(kThreads) void pass_kernel(Pass p, float *effect, f
     }
     if constexpr (kind == kEffect) s.store(p, effect, seg, head, col, g);
     if constexpr (kind == kDecay) {
-        __shared__ double sums[kWaves];
+        __shared__ double sums[WAVES];
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) decay_sum += __shfl_xor(decay_sum, off);
         if (lane == 0) sums[wave] = decay_sum;
         __syncthreads();
-        if (threadIdx.x == 0) p.part[(int64_t)head * p.segments * p.slices + seg * p.slices + slice] = sums[0] + sums[1] + sums[2] + sums[3];
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < WAVES; w++) decay_sum += sums[w];
+            p.part[(int64_t)head * p.segments * p.slices + seg * p.slices + slice] = decay_sum;
+        }
     }
 }
 
@@ -490,7 +465,7 @@ Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads) {
     int64_t parts = std::max<int64_t>(1, std::min((kWanted + units - 1) / units, len / kLeast));
     Cut c;
     c.seg_rows = std::max<int64_t>((len + parts - 1) / parts, 1);
-    c.seg_rows = (c.seg_rows + kRows - 1) / kRows * kRows;
+    c.seg_rows = (c.seg_rows + 63) / 64 * 64;
     parts = std::max<int64_t>(1, (len + c.seg_rows - 1) / c.seg_rows);
     c.parts = (int32_t)parts;
     c.segments = (int32_t)(packed ? parts : parts * num_seq);
@@ -498,25 +473,29 @@ Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads) {
     return c;
 }
 
-// columns that a workgroup takes: 64, or 128 where there are more and registers hold them
-int tiles_of(int32_t wa, int32_t wb) { return wb > 64 && wa <= 128 ? 2 : 1; }
-int32_t slices_of(int32_t wa, int32_t wb) { return (wb + 64 * tiles_of(wa, wb) - 1) / (64 * tiles_of(wa, wb)); }
+// Columns that a workgroup takes, 16 a wavefront: 64 where there are no more (two or three workgroups a compute unit), else 128
+int waves_of(int32_t wa, int32_t wb) { return wb > 64 || wa > 128 ? 8 : 4; }
+int32_t slices_of(int32_t wa, int32_t wb) { return (wb + 16 * waves_of(wa, wb) - 1) / (16 * waves_of(wa, wb)); }
 
-template <typename T, int KB, int NT>
+template <typename T, int KB, int WAVES>
 int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t st) {
-    auto *kernel = kind == kOut ? pass_kernel<T, KB, NT, kOut> : kind == kEffect ? pass_kernel<T, KB, NT, kEffect> : pass_kernel<T, KB, NT, kDecay>;
-    hipLaunchKernelGGL(kernel, grid_of((int64_t)p.segments * p.heads * p.slices), dim3(kThreads), 0, st, p, effect, gain);
+    // (rows of 32-bit elements or of two bf16 each do not find room for 64 of 256 places)
+    constexpr int R = KB == 8 && !std::is_same_v<T, bf16> ? 32 : 64;
+    auto *kernel = kind == kOut      ? pass_kernel<T, KB, WAVES, R, kOut>
+                   : kind == kEffect ? pass_kernel<T, KB, WAVES, R, kEffect>
+                                     : pass_kernel<T, KB, WAVES, R, kDecay>;
+    hipLaunchKernelGGL(kernel, grid_of((int64_t)p.segments * p.heads * p.slices), dim3(WAVES * kWave), 0, st, p, effect, gain);
     return launched();
 }
 
 int run(Kind kind, int type, Pass p, float *effect, float *gain, hipStream_t st) {
     p.slices = slices_of(p.wa, p.wb);
-    const int tiles = tiles_of(p.wa, p.wb);
+    const bool wide = waves_of(p.wa, p.wb) == 8;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        if (p.wa > 128) return run_sized<T, 8, 1>(kind, p, effect, gain, st);
-        if (p.wa > 64) return tiles == 2 ? run_sized<T, 4, 2>(kind, p, effect, gain, st) : run_sized<T, 4, 1>(kind, p, effect, gain, st);
-        return tiles == 2 ? run_sized<T, 2, 2>(kind, p, effect, gain, st) : run_sized<T, 2, 1>(kind, p, effect, gain, st);
+        if (p.wa > 128) return run_sized<T, 8, 8>(kind, p, effect, gain, st);
+        if (p.wa > 64) return wide ? run_sized<T, 4, 8>(kind, p, effect, gain, st) : run_sized<T, 4, 4>(kind, p, effect, gain, st);
+        return wide ? run_sized<T, 2, 8>(kind, p, effect, gain, st) : run_sized<T, 2, 4>(kind, p, effect, gain, st);
     });
 }
 

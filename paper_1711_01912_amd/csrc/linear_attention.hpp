@@ -9,8 +9,7 @@
 namespace cpeval {
 namespace attention {
 
-constexpr int kRows = 64;                // of a chunk
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256;            // of the kernels beside the pass
 
 // rows [rows][heads][width]: element c of head h of row r at r * ld + (h / group) * hd + c
 struct Operand {
@@ -110,21 +109,23 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Elements as the matrix instructions take them.  bf16 as it is; fp16 as the sum of two bf16, which is exact; what is computed in 32
-// bits (states, scores) as the sum of two bf16, off by at most 2^-16; float as it is, through the float instructions.
+// bits as the sum of bf16 too: of two, off by at most 2^-16, where the result has 16 bits itself (states and scores on their way to an output),
+// of three, off by 2^-24, where it has 32 (rows on their way to a state, all that the decays' gradient is made of).  float as it is,
+// through the float instructions.
 template <typename T>
 struct Form {
     using E = bf16;
-    static constexpr int kPlanes = 1, kSplit = 2;
+    static constexpr int kPlanes = 1, kSplit = 2, kFine = 3;
 };
 template <>
 struct Form<f16> {
     using E = bf16;
-    static constexpr int kPlanes = 2, kSplit = 2;
+    static constexpr int kPlanes = 2, kSplit = 2, kFine = 3;
 };
 template <>
 struct Form<float> {
     using E = float;
-    static constexpr int kPlanes = 1, kSplit = 1;
+    static constexpr int kPlanes = 1, kSplit = 1, kFine = 1;
 };
 
 // 16 x 32 of a matrix in a wavefront: lane l holds, of row (or column) l % 16, places 4 (l / 16) + 0..3 and 16 + 4 (l / 16) + 0..3.
@@ -139,10 +140,12 @@ struct Frag<float, 1> {
     float v[8];
 };
 
-template <int PA, int PB>
+// (the smallest parts first; parts that together lie beyond the finer operand's last are left out, unless all are asked for)
+template <bool ALL = false, int PA, int PB>
 __device__ __forceinline__ f32x4 product(const Frag<bf16, PA> &a, const Frag<bf16, PB> &b, f32x4 c) {
+    constexpr int kMost = ALL ? PA + PB - 1 : PA > PB ? PA : PB;
 #pragma unroll
-    for (int s = 1; s >= 0; s--)
+    for (int s = kMost - 1; s >= 0; s--)
 #pragma unroll
         for (int i = 0; i < PA; i++) {
             const int j = s - i;
@@ -150,6 +153,7 @@ __device__ __forceinline__ f32x4 product(const Frag<bf16, PA> &a, const Frag<bf1
         }
     return c;
 }
+template <bool ALL = false>
 __device__ __forceinline__ f32x4 product(const Frag<float, 1> &a, const Frag<float, 1> &b, f32x4 c) {
 #pragma unroll
     for (int i = 0; i < 8; i++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
@@ -160,12 +164,16 @@ __device__ __forceinline__ void split(const float (&v)[8], Frag<float, 1> &f) {
 #pragma unroll
     for (int e = 0; e < 8; e++) f.v[e] = v[e];
 }
-__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16, 2> &f) {
+template <int P>
+__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16, P> &f) {
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-        const bf16 hi = (bf16)v[e];
-        f.p[0][e] = hi;
-        f.p[1][e] = (bf16)(v[e] - (float)hi);
+        float rest = v[e];
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            f.p[i][e] = (bf16)rest;
+            rest -= (float)f.p[i][e];
+        }
     }
 }
 template <typename E, int P>
@@ -186,11 +194,11 @@ __device__ __forceinline__ void values(const Frag<bf16, P> &f, float (&v)[8]) {
     }
 }
 
-// Rows of a chunk in LDS; 16 bytes more from row to row than they hold, so that 16 rows' same places lie in different banks.
-template <typename E, int P, int W>
+// R rows of a chunk in LDS; 16 bytes more from row to row than they hold, so that 16 rows' same places lie in different banks.
+template <typename E, int P, int W, int R>
 struct Tile {
     static constexpr int kPitch = W + 16 / (int)sizeof(E);
-    E at[P][kRows][kPitch];
+    E at[P][R][kPitch];
 
     // rows r0 + 0..15, places 32 kb + 0..31
     __device__ __forceinline__ Frag<E, P> along(int r0, int kb, int lane) const {
@@ -227,6 +235,23 @@ struct Tile {
         }
         return f;
     }
+    // 4 places from c on of a row, as what is computed is kept
+    __device__ __forceinline__ void keep(int row, int c, f32x4 v) {
+        if constexpr (sizeof(E) == 4) *(f32x4 *)&at[0][row][c] = v;
+        else {
+            float rest[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                bf16x4 b;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    b[e] = (bf16)rest[e];
+                    rest[e] -= (float)b[e];
+                }
+                *(bf16x4 *)&at[i][row][c] = b;
+            }
+        }
+    }
 };
 
 template <typename T>
@@ -234,47 +259,57 @@ __device__ __forceinline__ bool endless(T v) {       // an infinity or a NaN
     return !(fabsf((float)v) < INFINITY);
 }
 
-// Rows of a chunk from memory to a tile: `count` rows from `row` on (upwards or downwards), places c0 .. c0 + W - 1 of `width`; zeros for the rest.
-// True where a value is an infinity or a NaN.
-template <typename T, typename E, int P, int W>
-__device__ __forceinline__ bool stage(Tile<E, P, W> &tile, const Operand &m, int32_t head, int64_t row, bool down, int count, int c0, int width) {
-    const T *base = (const T *)m.at + row * m.ld + (head / m.group) * m.hd + c0;
-    const int64_t step = down ? -m.ld : m.ld;
-    bool odd = false;
-    constexpr int kPer = W / 8;
+// Rows of a chunk on their way from memory to a tile, in registers: places c0 .. c0 + W - 1 of `width`; zeros where there are none.
+template <typename T, int W, int R, int THREADS>
+struct Rows {
+    static constexpr int kPer = W / 8, kLoads = (R * kPer + THREADS - 1) / THREADS;
+    Pack<T, 8> v[kLoads];
+
+    // `count` rows from `row` on, upwards or downwards
+    __device__ __forceinline__ void load(const Operand &m, int32_t head, int64_t row, bool down, int count, int c0, int width) {
+        const T *base = (const T *)m.at + row * m.ld + (head / m.group) * m.hd + c0;
+        const int64_t step = down ? -m.ld : m.ld;
 #pragma unroll
-    for (int k = 0; k < kRows * kPer / kThreads; k++) {
-        const int at = k * kThreads + (int)threadIdx.x, r = at / kPer, c = at % kPer * 8;
-        Pack<T, 8> v;
-        const T *from = base + r * step + c;
-        if (r < count && c0 + c + 8 <= width) v = load_pack<T, 8>(from);
-        else {
+        for (int k = 0; k < kLoads; k++) {
+            const int at = k * THREADS + (int)threadIdx.x, r = at / kPer, c = at % kPer * 8;
+            const T *from = base + r * step + c;
+            if (r < count && c0 + c + 8 <= width) v[k] = load_pack<T, 8>(from);
+            else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) v.v[e] = r < count && c0 + c + e < width ? from[e] : (T)0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; e++) odd |= endless(v.v[e]);
-        if constexpr (std::is_same_v<T, E>) *(Pack<T, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = v;
-        else {
-            Pack<E, 8> hi, lo;
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                hi.v[e] = (E)(float)v.v[e];
-                lo.v[e] = (E)((float)v.v[e] - (float)hi.v[e]);
+                for (int e = 0; e < 8; e++) v[k].v[e] = r < count && c0 + c + e < width ? from[e] : (T)0.0f;
             }
-            *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = hi;
-            *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[1][r][c], 16) = lo;
         }
     }
-    return odd;
-}
-
-// ---- states ------------------------------------------------------------------------------------------
-
-// element (row, col) of a state in memory
-__device__ __forceinline__ int64_t state_at(const Pass &p, int64_t index, int32_t head, int row, int col) {
-    return (index * p.heads + head) * ((int64_t)p.wa * p.wb) + (p.transposed ? (int64_t)col * p.wa + row : (int64_t)row * p.wb + col);
-}
+    // true where a value is an infinity or a NaN
+    template <typename E, int P>
+    __device__ __forceinline__ bool store(Tile<E, P, W, R> &tile, int count) const {
+        bool odd = false;
+#pragma unroll
+        for (int k = 0; k < kLoads; k++) {
+            const int at = k * THREADS + (int)threadIdx.x, r = at / kPer, c = at % kPer * 8;
+            if (R * kPer % THREADS && r >= R) break;
+            Pack<T, 8> u = v[k];
+            if (r >= count) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) u.v[e] = (T)0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) odd |= endless(u.v[e]);
+            if constexpr (std::is_same_v<T, E>) *(Pack<T, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = u;
+            else {
+                Pack<E, 8> hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    hi.v[e] = (E)(float)u.v[e];
+                    lo.v[e] = (E)((float)u.v[e] - (float)hi.v[e]);
+                }
+                *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = hi;
+                *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[1][r][c], 16) = lo;
+            }
+        }
+        return odd;
+    }
+};
 
 }  // namespace attention
 }  // namespace cpeval
