@@ -126,15 +126,54 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
         if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = whole && !ends ? power(lg, (int)(hi - lo)) : 0.0f;
         if (ends) lo = hi;
     }
+    // What does not change from chunk to chunk: the decays between a score's rows, of this wavefront's tiles, into rows from before
+    // the chunk, and from rows to its end
+    constexpr int kTiles = IT * (IT + 1) / 2, kMine = (kTiles + WAVES - 1) / WAVES;
+    float apart_[kMine][4], in_[IT], out_[JB][8];
+    const auto tile_of = [&](int k, int &it, int &jt) {
+        const int tile = wave + k * WAVES;
+        it = 0;
+#pragma unroll
+        for (int n = 1; n < IT; n++) it += tile >= n * (n + 1) / 2;
+        jt = tile - it * (it + 1) / 2;
+        return tile < kTiles;
+    };
+    if constexpr (kind != kEffect) {
+#pragma unroll
+        for (int k = 0; k < kMine; k++) {
+            int it, jt;
+            if (!tile_of(k, it, jt)) continue;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int apart = 16 * (it - jt) + l - 4 * g - e;
+                apart_[k][e] = apart < 0 ? 0.0f : power(lg, apart) * p.s_in;
+                if constexpr (kind == kDecay) apart_[k][e] *= (float)max(apart, 0);
+            }
+            // (right of a diagonal's tile, in its block of 32, lies one that is never written again)
+            if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
+        }
+#pragma unroll
+        for (int it = 0; it < IT; it++) in_[it] = power(lg, 16 * it + l + 1 - p.shift);
+    }
+    const auto behind = [&](int jb, int e, int count) { return max(count - 1 - (32 * jb + 16 * (e / 4) + 4 * g + e % 4), 0); };
+#pragma unroll
+    for (int jb = 0; jb < JB; jb++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) out_[jb][e] = power(lg, behind(jb, e, R) + p.shift) * p.s_in;
+    const float wane_ = power_less_one(lg, R);
+
     Rows<T, 32 * KB, R, kThreadsHere> a_rows, b_rows;
     Rows<T, kWide, R, kThreadsHere> x_rows;
+    x_rows.begin(p.x, head, p.back, c0, p.wb);
+    b_rows.begin(p.b, head, p.back, 0, p.wa);
+    if constexpr (kind != kEffect) a_rows.begin(p.a, head, p.back, 0, p.wa);
     while (lo < hi) {
         const Piece piece = piece_at(p, lo, hi);
         int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
         const auto fetch = [&](int count) {
-            x_rows.load(p.x, head, row, p.back, count, c0, p.wb);
-            b_rows.load(p.b, head, row, p.back, count, 0, p.wa);
-            if constexpr (kind != kEffect) a_rows.load(p.a, head, row, p.back, count, 0, p.wa);
+            x_rows.load(p.x, row, count, c0, p.wb);
+            b_rows.load(p.b, row, count, 0, p.wa);
+            if constexpr (kind != kEffect) a_rows.load(p.a, row, count, 0, p.wa);
         };
         int n = (int)min((int64_t)R, left);
         fetch(n);
@@ -143,10 +182,10 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
         else s.zero();
         if constexpr (kind == kDecay) r.zero();
         while (left > 0) {
-            const bool found = x_rows.store(x_tile, n);
-            b_rows.store(b_tile, n);
+            const bool found = x_rows.store(x_tile);
+            b_rows.store(b_tile);
             if constexpr (kind != kEffect) {
-                a_rows.store(a_tile, n);
+                a_rows.store(a_tile);
                 if (found) odd[turn] = 1;
             }
             __syncthreads();
@@ -158,7 +197,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                 if (bad && n > 1) {
                     n = 1;
                     __syncthreads();
-                    continue;                          // (the registers still hold the rows)
+                    fetch(n);
+                    continue;
                 }
             }
             // the next chunk is on its way while this one is computed
@@ -171,28 +211,17 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
 
             f32x4 o[IT];
             if constexpr (kind != kEffect) {
-                // scores of rows i (lanes) and j (places), with the decay between them: the tiles on and below the diagonal, shared out
+                // scores of rows i (lanes) and j (places): the tiles on and below the diagonal, shared out
 #pragma unroll
-                for (int k0 = 0; k0 < (IT * (IT + 1) / 2 + WAVES - 1) / WAVES; k0++) {
-                    const int tile = wave + k0 * WAVES;
-                    int it = 0;
-#pragma unroll
-                    for (int k = 1; k < IT; k++) it += tile >= k * (k + 1) / 2;
-                    const int jt = tile - it * (it + 1) / 2;
-                    if (tile >= IT * (IT + 1) / 2 || 16 * it >= count) continue;
+                for (int k0 = 0; k0 < kMine; k0++) {
+                    int it, jt;
+                    if (!tile_of(k0, it, jt)) continue;
                     f32x4 c = {0, 0, 0, 0};
 #pragma unroll
                     for (int k = 0; k < KB; k++) c = product<true>(b_tile.along(16 * jt, k, lane), a_tile.along(16 * it, k, lane), c);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const int apart = 16 * (it - jt) + l - 4 * g - e;
-                        // (what lies above the diagonal is not looked at)
-                        c[e] = apart < 0 ? 0.0f : c[e] * (power(lg, apart) * p.s_in);
-                        if constexpr (kind == kDecay) c[e] *= (float)max(apart, 0);
-                    }
+                    for (int e = 0; e < 4; e++) c[e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * apart_[k0][e];     // (what lies above the diagonal is not looked at)
                     s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
-                    // (the tile right of the diagonal shares its block of 32)
-                    if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
                 }
                 // what the state that enters gives
                 Frag<E, PS> sf[KB], rf[kind == kDecay ? KB : 1];
@@ -203,8 +232,6 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                 }
 #pragma unroll
                 for (int it = 0; it < IT; it++) {
-                    if (16 * it >= count) break;
-                    const int i = 16 * it + l;
                     f32x4 from_s = {0, 0, 0, 0}, from_r = {0, 0, 0, 0};
 #pragma unroll
                     for (int k = 0; k < KB; k++) {
@@ -212,9 +239,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                         from_s = product(sf[k], af, from_s);
                         if constexpr (kind == kDecay) from_r = product(rf[k], af, from_r);
                     }
-                    const float in = power(lg, i + 1 - p.shift);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) o[it][e] = (kind == kDecay ? from_r[e] + (float)(i + 1) * from_s[e] : from_s[e]) * in;
+                    for (int e = 0; e < 4; e++) o[it][e] = (kind == kDecay ? from_r[e] + (float)(16 * it + l + 1) * from_s[e] : from_s[e]) * in_[it];
                 }
                 __syncthreads();
             }
@@ -225,31 +251,42 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                 // and what its own rows give; lane l has row i, columns 4 g + 0..3
                 const int c = c0 + 16 * wave + 4 * g;
 #pragma unroll
-                for (int it = 0; it < IT; it++) {
-                    if (16 * it >= count) break;
-                    const int i = 16 * it + l;
+                for (int it = 0; it < IT; it++)
 #pragma unroll
                     for (int jb = 0; jb <= it / 2; jb++) o[it] = product(xf[jb], s_tile.along(16 * it, jb, lane), o[it]);
-                    if (i < count) {
-                        const int64_t at = here + (p.back ? -i : i);
-                        if constexpr (kind == kOut) {
-                            const int64_t to = at * p.ldo + head * p.hdo + c;
-                            if (p.wide) put((float *)p.o + to, o[it], p.s_out, p.wb - c);
-                            else put((T *)p.o + to, o[it], p.s_out, p.wb - c);
-                        } else {
-                            const T *from = (const T *)p.d.at + at * p.d.ld + (head / p.d.group) * p.d.hd + c;
-                            float sum = 0;
+                if constexpr (kind == kOut) {
+                    const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
+                    if (count == R && p.wb % 4 == 0 && !p.wide) {
+                        if (c < p.wb) {
 #pragma unroll
-                            for (int e = 0; e < 4; e++)
-                                if (c + e < p.wb) sum += (float)from[e] * o[it][e];
-                            decay_sum += (double)(sum * p.s_out);
+                            for (int it = 0; it < IT; it++) put((T *)p.o + to + it * step, o[it], p.s_out, 4);
                         }
+                    } else {
+#pragma unroll
+                        for (int it = 0; it < IT; it++) {
+                            if (16 * it + l >= count) continue;
+                            if (p.wide) put((float *)p.o + to + it * step, o[it], p.s_out, p.wb - c);
+                            else put((T *)p.o + to + it * step, o[it], p.s_out, p.wb - c);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int it = 0; it < IT; it++) {
+                        const int i = 16 * it + l;
+                        if (i >= count) continue;
+                        const T *from = (const T *)p.d.at + (here + (p.back ? -i : i)) * p.d.ld + (head / p.d.group) * p.d.hd + c;
+                        float sum = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (c + e < p.wb) sum += (float)from[e] * o[it][e];
+                        decay_sum += (double)(sum * p.s_out);
                     }
                 }
             }
 
             // the state behind the chunk
-            const float wane = power_less_one(lg, count);
+            float wane = wane_;
+            if (count != R) wane = power_less_one(lg, count);
             if constexpr (kind == kDecay) {
                 const float far_ = power(lg, count) * (float)count;
 #pragma unroll
@@ -263,18 +300,22 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                 for (int e = 0; e < 4; e++) s.at[k][e] = fmaf(s.at[k][e], wane, s.at[k][e]);
 #pragma unroll
             for (int jb = 0; jb < JB; jb++) {
-                if (32 * jb >= count) break;
                 float v[8], w[8];
                 values(xf[jb], v);
+                if (count == R) {
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const int behind = max(count - 1 - (32 * jb + 16 * (e / 4) + 4 * g + e % 4), 0);       // (rows behind the chunk's are zeros)
-                    v[e] *= power(lg, behind + p.shift) * p.s_in;
-                    w[e] = v[e] * (float)behind;
+                    for (int e = 0; e < 8; e++) v[e] *= out_[jb][e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] *= power(lg, behind(jb, e, count) + p.shift) * p.s_in;      // (rows behind the chunk's are zeros)
                 }
                 Frag<E, PU> vf, wf;
                 split(v, vf);
-                if constexpr (kind == kDecay) split(w, wf);
+                if constexpr (kind == kDecay) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) w[e] = v[e] * (float)behind(jb, e, count);
+                    split(w, wf);
+                }
 #pragma unroll
                 for (int k = 0; k < 2 * KB; k++) {
                     const Frag<E, P> bf = b_tile.across(16 * k, jb, lane);

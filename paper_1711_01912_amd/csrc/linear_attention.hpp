@@ -254,47 +254,69 @@ struct Tile {
     }
 };
 
+// whether 8 values hold an infinity or a NaN: all ones in an exponent
 template <typename T>
-__device__ __forceinline__ bool endless(T v) {       // an infinity or a NaN
-    return !(fabsf((float)v) < INFINITY);
+__device__ __forceinline__ uint32_t endless(const Pack<T, 8> &v) {
+    constexpr int kWords = 8 * sizeof(T) / 4;
+    constexpr uint32_t kOnes = std::is_same_v<T, float> ? 0x7f800000u : std::is_same_v<T, bf16> ? 0x7f807f80u : 0x7c007c00u;
+    constexpr uint32_t kOne = std::is_same_v<T, float> ? 0x00800000u : std::is_same_v<T, bf16> ? 0x00800080u : 0x04000400u;
+    uint32_t w[kWords], found = 0;
+    __builtin_memcpy(w, &v, sizeof(w));
+#pragma unroll
+    for (int i = 0; i < kWords; i++) found |= (w[i] & kOnes) + kOne;
+    return found & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u);
 }
 
 // Rows of a chunk on their way from memory to a tile, in registers: places c0 .. c0 + W - 1 of `width`; zeros where there are none.
 template <typename T, int W, int R, int THREADS>
 struct Rows {
-    static constexpr int kPer = W / 8, kLoads = (R * kPer + THREADS - 1) / THREADS;
+    static constexpr int kPer = W / 8, kLoads = (R * kPer + THREADS - 1) / THREADS, kApart = THREADS / kPer;      // rows from load to load
+    static_assert(THREADS % kPer == 0);
     Pack<T, 8> v[kLoads];
+    const T *mine;                       // the thread's first element, were the chunk's first row the operand's
+    int64_t step;
+    bool whole, here;                    // whether all vectors of 8 lie inside rows or behind them, and whether the thread's does
 
+    __device__ __forceinline__ void begin(const Operand &m, int32_t head, bool down, int c0, int width) {
+        const int r = (int)threadIdx.x / kPer, c = c0 + (int)threadIdx.x % kPer * 8;
+        step = down ? -m.ld : m.ld;
+        mine = (const T *)m.at + (head / m.group) * m.hd + r * step + c;
+        whole = width % 8 == 0;
+        here = c < width;
+        const Pack<T, 8> none{};
+#pragma unroll
+        for (int k = 0; k < kLoads; k++) v[k] = none;
+    }
     // `count` rows from `row` on, upwards or downwards
-    __device__ __forceinline__ void load(const Operand &m, int32_t head, int64_t row, bool down, int count, int c0, int width) {
-        const T *base = (const T *)m.at + row * m.ld + (head / m.group) * m.hd + c0;
-        const int64_t step = down ? -m.ld : m.ld;
+    __device__ __forceinline__ void load(const Operand &m, int64_t row, int count, int c0, int width) {
+        const T *from = mine + row * m.ld;
+        if (count == R && whole) {
+            if (here) {
+#pragma unroll
+                for (int k = 0; k < kLoads; k++)
+                    if (R * kPer % THREADS == 0 || (int)threadIdx.x / kPer + k * kApart < R) v[k] = load_pack<T, 8>(from + k * kApart * step);
+            }
+            return;
+        }
+        const int left = width - (c0 + (int)threadIdx.x % kPer * 8);
 #pragma unroll
         for (int k = 0; k < kLoads; k++) {
-            const int at = k * THREADS + (int)threadIdx.x, r = at / kPer, c = at % kPer * 8;
-            const T *from = base + r * step + c;
-            if (r < count && c0 + c + 8 <= width) v[k] = load_pack<T, 8>(from);
-            else {
+            const bool row_here = (int)threadIdx.x / kPer + k * kApart < count;
 #pragma unroll
-                for (int e = 0; e < 8; e++) v[k].v[e] = r < count && c0 + c + e < width ? from[e] : (T)0.0f;
-            }
+            for (int e = 0; e < 8; e++) v[k].v[e] = row_here && e < left ? from[k * kApart * step + e] : (T)0.0f;
         }
     }
     // true where a value is an infinity or a NaN
     template <typename E, int P>
-    __device__ __forceinline__ bool store(Tile<E, P, W, R> &tile, int count) const {
-        bool odd = false;
+    __device__ __forceinline__ bool store(Tile<E, P, W, R> &tile) const {
+        uint32_t odd = 0;
+        const int r0 = (int)threadIdx.x / kPer, c = (int)threadIdx.x % kPer * 8;
 #pragma unroll
         for (int k = 0; k < kLoads; k++) {
-            const int at = k * THREADS + (int)threadIdx.x, r = at / kPer, c = at % kPer * 8;
+            const int r = r0 + k * kApart;
             if (R * kPer % THREADS && r >= R) break;
-            Pack<T, 8> u = v[k];
-            if (r >= count) {
-#pragma unroll
-                for (int e = 0; e < 8; e++) u.v[e] = (T)0.0f;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; e++) odd |= endless(u.v[e]);
+            const Pack<T, 8> &u = v[k];
+            odd |= endless<T>(u);
             if constexpr (std::is_same_v<T, E>) *(Pack<T, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = u;
             else {
                 Pack<E, 8> hi, lo;
@@ -307,7 +329,7 @@ struct Rows {
                 *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[1][r][c], 16) = lo;
             }
         }
-        return odd;
+        return odd != 0;
     }
 };
 
