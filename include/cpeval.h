@@ -588,7 +588,7 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
  */
 int cp_linear_attention_workspace_bytes(int64_t rows, int32_t num_seq, int packed, int32_t heads, int32_t kv_heads, int32_t width_k,
                                         int32_t width_v, int backward, size_t *out_bytes);
-int cp_linear_attention_carry_states(int64_t rows, int32_t num_seq, int packed, int32_t heads, int64_t *out_states);
+int cp_linear_attention_carry_states(int64_t rows, int32_t num_seq, int packed, int32_t heads, int32_t width_k, int32_t width_v, int64_t *out_states);
 int cp_linear_attention(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, int32_t heads, int32_t kv_heads, int32_t width_k,
                         int32_t width_v, int type, int reverse, const void *q, int64_t ldq, int64_t hdq, const void *k, int64_t ldk,
                         int64_t hdk, const void *v, int64_t ldv, int64_t hdv, const float *log_decay, float scale, const float *h0, void *o,

@@ -63,9 +63,9 @@ def _shape(q, k, v, seq_ptr, device):
 
 
 @functools.lru_cache(maxsize=4096)
-def _carry_states(rows, count, packed, heads):
+def _carry_states(rows, count, packed, heads, wk, wv):
     found = C.c_int64(0)
-    rc = load_library().cp_linear_attention_carry_states(rows, count, packed, heads, C.byref(found))
+    rc = load_library().cp_linear_attention_carry_states(rows, count, packed, heads, wk, wv, C.byref(found))
     if rc:
         raise CpError(rc, "cp_linear_attention_carry_states")
     return int(found.value)
@@ -97,7 +97,7 @@ def cp_linear_attention(q, k, v, log_decay=None, *, scale=1.0, seq_ptr=None, h0=
         last_at = _vector_out(out, "last", state, f32, dev) if want_last or "last" in out else None
         carry_at = None
         if want_carry or "carry" in out:
-            carry_at = _vector_out(out, "carry", (_carry_states(rows, count, ptr is not None, heads), heads, wk, wv), f32, dev) or None
+            carry_at = _vector_out(out, "carry", (_carry_states(rows, count, ptr is not None, heads, wk, wv), heads, wk, wv), f32, dev) or None
         status_at = _vector_out(out, "status", (1,), torch.int32, dev) if ptr is not None else None
         work, work_at, room = _room(workspace, _need("cp_linear_attention_workspace_bytes", rows, count, ptr is not None, *sizes, 0), dev)
         rc = lib.cp_linear_attention(rows, count, ptr, *sizes, kind, int(bool(reverse)), *ins, decay_at, scale, h0_at, *o, last_at, carry_at,
@@ -123,7 +123,7 @@ def cp_linear_attention_backward(do, q, k, v, log_decay, carry, *, dlast=None, s
     ins = (*_heads(q, "q", lead, heads, wk, dt, dev), *_heads(k, "k", lead, kv_heads, wk, dt, dev), *_heads(v, "v", lead, kv_heads, wv, dt, dev))
     decay_at, state = _vector(log_decay, "log_decay", (heads,), f32, dev), (count, heads, wk, wv)
     h0_at, dlast_at = _vector(h0, "h0", state, f32, dev), _vector(dlast, "dlast", state, f32, dev)
-    carry_at = _vector(carry, "carry", (_carry_states(rows, count, ptr is not None, heads), heads, wk, wv), f32, dev) or None
+    carry_at = _vector(carry, "carry", (_carry_states(rows, count, ptr is not None, heads, wk, wv), heads, wk, wv), f32, dev) or None
     out = dict(out) if out else {}
     place, handle = _place(dev, stream)
     with place:

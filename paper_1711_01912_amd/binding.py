@@ -175,7 +175,7 @@ def load_library():
                                                i64, i64, vp, i64, vp, i64, vp]
     heads = [vp, i64, i64]
     lib.cp_linear_attention_workspace_bytes.argtypes = [i64, i32, C.c_int, i32, i32, i32, i32, C.c_int, szp]
-    lib.cp_linear_attention_carry_states.argtypes = [i64, i32, C.c_int, i32, C.POINTER(i64)]
+    lib.cp_linear_attention_carry_states.argtypes = [i64, i32, C.c_int, i32, i32, i32, C.POINTER(i64)]
     lib.cp_linear_attention.argtypes = [i64, i32, vp, i32, i32, i32, i32, C.c_int, C.c_int, *heads, *heads, *heads, vp, C.c_float, vp,
                                         *heads, vp, vp, vp, C.c_size_t, vp, vp]
     lib.cp_linear_attention_backward.argtypes = [i64, i32, vp, i32, i32, i32, i32, C.c_int, C.c_int, *heads, vp, *heads, *heads, *heads,

@@ -87,8 +87,8 @@ struct State {
 };
 
 // KB: blocks of 32 that the state's rows fill; WAVES: of a workgroup, 16 columns each; R: rows of a chunk
-template <typename T, int KB, int WAVES, int R, Kind kind>
-__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel(Pass p, float *effect, float *gain) {
+template <typename T, int KB, int WAVES, int R, Kind kind, bool EVEN>
+__global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *effect, float *gain) {
     using F = Form<T>;
     using E = typename F::E;
     constexpr int P = F::kPlanes, PS = kind == kDecay ? F::kFine : F::kSplit, PU = F::kFine;
@@ -162,8 +162,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
         for (int e = 0; e < 8; e++) out_[jb][e] = power(lg, behind(jb, e, R) + p.shift) * p.s_in;
     const float wane_ = power_less_one(lg, R);
 
-    Rows<T, 32 * KB, R, kThreadsHere> a_rows, b_rows;
-    Rows<T, kWide, R, kThreadsHere> x_rows;
+    Rows<T, 32 * KB, R, kThreadsHere, EVEN> a_rows, b_rows;
+    Rows<T, kWide, R, kThreadsHere, EVEN> x_rows;
     x_rows.begin(p.x, head, p.back, c0, p.wb);
     b_rows.begin(p.b, head, p.back, 0, p.wa);
     if constexpr (kind != kEffect) a_rows.begin(p.a, head, p.back, 0, p.wa);
@@ -171,9 +171,9 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
         const Piece piece = piece_at(p, lo, hi);
         int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
         const auto fetch = [&](int count) {
-            x_rows.load(p.x, row, count, c0, p.wb);
-            b_rows.load(p.b, row, count, 0, p.wa);
-            if constexpr (kind != kEffect) a_rows.load(p.a, row, count, 0, p.wa);
+            x_rows.load(p.x, row, count);
+            b_rows.load(p.b, row, count);
+            if constexpr (kind != kEffect) a_rows.load(p.a, row, count);
         };
         int n = (int)min((int64_t)R, left);
         fetch(n);
@@ -213,14 +213,23 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
             if constexpr (kind != kEffect) {
                 // scores of rows i (lanes) and j (places): the tiles on and below the diagonal, shared out
 #pragma unroll
-                for (int k0 = 0; k0 < kMine; k0++) {
+                for (int mine = 0; mine < kMine; mine++) {
                     int it, jt;
-                    if (!tile_of(k0, it, jt)) continue;
+                    if (!tile_of(mine, it, jt)) continue;
                     f32x4 c = {0, 0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < KB; k++) c = product<true>(b_tile.along(16 * jt, k, lane), a_tile.along(16 * it, k, lane), c);
+                    for (int k0 = 0; k0 < KB; k0 += 4) {
+                        Frag<E, P> bf[4], af[4];
 #pragma unroll
-                    for (int e = 0; e < 4; e++) c[e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * apart_[k0][e];     // (what lies above the diagonal is not looked at)
+                        for (int k = 0; k < 4; k++)
+                            if (k0 + k < KB) bf[k] = b_tile.along(16 * jt, k0 + k, lane), af[k] = a_tile.along(16 * it, k0 + k, lane);
+                        asked();
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+                            if (k0 + k < KB) c = product<true>(bf[k], af[k], c);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; e++) c[e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * apart_[mine][e];     // (what lies above the diagonal is not looked at)
                     s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
                 }
                 // what the state that enters gives
@@ -230,17 +239,27 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                     split(s.at[2 * k], s.at[2 * k + 1], sf[k]);
                     if constexpr (kind == kDecay) split(r.at[2 * k], r.at[2 * k + 1], rf[k]);
                 }
+                Frag<E, P> af[2][KB];
+                const auto ask = [&](int it) {
+#pragma unroll
+                    for (int k = 0; k < KB; k++) af[it % 2][k] = a_tile.along(16 * it, k, lane);
+                };
+                ask(0);
 #pragma unroll
                 for (int it = 0; it < IT; it++) {
-                    f32x4 from_s = {0, 0, 0, 0}, from_r = {0, 0, 0, 0};
+                    if (it + 1 < IT) ask(it + 1);
+                    asked();
+                    f32x4 from_s[2] = {}, from_r[2] = {};
 #pragma unroll
                     for (int k = 0; k < KB; k++) {
-                        const Frag<E, P> af = a_tile.along(16 * it, k, lane);
-                        from_s = product(sf[k], af, from_s);
-                        if constexpr (kind == kDecay) from_r = product(rf[k], af, from_r);
+                        from_s[k % 2] = product(sf[k], af[it % 2][k], from_s[k % 2]);
+                        if constexpr (kind == kDecay) from_r[k % 2] = product(rf[k], af[it % 2][k], from_r[k % 2]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; e++) o[it][e] = (kind == kDecay ? from_r[e] + (float)(16 * it + l + 1) * from_s[e] : from_s[e]) * in_[it];
+                    for (int e = 0; e < 4; e++) {
+                        const float one = from_s[0][e] + from_s[1][e];
+                        o[it][e] = (kind == kDecay ? from_r[0][e] + from_r[1][e] + (float)(16 * it + l + 1) * one : one) * in_[it];
+                    }
                 }
                 __syncthreads();
             }
@@ -251,22 +270,23 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                 // and what its own rows give; lane l has row i, columns 4 g + 0..3
                 const int c = c0 + 16 * wave + 4 * g;
 #pragma unroll
-                for (int it = 0; it < IT; it++)
+                for (int jb = 0; jb < JB; jb++) {
+                    Frag<E, PS> sc[IT];
 #pragma unroll
-                    for (int jb = 0; jb <= it / 2; jb++) o[it] = product(xf[jb], s_tile.along(16 * it, jb, lane), o[it]);
+                    for (int it = 2 * jb; it < IT; it++) sc[it] = s_tile.along(16 * it, jb, lane);
+                    asked();
+#pragma unroll
+                    for (int it = 2 * jb; it < IT; it++) o[it] = product(xf[jb], sc[it], o[it]);
+                }
                 if constexpr (kind == kOut) {
                     const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
-                    if (count == R && p.wb % 4 == 0 && !p.wide) {
-                        if (c < p.wb) {
-#pragma unroll
-                            for (int it = 0; it < IT; it++) put((T *)p.o + to + it * step, o[it], p.s_out, 4);
-                        }
-                    } else {
+                    const int places = EVEN ? 4 : p.wb - c;
+                    if (c < p.wb) {
 #pragma unroll
                         for (int it = 0; it < IT; it++) {
                             if (16 * it + l >= count) continue;
-                            if (p.wide) put((float *)p.o + to + it * step, o[it], p.s_out, p.wb - c);
-                            else put((T *)p.o + to + it * step, o[it], p.s_out, p.wb - c);
+                            if (p.wide) put((float *)p.o + to + it * step, o[it], p.s_out, places);
+                            else put((T *)p.o + to + it * step, o[it], p.s_out, places);
                         }
                     }
                 } else {
@@ -316,11 +336,15 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void pass_kernel
                     for (int e = 0; e < 8; e++) w[e] = v[e] * (float)behind(jb, e, count);
                     split(w, wf);
                 }
+                constexpr int kGroup = std::is_same_v<T, bf16> ? 8 : 4, kSome = kGroup < 2 * KB ? kGroup : 2 * KB;
 #pragma unroll
-                for (int k = 0; k < 2 * KB; k++) {
-                    const Frag<E, P> bf = b_tile.across(16 * k, jb, lane);
-                    s.at[k] = product(bf, vf, s.at[k]);
-                    if constexpr (kind == kDecay) r.at[k] = product(bf, wf, r.at[k]);
+                for (int k0 = 0; k0 < 2 * KB; k0 += kSome) {
+                    Frag<E, P> bf[kSome];
+#pragma unroll
+                    for (int k = 0; k < kSome; k++) bf[k] = b_tile.across(16 * (k0 + k), jb, lane);
+                    asked();
+                    products(bf, vf, &s.at[k0]);
+                    if constexpr (kind == kDecay) products(bf, wf, &r.at[k0]);
                 }
             }
             __syncthreads();
@@ -491,16 +515,17 @@ __global__ void set_status_kernel(int32_t *status, int32_t value) { *status = va
 
 constexpr int kMaxWidth = CP_ATTENTION_MAX_WIDTH, kMaxHeads = CP_ATTENTION_MAX_HEADS;
 
-// Segments: workgroups enough for the chip (two a compute unit), of 128 rows at least.  The same for all types and for both
+// Segments: workgroups enough for the chip, one a compute unit (two of narrow heads), of 128 rows at least.  The same for all types and for both
 // directions, since the backward pass reads the states that the forward call kept.
 struct Cut {
     int64_t seg_rows;
     int32_t parts, segments;
     bool split;                          // whether a sequence may be cut
 };
-constexpr int64_t kWanted = 512, kLeast = 128;
+constexpr int64_t kLeast = 128;
 
-Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads) {
+Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads, int32_t wk, int32_t wv) {
+    const int64_t kWanted = std::max(wk, wv) > 64 ? 256 : 512;
     const int64_t len = packed ? rows : rows / num_seq;
     const int64_t units = (int64_t)heads * (packed ? 1 : num_seq);
     int64_t parts = std::max<int64_t>(1, std::min((kWanted + units - 1) / units, len / kLeast));
@@ -518,25 +543,27 @@ Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads) {
 int waves_of(int32_t wa, int32_t wb) { return wb > 64 || wa > 128 ? 8 : 4; }
 int32_t slices_of(int32_t wa, int32_t wb) { return (wb + 16 * waves_of(wa, wb) - 1) / (16 * waves_of(wa, wb)); }
 
-template <typename T, int KB, int WAVES>
+template <typename T, int KB, int WAVES, bool EVEN>
 int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t st) {
     // (rows of 32-bit elements or of two bf16 each do not find room for 64 of 256 places)
     constexpr int R = KB == 8 && !std::is_same_v<T, bf16> ? 32 : 64;
-    auto *kernel = kind == kOut      ? pass_kernel<T, KB, WAVES, R, kOut>
-                   : kind == kEffect ? pass_kernel<T, KB, WAVES, R, kEffect>
-                                     : pass_kernel<T, KB, WAVES, R, kDecay>;
+    auto *kernel = kind == kOut      ? pass_kernel<T, KB, WAVES, R, kOut, EVEN>
+                   : kind == kEffect ? pass_kernel<T, KB, WAVES, R, kEffect, EVEN>
+                                     : pass_kernel<T, KB, WAVES, R, kDecay, EVEN>;
     hipLaunchKernelGGL(kernel, grid_of((int64_t)p.segments * p.heads * p.slices), dim3(WAVES * kWave), 0, st, p, effect, gain);
     return launched();
 }
 
 int run(Kind kind, int type, Pass p, float *effect, float *gain, hipStream_t st) {
+    const bool even = p.wa % 8 == 0 && p.wb % 8 == 0, wide = waves_of(p.wa, p.wb) == 8;
     p.slices = slices_of(p.wa, p.wb);
-    const bool wide = waves_of(p.wa, p.wb) == 8;
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        if (p.wa > 128) return run_sized<T, 8, 8>(kind, p, effect, gain, st);
-        if (p.wa > 64) return wide ? run_sized<T, 4, 8>(kind, p, effect, gain, st) : run_sized<T, 4, 4>(kind, p, effect, gain, st);
-        return wide ? run_sized<T, 2, 8>(kind, p, effect, gain, st) : run_sized<T, 2, 4>(kind, p, effect, gain, st);
+        if (p.wa > 128) return even ? run_sized<T, 8, 8, true>(kind, p, effect, gain, st) : run_sized<T, 8, 8, false>(kind, p, effect, gain, st);
+        if (wide && p.wa > 64) return even ? run_sized<T, 4, 8, true>(kind, p, effect, gain, st) : run_sized<T, 4, 8, false>(kind, p, effect, gain, st);
+        if (wide) return even ? run_sized<T, 2, 8, true>(kind, p, effect, gain, st) : run_sized<T, 2, 8, false>(kind, p, effect, gain, st);
+        if (p.wa > 64) return even ? run_sized<T, 4, 4, true>(kind, p, effect, gain, st) : run_sized<T, 4, 4, false>(kind, p, effect, gain, st);
+        return even ? run_sized<T, 2, 4, true>(kind, p, effect, gain, st) : run_sized<T, 2, 4, false>(kind, p, effect, gain, st);
     });
 }
 
@@ -577,7 +604,7 @@ size_t part_bytes(const Shape &s, const Cut &c) { return align_up((size_t)s.head
 size_t share_bytes(const Shape &s) { return s.heads == s.kv_heads ? 0 : align_up((size_t)s.rows * s.heads * std::max(s.wk, s.wv) * sizeof(float)); }
 
 size_t need_of(const Shape &s, bool backward) {
-    const Cut c = cut_of(s.rows, s.num_seq, s.ptr != nullptr, s.heads);
+    const Cut c = cut_of(s.rows, s.num_seq, s.ptr != nullptr, s.heads, s.wk, s.wv);
     return enter_bytes(s, c) + gain_bytes(s, c) + (backward ? part_bytes(s, c) + share_bytes(s) : 0);
 }
 
@@ -636,12 +663,12 @@ int cp_linear_attention_workspace_bytes(int64_t rows, int32_t num_seq, int packe
     return CP_OK;
 }
 
-int cp_linear_attention_carry_states(int64_t rows, int32_t num_seq, int packed, int32_t heads, int64_t *out_states) {
+int cp_linear_attention_carry_states(int64_t rows, int32_t num_seq, int packed, int32_t heads, int32_t width_k, int32_t width_v, int64_t *out_states) {
     if (!out_states) return CP_ERR_NULL;
     const int32_t some = 0;
-    const int rc = check({rows, num_seq, packed ? &some : nullptr, heads, heads, 1, 1, CP_TYPE_F32}, 0);
+    const int rc = check({rows, num_seq, packed ? &some : nullptr, heads, heads, width_k, width_v, CP_TYPE_F32}, 0);
     if (rc) return rc;
-    const Cut c = cut_of(rows, num_seq, packed != 0, heads);
+    const Cut c = cut_of(rows, num_seq, packed != 0, heads, width_k, width_v);
     *out_states = c.split ? c.segments : 0;
     return CP_OK;
 }
@@ -658,7 +685,7 @@ int cp_linear_attention(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, i
     const Heads mq{q, ldq, hdq, heads, width_k, false}, mk{k, ldk, hdk, kv_heads, width_k, false}, mv{v, ldv, hdv, kv_heads, width_v, false},
         mo{o, ldo, hdo, heads, width_v, true};
     if (rows > 0 && (!fits(mq, rows) || !fits(mk, rows) || !fits(mv, rows) || !fits(mo, rows))) return CP_ERR_SIZE;
-    const Cut c = cut_of(rows, num_seq, seq_ptr != nullptr, heads);
+    const Cut c = cut_of(rows, num_seq, seq_ptr != nullptr, heads, width_k, width_v);
     const size_t enter = enter_bytes(s, c), need = gain_bytes(s, c) + (carry ? 0 : enter);
     if (need) {
         if (!workspace) return CP_ERR_NULL;
@@ -701,7 +728,7 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
     const Shape s{rows, num_seq, seq_ptr, heads, kv_heads, width_k, width_v, type};
     int rc = check(s, reverse);
     if (rc) return rc;
-    const Cut c = cut_of(rows, num_seq, seq_ptr != nullptr, heads);
+    const Cut c = cut_of(rows, num_seq, seq_ptr != nullptr, heads, width_k, width_v);
     if ((rows > 0 && (!d_o || !q || !k || !v || !dq || !dk || !dv || (c.split && !carry))) || (seq_ptr && !status_out)) return CP_ERR_NULL;
     const Heads mo{d_o, lddo, hddo, heads, width_v, false}, mq{q, ldq, hdq, heads, width_k, false}, mk{k, ldk, hdk, kv_heads, width_k, false},
         mv{v, ldv, hdv, kv_heads, width_v, false}, nq{dq, lddq, hddq, heads, width_k, true}, nk{dk, lddk, hddk, kv_heads, width_k, true},

@@ -160,6 +160,32 @@ __device__ __forceinline__ f32x4 product(const Frag<float, 1> &a, const Frag<flo
     return c;
 }
 
+// N results at once, part by part, so that neighbouring instructions do not wait for each other: c[k] += a[k] b
+template <int N, int PA, int PB>
+__device__ __forceinline__ void products(const Frag<bf16, PA> (&a)[N], const Frag<bf16, PB> &b, f32x4 *c) {
+    constexpr int kMost = PA > PB ? PA : PB;
+#pragma unroll
+    for (int s = kMost - 1; s >= 0; s--)
+#pragma unroll
+        for (int i = 0; i < PA; i++) {
+            const int j = s - i;
+            if (j >= 0 && j < PB) {
+#pragma unroll
+                for (int k = 0; k < N; k++) c[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k].p[i], b.p[j], c[k], 0, 0, 0);
+            }
+        }
+}
+template <int N>
+__device__ __forceinline__ void products(const Frag<float, 1> (&a)[N], const Frag<float, 1> &b, f32x4 *c) {
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int k = 0; k < N; k++) c[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k].v[i], b.v[i], c[k], 0, 0, 0);
+}
+// What was asked of LDS before it is under way before what comes after it begins.  (The compiler else asks for each operand right
+// before its product and waits for it.)
+__device__ __forceinline__ void asked() { __builtin_amdgcn_sched_barrier(0); }
+
 __device__ __forceinline__ void split(const float (&v)[8], Frag<float, 1> &f) {
 #pragma unroll
     for (int e = 0; e < 8; e++) f.v[e] = v[e];
@@ -268,42 +294,48 @@ __device__ __forceinline__ uint32_t endless(const Pack<T, 8> &v) {
 }
 
 // Rows of a chunk on their way from memory to a tile, in registers: places c0 .. c0 + W - 1 of `width`; zeros where there are none.
-template <typename T, int W, int R, int THREADS>
+// EVEN: the width is a multiple of 8, so that all vectors of 8 lie inside rows or behind them.
+template <typename T, int W, int R, int THREADS, bool EVEN>
 struct Rows {
     static constexpr int kPer = W / 8, kLoads = (R * kPer + THREADS - 1) / THREADS, kApart = THREADS / kPer;      // rows from load to load
-    static_assert(THREADS % kPer == 0);
+    static_assert(THREADS % kPer == 0 && (R * kPer % THREADS == 0 || kLoads == 1));
     Pack<T, 8> v[kLoads];
     const T *mine;                       // the thread's first element, were the chunk's first row the operand's
     int64_t step;
-    bool whole, here;                    // whether all vectors of 8 lie inside rows or behind them, and whether the thread's does
+    int left;                            // places from the thread's first on
 
     __device__ __forceinline__ void begin(const Operand &m, int32_t head, bool down, int c0, int width) {
         const int r = (int)threadIdx.x / kPer, c = c0 + (int)threadIdx.x % kPer * 8;
         step = down ? -m.ld : m.ld;
         mine = (const T *)m.at + (head / m.group) * m.hd + r * step + c;
-        whole = width % 8 == 0;
-        here = c < width;
+        left = width - c;
         const Pack<T, 8> none{};
 #pragma unroll
         for (int k = 0; k < kLoads; k++) v[k] = none;
     }
     // `count` rows from `row` on, upwards or downwards
-    __device__ __forceinline__ void load(const Operand &m, int64_t row, int count, int c0, int width) {
+    __device__ __forceinline__ void load(const Operand &m, int64_t row, int count) {
         const T *from = mine + row * m.ld;
-        if (count == R && whole) {
-            if (here) {
+        const int r = (int)threadIdx.x / kPer;
+        if constexpr (EVEN) {
+            if (count == R) {
+                if (left > 0 && (R * kPer % THREADS == 0 || r < R)) {
 #pragma unroll
-                for (int k = 0; k < kLoads; k++)
-                    if (R * kPer % THREADS == 0 || (int)threadIdx.x / kPer + k * kApart < R) v[k] = load_pack<T, 8>(from + k * kApart * step);
+                    for (int k = 0; k < kLoads; k++) v[k] = load_pack<T, 8>(from + k * kApart * step);
+                }
+                return;
             }
-            return;
         }
-        const int left = width - (c0 + (int)threadIdx.x % kPer * 8);
 #pragma unroll
         for (int k = 0; k < kLoads; k++) {
-            const bool row_here = (int)threadIdx.x / kPer + k * kApart < count;
+            const bool here = r + k * kApart < count;
+            if constexpr (EVEN) {
+                v[k] = Pack<T, 8>{};
+                if (here && left > 0) v[k] = load_pack<T, 8>(from + k * kApart * step);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[k].v[e] = row_here && e < left ? from[k * kApart * step + e] : (T)0.0f;
+                for (int e = 0; e < 8; e++) v[k].v[e] = here && e < left ? from[k * kApart * step + e] : (T)0.0f;
+            }
         }
     }
     // true where a value is an infinity or a NaN
