@@ -7,7 +7,7 @@
 //   o_i = scale (gamma^(i+1) q_i S + sum_{j <= i} gamma^(i-j) (q_i . k_j) v_j)
 //   S'  = gamma^n S + sum_j gamma^(n-1-j) k_j^T v_j
 //
-// A wavefront owns 16 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS, the next chunk is on its
+// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS, the next chunk is on its
 // way in registers.  The scores, of which only the tiles on and below the diagonal are computed, are shared out among the wavefronts.
 //
 // The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
@@ -47,13 +47,15 @@ __device__ __forceinline__ void put(T *to, f32x4 o, float scale, int count) {
 // kOut: outputs; kEffect: a segment's effect on the state alone; kDecay: the decays' gradient
 enum Kind { kOut, kEffect, kDecay };
 
-// 16 columns of a state, all of its rows, in a wavefront's registers: lane l has column l % 16, rows 16 k + 4 (l / 16) + 0..3
-template <int KB>
+// NT times 16 columns of a state, all of its rows, in a wavefront's registers: lane l has column l % 16, rows 16 k + 4 (l / 16) + 0..3
+template <int KB, int NT>
 struct State {
-    f32x4 at[2 * KB];
+    f32x4 at[NT][2 * KB];
     __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int k = 0; k < 2 * KB; k++) at[k] = f32x4{0, 0, 0, 0};
+        for (int t = 0; t < NT; t++)
+#pragma unroll
+            for (int k = 0; k < 2 * KB; k++) at[t][k] = f32x4{0, 0, 0, 0};
     }
     // (where the lane's first element lies is hidden from the compiler, which else keeps the addresses of all of them, and whether they
     // are there, in registers throughout the pass)
@@ -63,14 +65,15 @@ struct State {
         asm volatile("" : "+v"(row0));
         const int64_t base = (index * p.heads + head) * ((int64_t)p.wa * p.wb);
         const int across = p.transposed ? p.wa : 1, down = p.transposed ? 1 : p.wb;
-        const int at0 = col * across;
 #pragma unroll
-        for (int k = 0; k < 2 * KB; k++)
+        for (int t = 0; t < NT; t++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int row = row0 + 16 * k + e;
-                if (row < p.wa && col < p.wb) at[k][e] = f(at[k][e], base + (at0 + row * down));
-            }
+            for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int row = row0 + 16 * k + e, c = col + 16 * t;
+                    if (row < p.wa && c < p.wb) at[t][k][e] = f(at[t][k][e], base + (c * across + row * down));
+                }
     }
     __device__ __forceinline__ void load(const Pass &p, const float *from, int64_t index, int32_t head, int col, int g) {
         zero();
@@ -84,26 +87,44 @@ struct State {
         each(p, index, head, col, g, [&](float v, int64_t i) { return sum += (double)(v * with[i]), v; });
         return sum;
     }
+    // (off by half a step of the state: see power_less_one)
+    __device__ __forceinline__ void decay(float less_one) {
+#pragma unroll
+        for (int t = 0; t < NT; t++)
+#pragma unroll
+            for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) at[t][k][e] = fmaf(at[t][k][e], less_one, at[t][k][e]);
+    }
+    __device__ __forceinline__ void add(const State &s, float by) {
+#pragma unroll
+        for (int t = 0; t < NT; t++)
+#pragma unroll
+            for (int k = 0; k < 2 * KB; k++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) at[t][k][e] = fmaf(s.at[t][k][e], by, at[t][k][e]);
+    }
 };
 
-// KB: blocks of 32 that the state's rows fill; WAVES: of a workgroup, 16 columns each; R: rows of a chunk
-template <typename T, int KB, int WAVES, int R, Kind kind, bool EVEN>
+// KB: blocks of 32 that the state's rows fill; NT: of 16 columns that a wavefront has; WAVES: of a workgroup; R: rows of a chunk;
+// EVEN: widths are multiples of 8
+template <typename T, int KB, int NT, int WAVES, int R, Kind kind, bool EVEN>
 __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *effect, float *gain) {
     using F = Form<T>;
     using E = typename F::E;
     constexpr int P = F::kPlanes, PS = kind == kDecay ? F::kFine : F::kSplit, PU = F::kFine;
-    constexpr int kThreadsHere = WAVES * kWave, kWide = 16 * WAVES, IT = R / 16, JB = R / 32;
-    __shared__ Tile<E, P, 32 * KB, R> b_tile;
-    __shared__ Tile<E, P, kWide, R> x_tile;
-    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R> a_tile;
-    __shared__ Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R> s_tile;       // scores [row][place]
+    constexpr int kThreadsHere = WAVES * kWave, kWide = 16 * NT * WAVES, IT = R / 16, JB = R / 32;
+    __shared__ Tile<E, P, 32 * KB, R, 32> b_tile;
+    __shared__ Tile<E, P, kWide, R, 32> x_tile;
+    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R, 16> a_tile;
+    __shared__ Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R, 16> s_tile;       // scores [row][place]
     __shared__ int odd[2];
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane % 16, g = lane / 16;
     const uint32_t group = group_number();
     const int32_t slice = group % p.slices, head = group / p.slices % p.heads, seg = group / p.slices / p.heads;
     if (seg >= p.segments) return;                     // (the whole workgroup)
-    const int c0 = slice * kWide, col = c0 + 16 * wave + l;
+    const int c0 = slice * kWide, mine = 16 * NT * wave, col = c0 + mine + l;
     const float lg = lg_of(p.log_decay ? p.log_decay[head] : 0.0f);
 
     int64_t lo, hi;
@@ -111,7 +132,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
     if (threadIdx.x == 0) odd[0] = odd[1] = 0;
     double decay_sum = 0;
     int turn = 0;
-    State<KB> s, r;
+    State<KB, NT> s, r;
     if constexpr (kind == kEffect) {
         // only the sequence that goes on behind the segment: the last piece in the order of the pass, which is the first one seen from there
         s.zero();
@@ -209,13 +230,13 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
             n = (int)min((int64_t)R, left);
             if (left > 0) fetch(n);
 
-            f32x4 o[IT];
+            f32x4 o[NT][IT];
             if constexpr (kind != kEffect) {
                 // scores of rows i (lanes) and j (places): the tiles on and below the diagonal, shared out
 #pragma unroll
-                for (int mine = 0; mine < kMine; mine++) {
+                for (int m = 0; m < kMine; m++) {
                     int it, jt;
-                    if (!tile_of(mine, it, jt)) continue;
+                    if (!tile_of(m, it, jt)) continue;
                     f32x4 c = {0, 0, 0, 0};
 #pragma unroll
                     for (int k0 = 0; k0 < KB; k0 += 4) {
@@ -229,46 +250,57 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
                             if (k0 + k < KB) c = product<true>(bf[k], af[k], c);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; e++) c[e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * apart_[mine][e];     // (what lies above the diagonal is not looked at)
+                    for (int e = 0; e < 4; e++) c[e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * apart_[m][e];     // (what lies above the diagonal is not looked at)
                     s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
                 }
-                // what the state that enters gives
-                Frag<E, PS> sf[KB], rf[kind == kDecay ? KB : 1];
+                // what the state that enters gives, 32 of its rows at a time
+                f32x4 more[NT][kind == kDecay ? IT : 1];
 #pragma unroll
-                for (int k = 0; k < KB; k++) {
-                    split(s.at[2 * k], s.at[2 * k + 1], sf[k]);
-                    if constexpr (kind == kDecay) split(r.at[2 * k], r.at[2 * k + 1], rf[k]);
-                }
-                Frag<E, P> af[2][KB];
-                const auto ask = [&](int it) {
+                for (int t = 0; t < NT; t++)
 #pragma unroll
-                    for (int k = 0; k < KB; k++) af[it % 2][k] = a_tile.along(16 * it, k, lane);
+                    for (int it = 0; it < IT; it++) {
+                        o[t][it] = f32x4{0, 0, 0, 0};
+                        if constexpr (kind == kDecay) more[t][it] = f32x4{0, 0, 0, 0};
+                    }
+                Frag<E, P> af[2][IT];
+                const auto ask = [&](int k) {
+#pragma unroll
+                    for (int it = 0; it < IT; it++) af[k % 2][it] = a_tile.along(16 * it, k, lane);
                 };
                 ask(0);
 #pragma unroll
-                for (int it = 0; it < IT; it++) {
-                    if (it + 1 < IT) ask(it + 1);
+                for (int k = 0; k < KB; k++) {
+                    if (k + 1 < KB) ask(k + 1);
                     asked();
-                    f32x4 from_s[2] = {}, from_r[2] = {};
 #pragma unroll
-                    for (int k = 0; k < KB; k++) {
-                        from_s[k % 2] = product(sf[k], af[it % 2][k], from_s[k % 2]);
-                        if constexpr (kind == kDecay) from_r[k % 2] = product(rf[k], af[it % 2][k], from_r[k % 2]);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const float one = from_s[0][e] + from_s[1][e];
-                        o[it][e] = (kind == kDecay ? from_r[0][e] + from_r[1][e] + (float)(16 * it + l + 1) * one : one) * in_[it];
+                    for (int t = 0; t < NT; t++) {
+                        Frag<E, PS> sf;
+                        split(s.at[t][2 * k], s.at[t][2 * k + 1], sf);
+                        products<true>(af[k % 2], sf, o[t]);
+                        if constexpr (kind == kDecay) {
+                            split(r.at[t][2 * k], r.at[t][2 * k + 1], sf);
+                            products<true>(af[k % 2], sf, more[t]);
+                        }
                     }
                 }
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int it = 0; it < IT; it++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            if constexpr (kind == kDecay) o[t][it][e] = more[t][it][e] + (float)(16 * it + l + 1) * o[t][it][e];
+                            o[t][it][e] *= in_[it];
+                        }
                 __syncthreads();
             }
-            Frag<E, P> xf[JB];
+            Frag<E, P> xf[NT][JB];
 #pragma unroll
-            for (int jb = 0; jb < JB; jb++) xf[jb] = x_tile.across(16 * wave, jb, lane);
+            for (int t = 0; t < NT; t++)
+#pragma unroll
+                for (int jb = 0; jb < JB; jb++) xf[t][jb] = x_tile.across(mine + 16 * t, jb, lane);
             if constexpr (kind != kEffect) {
-                // and what its own rows give; lane l has row i, columns 4 g + 0..3
-                const int c = c0 + 16 * wave + 4 * g;
+                // and what its own rows give
 #pragma unroll
                 for (int jb = 0; jb < JB; jb++) {
                     Frag<E, PS> sc[IT];
@@ -276,30 +308,36 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
                     for (int it = 2 * jb; it < IT; it++) sc[it] = s_tile.along(16 * it, jb, lane);
                     asked();
 #pragma unroll
-                    for (int it = 2 * jb; it < IT; it++) o[it] = product(xf[jb], sc[it], o[it]);
+                    for (int t = 0; t < NT; t++)
+#pragma unroll
+                        for (int it = 2 * jb; it < IT; it++) o[t][it] = product(xf[t][jb], sc[it], o[t][it]);
                 }
-                if constexpr (kind == kOut) {
-                    const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
-                    const int places = EVEN ? 4 : p.wb - c;
-                    if (c < p.wb) {
+#pragma unroll
+                for (int t = 0; t < NT; t++) {
+                    const int c = c0 + mine + 16 * t + 4 * g;
+                    if constexpr (kind == kOut) {
+                        const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
+                        const int places = EVEN ? 4 : p.wb - c;
+                        if (c < p.wb) {
+#pragma unroll
+                            for (int it = 0; it < IT; it++) {
+                                if (16 * it + l >= count) continue;
+                                if (p.wide) put((float *)p.o + to + it * step, o[t][it], p.s_out, places);
+                                else put((T *)p.o + to + it * step, o[t][it], p.s_out, places);
+                            }
+                        }
+                    } else {
 #pragma unroll
                         for (int it = 0; it < IT; it++) {
-                            if (16 * it + l >= count) continue;
-                            if (p.wide) put((float *)p.o + to + it * step, o[it], p.s_out, places);
-                            else put((T *)p.o + to + it * step, o[it], p.s_out, places);
+                            const int i = 16 * it + l;
+                            if (i >= count) continue;
+                            const T *from = (const T *)p.d.at + (here + (p.back ? -i : i)) * p.d.ld + (head / p.d.group) * p.d.hd + c;
+                            float sum = 0;
+#pragma unroll
+                            for (int e = 0; e < 4; e++)
+                                if (c + e < p.wb) sum += (float)from[e] * o[t][it][e];
+                            decay_sum += (double)(sum * p.s_out);
                         }
-                    }
-                } else {
-#pragma unroll
-                    for (int it = 0; it < IT; it++) {
-                        const int i = 16 * it + l;
-                        if (i >= count) continue;
-                        const T *from = (const T *)p.d.at + (here + (p.back ? -i : i)) * p.d.ld + (head / p.d.group) * p.d.hd + c;
-                        float sum = 0;
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (c + e < p.wb) sum += (float)from[e] * o[it][e];
-                        decay_sum += (double)(sum * p.s_out);
                     }
                 }
             }
@@ -308,43 +346,45 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
             float wane = wane_;
             if (count != R) wane = power_less_one(lg, count);
             if constexpr (kind == kDecay) {
-                const float far_ = power(lg, count) * (float)count;
-#pragma unroll
-                for (int k = 0; k < 2 * KB; k++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) r.at[k][e] = fmaf(r.at[k][e], wane, r.at[k][e]) + far_ * s.at[k][e];
+                r.decay(wane);
+                r.add(s, power(lg, count) * (float)count);
             }
-#pragma unroll
-            for (int k = 0; k < 2 * KB; k++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) s.at[k][e] = fmaf(s.at[k][e], wane, s.at[k][e]);
+            s.decay(wane);
 #pragma unroll
             for (int jb = 0; jb < JB; jb++) {
-                float v[8], w[8];
-                values(xf[jb], v);
-                if (count == R) {
+                float by[8];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] *= out_[jb][e];
-                } else {
+                for (int e = 0; e < 8; e++) by[e] = out_[jb][e];
+                if (count != R) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] *= power(lg, behind(jb, e, count) + p.shift) * p.s_in;      // (rows behind the chunk's are zeros)
+                    for (int e = 0; e < 8; e++) by[e] = power(lg, behind(jb, e, count) + p.shift) * p.s_in;      // (rows behind the chunk's are zeros)
                 }
-                Frag<E, PU> vf, wf;
-                split(v, vf);
-                if constexpr (kind == kDecay) {
+                Frag<E, PU> vf[NT], wf[kind == kDecay ? NT : 1];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) w[e] = v[e] * (float)behind(jb, e, count);
-                    split(w, wf);
+                for (int t = 0; t < NT; t++) {
+                    float v[8];
+                    values(xf[t][jb], v);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] *= by[e];
+                    split(v, vf[t]);
+                    if constexpr (kind == kDecay) {
+#pragma unroll
+                        for (int e = 0; e < 8; e++) v[e] *= (float)behind(jb, e, count);
+                        split(v, wf[t]);
+                    }
                 }
-                constexpr int kGroup = std::is_same_v<T, bf16> ? 8 : 4, kSome = kGroup < 2 * KB ? kGroup : 2 * KB;
+                constexpr int kGroup = 4;
 #pragma unroll
-                for (int k0 = 0; k0 < 2 * KB; k0 += kSome) {
-                    Frag<E, P> bf[kSome];
+                for (int k0 = 0; k0 < 2 * KB; k0 += kGroup) {
+                    Frag<E, P> bf[kGroup];
 #pragma unroll
-                    for (int k = 0; k < kSome; k++) bf[k] = b_tile.across(16 * (k0 + k), jb, lane);
+                    for (int k = 0; k < kGroup; k++) bf[k] = b_tile.across(16 * (k0 + k), jb, lane);
                     asked();
-                    products(bf, vf, &s.at[k0]);
-                    if constexpr (kind == kDecay) products(bf, wf, &r.at[k0]);
+#pragma unroll
+                    for (int t = 0; t < NT; t++) {
+                        products(bf, vf[t], &s.at[t][k0]);
+                        if constexpr (kind == kDecay) products(bf, wf[t], &r.at[t][k0]);
+                    }
                 }
             }
             __syncthreads();
@@ -515,7 +555,7 @@ __global__ void set_status_kernel(int32_t *status, int32_t value) { *status = va
 
 constexpr int kMaxWidth = CP_ATTENTION_MAX_WIDTH, kMaxHeads = CP_ATTENTION_MAX_HEADS;
 
-// Segments: workgroups enough for the chip, one a compute unit (two of narrow heads), of 128 rows at least.  The same for all types and for both
+// Segments: workgroups enough for the chip, two a compute unit, of 128 rows at least.  The same for all types and for both
 // directions, since the backward pass reads the states that the forward call kept.
 struct Cut {
     int64_t seg_rows;
@@ -525,7 +565,7 @@ struct Cut {
 constexpr int64_t kLeast = 128;
 
 Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads, int32_t wk, int32_t wv) {
-    const int64_t kWanted = std::max(wk, wv) > 64 ? 256 : 512;
+    constexpr int64_t kWanted = 512;
     const int64_t len = packed ? rows : rows / num_seq;
     const int64_t units = (int64_t)heads * (packed ? 1 : num_seq);
     int64_t parts = std::max<int64_t>(1, std::min((kWanted + units - 1) / units, len / kLeast));
@@ -539,31 +579,33 @@ Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads, int32_t wk
     return c;
 }
 
-// Columns that a workgroup takes, 16 a wavefront: 64 where there are no more (two or three workgroups a compute unit), else 128
-int waves_of(int32_t wa, int32_t wb) { return wb > 64 || wa > 128 ? 8 : 4; }
-int32_t slices_of(int32_t wa, int32_t wb) { return (wb + 16 * waves_of(wa, wb) - 1) / (16 * waves_of(wa, wb)); }
+// Columns that a workgroup takes: 64 where there are no more, else 128
+int32_t columns_of(int32_t wa, int32_t wb) { return wb > 64 || wa > 128 ? 128 : 64; }
+int32_t slices_of(int32_t wa, int32_t wb) { return (wb + columns_of(wa, wb) - 1) / columns_of(wa, wb); }
 
-template <typename T, int KB, int WAVES, bool EVEN>
+template <typename T, int KB, int COLUMNS, bool EVEN>
 int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t st) {
-    // (rows of 32-bit elements or of two bf16 each do not find room for 64 of 256 places)
-    constexpr int R = KB == 8 && !std::is_same_v<T, bf16> ? 32 : 64;
-    auto *kernel = kind == kOut      ? pass_kernel<T, KB, WAVES, R, kOut, EVEN>
-                   : kind == kEffect ? pass_kernel<T, KB, WAVES, R, kEffect, EVEN>
-                                     : pass_kernel<T, KB, WAVES, R, kDecay, EVEN>;
+    // bf16 heads of up to 128: two workgroups of four wavefronts a compute unit, which have 32 columns each of 128.  The other types' rows leave
+    // room for one such in LDS, and those of 256 places for 64 rows only of bf16.
+    constexpr bool kHalf = std::is_same_v<T, bf16>;
+    constexpr int R = KB == 8 && !kHalf ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
+    auto *kernel = kind == kOut      ? pass_kernel<T, KB, NT, WAVES, R, kOut, EVEN>
+                   : kind == kEffect ? pass_kernel<T, KB, NT, WAVES, R, kEffect, EVEN>
+                                     : pass_kernel<T, KB, NT, WAVES, R, kDecay, EVEN>;
     hipLaunchKernelGGL(kernel, grid_of((int64_t)p.segments * p.heads * p.slices), dim3(WAVES * kWave), 0, st, p, effect, gain);
     return launched();
 }
 
 int run(Kind kind, int type, Pass p, float *effect, float *gain, hipStream_t st) {
-    const bool even = p.wa % 8 == 0 && p.wb % 8 == 0, wide = waves_of(p.wa, p.wb) == 8;
+    const bool even = p.wa % 8 == 0 && p.wb % 8 == 0, wide = columns_of(p.wa, p.wb) == 128;
     p.slices = slices_of(p.wa, p.wb);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        if (p.wa > 128) return even ? run_sized<T, 8, 8, true>(kind, p, effect, gain, st) : run_sized<T, 8, 8, false>(kind, p, effect, gain, st);
-        if (wide && p.wa > 64) return even ? run_sized<T, 4, 8, true>(kind, p, effect, gain, st) : run_sized<T, 4, 8, false>(kind, p, effect, gain, st);
-        if (wide) return even ? run_sized<T, 2, 8, true>(kind, p, effect, gain, st) : run_sized<T, 2, 8, false>(kind, p, effect, gain, st);
-        if (p.wa > 64) return even ? run_sized<T, 4, 4, true>(kind, p, effect, gain, st) : run_sized<T, 4, 4, false>(kind, p, effect, gain, st);
-        return even ? run_sized<T, 2, 4, true>(kind, p, effect, gain, st) : run_sized<T, 2, 4, false>(kind, p, effect, gain, st);
+        if (p.wa > 128) return even ? run_sized<T, 8, 128, true>(kind, p, effect, gain, st) : run_sized<T, 8, 128, false>(kind, p, effect, gain, st);
+        if (wide && p.wa > 64) return even ? run_sized<T, 4, 128, true>(kind, p, effect, gain, st) : run_sized<T, 4, 128, false>(kind, p, effect, gain, st);
+        if (wide) return even ? run_sized<T, 2, 128, true>(kind, p, effect, gain, st) : run_sized<T, 2, 128, false>(kind, p, effect, gain, st);
+        if (p.wa > 64) return even ? run_sized<T, 4, 64, true>(kind, p, effect, gain, st) : run_sized<T, 4, 64, false>(kind, p, effect, gain, st);
+        return even ? run_sized<T, 2, 64, true>(kind, p, effect, gain, st) : run_sized<T, 2, 64, false>(kind, p, effect, gain, st);
     });
 }
 

@@ -160,8 +160,8 @@ __device__ __forceinline__ f32x4 product(const Frag<float, 1> &a, const Frag<flo
     return c;
 }
 
-// N results at once, part by part, so that neighbouring instructions do not wait for each other: c[k] += a[k] b
-template <int N, int PA, int PB>
+// N results at once, part by part, so that neighbouring instructions do not wait for each other: c[k] += a[k] b, or b a[k] if TURNED
+template <bool TURNED = false, int N, int PA, int PB>
 __device__ __forceinline__ void products(const Frag<bf16, PA> (&a)[N], const Frag<bf16, PB> &b, f32x4 *c) {
     constexpr int kMost = PA > PB ? PA : PB;
 #pragma unroll
@@ -171,16 +171,17 @@ __device__ __forceinline__ void products(const Frag<bf16, PA> (&a)[N], const Fra
             const int j = s - i;
             if (j >= 0 && j < PB) {
 #pragma unroll
-                for (int k = 0; k < N; k++) c[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k].p[i], b.p[j], c[k], 0, 0, 0);
+                for (int k = 0; k < N; k++)
+                    c[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(TURNED ? b.p[j] : a[k].p[i], TURNED ? a[k].p[i] : b.p[j], c[k], 0, 0, 0);
             }
         }
 }
-template <int N>
+template <bool TURNED = false, int N>
 __device__ __forceinline__ void products(const Frag<float, 1> (&a)[N], const Frag<float, 1> &b, f32x4 *c) {
 #pragma unroll
     for (int i = 0; i < 8; i++)
 #pragma unroll
-        for (int k = 0; k < N; k++) c[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k].v[i], b.v[i], c[k], 0, 0, 0);
+        for (int k = 0; k < N; k++) c[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(TURNED ? b.v[i] : a[k].v[i], TURNED ? a[k].v[i] : b.v[i], c[k], 0, 0, 0);
 }
 // What was asked of LDS before it is under way before what comes after it begins.  (The compiler else asks for each operand right
 // before its product and waits for it.)
@@ -220,10 +221,11 @@ __device__ __forceinline__ void values(const Frag<bf16, P> &f, float (&v)[8]) {
     }
 }
 
-// R rows of a chunk in LDS; 16 bytes more from row to row than they hold, so that 16 rows' same places lie in different banks.
-template <typename E, int P, int W, int R>
+// R rows of a chunk in LDS, PAD bytes more from row to row than they hold: with 16 the lanes that read along rows meet in no bank (2.9
+// cycles an instruction, 4.7 with 32), with 32 those that read across them (2.8, 4.8 with 16).
+template <typename E, int P, int W, int R, int PAD>
 struct Tile {
-    static constexpr int kPitch = W + 16 / (int)sizeof(E);
+    static constexpr int kPitch = W + PAD / (int)sizeof(E);
     E at[P][R][kPitch];
 
     // rows r0 + 0..15, places 32 kb + 0..31
@@ -339,8 +341,8 @@ struct Rows {
         }
     }
     // true where a value is an infinity or a NaN
-    template <typename E, int P>
-    __device__ __forceinline__ bool store(Tile<E, P, W, R> &tile) const {
+    template <typename E, int P, int PAD>
+    __device__ __forceinline__ bool store(Tile<E, P, W, R, PAD> &tile) const {
         uint32_t odd = 0;
         const int r0 = (int)threadIdx.x / kPer, c = (int)threadIdx.x % kPer * 8;
 #pragma unroll
