@@ -7,8 +7,7 @@
 //   o_i = scale (gamma^(i+1) q_i S + sum_{j <= i} gamma^(i-j) (q_i . k_j) v_j)
 //   S'  = gamma^n S + sum_j gamma^(n-1-j) k_j^T v_j
 //
-// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS, the next chunk is on its
-// way in registers.  The scores, of which only the tiles on and below the diagonal are computed, are shared out among the wavefronts.
+// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS.  The scores, of which only the tiles on and below the diagonal are computed, are shared out among the wavefronts.
 //
 // The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
 //   dq_t = scale do_t S_t^T (the pass with do, v, k in the places of q, k, v),   dv_t = k_t D_t and dk_t = v_t D_t^T (from the last
@@ -114,10 +113,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
     using E = typename F::E;
     constexpr int P = F::kPlanes, PS = kind == kDecay ? F::kFine : F::kSplit, PU = F::kFine;
     constexpr int kThreadsHere = WAVES * kWave, kWide = 16 * NT * WAVES, IT = R / 16, JB = R / 32;
-    __shared__ Tile<E, P, 32 * KB, R, 32> b_tile;
-    __shared__ Tile<E, P, kWide, R, 32> x_tile;
-    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R, 16> a_tile;
-    __shared__ Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R, 16> s_tile;       // scores [row][place]
+    __shared__ Tile<E, P, 32 * KB, R, false> b_tile;
+    __shared__ Tile<E, P, kWide, R, false> x_tile;
+    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R, true> a_tile;
+    __shared__ Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R, true> s_tile;       // scores [row][place]
     __shared__ int odd[2];
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane % 16, g = lane / 16;
@@ -183,31 +182,31 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
         for (int e = 0; e < 8; e++) out_[jb][e] = power(lg, behind(jb, e, R) + p.shift) * p.s_in;
     const float wane_ = power_less_one(lg, R);
 
-    Rows<T, 32 * KB, R, kThreadsHere, EVEN> a_rows, b_rows;
-    Rows<T, kWide, R, kThreadsHere, EVEN> x_rows;
-    x_rows.begin(p.x, head, p.back, c0, p.wb);
-    b_rows.begin(p.b, head, p.back, 0, p.wa);
-    if constexpr (kind != kEffect) a_rows.begin(p.a, head, p.back, 0, p.wa);
+    const RowsOf<T, 32 * KB, R, kThreadsHere, EVEN> a_rows(p.a, head, p.back, 0, p.wa), b_rows(p.b, head, p.back, 0, p.wa);
+    const RowsOf<T, kWide, R, kThreadsHere, EVEN> x_rows(p.x, head, p.back, c0, p.wb);
     while (lo < hi) {
         const Piece piece = piece_at(p, lo, hi);
         int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
-        const auto fetch = [&](int count) {
-            x_rows.load(p.x, row, count);
-            b_rows.load(p.b, row, count);
-            if constexpr (kind != kEffect) a_rows.load(p.a, row, count);
-        };
-        int n = (int)min((int64_t)R, left);
-        fetch(n);
         if (piece.starts && p.init) s.load(p, p.init, piece.seq, head, col, g);
         else if (kind != kEffect && !piece.starts && p.enter) s.load(p, p.enter, seg, head, col, g);
         else s.zero();
         if constexpr (kind == kDecay) r.zero();
+        int most = R;
         while (left > 0) {
-            const bool found = x_rows.store(x_tile);
-            b_rows.store(b_tile);
-            if constexpr (kind != kEffect) {
-                a_rows.store(a_tile);
-                if (found) odd[turn] = 1;
+            const int count = (int)min((int64_t)most, left);
+            const int64_t here = row;
+            {
+                Rows<T, 32 * KB, R, kThreadsHere> a_now, b_now;
+                Rows<T, kWide, R, kThreadsHere> x_now;
+                x_rows.load(x_now, p.x, row, count);
+                b_rows.load(b_now, p.b, row, count);
+                if constexpr (kind != kEffect) a_rows.load(a_now, p.a, row, count);
+                const bool found = x_now.store(x_tile);
+                b_now.store(b_tile);
+                if constexpr (kind != kEffect) {
+                    a_now.store(a_tile);
+                    if (found) odd[turn] = 1;
+                }
             }
             __syncthreads();
             if constexpr (kind != kEffect) {
@@ -215,20 +214,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
                 const bool bad = __builtin_amdgcn_readfirstlane(odd[turn]);
                 turn ^= 1;
                 if (threadIdx.x == 0) odd[turn] = 0;
-                if (bad && n > 1) {
-                    n = 1;
+                if (bad && count > 1) {
+                    most = 1;
                     __syncthreads();
-                    fetch(n);
                     continue;
                 }
+                most = R;
             }
-            // the next chunk is on its way while this one is computed
-            const int64_t here = row;
-            const int count = n;
-            left -= n;
-            row += p.back ? -n : n;
-            n = (int)min((int64_t)R, left);
-            if (left > 0) fetch(n);
+            left -= count;
+            row += p.back ? -count : count;
 
             f32x4 o[NT][IT];
             if constexpr (kind != kEffect) {

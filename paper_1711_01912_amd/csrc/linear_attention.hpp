@@ -221,12 +221,17 @@ __device__ __forceinline__ void values(const Frag<bf16, P> &f, float (&v)[8]) {
     }
 }
 
-// R rows of a chunk in LDS, PAD bytes more from row to row than they hold: with 16 the lanes that read along rows meet in no bank (2.9
-// cycles an instruction, 4.7 with 32), with 32 those that read across them (2.8, 4.8 with 16).
-template <typename E, int P, int W, int R, int PAD>
+// R rows of a chunk in LDS, 32 bytes more from row to row than they hold: then the lanes of an instruction meet in no bank, whether they read
+// 16 bytes along rows (4.4 cycles; 8.4 with 16 bytes more) or across them (2.8 cycles; 4.8).
+// ORDERED: of 32 places those that a lane reads along a row, 4 and 4 that are 16 apart, are neighbours.
+template <typename E, int P, int W, int R, bool ORDERED>
 struct Tile {
-    static constexpr int kPitch = W + PAD / (int)sizeof(E);
+    static constexpr int kPitch = W + 32 / (int)sizeof(E);
+    static constexpr bool kOrdered = ORDERED && sizeof(E) == 2;
     E at[P][R][kPitch];
+
+    // where 4 places from c on lie
+    __device__ __forceinline__ static int place(int c) { return kOrdered ? c / 32 * 32 + c % 16 * 2 + c % 32 / 16 * 4 : c; }
 
     // rows r0 + 0..15, places 32 kb + 0..31
     __device__ __forceinline__ Frag<E, P> along(int r0, int kb, int lane) const {
@@ -239,14 +244,18 @@ struct Tile {
         } else {
 #pragma unroll
             for (int i = 0; i < P; i++) {
-                const bf16x4 a = *(const bf16x4 *)&at[i][row][c], b = *(const bf16x4 *)&at[i][row][c + 16];
-                f.p[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+                if constexpr (kOrdered) f.p[i] = *(const bf16x8 *)&at[i][row][place(c)];
+                else {
+                    const bf16x4 a = *(const bf16x4 *)&at[i][row][c], b = *(const bf16x4 *)&at[i][row][c + 16];
+                    f.p[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
             }
         }
         return f;
     }
     // columns c0 + 0..15, rows 32 jb + 0..31 as places (16 bits: transposed as they are read, 4 rows of 16 places by 16 lanes)
     __device__ __forceinline__ Frag<E, P> across(int c0, int jb, int lane) const {
+        static_assert(!kOrdered);
         Frag<E, P> f;
         const int i = lane % 16, row = 32 * jb + 4 * (lane / 16);
         if constexpr (sizeof(E) == 4) {
@@ -263,6 +272,15 @@ struct Tile {
         }
         return f;
     }
+    // 8 places from c on, a multiple of 8, of a row
+    __device__ __forceinline__ void put(int plane, int row, int c, const Pack<E, 8> &v) {
+        if constexpr (kOrdered) {
+            bf16x4 half[2];
+            __builtin_memcpy(half, &v, sizeof(half));
+            *(bf16x4 *)&at[plane][row][place(c)] = half[0];
+            *(bf16x4 *)&at[plane][row][place(c) + 8] = half[1];
+        } else *(Pack<E, 8> *)__builtin_assume_aligned(&at[plane][row][c], 16) = v;
+    }
     // 4 places from c on of a row, as what is computed is kept
     __device__ __forceinline__ void keep(int row, int c, f32x4 v) {
         if constexpr (sizeof(E) == 4) *(f32x4 *)&at[0][row][c] = v;
@@ -276,7 +294,7 @@ struct Tile {
                     b[e] = (bf16)rest[e];
                     rest[e] -= (float)b[e];
                 }
-                *(bf16x4 *)&at[i][row][c] = b;
+                *(bf16x4 *)&at[i][row][place(c)] = b;
             }
         }
     }
@@ -295,63 +313,26 @@ __device__ __forceinline__ uint32_t endless(const Pack<T, 8> &v) {
     return found & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u);
 }
 
-// Rows of a chunk on their way from memory to a tile, in registers: places c0 .. c0 + W - 1 of `width`; zeros where there are none.
-// EVEN: the width is a multiple of 8, so that all vectors of 8 lie inside rows or behind them.
-template <typename T, int W, int R, int THREADS, bool EVEN>
+// Rows of a chunk on their way from memory to a tile: the thread's vectors of 8 places
+template <typename T, int W, int R, int THREADS>
 struct Rows {
-    static constexpr int kPer = W / 8, kLoads = (R * kPer + THREADS - 1) / THREADS, kApart = THREADS / kPer;      // rows from load to load
+    static constexpr int kPer = W / 8, kLoads = (R * kPer + THREADS - 1) / THREADS, kApart = THREADS / kPer;      // rows from vector to vector
     static_assert(THREADS % kPer == 0 && (R * kPer % THREADS == 0 || kLoads == 1));
+    static constexpr bool kAll = R * kPer % THREADS == 0;      // whether all threads have a vector
     Pack<T, 8> v[kLoads];
-    const T *mine;                       // the thread's first element, were the chunk's first row the operand's
-    int64_t step;
-    int left;                            // places from the thread's first on
 
-    __device__ __forceinline__ void begin(const Operand &m, int32_t head, bool down, int c0, int width) {
-        const int r = (int)threadIdx.x / kPer, c = c0 + (int)threadIdx.x % kPer * 8;
-        step = down ? -m.ld : m.ld;
-        mine = (const T *)m.at + (head / m.group) * m.hd + r * step + c;
-        left = width - c;
-        const Pack<T, 8> none{};
-#pragma unroll
-        for (int k = 0; k < kLoads; k++) v[k] = none;
-    }
-    // `count` rows from `row` on, upwards or downwards
-    __device__ __forceinline__ void load(const Operand &m, int64_t row, int count) {
-        const T *from = mine + row * m.ld;
-        const int r = (int)threadIdx.x / kPer;
-        if constexpr (EVEN) {
-            if (count == R) {
-                if (left > 0 && (R * kPer % THREADS == 0 || r < R)) {
-#pragma unroll
-                    for (int k = 0; k < kLoads; k++) v[k] = load_pack<T, 8>(from + k * kApart * step);
-                }
-                return;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kLoads; k++) {
-            const bool here = r + k * kApart < count;
-            if constexpr (EVEN) {
-                v[k] = Pack<T, 8>{};
-                if (here && left > 0) v[k] = load_pack<T, 8>(from + k * kApart * step);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) v[k].v[e] = here && e < left ? from[k * kApart * step + e] : (T)0.0f;
-            }
-        }
-    }
     // true where a value is an infinity or a NaN
-    template <typename E, int P, int PAD>
-    __device__ __forceinline__ bool store(Tile<E, P, W, R, PAD> &tile) const {
+    template <typename E, int P, bool ORDERED>
+    __device__ __forceinline__ bool store(Tile<E, P, W, R, ORDERED> &tile) const {
         uint32_t odd = 0;
         const int r0 = (int)threadIdx.x / kPer, c = (int)threadIdx.x % kPer * 8;
 #pragma unroll
         for (int k = 0; k < kLoads; k++) {
             const int r = r0 + k * kApart;
-            if (R * kPer % THREADS && r >= R) break;
+            if (!kAll && r >= R) break;
             const Pack<T, 8> &u = v[k];
             odd |= endless<T>(u);
-            if constexpr (std::is_same_v<T, E>) *(Pack<T, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = u;
+            if constexpr (std::is_same_v<T, E>) tile.put(0, r, c, u);
             else {
                 Pack<E, 8> hi, lo;
 #pragma unroll
@@ -359,11 +340,55 @@ struct Rows {
                     hi.v[e] = (E)(float)u.v[e];
                     lo.v[e] = (E)((float)u.v[e] - (float)hi.v[e]);
                 }
-                *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[0][r][c], 16) = hi;
-                *(Pack<E, 8> *)__builtin_assume_aligned(&tile.at[1][r][c], 16) = lo;
+                tile.put(0, r, c, hi);
+                tile.put(1, r, c, lo);
             }
         }
         return odd != 0;
+    }
+};
+
+// Where a thread finds them: places c0 .. c0 + W - 1 of `width`; zeros where there are none.  EVEN: the width is a multiple of 8, so that
+// all vectors of 8 lie inside rows or behind them.
+template <typename T, int W, int R, int THREADS, bool EVEN>
+struct RowsOf {
+    using To = Rows<T, W, R, THREADS>;
+    const T *mine;                       // the thread's first element, were the chunk's first row the operand's
+    int64_t step;
+    int left;                            // places from the thread's first on
+
+    __device__ __forceinline__ RowsOf(const Operand &m, int32_t head, bool down, int c0, int width) {
+        const int r = (int)threadIdx.x / To::kPer, c = c0 + (int)threadIdx.x % To::kPer * 8;
+        step = down ? -m.ld : m.ld;
+        mine = (const T *)m.at + (head / m.group) * m.hd + r * step + c;
+        left = width - c;
+    }
+    // `count` rows from `row` on, upwards or downwards
+    __device__ __forceinline__ void load(To &to, const Operand &m, int64_t row, int count) const {
+        const T *from = mine + row * m.ld;
+        const int r = (int)threadIdx.x / To::kPer;
+#pragma unroll
+        for (int k = 0; k < To::kLoads; k++) to.v[k] = Pack<T, 8>{};
+        if constexpr (EVEN) {
+            if (count == R) {
+                if (left > 0 && (To::kAll || r < R)) {
+#pragma unroll
+                    for (int k = 0; k < To::kLoads; k++) to.v[k] = load_pack<T, 8>(from + k * To::kApart * step);
+                }
+                return;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < To::kLoads; k++) {
+            const bool here = r + k * To::kApart < count;
+            if constexpr (EVEN) {
+                if (here && left > 0) to.v[k] = load_pack<T, 8>(from + k * To::kApart * step);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (here && e < left) to.v[k].v[e] = from[k * To::kApart * step + e];
+            }
+        }
     }
 };
 
