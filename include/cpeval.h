@@ -580,7 +580,8 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
  *   carry         [cp_linear_attention_carry_states][heads][width_k][width_v] for the backward pass, or NULL
  *   status_out    device int32, required with seq_ptr: CP_STATUS_BAD_SEQUENCE where seq_ptr does not rise from 0 to at most
  *                 rows (no access leaves the arrays)
- * 16-bit products are exact and summed in 32 bits; states and scores go into them as the sum of two bf16, off by at most 2^-16.  An
+ * 16-bit products are exact and summed in 32 bits; states and scores on their way to o as the sum of two bf16, off by at most 2^-15, rows on their way to a state as they
+ * are.  An
  * infinity or a NaN makes results from its row to its sequence's end infinite or NaN, of its head alone.
  * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, widths, heads, num_seq < 1, num_seq * heads of equal
  * parts above 2^28, rows no multiple of num_seq without seq_ptr, distances; results whose rows or heads overlap),

@@ -108,7 +108,7 @@ struct State {
 // KB: blocks of 32 that the state's rows fill; NT: of 16 columns that a wavefront has; WAVES: of a workgroup; R: rows of a chunk;
 // EVEN: widths are multiples of 8
 template <typename T, int KB, int NT, int WAVES, int R, Kind kind, bool EVEN>
-__global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *effect, float *gain) {
+__global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind != kDecay && KB < 8 && WAVES == 8 ? 4 : 2) void pass_kernel(Pass p, float *effect, float *gain) {
     using F = Form<T>;
     using E = typename F::E;
     constexpr int P = F::kPlanes, PS = kind == kDecay ? F::kFine : F::kSplit, PU = F::kFine;

@@ -109,8 +109,8 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Elements as the matrix instructions take them.  bf16 as it is; fp16 as the sum of two bf16, which is exact; what is computed in 32
-// bits as the sum of bf16 too: of two, off by at most 2^-16, where the result has 16 bits itself (states and scores on their way to an output),
-// of three, off by 2^-24, where it has 32 (rows on their way to a state, all that the decays' gradient is made of).  float as it is,
+// bits as the sum of bf16 too: of two, off by at most 2^-15, where the result has 16 bits itself (states and scores on their way to an output),
+// of three, which is exact, where it has 32 (rows on their way to a state, all that the decays' gradient is made of).  float as it is,
 // through the float instructions.
 template <typename T>
 struct Form {
@@ -191,17 +191,31 @@ __device__ __forceinline__ void split(const float (&v)[8], Frag<float, 1> &f) {
 #pragma unroll
     for (int e = 0; e < 8; e++) f.v[e] = v[e];
 }
+// The parts of two values, each part's in one word: all but the last are the upper half of what is left, the last is rounded.  (Three hold all
+// 24 bits of a float.)
+template <int P>
+__device__ __forceinline__ void parts(float a, float b, uint32_t (&w)[P]) {
+#pragma unroll
+    for (int i = 0; i + 1 < P; i++) {
+        w[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+        a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+        b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+    }
+    typedef bf16 pair __attribute__((ext_vector_type(2)));
+    w[P - 1] = __builtin_bit_cast(uint32_t, pair{(bf16)a, (bf16)b});
+}
 template <int P>
 __device__ __forceinline__ void split(const float (&v)[8], Frag<bf16, P> &f) {
+    uint32_t w[P][4];
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        float rest = v[e];
+    for (int e = 0; e < 4; e++) {
+        uint32_t two[P];
+        parts<P>(v[2 * e], v[2 * e + 1], two);
 #pragma unroll
-        for (int i = 0; i < P; i++) {
-            f.p[i][e] = (bf16)rest;
-            rest -= (float)f.p[i][e];
-        }
+        for (int i = 0; i < P; i++) w[i][e] = two[i];
     }
+#pragma unroll
+    for (int i = 0; i < P; i++) __builtin_memcpy(&f.p[i], w[i], sizeof(w[i]));
 }
 template <typename E, int P>
 __device__ __forceinline__ void split(f32x4 a, f32x4 b, Frag<E, P> &f) {
@@ -285,17 +299,11 @@ struct Tile {
     __device__ __forceinline__ void keep(int row, int c, f32x4 v) {
         if constexpr (sizeof(E) == 4) *(f32x4 *)&at[0][row][c] = v;
         else {
-            float rest[4] = {v[0], v[1], v[2], v[3]};
+            uint32_t one[P], two[P];
+            parts<P>(v[0], v[1], one);
+            parts<P>(v[2], v[3], two);
 #pragma unroll
-            for (int i = 0; i < P; i++) {
-                bf16x4 b;
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    b[e] = (bf16)rest[e];
-                    rest[e] -= (float)b[e];
-                }
-                *(bf16x4 *)&at[i][row][place(c)] = b;
-            }
+            for (int i = 0; i < P; i++) *(uint2 *)&at[i][row][place(c)] = uint2{one[i], two[i]};
         }
     }
 };
@@ -356,30 +364,27 @@ struct RowsOf {
     const T *mine;                       // the thread's first element, were the chunk's first row the operand's
     int64_t step;
     int left;                            // places from the thread's first on
+    bool full;                           // whether all threads have some, the whole of 8
 
     __device__ __forceinline__ RowsOf(const Operand &m, int32_t head, bool down, int c0, int width) {
         const int r = (int)threadIdx.x / To::kPer, c = c0 + (int)threadIdx.x % To::kPer * 8;
         step = down ? -m.ld : m.ld;
         mine = (const T *)m.at + (head / m.group) * m.hd + r * step + c;
         left = width - c;
+        full = EVEN && To::kAll && width - c0 >= W;
     }
     // `count` rows from `row` on, upwards or downwards
     __device__ __forceinline__ void load(To &to, const Operand &m, int64_t row, int count) const {
         const T *from = mine + row * m.ld;
         const int r = (int)threadIdx.x / To::kPer;
+        if (count == R && full) {
 #pragma unroll
-        for (int k = 0; k < To::kLoads; k++) to.v[k] = Pack<T, 8>{};
-        if constexpr (EVEN) {
-            if (count == R) {
-                if (left > 0 && (To::kAll || r < R)) {
-#pragma unroll
-                    for (int k = 0; k < To::kLoads; k++) to.v[k] = load_pack<T, 8>(from + k * To::kApart * step);
-                }
-                return;
-            }
+            for (int k = 0; k < To::kLoads; k++) to.v[k] = load_pack<T, 8>(from + k * To::kApart * step);
+            return;
         }
 #pragma unroll
         for (int k = 0; k < To::kLoads; k++) {
+            to.v[k] = Pack<T, 8>{};
             const bool here = r + k * To::kApart < count;
             if constexpr (EVEN) {
                 if (here && left > 0) to.v[k] = load_pack<T, 8>(from + k * To::kApart * step);
