@@ -11,8 +11,7 @@
 //
 // The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
 //   dq_t = scale do_t S_t^T (the pass with do, v, k in the places of q, k, v),   dv_t = k_t D_t and dk_t = v_t D_t^T (from the last
-//   row on, with k, q, do and v, do, q),   dlog_decay = sum_t <D_t, gamma S_{t-1}> = sum_i scale do_i . do_i/dlog(gamma),
-// the last by carrying R = dS / dlog(gamma) along with S.
+//   row on, with k, q, do and v, do, q),   dlog_decay = sum_t <D_t, gamma S_{t-1}>, which the last two add up.
 //
 // Where sequences and heads do not fill the chip, the rows are cut into segments: each segment's effect on the state first, then the
 // states that enter them, segment by segment, then the outputs.
@@ -43,8 +42,12 @@ __device__ __forceinline__ void put(T *to, f32x4 o, float scale, int count) {
 
 // ---- the pass ----------------------------------------------------------------------------------------
 
-// kOut: outputs; kEffect: a segment's effect on the state alone; kDecay: the decays' gradient
-enum Kind { kOut, kEffect, kDecay };
+// kOut: outputs; kEffect: a segment's effect on the state alone.  The other two add to outputs their part of the decays' gradient.  That is, for
+// every chunk with S the state that enters it, X the gradient of the state behind it and P the scores,
+//   sum_i (i + 1) q_i . dq_i by S + sum_ij (i - j) P_ij (q_i . k_j) + sum_j (n - 1 - j) k_j . dk_j by X + n gamma^n <S, X>
+// kGrad: the first two in the pass for dq, and the last by carrying R' = gamma^n (R + n S) along, as sum_i q_i . dq_i by R and what R
+// ends in times its gradient.  kLeave: the third in the pass for dk.
+enum Kind { kOut, kEffect, kGrad, kLeave };
 
 // NT times 16 columns of a state, all of its rows, in a wavefront's registers: lane l has column l % 16, rows 16 k + 4 (l / 16) + 0..3
 template <int KB, int NT>
@@ -108,15 +111,20 @@ struct State {
 // KB: blocks of 32 that the state's rows fill; NT: of 16 columns that a wavefront has; WAVES: of a workgroup; R: rows of a chunk;
 // EVEN: widths are multiples of 8
 template <typename T, int KB, int NT, int WAVES, int R, Kind kind, bool EVEN>
-__global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind != kDecay && KB < 8 && WAVES == 8 ? 4 : 2) void pass_kernel(Pass p, float *effect, float *gain) {
+__global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *effect, float *gain) {
     using F = Form<T>;
     using E = typename F::E;
-    constexpr int P = F::kPlanes, PS = kind == kDecay ? F::kFine : F::kSplit, PU = F::kFine;
+    constexpr int P = F::kPlanes, PS = F::kSplit, PI = kind == kGrad || kind == kLeave ? F::kFine : F::kSplit, PU = F::kFine;
     constexpr int kThreadsHere = WAVES * kWave, kWide = 16 * NT * WAVES, IT = R / 16, JB = R / 32;
     __shared__ Tile<E, P, 32 * KB, R, false> b_tile;
     __shared__ Tile<E, P, kWide, R, false> x_tile;
     __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R, true> a_tile;
-    __shared__ Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R, true> s_tile;       // scores [row][place]
+    // scores [row][place], in the place of q's rows
+    using Scores = Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R, true>;
+    using Third = Tile<E, P, kind == kGrad ? kWide : 8, kind == kGrad ? R : 1, true>;
+    __shared__ __attribute__((aligned(16))) char shared_[sizeof(Scores) > sizeof(Third) ? sizeof(Scores) : sizeof(Third)];
+    Scores &s_tile = *(Scores *)shared_;
+    Third &d_tile = *(Third *)shared_;
     __shared__ int odd[2];
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane % 16, g = lane / 16;
@@ -167,10 +175,9 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
             for (int e = 0; e < 4; e++) {
                 const int apart = 16 * (it - jt) + l - 4 * g - e;
                 apart_[k][e] = apart < 0 ? 0.0f : power(lg, apart) * p.s_in;
-                if constexpr (kind == kDecay) apart_[k][e] *= (float)max(apart, 0);
             }
-            // (right of a diagonal's tile, in its block of 32, lies one that is never written again)
-            if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
+            // (right of a diagonal's tile, in its block of 32, lies one that is never written again, unless q's rows are)
+            if (kind != kGrad && it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
         }
 #pragma unroll
         for (int it = 0; it < IT; it++) in_[it] = power(lg, 16 * it + l + 1 - p.shift);
@@ -183,15 +190,17 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
     const float wane_ = power_less_one(lg, R);
 
     const RowsOf<T, 32 * KB, R, kThreadsHere, EVEN> a_rows(p.a, head, p.back, 0, p.wa), b_rows(p.b, head, p.back, 0, p.wa);
-    const RowsOf<T, kWide, R, kThreadsHere, EVEN> x_rows(p.x, head, p.back, c0, p.wb);
+    const RowsOf<T, kWide, R, kThreadsHere, EVEN> x_rows(p.x, head, p.back, c0, p.wb), d_rows(p.d, head, p.back, c0, p.wb);
+    const bool remembers = lg * R > -40.0f;            // whether what lies before a chunk counts behind it (2^-40: no more in 32 bits)
     while (lo < hi) {
         const Piece piece = piece_at(p, lo, hi);
         int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
         if (piece.starts && p.init) s.load(p, p.init, piece.seq, head, col, g);
         else if (kind != kEffect && !piece.starts && p.enter) s.load(p, p.enter, seg, head, col, g);
         else s.zero();
-        if constexpr (kind == kDecay) r.zero();
-        int most = R;
+        if constexpr (kind == kGrad) r.zero();
+        // (from the last row on, the first chunk is the shorter one, so that all passes have the same)
+        int most = kind != kEffect && p.last_first ? (int)((left - 1) % R) + 1 : R;
         while (left > 0) {
             const int count = (int)min((int64_t)most, left);
             const int64_t here = row;
@@ -206,6 +215,11 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
                 if constexpr (kind != kEffect) {
                     a_now.store(a_tile);
                     if (found) odd[turn] = 1;
+                }
+                if constexpr (kind == kGrad) {
+                    Rows<T, kWide, R, kThreadsHere> d_now;
+                    d_rows.load(d_now, p.d, row, count);
+                    d_now.store(d_tile);
                 }
             }
             __syncthreads();
@@ -227,6 +241,7 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
             f32x4 o[NT][IT];
             if constexpr (kind != kEffect) {
                 // scores of rows i (lanes) and j (places): the tiles on and below the diagonal, shared out
+                f32x4 score[kMine];
 #pragma unroll
                 for (int m = 0; m < kMine; m++) {
                     int it, jt;
@@ -245,16 +260,38 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
                     }
 #pragma unroll
                     for (int e = 0; e < 4; e++) c[e] = it == jt && 4 * g + e > l ? 0.0f : c[e] * apart_[m][e];     // (what lies above the diagonal is not looked at)
-                    s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
+                    if constexpr (kind == kGrad) {
+                        f32x4 other = {0, 0, 0, 0};
+#pragma unroll
+                        for (int k = 0; k < kWide / 32; k++) other = product<true>(x_tile.along(16 * jt, k, lane), d_tile.along(16 * it, k, lane), other);
+                        float sum = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const int apart = 16 * (it - jt) + l - 4 * g - e;
+                            if (apart > 0) sum += (float)apart * c[e] * other[e];
+                        }
+                        decay_sum += (double)(sum * p.s_out);
+                        score[m] = c;
+                    } else s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
+                }
+                if constexpr (kind == kGrad) {
+                    __syncthreads();
+#pragma unroll
+                    for (int m = 0; m < kMine; m++) {
+                        int it, jt;
+                        if (!tile_of(m, it, jt)) continue;
+                        s_tile.keep(16 * it + l, 16 * jt + 4 * g, score[m]);
+                        if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
+                    }
                 }
                 // what the state that enters gives, 32 of its rows at a time
-                f32x4 more[NT][kind == kDecay ? IT : 1];
+                f32x4 more[NT][kind == kGrad ? IT : 1];
 #pragma unroll
                 for (int t = 0; t < NT; t++)
 #pragma unroll
                     for (int it = 0; it < IT; it++) {
                         o[t][it] = f32x4{0, 0, 0, 0};
-                        if constexpr (kind == kDecay) more[t][it] = f32x4{0, 0, 0, 0};
+                        if constexpr (kind == kGrad) more[t][it] = f32x4{0, 0, 0, 0};
                     }
                 Frag<E, P> af[2][IT];
                 const auto ask = [&](int k) {
@@ -268,24 +305,45 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
                     asked();
 #pragma unroll
                     for (int t = 0; t < NT; t++) {
-                        Frag<E, PS> sf;
+                        Frag<E, PI> sf;
                         split(s.at[t][2 * k], s.at[t][2 * k + 1], sf);
                         products<true>(af[k % 2], sf, o[t]);
-                        if constexpr (kind == kDecay) {
-                            split(r.at[t][2 * k], r.at[t][2 * k + 1], sf);
-                            products<true>(af[k % 2], sf, more[t]);
+                        if constexpr (kind == kGrad) {
+                            if (remembers) {
+                                split(r.at[t][2 * k], r.at[t][2 * k + 1], sf);
+                                products<true>(af[k % 2], sf, more[t]);
+                            }
                         }
                     }
                 }
 #pragma unroll
-                for (int t = 0; t < NT; t++)
+                for (int t = 0; t < NT; t++) {
+                    const int c = c0 + mine + 16 * t + 4 * g;
 #pragma unroll
-                    for (int it = 0; it < IT; it++)
+                    for (int it = 0; it < IT; it++) {
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            if constexpr (kind == kDecay) o[t][it][e] = more[t][it][e] + (float)(16 * it + l + 1) * o[t][it][e];
-                            o[t][it][e] *= in_[it];
+                        for (int e = 0; e < 4; e++) o[t][it][e] *= in_[it];
+                        if constexpr (kind == kGrad || kind == kLeave) {
+                            const int i = 16 * it + l;
+                            if (i >= count || c >= p.wb) continue;
+                            const T *from = (const T *)p.d.at + (here + (p.back ? -i : i)) * p.d.ld + (head / p.d.group) * p.d.hd + c;
+                            float sum = 0;
+                            Pack<T, 4> with{};
+                            if constexpr (EVEN) with = load_pack<T, 4>(from);
+                            else {
+#pragma unroll
+                                for (int e = 0; e < 4; e++)
+                                    if (c + e < p.wb) with.v[e] = from[e];
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                const float one = kind == kGrad ? fmaf(more[t][kind == kGrad ? it : 0][e], in_[it], (float)(i + 1) * o[t][it][e]) : (float)i * o[t][it][e];
+                                sum = fmaf((float)with.v[e], one, sum);
+                            }
+                            decay_sum += (double)(sum * p.s_out);
                         }
+                    }
+                }
                 __syncthreads();
             }
             Frag<E, P> xf[NT][JB];
@@ -309,28 +367,14 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
 #pragma unroll
                 for (int t = 0; t < NT; t++) {
                     const int c = c0 + mine + 16 * t + 4 * g;
-                    if constexpr (kind == kOut) {
-                        const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
-                        const int places = EVEN ? 4 : p.wb - c;
-                        if (c < p.wb) {
-#pragma unroll
-                            for (int it = 0; it < IT; it++) {
-                                if (16 * it + l >= count) continue;
-                                if (p.wide) put((float *)p.o + to + it * step, o[t][it], p.s_out, places);
-                                else put((T *)p.o + to + it * step, o[t][it], p.s_out, places);
-                            }
-                        }
-                    } else {
+                    const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
+                    const int places = EVEN ? 4 : p.wb - c;
+                    if (c < p.wb) {
 #pragma unroll
                         for (int it = 0; it < IT; it++) {
-                            const int i = 16 * it + l;
-                            if (i >= count) continue;
-                            const T *from = (const T *)p.d.at + (here + (p.back ? -i : i)) * p.d.ld + (head / p.d.group) * p.d.hd + c;
-                            float sum = 0;
-#pragma unroll
-                            for (int e = 0; e < 4; e++)
-                                if (c + e < p.wb) sum += (float)from[e] * o[t][it][e];
-                            decay_sum += (double)(sum * p.s_out);
+                            if (16 * it + l >= count) continue;
+                            if (p.wide) put((float *)p.o + to + it * step, o[t][it], p.s_out, places);
+                            else put((T *)p.o + to + it * step, o[t][it], p.s_out, places);
                         }
                     }
                 }
@@ -339,9 +383,9 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
             // the state behind the chunk
             float wane = wane_;
             if (count != R) wane = power_less_one(lg, count);
-            if constexpr (kind == kDecay) {
+            if constexpr (kind == kGrad) {
+                r.add(s, (float)count);
                 r.decay(wane);
-                r.add(s, power(lg, count) * (float)count);
             }
             s.decay(wane);
 #pragma unroll
@@ -353,7 +397,7 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
 #pragma unroll
                     for (int e = 0; e < 8; e++) by[e] = power(lg, behind(jb, e, count) + p.shift) * p.s_in;      // (rows behind the chunk's are zeros)
                 }
-                Frag<E, PU> vf[NT], wf[kind == kDecay ? NT : 1];
+                Frag<E, PU> vf[NT];
 #pragma unroll
                 for (int t = 0; t < NT; t++) {
                     float v[8];
@@ -361,11 +405,6 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
 #pragma unroll
                     for (int e = 0; e < 8; e++) v[e] *= by[e];
                     split(v, vf[t]);
-                    if constexpr (kind == kDecay) {
-#pragma unroll
-                        for (int e = 0; e < 8; e++) v[e] *= (float)behind(jb, e, count);
-                        split(v, wf[t]);
-                    }
                 }
                 constexpr int kGroup = 4;
 #pragma unroll
@@ -375,10 +414,7 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
                     for (int k = 0; k < kGroup; k++) bf[k] = b_tile.across(16 * (k0 + k), jb, lane);
                     asked();
 #pragma unroll
-                    for (int t = 0; t < NT; t++) {
-                        products(bf, vf[t], &s.at[t][k0]);
-                        if constexpr (kind == kDecay) products(bf, wf[t], &r.at[t][k0]);
-                    }
+                    for (int t = 0; t < NT; t++) products(bf, vf[t], &s.at[t][k0]);
                 }
             }
             __syncthreads();
@@ -386,7 +422,7 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
         if constexpr (kind == kOut) {
             if (piece.ends && p.last) s.store(p, p.last, piece.seq, head, col, g);
         }
-        if constexpr (kind == kDecay) {
+        if constexpr (kind == kGrad) {
             if (piece.ends) {
                 if (p.dlast) decay_sum += r.dot(p, p.dlast, piece.seq, head, col, g);
             } else if (p.denter) decay_sum += r.dot(p, p.denter, seg, head, col, g);
@@ -395,7 +431,7 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
         else lo = piece.hi;
     }
     if constexpr (kind == kEffect) s.store(p, effect, seg, head, col, g);
-    if constexpr (kind == kDecay) {
+    if constexpr (kind == kGrad || kind == kLeave) {
         __shared__ double sums[WAVES];
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) decay_sum += __shfl_xor(decay_sum, off);
@@ -403,7 +439,7 @@ __global__ __launch_bounds__(WAVES * kWave, (std::is_same_v<T, bf16>) && kind !=
         __syncthreads();
         if (threadIdx.x == 0) {
             for (int w = 1; w < WAVES; w++) decay_sum += sums[w];
-            p.part[(int64_t)head * p.segments * p.slices + seg * p.slices + slice] = decay_sum;
+            p.part[head * p.part_step + (int64_t)seg * p.slices + slice] = decay_sum;
         }
     }
 }
@@ -583,9 +619,14 @@ int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t 
     // room for one such in LDS, and those of 256 places for 64 rows only of bf16.
     constexpr bool kHalf = std::is_same_v<T, bf16>;
     constexpr int R = KB == 8 && !kHalf ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
+    if (kind == kGrad) {       // (two states: 16 columns a wavefront)
+        hipLaunchKernelGGL((pass_kernel<T, KB, 1, COLUMNS / 16, R, kGrad, EVEN>), grid_of((int64_t)p.segments * p.heads * p.slices), dim3(COLUMNS * 4), 0, st, p,
+                           effect, gain);
+        return launched();
+    }
     auto *kernel = kind == kOut      ? pass_kernel<T, KB, NT, WAVES, R, kOut, EVEN>
                    : kind == kEffect ? pass_kernel<T, KB, NT, WAVES, R, kEffect, EVEN>
-                                     : pass_kernel<T, KB, NT, WAVES, R, kDecay, EVEN>;
+                                     : pass_kernel<T, KB, NT, WAVES, R, kLeave, EVEN>;
     hipLaunchKernelGGL(kernel, grid_of((int64_t)p.segments * p.heads * p.slices), dim3(WAVES * kWave), 0, st, p, effect, gain);
     return launched();
 }
@@ -636,7 +677,9 @@ size_t state_floats(const Shape &s) { return (size_t)s.heads * s.wk * s.wv; }
 // of the states that enter segments, and of their gains
 size_t enter_bytes(const Shape &s, const Cut &c) { return c.split ? align_up(c.segments * state_floats(s) * sizeof(float)) : 0; }
 size_t gain_bytes(const Shape &s, const Cut &c) { return c.split ? align_up((size_t)c.segments * s.heads * sizeof(float)) : 0; }
-size_t part_bytes(const Shape &s, const Cut &c) { return align_up((size_t)s.heads * c.segments * slices_of(s.wk, s.wv) * sizeof(double)); }
+// (of the passes for dq and dk, both of width_k columns)
+int64_t part_count(const Shape &s, const Cut &c) { return 2 * (int64_t)c.segments * slices_of(s.wv, s.wk); }
+size_t part_bytes(const Shape &s, const Cut &c) { return align_up((size_t)s.heads * part_count(s, c) * sizeof(double)); }
 size_t share_bytes(const Shape &s) { return s.heads == s.kv_heads ? 0 : align_up((size_t)s.rows * s.heads * std::max(s.wk, s.wv) * sizeof(float)); }
 
 size_t need_of(const Shape &s, bool backward) {
@@ -807,7 +850,7 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
 
     // dv: keys read the gradient of the state
     Pass b = p;
-    b.wa = width_k, b.wb = width_v, b.back = reverse == 0, b.shift = 1, b.s_in = scale, b.s_out = 1.0f;
+    b.wa = width_k, b.wb = width_v, b.back = reverse == 0, b.last_first = true, b.shift = 1, b.s_in = scale, b.s_out = 1.0f;
     b.a = in_k, b.b = in_q, b.x = in_do, b.init = dlast, b.last = dh0;
     if (c.split) {
         rc = run_enter(type, b, denter, gain, st);
@@ -815,13 +858,13 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
         b.enter = denter;
     }
     // (heads that share keys and values: their gradients apart first, in 32 bits)
-    const auto gradient = [&](Pass pass, void *to, int64_t ld, int64_t hd) {
+    const auto gradient = [&](Kind kind, Pass pass, void *to, int64_t ld, int64_t hd) {
         if (group == 1) {
             pass.o = to, pass.ldo = ld, pass.hdo = hd;
-            return run(kOut, type, pass, nullptr, nullptr, st);
+            return run(kind, type, pass, nullptr, nullptr, st);
         }
         pass.o = share, pass.hdo = pass.wb, pass.ldo = (int64_t)heads * pass.wb, pass.wide = true;
-        const int code = run(kOut, type, pass, nullptr, nullptr, st);
+        const int code = run(kind, type, pass, nullptr, nullptr, st);
         if (code) return code;
         const int64_t blocks = (rows * kv_heads * pass.wb + kThreads - 1) / kThreads;
         return by_type(type, [&](auto t) {
@@ -831,27 +874,23 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
             return launched();
         });
     };
-    rc = gradient(b, dv, lddv, hddv);
+    rc = gradient(kOut, b, dv, lddv, hddv);
     if (rc) return rc;
     // dk: values read it, transposed
+    const int64_t parts = part_count(s, c);
     b.wa = width_v, b.wb = width_k, b.transposed = true, b.last = nullptr;
-    b.a = in_v, b.b = in_do, b.x = in_q;
-    rc = gradient(b, dk, lddk, hddk);
+    b.a = in_v, b.b = in_do, b.x = in_q, b.d = in_k, b.part = part + parts / 2, b.part_step = parts;
+    rc = gradient(dlog_decay ? kLeave : kOut, b, dk, lddk, hddk);
     if (rc) return rc;
     // dq: the gradients of the outputs read the state, transposed
     Pass a = p;
     a.wa = width_v, a.wb = width_k, a.transposed = true, a.back = reverse != 0, a.s_in = 1.0f, a.s_out = scale;
-    a.a = in_do, a.b = in_v, a.x = in_k, a.init = h0, a.enter = c.split ? carry : nullptr;
+    a.a = in_do, a.b = in_v, a.x = in_k, a.d = in_q, a.init = h0, a.enter = c.split ? carry : nullptr;
     a.o = dq, a.ldo = lddq, a.hdo = hddq;
-    rc = run(kOut, type, a, nullptr, nullptr, st);
+    a.dlast = dlast, a.denter = c.split ? denter : nullptr, a.part = part, a.part_step = parts;
+    rc = run(dlog_decay ? kGrad : kOut, type, a, nullptr, nullptr, st);
     if (rc || !dlog_decay) return rc;
-    Pass e = p;
-    e.wa = width_k, e.wb = width_v, e.back = reverse != 0, e.s_in = 1.0f, e.s_out = scale;
-    e.a = in_q, e.b = in_k, e.x = in_v, e.d = in_do, e.init = h0, e.enter = c.split ? carry : nullptr;
-    e.dlast = dlast, e.denter = c.split ? denter : nullptr, e.part = part;
-    rc = run(kDecay, type, e, nullptr, nullptr, st);
-    if (rc) return rc;
-    hipLaunchKernelGGL(decay_kernel, dim3((unsigned)heads), dim3(kThreads), 0, st, part, (int64_t)c.segments * slices_of(width_k, width_v), dlog_decay);
+    hipLaunchKernelGGL(decay_kernel, dim3((unsigned)heads), dim3(kThreads), 0, st, part, parts, dlog_decay);
     return launched();
 }
 

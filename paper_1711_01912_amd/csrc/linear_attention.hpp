@@ -38,10 +38,12 @@ struct Pass {
     void *o;                             // rows as a's heads
     int64_t ldo, hdo;
     bool wide;                           // o in floats, whatever the type
-    // of the pass for the decays' gradient
-    Operand d;                           // do
+    bool last_first;                     // chunks as those of a pass from the other end
+    // of passes that add to the decays' gradient
+    Operand d;                           // what o is the gradient of
     const float *dlast, *denter;         // gradients of the states behind sequences and segments, or null
-    double *part;                        // [heads][segments * slices]
+    double *part;                        // of a head: [segments][slices], part_step from head to head
+    int64_t part_step;
 };
 
 // ---- sequences ---------------------------------------------------------------------------------------
