@@ -67,16 +67,33 @@ __device__ __forceinline__ void put_token(const Draw &d, int64_t row, int32_t g,
     else ((int64_t *)d.tokens)[at] = token;
 }
 
-// Row's g-th random number.  Below 0, and NaN, it counts as 0, from 1 on as the last number below 1.
-__device__ __forceinline__ float number(const Draw &d, int64_t row, int32_t g) {
-    return fminf(fmaxf(d.u[row * d.u_row + g * d.u_step], 0.0f), 0x1.fffffep-1f);
-}
+// A random number below 0, and NaN, counts as 0, from 1 on as the last number below 1.
+__device__ __forceinline__ float counted(float u) { return fminf(fmaxf(u, 0.0f), 0x1.fffffep-1f); }
 
 // the first float that is not below v >= 0
 __device__ __forceinline__ float float_above(double v) {
     const float f = (float)v;
     return (double)f < v ? __uint_as_float(__float_as_uint(f) + 1) : f;
 }
+
+// 2^t for t <= 0 with the relative error of a few roundings of 64 bits: Taylor's polynomial of 2^f, |f| <= 1/2, is off by 0.35^12 / 12! = 7e-15
+__device__ __forceinline__ double power_of_two(double t) {
+    const double n = __builtin_rint(fmax(t, -1080.0)), f = (fmax(t, -1080.0) - n) * 0.69314718055994530942;
+    double p = 1.0 / 39916800;
+    p = fma(p, f, 1.0 / 3628800);
+    p = fma(p, f, 1.0 / 362880);
+    p = fma(p, f, 1.0 / 40320);
+    p = fma(p, f, 1.0 / 5040);
+    p = fma(p, f, 1.0 / 720);
+    p = fma(p, f, 1.0 / 120);
+    p = fma(p, f, 1.0 / 24);
+    p = fma(p, f, 1.0 / 6);
+    p = fma(p, f, 0.5);
+    p = fma(p, f, 1.0);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+constexpr double kLog2eWide = 1.44269504088896340736;
 
 // larger logits have larger keys, equal ones (0 and -0) the same
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -111,14 +128,73 @@ __device__ __forceinline__ double sum_upto(double v, int lane) {
 
 constexpr int kFew = 256, kFewThreads = 256;
 
+// The row's draws, `side` of them side by side from `first` on.  Their number of borders that are not above u: counted where there are few, else by
+// halving.
+template <typename TT, int E>
+__device__ __forceinline__ void draw_more(const Draw &d, int64_t row, const float *edge, const float *lp, bool none, int32_t first, int32_t side) {
+    const int V = d.vocab;
+    const bool neighbours = d.u_step == 1 && d.t_step == 1;
+    float at[E > 0 ? E : 1];
+#pragma unroll
+    for (int v = 0; v < E; v++) at[v] = v < V - 1 ? edge[v] : INFINITY;
+    const auto draw = [&](float u) {
+        int n = 0;
+        if constexpr (E > 0) {
+#pragma unroll
+            for (int v = 0; v < E; v++) n += !(u < at[v]);
+        } else {
+            int hi = V - 1;                  // the first border above u
+            while (n < hi) {
+                const int mid = (n + hi) / 2;
+                if (!(u < edge[mid])) n = mid + 1;
+                else hi = mid;
+            }
+        }
+        return n;
+    };
+    TT *to = (TT *)d.tokens + row * d.t_row;
+    const float *u = d.u + row * d.u_row;
+    float *logp = d.logp ? d.logp + row * d.given : nullptr;
+    int32_t done = 0;
+    if (neighbours && side == kWave) {
+        // four neighbouring draws a lane
+        for (int32_t g = 4 * first; g + 4 <= d.given; g += 4 * side) {
+            const Pack<float, 4> four = load_pack<float, 4>(u + g);
+            Pack<TT, 4> token;
+            Pack<float, 4> l;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int n = none ? -1 : draw(counted(four.v[e]));
+                token.v[e] = (TT)n;
+                if (logp) l.v[e] = none ? 0.0f : lp[n];
+            }
+            store_pack<TT, 4>(to + g, token);
+            if (logp) store_pack<float, 4>(logp + g, l);
+        }
+        done = d.given & ~3;
+    }
+    for (int32_t g = done + first; g < d.given; g += side) {
+        const int n = none ? -1 : draw(counted(u[g * d.u_step]));
+        to[g * d.t_step] = (TT)n;
+        if (logp) logp[g] = none ? 0.0f : lp[n];
+    }
+}
+template <typename TT>
+__device__ __forceinline__ void draw_row(const Draw &d, int64_t row, const float *edge, const float *lp, bool none, int32_t first, int32_t side) {
+    if (d.vocab <= 8) draw_more<TT, 7>(d, row, edge, lp, none, first, side);
+    else if (d.vocab <= 16) draw_more<TT, 15>(d, row, edge, lp, none, first, side);
+    else draw_more<TT, 0>(d, row, edge, lp, none, first, side);
+}
+
 // L lanes a row, places 4 lane .. 4 lane + 3 of each where there are more than L, else one each.  A row's borders, cumulated
 // shares of its mass, are rounded up to floats: u, a float, is below one just if it is below the other.  A draw then is the number of borders
 // that are not above u.
-template <typename T, int L>
+template <typename T, int L, typename TT>
 __global__ __launch_bounds__(kFewThreads) void few_sample_kernel(Draw d) {
     constexpr int kRowsHere = kFewThreads / L, kPer = L == 64 ? 4 : 1, kRoom = L * kPer;
     __shared__ float border[kRowsHere][kRoom + 1], lp[kRowsHere][kRoom + 1], xs[kRowsHere][kRoom + 1];
     __shared__ double ps[kRowsHere][kRoom];
+    __shared__ bool empty[kRowsHere];
     const int lane = threadIdx.x % L, mine = threadIdx.x / L;
     const int64_t row = (int64_t)group_number() * kRowsHere + mine;
     const bool here = row < d.rows;
@@ -150,7 +226,7 @@ __global__ __launch_bounds__(kFewThreads) void few_sample_kernel(Draw d) {
     if (here && !rule.fine && lane == 0) atomicOr(d.status, CP_STATUS_BAD_SAMPLING);
     double p[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; i++) p[i] = none || x[i] == -INFINITY ? 0.0 : exp(((double)x[i] - (double)m) * rule.scale);
+    for (int i = 0; i < kPer; i++) p[i] = none || x[i] == -INFINITY ? 0.0 : power_of_two(((double)x[i] - (double)m) * rule.scale * kLog2eWide);
     const bool sorts = !none && rule.sorts();
     if (sorts) {
 #pragma unroll
@@ -210,64 +286,113 @@ __global__ __launch_bounds__(kFewThreads) void few_sample_kernel(Draw d) {
             if (d.logp) lp[mine][v] = (float)(((double)x[i] - (double)m) * rule.scale - logs);
         }
     }
+    if (lane == 0) empty[mine] = none;
     __syncthreads();
-    if (!here) return;
-    const float *edge = border[mine];
-    float at[15];
-#pragma unroll
-    for (int v = 0; v < 15; v++) at[v] = v < V - 1 ? edge[v] : INFINITY;
-    auto draw = [&](float u) {
-        int n = 0, hi = V - 1;               // the first border above u
-        if (V <= 16) {
-#pragma unroll
-            for (int v = 0; v < 15; v++) n += !(u < at[v]);
-            return n;
+    // The draws: a wavefront a row where a row has many, else one after the other
+    const int64_t row0 = (int64_t)group_number() * kRowsHere;
+    const int rows = (int)min((int64_t)kRowsHere, d.rows - row0);
+    if (d.given >= kWave) {
+        const int wlane = threadIdx.x % kWave;
+        for (int r = threadIdx.x / kWave; r < rows; r += kFewThreads / kWave) draw_row<TT>(d, row0 + r, border[r], lp[r], empty[r], wlane, kWave);
+    } else {
+        const int all = rows * d.given;
+        for (int i = threadIdx.x; i < all; i += kFewThreads) {
+            const int r = i / d.given;
+            draw_row<TT>(d, row0 + r, border[r], lp[r], empty[r], i % d.given, INT32_MAX / 2);
         }
-        while (n < hi) {
-            const int mid = (n + hi) / 2;
-            if (!(u < edge[mid])) n = mid + 1;
-            else hi = mid;
-        }
-        return n;
-    };
-    for (int32_t g = lane; g < d.given; g += L) {
-        int token = -1;
-        if (!none) token = draw(number(d, row, g));
-        put_token(d, row, g, token);
-        if (d.logp) d.logp[row * d.given + g] = none ? 0.0f : lp[mine][token];
     }
 }
 
 // ---- rows of many places -----------------------------------------------------------------------------
 
-constexpr int kManyThreads = 1024, kManyWaves = kManyThreads / kWave;
-constexpr int kBins = 2048, kChunks = 2048;
+constexpr int kChunks = 2048;                // of a row, whose masses are kept
+constexpr int kBins = 2048, kCopies = 2;     // of the digits of a key; lanes that meet in a bin go to copies
+constexpr int kSteps = 256, kLanes = 16;     // of mass by depth below the best; as many copies
+constexpr int kListed = 2048;                // places that a list has room for
+constexpr int kRanked = 512;                 // up to which a list is put in order by counting
+static_assert(kBins * kCopies == kSteps * kLanes);
 
-// sums over the threads in front of one's own; total of all
-template <typename N>
-__device__ __forceinline__ N block_before(N v, N *room, N &total) {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    N upto = v;
+template <int THREADS>
+struct Block {
+    static constexpr int kWaves = THREADS / kWave;
+    union {
+        float f[kWaves];
+        uint64_t u[kWaves];
+        double d[kWaves];
+        int32_t i[kWaves];
+    };
+    __device__ __forceinline__ float *of(float) { return f; }
+    __device__ __forceinline__ uint64_t *of(uint64_t) { return u; }
+    __device__ __forceinline__ double *of(double) { return d; }
+    __device__ __forceinline__ int32_t *of(int32_t) { return i; }
+
+    // the sum over the threads in front of one's own; total of all
+    template <typename N>
+    __device__ __forceinline__ N before(N v, N &total) {
+        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+        N upto = v;
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const N o = __shfl_up(upto, off);
-        if (lane >= off) upto += o;
+        for (int off = 1; off < kWave; off <<= 1) {
+            const N o = __shfl_up(upto, off);
+            if (lane >= off) upto += o;
+        }
+        N *room = of(N{});
+        __syncthreads();
+        if (lane == kWave - 1) room[wave] = upto;
+        __syncthreads();
+        N front = 0;
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) {
+            if (w < wave) front += room[w];
+            total += room[w];
+        }
+        return front + upto - v;
     }
-    __syncthreads();
-    if (lane == kWave - 1) room[wave] = upto;
-    __syncthreads();
-    N before = 0;
-    total = 0;
-    for (int w = 0; w < kManyWaves; w++) {
-        if (w < wave) before += room[w];
-        total += room[w];
+};
+
+// The words of a list from the largest on.  Few are counted into their places, more go through a sorting network.
+template <int THREADS>
+__device__ __forceinline__ void put_in_order(uint64_t *list, int count) {
+    if (count <= kRanked) {
+        constexpr int kOwn = (kRanked + THREADS - 1) / THREADS;
+        uint64_t own[kOwn];
+        int rank[kOwn];
+#pragma unroll
+        for (int o = 0; o < kOwn; o++) {
+            const int i = threadIdx.x + o * THREADS;
+            own[o] = i < count ? list[i] : 0, rank[o] = 0;
+        }
+        if (count > (int)(threadIdx.x & ~(kWave - 1)))         // (a wavefront with words)
+            for (int k = 0; k < count; k++) {
+                const uint64_t other = list[k];
+#pragma unroll
+                for (int o = 0; o < kOwn; o++) rank[o] += other > own[o];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int o = 0; o < kOwn; o++)
+            if ((int)threadIdx.x + o * THREADS < count) list[rank[o]] = own[o];
+        __syncthreads();
+        return;
     }
-    return before + upto - v;
+    int size = 2;
+    while (size < count) size *= 2;
+    for (int i = count + (int)threadIdx.x; i < size; i += THREADS) list[i] = 0;
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+        for (int step = run / 2; step > 0; step /= 2) {
+            for (int k = threadIdx.x; k < size / 2; k += THREADS) {
+                const int i = 2 * k - (k & (step - 1)), j = i + step;
+                const uint64_t a = list[i], b = list[j];
+                if ((a < b) == ((i & run) == 0)) list[i] = b, list[j] = a;
+            }
+            __syncthreads();
+        }
 }
 
-// A workgroup a row, which is read from the caches for each of: the maximum; the logit that top_k and top_p end at, digit by digit of its
-// key from a histogram of places or of mass (in whole numbers, which add up the same in any order); the mass of each chunk; the draws.
-template <typename T>
+// A workgroup a row, which is read from the caches for each of: the maximum; where what is kept ends; the mass of each chunk; the draws.
+template <typename T, int THREADS>
 struct Many {
     static constexpr int kVec = 16 / (int)sizeof(T), kStep = kWave * kVec;      // places of a lane and of a wavefront's load
     static constexpr int kLevels = sizeof(T) == 2 ? 2 : 3, kDrop = sizeof(T) == 2 ? 10 : 0;        // digits of 11, 11 and 10 bits
@@ -276,7 +401,7 @@ struct Many {
     const uint64_t *allow;
     int32_t V;
     float m;
-    double scale;
+    double scale;                        // (of exponents of 2)
 
     // kVec places from v on; what is not there or not allowed is -inf
     __device__ __forceinline__ void load(int32_t v, float (&x)[kVec]) const {
@@ -291,7 +416,34 @@ struct Many {
             for (int i = 0; i < kVec; i++) x[i] = v + i < V && (bits >> i & 1) ? (float)row[v + i] : -INFINITY;
         }
     }
-    __device__ __forceinline__ double share(float x) const { return x == -INFINITY ? 0.0 : exp(((double)x - (double)m) * scale); }
+    // f(place, its logit) for all places, the workgroup's threads side by side, with AHEAD vectors a thread under way at once
+    template <int AHEAD, typename F>
+    __device__ __forceinline__ void each(F f) const {
+        constexpr int kSide = THREADS * kVec;
+        int32_t v = threadIdx.x * kVec;
+        const int32_t whole = V / (kSide * AHEAD) * (kSide * AHEAD);
+        for (; v < whole; v += kSide * AHEAD) {
+            Pack<T, kVec> at[AHEAD];
+            uint64_t bits[AHEAD];
+#pragma unroll
+            for (int q = 0; q < AHEAD; q++) at[q] = load_pack<T, kVec>(row + v + q * kSide);
+#pragma unroll
+            for (int q = 0; q < AHEAD; q++) bits[q] = allow ? allow[(v + q * kSide) >> 6] >> (v & 63) : ~0ull;      // (64 divides kSide)
+#pragma unroll
+            for (int q = 0; q < AHEAD; q++)
+#pragma unroll
+                for (int i = 0; i < kVec; i++) f(v + q * kSide + i, bits[q] >> i & 1 ? (float)at[q].v[i] : -INFINITY);
+        }
+        for (; v < V; v += kSide) {
+            float x[kVec];
+            load(v, x);
+#pragma unroll
+            for (int i = 0; i < kVec; i++)
+                if (v + i < V) f(v + i, x[i]);
+        }
+    }
+    __device__ __forceinline__ double depth(float x) const { return ((double)m - (double)x) * scale; }
+    __device__ __forceinline__ double share(float x) const { return x == -INFINITY ? 0.0 : power_of_two(-depth(x)); }
     __device__ __forceinline__ static uint32_t key(float x) { return order_key(x) >> kDrop; }
     __device__ __forceinline__ static float value(uint32_t key) {
         uint32_t b = key << kDrop;
@@ -302,152 +454,301 @@ struct Many {
     __device__ __forceinline__ static int shift(int level) { return kLevels == 2 ? 11 - 11 * level : 21 - 11 * level + (level == 2); }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kManyThreads) void many_sample_kernel(Draw d) {
-    using M = Many<T>;
-    constexpr int kVec = M::kVec, kStep = M::kStep;
-    __shared__ uint64_t bins[kBins];
+__device__ __forceinline__ uint64_t listed(uint32_t key, int32_t place) { return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)place); }
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void many_sample_kernel(Draw d) {
+    using M = Many<T, THREADS>;
+    constexpr int kVec = M::kVec, kStep = M::kStep, kWaves = THREADS / kWave;
+    __shared__ uint64_t bins[kBins * kCopies], list[kListed];
     __shared__ double mass[kChunks];
     __shared__ int32_t ties[kChunks];
-    __shared__ union { float f[kManyWaves]; uint64_t u[kManyWaves]; double d[kManyWaves]; int32_t i[kManyWaves]; } room;
-    __shared__ int odd_, found_bin;
+    __shared__ Block<THREADS> block;
+    __shared__ int odd_, found_at, counted_;
     __shared__ uint64_t found_above;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int64_t row = group_number();
     if (row >= d.rows) return;
     Rule rule = rule_of(d.set, row);
     if (rule.top_p == 0.0) rule.top_p = 1.0, rule.top_k = 1;       // (the best alone)
-    M a{(const T *)d.logits + row * d.ld, d.allow ? d.allow + row * d.words : nullptr, d.vocab, 0.0f, rule.scale};
     const int32_t V = d.vocab;
+    if (rule.top_k >= V) rule.top_k = 0;
+    M a{(const T *)d.logits + row * d.ld, d.allow ? d.allow + row * d.words : nullptr, V, 0.0f, rule.scale * kLog2eWide};
+    const auto draw_of = [&](int32_t g) { return (double)counted(d.u[row * d.u_row + g * d.u_step]); };
+    const auto put_logp = [&](int32_t g, float x, double logs) {
+        if (d.logp) d.logp[row * d.given + g] = (float)(((double)x - (double)a.m) * rule.scale - logs);
+    };
 
-    if (threadIdx.x == 0) odd_ = 0;
-    __syncthreads();
+    if (threadIdx.x == 0) odd_ = counted_ = 0;
     float m = -INFINITY;
     bool odd = false;
-    for (int64_t v = (int64_t)threadIdx.x * kVec; v < V; v += kManyThreads * kVec) {
-        float x[kVec];
-        a.load((int32_t)v, x);
-#pragma unroll
-        for (int i = 0; i < kVec; i++) odd |= !(x[i] < INFINITY), m = fmaxf(m, x[i]);
-    }
+    a.template each<4>([&](int32_t, float x) { odd |= !(x < INFINITY), m = fmaxf(m, x); });
+    const float own = m;
     m = most_of<kWave>(m);
-    if (lane == 0) room.f[wave] = m;
-    if (odd) odd_ = 1;
+    if (lane == 0) block.f[wave] = m;
     __syncthreads();
-    for (int w = 0; w < kManyWaves; w++) m = fmaxf(m, room.f[w]);
+    if (odd) odd_ = 1;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) m = fmaxf(m, block.f[w]);
     a.m = m;
+    __syncthreads();
     if (odd_ || m == -INFINITY || !rule.fine) {
         if (!rule.fine && threadIdx.x == 0) atomicOr(d.status, CP_STATUS_BAD_SAMPLING);
-        for (int32_t g = threadIdx.x; g < d.given; g += kManyThreads) {
+        for (int32_t g = threadIdx.x; g < d.given; g += THREADS) {
             put_token(d, row, g, -1);
             if (d.logp) d.logp[row * d.given + g] = 0.0f;
         }
         return;
     }
+    // adds a place to the list; true if there was room
+    const auto note = [&](float x, int32_t v) {
+        const int at = atomicAdd(&counted_, 1);
+        if (at < kListed) list[at] = listed(M::key(x), v);
+    };
+
+    // Few are left: they are listed, put in order, and all the rest is a matter of the list.  The bound that they are at or above is the least of what a
+    // few threads' own best places of each wavefront reach; a thread has few of a row's best.
+    if (rule.top_k > 0 && rule.top_k <= THREADS) {
+        const int share = (rule.top_k + kWaves - 1) / kWaves;
+        const uint32_t key = M::key(own);
+        uint32_t low = 0, high = M::key(m) + 1;
+        for (int n = 0; n < 32 && high - low > 1; n++) {
+            const uint32_t mid = low + (high - low) / 2;
+            if (__popcll(__ballot(key >= mid)) >= share) low = mid;
+            else high = mid;
+        }
+        if (lane == 0) block.i[wave] = (int32_t)(low ^ 0x80000000u);
+        __syncthreads();
+        int32_t least = block.i[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; w++) least = min(least, block.i[w]);
+        low = (uint32_t)least ^ 0x80000000u;
+        a.template each<4>([&](int32_t v, float x) {
+            if (M::key(x) >= low && x > -INFINITY) note(x, v);
+        });
+        __syncthreads();
+        const int count = counted_;
+        __syncthreads();
+        if (threadIdx.x == 0) counted_ = 0;
+        if (count <= kListed) {
+            put_in_order<THREADS>(list, count);
+            // by rank: shares, what lies in front, what is kept (the first ones)
+            const int n = min(count, rule.top_k), i = threadIdx.x;
+            const uint64_t one = i < n ? list[i] : 0;
+            const double p = i < n ? a.share(M::value((uint32_t)(one >> 32))) : 0.0;
+            double total;
+            const double ahead = block.before(p, total);
+            const bool keep = i < n && (i == 0 || rule.top_p >= 1.0 || ahead < rule.top_p * total) && p >= rule.min_p;
+            const int kept = __syncthreads_count(keep);
+            // and by place
+            if (keep) list[i] = (uint64_t)(uint32_t)one << 32 | (uint32_t)(one >> 32);
+            __syncthreads();
+            put_in_order<THREADS>(list, kept);
+            const double q = i < kept ? a.share(M::value((uint32_t)list[i])) : 0.0;
+            double all;
+            const double before = block.before(q, all);
+            if (i < kept) mass[i] = before + q;
+            __syncthreads();
+            for (int32_t g = threadIdx.x; g < d.given; g += THREADS) {
+                const double target = draw_of(g) * all;
+                int lo = 0, hi = kept - 1;
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (mass[mid] > target) hi = mid;
+                    else lo = mid + 1;
+                }
+                put_token(d, row, g, (int32_t)(0xffffffffu - (uint32_t)(list[lo] >> 32)));
+                put_logp(g, M::value((uint32_t)list[lo]), d.logp ? log(all) : 0.0);
+            }
+            return;
+        }
+    }
 
     // The place in the order where what is kept ends: keys above `key_end`, and `keep_ties` of those that equal it
     uint32_t key_end = 0;
     int64_t keep_ties = INT64_MAX;
-    // finds the bin, from the highest on, in which the weight reaches `want` (past what lies above the bins)
-    auto seek = [&](double want, uint64_t above) {
-        // (thread t has the t-th pair of bins from the top)
-        const int top = kBins - 1 - 2 * (int)threadIdx.x;
-        const uint64_t first = bins[top], second = bins[top - 1];
-        uint64_t total;
-        const uint64_t before = above + block_before<uint64_t>(first + second, room.u, total);
-        if (threadIdx.x == 0) found_bin = 0, found_above = above + total;      // (rounding: the lowest)
-        __syncthreads();
-        if ((double)before < want && !((double)(before + first + second) < want)) {
-            const bool one = !((double)(before + first) < want);
-            found_bin = one ? top : top - 1, found_above = one ? before : before + first;
-        }
-        __syncthreads();
-        return total;
-    };
-    auto clear = [&] {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kBins; i += kManyThreads) bins[i] = 0;
-        __syncthreads();
-    };
-    if (rule.top_k > 0 && rule.top_k < V) {
+    // mass in units so small that a sum of all places stays below 2^62: whole numbers, which add up the same in any order
+    const double unit = ldexp(1.0, 62 - (32 - __clz(V)));
+    const auto weight = [&](double p) { return (uint64_t)(p * unit + 0.5); };
+    if (rule.top_p < 1.0 && rule.top_k == 0) {
+        // By how far places lie below the best: 256 steps of a twelfth of a power of two, the step in which top_p is reached again in 256, and so on until the
+        // places of a step are few, which are listed and put in order.
+        constexpr int kDepth = 6;
+        __shared__ double from[kDepth + 1], per[kDepth + 1];
+        __shared__ int at[kDepth + 1];
         uint64_t above = 0;
-        uint32_t prefix = 0;
-        for (int level = 0; level < M::kLevels; level++) {
-            const int sh = M::shift(level), width = level == 2 ? 10 : 11;
-            clear();
-            for (int64_t v = (int64_t)threadIdx.x * kVec; v < V; v += kManyThreads * kVec) {
-                float x[kVec];
-                a.load((int32_t)v, x);
-#pragma unroll
-                for (int i = 0; i < kVec; i++) {
-                    const uint32_t k = M::key(x[i]);
-                    if (v + i < V && (level == 0 || k >> (sh + width) == prefix)) atomicAdd((unsigned int *)&bins[k >> sh & ((1u << width) - 1)], 1u);
-                }
-            }
-            __syncthreads();
-            seek((double)rule.top_k, above);
-            prefix = prefix << width | (uint32_t)found_bin, above = found_above;
-            __syncthreads();
-        }
-        key_end = prefix, keep_ties = (int64_t)rule.top_k - (int64_t)above;
-    }
-    if (rule.top_p < 1.0) {
-        // mass in units so small that a sum of all places stays below 2^62
-        const double unit = ldexp(1.0, 62 - (32 - __clz(V)));
-        const uint32_t least = key_end;
-        const int64_t least_ties = keep_ties;
-        uint64_t above = 0;
-        uint32_t prefix = 0;
         double want = 0;
-        for (int level = 0; level < M::kLevels; level++) {
-            const int sh = M::shift(level), width = level == 2 ? 10 : 11;
-            clear();
-            for (int64_t v = (int64_t)threadIdx.x * kVec; v < V; v += kManyThreads * kVec) {
-                float x[kVec];
-                a.load((int32_t)v, x);
-#pragma unroll
-                for (int i = 0; i < kVec; i++) {
-                    const uint32_t k = M::key(x[i]);
-                    // (of those that equal the last of the top_k, added below, only some are left)
-                    if (x[i] > -INFINITY && (k > least || least_ties == INT64_MAX) && (level == 0 || k >> (sh + width) == prefix))
-                        atomicAdd((unsigned long long *)&bins[k >> sh & ((1u << width) - 1)], (unsigned long long)(a.share(x[i]) * unit + 0.5));
+        if (threadIdx.x == 0) from[0] = 0, per[0] = 12.0;
+        const auto step_of = [&](double depth, int level) { return (int)fmin(fmax((depth - from[level]) * per[level], 0.0), kSteps - 1.0); };
+        const auto inside = [&](double depth, int level) {     // whether it lies in the step of all levels before this one
+            bool in = true;
+            for (int k = 0; k < level; k++) in &= step_of(depth, k) == at[k];
+            return in;
+        };
+        for (int level = 0; level < kDepth && keep_ties == INT64_MAX; level++) {
+            for (int i = threadIdx.x; i < kSteps * kLanes; i += THREADS) bins[i] = 0;
+            if (threadIdx.x == 0) counted_ = 0;
+            __syncthreads();
+            a.template each<2>([&](int32_t v, float x) {
+                const double depth = a.depth(x);
+                if (x > -INFINITY && inside(depth, level)) {
+                    atomicAdd((unsigned long long *)&bins[step_of(depth, level) * kLanes + lane % kLanes], (unsigned long long)weight(power_of_two(-depth)));
+                    if (level > 0) note(x, v);
                 }
+            });
+            __syncthreads();
+            // (thread t has steps 256 / THREADS t and on)
+            constexpr int kEach = THREADS < kSteps ? kSteps / THREADS : 1;
+            uint64_t sum = 0, one[kEach];
+#pragma unroll
+            for (int e = 0; e < kEach; e++) {
+                one[e] = 0;
+                const int step = (int)threadIdx.x * kEach + e;
+                if (step < kSteps)
+                    for (int k = 0; k < kLanes; k++) one[e] += bins[step * kLanes + k];
+                sum += one[e];
+            }
+            uint64_t total;
+            uint64_t front = above + block.before(sum, total);
+            if (level == 0) want = (double)total * rule.top_p;
+            if (threadIdx.x == 0) found_at = kSteps - 1, found_above = above + total;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kEach; e++) {
+                const int step = (int)threadIdx.x * kEach + e;
+                if (step < kSteps && (double)front < want && !((double)(front + one[e]) < want)) found_at = step, found_above = front;
+                front += one[e];
             }
             __syncthreads();
-            if (threadIdx.x == 0 && least_ties != INT64_MAX && (level == 0 || least >> (sh + width) == prefix))
-                bins[least >> sh & ((1u << width) - 1)] += (uint64_t)least_ties * (uint64_t)(a.share(M::value(least)) * unit + 0.5);
-            __syncthreads();
-            if (level == 0) {
-                uint64_t total = 0;
-                block_before<uint64_t>(bins[2 * threadIdx.x] + bins[2 * threadIdx.x + 1], room.u, total);
-                want = (double)total * rule.top_p;
+            const int step = found_at, count = level > 0 ? counted_ : INT_MAX;
+            above = found_above;
+            if (threadIdx.x == 0) {
+                at[level] = step;
+                from[level + 1] = from[level] + step / per[level];
+                per[level + 1] = step == kSteps - 1 && level == 0 ? kSteps / 1100.0 : per[level] * kSteps;
+                counted_ = 0;
             }
-            seek(want, above);
-            prefix = prefix << width | (uint32_t)found_bin, above = found_above;
             __syncthreads();
+            if (count > kListed) continue;
+            // those of the list that lie in the step
+            constexpr int kOwn = (kListed + THREADS - 1) / THREADS;
+            uint64_t mine[kOwn];
+#pragma unroll
+            for (int o = 0; o < kOwn; o++) mine[o] = (int)threadIdx.x + o * THREADS < count ? list[threadIdx.x + o * THREADS] : 0;
+            __syncthreads();
+#pragma unroll
+            for (int o = 0; o < kOwn; o++)
+                if (mine[o] && step_of(a.depth(M::value((uint32_t)(mine[o] >> 32))), level) == step) list[atomicAdd(&counted_, 1)] = mine[o];
+            __syncthreads();
+            const int few = counted_;
+            if (few == 0) continue;                    // (a rounding of `want`)
+            put_in_order<THREADS>(list, few);
+            int kept = 0;
+            for (int i0 = 0; i0 < few; i0 += THREADS) {
+                const int i = i0 + threadIdx.x;
+                const uint64_t w = i < few ? weight(a.share(M::value((uint32_t)(list[i] >> 32)))) : 0;
+                uint64_t all;
+                const uint64_t ahead = above + block.before(w, all);
+                kept += __syncthreads_count(i < few && (i == 0 || (double)ahead < want));
+                above += all;
+            }
+            key_end = (uint32_t)(list[kept - 1] >> 32);
+            keep_ties = 0;
+            for (int i0 = 0; i0 < kept; i0 += THREADS)
+                keep_ties += __syncthreads_count(i0 + (int)threadIdx.x < kept && (uint32_t)(list[min(i0 + (int)threadIdx.x, kListed - 1)] >> 32) == key_end);
         }
-        // places that equal the last one: as long as less than `want` lies in front of them, the first in any case
-        const uint64_t each = (uint64_t)(a.share(M::value(prefix)) * unit + 0.5);
-        int64_t more = V;
-        if (each > 0) {
-            more = max((int64_t)(((double)want - (double)above) / (double)each), (int64_t)0);
-            while (more > 0 && !((double)(above + (uint64_t)(more - 1) * each) < want)) more--;
-            while ((double)(above + (uint64_t)more * each) < want) more++;
+    }
+    if (keep_ties == INT64_MAX && (rule.top_k > 0 || rule.top_p < 1.0)) {
+        // Many, or all alike: by the digits of their keys, from the highest on, first as many as top_k, then as much as top_p
+        const auto bin = [&](int i) { return bins[i] + bins[kBins + i]; };
+        const auto seek = [&](double want, uint64_t above) {
+            // (thread t has the t-th few bins from the top)
+            constexpr int kEach = kBins / THREADS;
+            uint64_t one[kEach], sum = 0, total;
+#pragma unroll
+            for (int e = 0; e < kEach; e++) sum += one[e] = bin(kBins - 1 - kEach * (int)threadIdx.x - e);
+            uint64_t front = above + block.before(sum, total);
+            if (threadIdx.x == 0) found_at = 0, found_above = above + total;       // (rounding: the lowest)
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kEach; e++) {
+                if ((double)front < want && !((double)(front + one[e]) < want)) found_at = kBins - 1 - kEach * (int)threadIdx.x - e, found_above = front;
+                front += one[e];
+            }
+            __syncthreads();
+        };
+        const auto clear = [&] {
+            __syncthreads();
+            for (int i = threadIdx.x; i < kBins * kCopies; i += THREADS) bins[i] = 0;
+            __syncthreads();
+        };
+        if (rule.top_k > 0) {
+            uint64_t above = 0;
+            uint32_t prefix = 0;
+            for (int level = 0; level < M::kLevels; level++) {
+                const int sh = M::shift(level), width = level == 2 ? 10 : 11;
+                clear();
+                a.template each<2>([&](int32_t, float x) {
+                    const uint32_t k = M::key(x);
+                    if (level == 0 || k >> (sh + width) == prefix) atomicAdd((unsigned int *)&bins[lane % kCopies * kBins + (k >> sh & ((1u << width) - 1))], 1u);
+                });
+                __syncthreads();
+                seek((double)rule.top_k, above);
+                prefix = prefix << width | (uint32_t)found_at, above = found_above;
+            }
+            key_end = prefix, keep_ties = (int64_t)rule.top_k - (int64_t)above;
         }
-        more = max(more, (int64_t)(above == 0));
-        if (prefix == least) more = min(more, least_ties);
-        key_end = prefix, keep_ties = more;
+        if (rule.top_p < 1.0) {
+            const uint32_t least = key_end;
+            const int64_t least_ties = keep_ties;
+            uint64_t above = 0;
+            uint32_t prefix = 0;
+            double want = 0;
+            for (int level = 0; level < M::kLevels; level++) {
+                const int sh = M::shift(level), width = level == 2 ? 10 : 11;
+                clear();
+                a.template each<1>([&](int32_t, float x) {
+                    const uint32_t k = M::key(x);
+                    // (of those that equal the last of the top_k, added below, only some are left)
+                    if (x > -INFINITY && (k > least || least_ties == INT64_MAX) && (level == 0 || k >> (sh + width) == prefix))
+                        atomicAdd((unsigned long long *)&bins[lane % kCopies * kBins + (k >> sh & ((1u << width) - 1))], (unsigned long long)weight(a.share(x)));
+                });
+                __syncthreads();
+                if (threadIdx.x == 0 && least_ties != INT64_MAX && (level == 0 || least >> (sh + width) == prefix))
+                    bins[least >> sh & ((1u << width) - 1)] += (uint64_t)least_ties * weight(a.share(M::value(least)));
+                __syncthreads();
+                if (level == 0) {
+                    uint64_t sum = 0, total;
+                    for (int i = threadIdx.x; i < kBins; i += THREADS) sum += bin(i);
+                    block.before(sum, total);
+                    want = (double)total * rule.top_p;
+                }
+                seek(want, above);
+                prefix = prefix << width | (uint32_t)found_at, above = found_above;
+            }
+            // places that equal the last one: as long as less than `want` lies in front of them, the first in any case
+            const uint64_t each = weight(a.share(M::value(prefix)));
+            int64_t more = V;
+            if (each > 0) {
+                more = max((int64_t)((want - (double)above) / (double)each), (int64_t)0);
+                while (more > 0 && !((double)(above + (uint64_t)(more - 1) * each) < want)) more--;
+                while ((double)(above + (uint64_t)more * each) < want) more++;
+            }
+            more = max(more, (int64_t)(above == 0));
+            if (prefix == least) more = min(more, least_ties);
+            key_end = prefix, keep_ties = more;
+        }
     }
     // what equals the last one and is less likely than min_p goes too
     const double end_share = keep_ties == INT64_MAX ? 0.0 : a.share(M::value(key_end));
     if (keep_ties != INT64_MAX && end_share < rule.min_p) keep_ties = 0;
     const bool cut = keep_ties != INT64_MAX;
 
-    // The row in chunks, one after the other, a wavefront each: mass above the end, and how many equal it
+    // The row in chunks, one after the other: mass above the end, and how many equal it
     const int32_t steps = (int32_t)(((int64_t)V + (int64_t)kStep * kChunks - 1) / ((int64_t)kStep * kChunks));       // of a chunk
     const int64_t size = (int64_t)steps * kStep;
     const int32_t chunks = (int32_t)((V + size - 1) / size);
-    auto kept = [&](float x, bool &tie) {
+    const auto kept = [&](float x, bool &tie) {
         tie = false;
         if (x == -INFINITY) return 0.0;
         if (cut) {
@@ -458,45 +759,62 @@ __global__ __launch_bounds__(kManyThreads) void many_sample_kernel(Draw d) {
         const double p = a.share(x);
         return p < rule.min_p ? 0.0 : p;
     };
-    for (int32_t c = wave; c < chunks; c += kManyWaves) {
-        double sum = 0;
-        int32_t same = 0;
+    constexpr int kAtOnce = 2;                         // chunks of a wavefront under way at once
+    for (int32_t first = wave * kAtOnce; first < chunks; first += kWaves * kAtOnce) {
+        double sum[kAtOnce] = {};
+        int32_t same[kAtOnce] = {};
         for (int32_t s = 0; s < steps; s++) {
-            const int64_t v = c * size + s * kStep + lane * kVec;
-            if (v >= V) break;
-            float x[kVec];
-            a.load((int32_t)v, x);
+            float x[kAtOnce][kVec];
 #pragma unroll
-            for (int i = 0; i < kVec; i++) {
-                bool tie;
-                sum += kept(x[i], tie);
-                same += tie;
-            }
+            for (int q = 0; q < kAtOnce; q++) a.load((int32_t)min((first + q) * size + s * kStep + lane * kVec, (int64_t)V), x[q]);
+#pragma unroll
+            for (int q = 0; q < kAtOnce; q++)
+#pragma unroll
+                for (int i = 0; i < kVec; i++) {
+                    bool tie;
+                    sum[q] += kept(x[q][i], tie);
+                    same[q] += tie;
+                }
         }
-        sum = sum_of<kWave>(sum);
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) same += __shfl_xor(same, off);
-        if (lane == 0) mass[c] = sum, ties[c] = same;
+        for (int q = 0; q < kAtOnce; q++) {
+            sum[q] = sum_of<kWave>(sum[q]);
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) same[q] += __shfl_xor(same[q], off);
+            if (lane == 0 && first + q < chunks) mass[first + q] = sum[q], ties[first + q] = same[q];
+        }
     }
     __syncthreads();
-    // of the ties, the first ones by place
-    const int32_t c0 = 2 * threadIdx.x, c1 = c0 + 1;
-    int32_t t0 = c0 < chunks ? ties[c0] : 0, t1 = c1 < chunks ? ties[c1] : 0, all_ties;
-    const int32_t ties_before = block_before<int32_t>(t0 + t1, room.i, all_ties);
-    double m0 = c0 < chunks ? mass[c0] : 0, m1 = c1 < chunks ? mass[c1] : 0;
-    if (cut) {
-        m0 += (double)max(min((int64_t)t0, keep_ties - ties_before), (int64_t)0) * end_share;
-        m1 += (double)max(min((int64_t)t1, keep_ties - ties_before - t0), (int64_t)0) * end_share;
+    // masses up to and with each chunk, and ties in front of it, of which the first ones by place are kept
+    double total = 0;
+    {
+        constexpr int kEach = kChunks / THREADS;
+        const int32_t c0 = kEach * threadIdx.x;
+        int32_t own_ties[kEach], sum_ties = 0, all_ties;
+        double own_mass[kEach], sum_mass = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; e++) sum_ties += own_ties[e] = c0 + e < chunks ? ties[c0 + e] : 0;
+        int64_t front = block.before(sum_ties, all_ties);
+#pragma unroll
+        for (int e = 0; e < kEach; e++) {
+            own_mass[e] = c0 + e < chunks ? mass[c0 + e] : 0;
+            if (cut) own_mass[e] += (double)max(min((int64_t)own_ties[e], keep_ties - front), (int64_t)0) * end_share;
+            if (c0 + e < chunks) ties[c0 + e] = (int32_t)front;
+            front += own_ties[e];
+            sum_mass += own_mass[e];
+        }
+        double upto = block.before(sum_mass, total);
+#pragma unroll
+        for (int e = 0; e < kEach; e++) {
+            upto += own_mass[e];
+            if (c0 + e < chunks) mass[c0 + e] = upto;
+        }
     }
-    double total;
-    const double mass_before = block_before<double>(m0 + m1, room.d, total);
-    if (c0 < chunks) mass[c0] = mass_before + m0, ties[c0] = ties_before;
-    if (c1 < chunks) mass[c1] = mass_before + m0 + m1, ties[c1] = ties_before + t0;
     __syncthreads();
     const double logs = d.logp ? log(total) : 0.0;
 
-    for (int32_t g = wave; g < d.given; g += kManyWaves) {
-        const double target = (double)number(d, row, g) * total;
+    for (int32_t g = wave; g < d.given; g += kWaves) {
+        const double target = draw_of(g) * total;
         int32_t lo = 0, hi = chunks - 1;     // the first chunk that reaches beyond, or the last
         while (lo < hi) {
             const int32_t mid = (lo + hi) / 2;
@@ -543,14 +861,12 @@ __global__ __launch_bounds__(kManyThreads) void many_sample_kernel(Draw d) {
                 const double upto = sum_upto<kWave>(sum, lane);
                 const uint64_t beyond = __ballot(before + upto > target && sum > 0);
                 if (beyond) {
-                    double at = before + (upto - sum);
+                    double here = before + upto;
 #pragma unroll
                     for (int i = kVec - 1; i >= 0; i--) {
-                        // (from the back: the first place that reaches beyond is the last one seen)
-                        double here = at;
-#pragma unroll
-                        for (int k = 0; k <= i; k++) here += p[k];
+                        // (from the back: the first place that reaches beyond is the last one seen; the lane's last place in any case)
                         if (p[i] > 0 && here > target) hit = (int32_t)v + i;
+                        here -= p[i];
                     }
                     token = __shfl(hit, __ffsll((unsigned long long)beyond) - 1);
                 }
@@ -564,10 +880,7 @@ __global__ __launch_bounds__(kManyThreads) void many_sample_kernel(Draw d) {
         }
         if (lane == 0) {
             put_token(d, row, g, token);
-            if (d.logp) {
-                const float x = (float)((const T *)d.logits)[row * d.ld + max(token, 0)];
-                d.logp[row * d.given + g] = (float)(((double)x - (double)m) * rule.scale - logs);
-            }
+            put_logp(g, (float)a.row[max(token, 0)], logs);
         }
     }
 }
@@ -629,17 +942,22 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         if (vocab > kFew) {
-            hipLaunchKernelGGL(many_sample_kernel<T>, grid_of(rows), dim3(kManyThreads), 0, st, d);
+            // (a workgroup as large as has work for its threads: 2048 x 4000 bf16 85 us of 1,024 threads)
+            if (vocab <= 8192) hipLaunchKernelGGL((many_sample_kernel<T, 256>), grid_of(rows), dim3(256), 0, st, d);
+            else hipLaunchKernelGGL((many_sample_kernel<T, 1024>), grid_of(rows), dim3(1024), 0, st, d);
             return launched();
         }
         auto go = [&](auto l) {
             constexpr int L = decltype(l)::value;
-            hipLaunchKernelGGL((few_sample_kernel<T, L>), grid_of((rows + kFewThreads / L - 1) / (kFewThreads / L)), dim3(kFewThreads), 0, st, d);
+            auto *kernel = token_type == CP_TOKEN_U8    ? few_sample_kernel<T, L, uint8_t>
+                           : token_type == CP_TOKEN_I32 ? few_sample_kernel<T, L, int32_t>
+                                                        : few_sample_kernel<T, L, int64_t>;
+            hipLaunchKernelGGL(kernel, grid_of((rows + kFewThreads / L - 1) / (kFewThreads / L)), dim3(kFewThreads), 0, st, d);
             return launched();
         };
-        if (vocab <= 8 && given <= 32) return go(std::integral_constant<int, 8>{});
-        if (vocab <= 16 && given <= 64) return go(std::integral_constant<int, 16>{});
-        if (vocab <= 32 && given <= 128) return go(std::integral_constant<int, 32>{});
+        if (vocab <= 8) return go(std::integral_constant<int, 8>{});
+        if (vocab <= 16) return go(std::integral_constant<int, 16>{});
+        if (vocab <= 32) return go(std::integral_constant<int, 32>{});
         return go(std::integral_constant<int, 64>{});
     });
 }
