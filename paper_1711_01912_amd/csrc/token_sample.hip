@@ -186,12 +186,12 @@ __device__ __forceinline__ void draw_row(const Draw &d, int64_t row, const float
     else draw_more<TT, 0>(d, row, edge, lp, none, first, side);
 }
 
-// L lanes a row, places 4 lane .. 4 lane + 3 of each where there are more than L, else one each.  A row's borders, cumulated
+// L lanes a row, PER neighbouring places each at most.  A row's borders, cumulated
 // shares of its mass, are rounded up to floats: u, a float, is below one just if it is below the other.  A draw then is the number of borders
 // that are not above u.
-template <typename T, int L, typename TT>
+template <typename T, int L, int PER, typename TT>
 __global__ __launch_bounds__(kFewThreads) void few_sample_kernel(Draw d) {
-    constexpr int kRowsHere = kFewThreads / L, kPer = L == 64 ? 4 : 1, kRoom = L * kPer;
+    constexpr int kRowsHere = kFewThreads / L, kPer = PER, kRoom = L * kPer;
     __shared__ float border[kRowsHere][kRoom + 1], lp[kRowsHere][kRoom + 1], xs[kRowsHere][kRoom + 1];
     __shared__ double ps[kRowsHere][kRoom];
     __shared__ bool empty[kRowsHere];
@@ -457,7 +457,7 @@ struct Many {
 __device__ __forceinline__ uint64_t listed(uint32_t key, int32_t place) { return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)place); }
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void many_sample_kernel(Draw d) {
+__global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_kernel(Draw d) {
     using M = Many<T, THREADS>;
     constexpr int kVec = M::kVec, kStep = M::kStep, kWaves = THREADS / kWave;
     __shared__ uint64_t bins[kBins * kCopies], list[kListed];
@@ -942,23 +942,27 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         if (vocab > kFew) {
-            // (a workgroup as large as has work for its threads: 2048 x 4000 bf16 85 us of 1,024 threads)
+            // A workgroup as large as has work for its threads (2048 x 4000 bf16 46 us, 85 of 1,024 threads), two a compute unit where there are more rows than
+            // compute units.
             if (vocab <= 8192) hipLaunchKernelGGL((many_sample_kernel<T, 256>), grid_of(rows), dim3(256), 0, st, d);
+            else if (rows > 256) hipLaunchKernelGGL((many_sample_kernel<T, 512>), grid_of(rows), dim3(512), 0, st, d);
             else hipLaunchKernelGGL((many_sample_kernel<T, 1024>), grid_of(rows), dim3(1024), 0, st, d);
             return launched();
         }
-        auto go = [&](auto l) {
-            constexpr int L = decltype(l)::value;
-            auto *kernel = token_type == CP_TOKEN_U8    ? few_sample_kernel<T, L, uint8_t>
-                           : token_type == CP_TOKEN_I32 ? few_sample_kernel<T, L, int32_t>
-                                                        : few_sample_kernel<T, L, int64_t>;
+        auto go = [&](auto l, auto each) {
+            constexpr int L = decltype(l)::value, PER = decltype(each)::value;
+            auto *kernel = token_type == CP_TOKEN_U8    ? few_sample_kernel<T, L, PER, uint8_t>
+                           : token_type == CP_TOKEN_I32 ? few_sample_kernel<T, L, PER, int32_t>
+                                                        : few_sample_kernel<T, L, PER, int64_t>;
             hipLaunchKernelGGL(kernel, grid_of((rows + kFewThreads / L - 1) / (kFewThreads / L)), dim3(kFewThreads), 0, st, d);
             return launched();
         };
-        if (vocab <= 8) return go(std::integral_constant<int, 8>{});
-        if (vocab <= 16) return go(std::integral_constant<int, 16>{});
-        if (vocab <= 32) return go(std::integral_constant<int, 32>{});
-        return go(std::integral_constant<int, 64>{});
+        const std::integral_constant<int, 1> one;
+        if (vocab <= 8) return go(std::integral_constant<int, 8>{}, one);
+        if (vocab <= 16) return go(std::integral_constant<int, 16>{}, one);
+        if (vocab <= 32) return go(std::integral_constant<int, 32>{}, one);
+        if (vocab <= 64) return go(std::integral_constant<int, 64>{}, one);
+        return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
     });
 }
 
