@@ -1,6 +1,6 @@
 """A placement policy that is trained by the critical-path times of the partitions it draws.
 
-    python examples/learn_placement.py --workload inception --steps 100
+    python examples/learn_placement.py --workload inception --steps 100 [--layer attention]
 
 The vertices of a data-flow graph are read in topological order.  Each block of the policy is
 
@@ -8,10 +8,16 @@ The vertices of a data-flow graph are read in topological order.  Each block of 
     f, v, gate = slices of z @ W       one product of the library
     y  = recurrence(f, v) @ U          a vertex sees those before it               (recurrence)
 
+or, with ``--layer attention``, with a matrix a head as the state of a sequence,
+
+    q, k, v, gate = slices of z @ W
+    y  = linear_attention(q, k, v) @ U     a decay for each head                   (linear_attention)
+
 and the head gives every vertex a row of logits over the devices.  A step draws partitions from the rows,
 ``cp_eval`` rates them, and the log probabilities of what was drawn (token_logprobs), weighted by the ratings
 and with the rows' entropy added, are the loss.  ``place`` runs the trained policy vertex by vertex
-(cp_recurrence_step), as a program does that places a graph while it is being built.
+(cp_recurrence_step), as a program does that places a graph while it is being built; ``AttentionPolicy.step``
+and ``draw_tokens`` (cp_linear_attention_step, cp_token_sample) do so for many partitions at once.
 """
 from __future__ import annotations
 
@@ -73,6 +79,9 @@ class Policy(torch.nn.Module):
             return norm_gate(x, w_pre=self.w_pre[0], z_dtype=self.dtype)
         return norm_gate(x, y, gate, w_pre=self.w_pre[i], w_post=self.w_post[i - 1], gate_act="silu", scale=0.5)
 
+    def states(self, sequences, device):
+        return torch.zeros(self.blocks, sequences, self.width, device=device)
+
     @torch.no_grad()
     def step(self, inputs, states):
         """Logits [sequences][devices] of one more vertex of each sequence; ``states``: float32 [blocks][sequences][width],
@@ -90,6 +99,57 @@ class Policy(torch.nn.Module):
         return self._joint(joint, self.blocks, x, y, gate)[1] @ self.head
 
 
+class AttentionPolicy(Policy):
+    """The same with linear attention as the sequence layer."""
+
+    def __init__(self, devices, width=128, blocks=2, dtype=torch.bfloat16, inputs=6, seed=0, heads=4):
+        super().__init__(devices, width, blocks, dtype, inputs, seed)
+        g = torch.Generator().manual_seed(seed + 1)
+        self.heads = heads
+        self.into = torch.nn.ParameterList(torch.nn.Parameter((torch.randn(width, 4 * width, generator=g) / width ** 0.5).to(dtype))
+                                           for _ in range(blocks))
+        # heads that look from two vertices to a few hundred back
+        self.bias = torch.nn.ParameterList(torch.nn.Parameter(torch.linspace(-0.7, -5.5, heads)) for _ in range(blocks))
+
+    def forward(self, inputs):
+        x, y, gate = (inputs.to(self.dtype) @ self.embed).float(), None, None
+        for i in range(self.blocks):
+            x, z = self._joint(autograd.norm_gate, i, x, y, gate)
+            q, k, v, gate = self._slices(z, i)
+            o, _ = autograd.linear_attention(q, k, v, -torch.exp(self.bias[i]), scale=q.shape[-1] ** -0.5)
+            y = o.flatten(1) @ self.back[i]
+        return self._joint(autograd.norm_gate, self.blocks, x, y, gate)[1] @ self.head
+
+    def _slices(self, z, i):
+        *heads, gate = (z @ self.into[i]).split(self.width, 1)
+        return *(t.unflatten(1, (self.heads, -1)) for t in heads), gate
+
+    def states(self, sequences, device):
+        each = self.width // self.heads
+        return torch.zeros(self.blocks, sequences, self.heads, each, each, device=device)
+
+    @torch.no_grad()
+    def step(self, inputs, states):
+        """Logits [sequences][devices] of one more vertex of each sequence; ``states`` are updated in place."""
+        def joint(x, y=None, gate=None, **kw):
+            out = cpe.cp_norm_gate(x, y, gate, **kw)
+            return out.get("r", x), out["z"]
+
+        x, y, gate = (inputs.to(self.dtype) @ self.embed).float(), None, None
+        for i in range(self.blocks):
+            x, z = self._joint(joint, i, x, y, gate)
+            q, k, v, gate = self._slices(z, i)
+            o = cpe.cp_linear_attention_step(q, k, v, states[i], -torch.exp(self.bias[i]), scale=q.shape[-1] ** -0.5, check_status=False)["o"]
+            y = o.flatten(1) @ self.back[i]
+        return self._joint(joint, self.blocks, x, y, gate)[1] @ self.head
+
+
+def draw_tokens(logits, partitions, generator=None, **filters):
+    """uint8 [n][partitions], drawn by cp_token_sample"""
+    u = torch.rand(logits.shape[0], partitions, device=logits.device, generator=generator)
+    return cpe.cp_token_sample(logits, u, dtype=torch.uint8, check_status=False, **filters)["tokens"]
+
+
 def draw(logits, partitions, generator=None):
     """uint8 [n][partitions]"""
     return torch.multinomial(logits.float().softmax(-1), partitions, replacement=True, generator=generator).to(torch.uint8)
@@ -103,19 +163,19 @@ def rate(graph, w, order, tokens):
     return out["cp"].double()
 
 
-def train(w, steps=100, partitions=256, width=128, blocks=2, lr=3e-3, dtype=torch.bfloat16, seed=0, say=None):
+def train(w, steps=100, partitions=256, width=128, blocks=2, lr=3e-3, dtype=torch.bfloat16, seed=0, say=None, layer="recurrence"):
     """(policy, mean critical-path time of each step's partitions, best partition's time)"""
     device = torch.device("cuda:0")
     graph = cpe.CpGraph.from_workload(w, device="cuda:0")
     inputs, order = (t.to(device) for t in features(w))
-    policy = Policy(w.k, width, blocks, dtype, seed=seed).to(device)
+    policy = (AttentionPolicy if layer == "attention" else Policy)(w.k, width, blocks, dtype, seed=seed).to(device)
     generator = torch.Generator(device=device)
     generator.manual_seed(seed)
     optimizer = torch.optim.Adam(policy.parameters(), lr=lr)
     history, best = [], float("inf")
     for step in range(steps):
         logits = policy(inputs)
-        tokens = draw(logits.detach(), partitions, generator)
+        tokens = (draw_tokens if layer == "attention" else draw)(logits.detach(), partitions, generator)
         cp = rate(graph, w, order, tokens)
         gain = ((cp.mean() - cp) / (cp.std() + 1e-9)).float()
         logp, entropy = autograd.token_logprobs(logits, tokens)
@@ -134,7 +194,7 @@ def place(policy, w):
     """The policy's most likely device of every vertex, uint8 [n], vertex by vertex."""
     device = policy.head.device
     inputs, order = (t.to(device) for t in features(w))
-    states = torch.zeros(policy.blocks, 1, policy.width, device=device)
+    states = policy.states(1, device)
     found = torch.empty(w.n, dtype=torch.uint8, device=device)
     for t in range(w.n):
         logits = policy.step(inputs[t:t + 1], states)
@@ -150,9 +210,10 @@ def main():
     ap.add_argument("--workload", default="inception", choices=CONFIG_NAMES)
     ap.add_argument("--steps", type=int, default=100)
     ap.add_argument("--partitions", type=int, default=256)
+    ap.add_argument("--layer", default="recurrence", choices=("recurrence", "attention"))
     args = ap.parse_args()
     w = make_workload(args.workload)
-    policy, _, best = train(w, args.steps, args.partitions, say=print)
+    policy, _, best = train(w, args.steps, args.partitions, say=print, layer=args.layer)
     if w.n <= 10000:
         tokens = place(policy, w)
         graph = cpe.CpGraph.from_workload(w, device="cuda:0")

@@ -1,7 +1,7 @@
 """The operators of a learned placement policy as differentiable functions of torch tensors.
 
-``recurrence``, ``norm_gate`` and ``token_logprobs`` call the forward entry points of ``policy`` and, when a
-gradient is asked for, the backward ones; what these need is kept by the graph as usual.  Everything runs on the
+``recurrence``, ``norm_gate``, ``token_logprobs`` and ``linear_attention`` call the forward entry points of ``policy`` and
+``attention`` and, when a gradient is asked for, the backward ones; what these need is kept by the graph as usual.  Everything runs on the
 current stream.  Pointers and tokens are told to be bad by ``policy``'s own calls with ``check_status``; here
 nothing is synchronised, and so the functions may be captured into a HIP graph.  (A backward pass is captured
 while no eager graph of the same leaves is alive: torch would join the capture with the stream that such a graph
@@ -12,7 +12,7 @@ from __future__ import annotations
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import policy
+from . import attention, policy
 
 
 def _rows(grad, like):
@@ -95,3 +95,31 @@ class _TokenLogprobs(torch.autograd.Function):
 def token_logprobs(logits, tokens, *, scale=1.0, allow=None):
     """(logp, entropy) of policy.cp_token_logprobs, differentiable in the logits."""
     return _TokenLogprobs.apply(logits, tokens, allow, scale)
+
+
+class _LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, h0, scale, seq_ptr, reverse):
+        kw = dict(scale=scale, h0=h0, seq_ptr=seq_ptr, reverse=reverse, check_status=False)
+        # (rows behind the last sequence are left alone, so they have to be something before)
+        out = None if seq_ptr is None else {"o": q.new_zeros(*q.shape[:-1], v.shape[-1])}
+        out = attention.cp_linear_attention(q, k, v, log_decay, want_last=True, want_carry=any(ctx.needs_input_grad), out=out, **kw)
+        ctx.save_for_backward(q, k, v, log_decay, h0, seq_ptr, out.get("carry"))
+        ctx.options = dict(scale=scale, reverse=reverse)
+        ctx.set_materialize_grads(False)
+        return out["o"], out["last"]
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, do, dlast):
+        q, k, v, log_decay, h0, seq_ptr, carry = ctx.saved_tensors
+        do = q.new_zeros(*q.shape[:-1], v.shape[-1]) if do is None else do.contiguous()
+        out = None if seq_ptr is None else {"d" + n: torch.zeros_like(t, memory_format=torch.contiguous_format) for n, t in zip("qkv", (q, k, v))}
+        out = attention.cp_linear_attention_backward(do, q, k, v, log_decay, carry, dlast=None if dlast is None else dlast.contiguous(),
+                                                     h0=h0, seq_ptr=seq_ptr, check_status=False, out=out, **ctx.options)
+        return out["dq"], out["dk"], out["dv"], out.get("dlog_decay"), out.get("dh0"), None, None, None
+
+
+def linear_attention(q, k, v, log_decay=None, *, scale=1.0, h0=None, seq_ptr=None, reverse=False):
+    """(o, last) of attention.cp_linear_attention, differentiable in q, k, v, log_decay and h0."""
+    return _LinearAttention.apply(q, k, v, log_decay, h0, scale, seq_ptr, reverse)

@@ -482,24 +482,32 @@ __global__ __launch_bounds__(kThreads) void check_kernel(const int32_t *ptr, int
 __global__ __launch_bounds__(kThreads) void empty_kernel(const int32_t *ptr, int64_t len, int32_t num_seq, int64_t state, const float *from, float *to) {
     for (int64_t s = blockIdx.x; s < num_seq; s += gridDim.x) {
         if (ptr ? ptr[s + 1] > ptr[s] : len > 0) continue;
-        for (int64_t i = threadIdx.x; i < state; i += kThreads) to[s * state + i] = from ? from[s * state + i] : 0.0f;
+        for (int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x; i < state; i += (int64_t)gridDim.y * kThreads)
+            to[s * state + i] = from ? from[s * state + i] : 0.0f;
     }
 }
 
-// Gradients of a head's keys or values from those of the heads that share it, in their order
-template <typename T>
+// Gradients of a head's keys or values from those of the heads that share it, in their order; V neighbouring values a thread
+template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void share_kernel(const float *part, const int32_t *ptr, int32_t num_seq, int64_t rows, int32_t heads, int32_t group,
                                                          int32_t width, T *to, int64_t ld, int64_t hd) {
     const int64_t total = ptr ? min((int64_t)max(ptr[num_seq], 0), rows) : rows;
-    const int32_t kv = heads / group, line = kv * width;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total * line; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t row = i / line;
-        const int32_t h = (int32_t)(i % line) / width, c = (int32_t)(i % line) % width;
-        const float *from = part + (row * heads + (int64_t)h * group) * width + c;
-        float sum = 0;
-        for (int32_t k = 0; k < group; k++) sum += from[(int64_t)k * width];
-        to[row * ld + h * hd + c] = (T)sum;
-    }
+    const int32_t line = heads / group * width / V;
+    for (int64_t row = blockIdx.x; row < total; row += gridDim.x)
+        for (int32_t i = threadIdx.x; i < line; i += kThreads) {
+            const int32_t h = i * V / width, c = i * V % width;
+            const float *from = part + (row * heads + (int64_t)h * group) * width + c;
+            Pack<float, V> sum = load_pack<float, V>(from);
+            for (int32_t k = 1; k < group; k++) {
+                const Pack<float, V> one = load_pack<float, V>(from + (int64_t)k * width);
+#pragma unroll
+                for (int e = 0; e < V; e++) sum.v[e] += one.v[e];
+            }
+            Pack<T, V> put;
+#pragma unroll
+            for (int e = 0; e < V; e++) put.v[e] = (T)sum.v[e];
+            store_pack<T, V>(to + row * ld + h * hd + c, put);
+        }
 }
 
 __global__ __launch_bounds__(kThreads) void decay_kernel(const double *part, int64_t each, float *to) {
@@ -722,6 +730,37 @@ Extent extent(const Heads &m, int64_t rows, int type) {
     return {m.at, 1, all, all, (size_t)each};
 }
 
+// Whether two such share any byte: exactly where their rows are equally far apart, and their heads (slices of one buffer)
+bool meet(const Heads &a, const Heads &b, int64_t rows, int type) {
+    if (!a.at || !b.at || rows < 1) return false;
+    const int64_t each = (int64_t)type_bytes(type);
+    const bool alike = (rows == 1 || a.ld == b.ld) && (a.heads == 1 || b.heads == 1 || a.hd == b.hd);
+    if (!alike || (rows > 1 && a.ld == 0)) return share(extent(a, rows, type), extent(b, rows, type));
+    const int64_t ld = rows > 1 ? a.ld * each : 1, hd = (a.heads > 1 ? a.hd : b.hd) * each, apart = (int64_t)(uintptr_t)b.at - (int64_t)(uintptr_t)a.at;
+    for (int64_t h = 1 - (int64_t)b.heads; h < a.heads; h++) {
+        // one of b's heads lies `off` bytes behind one of a's in a row, and `rows` rows on by multiples of ld
+        const int64_t off = apart - h * hd;
+        for (int64_t r = -off / ld - 1; r <= -off / ld + 1; r++)
+            if (r > -rows && r < rows && off + r * ld < a.width * each && off + r * ld > -b.width * each) return true;
+    }
+    return false;
+}
+// Whether a result shares memory with another result or with an input, rows of heads or others
+bool in_the_way(std::initializer_list<Heads> in, std::initializer_list<Heads> out, std::initializer_list<Extent> more_in, std::initializer_list<Extent> more_out,
+                int64_t rows, int type) {
+    if (cpeval::in_the_way(more_in, more_out)) return true;
+    for (const Heads *o = out.begin(); o != out.end(); o++) {
+        for (const Heads &i : in)
+            if (meet(i, *o, rows, type)) return true;
+        for (const Heads *p = out.begin(); p != o; p++)
+            if (meet(*p, *o, rows, type)) return true;
+        if (cpeval::in_the_way(more_in, {extent(*o, rows, type)}) || cpeval::in_the_way(more_out, {extent(*o, rows, type)})) return true;
+    }
+    for (const Heads &i : in)
+        if (cpeval::in_the_way({extent(i, rows, type)}, more_out)) return true;
+    return false;
+}
+
 }  // namespace
 }  // namespace attention
 }  // namespace cpeval
@@ -771,15 +810,15 @@ int cp_linear_attention(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, i
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
     }
     const auto states = [&](const void *at) { return vector_at(at, (int64_t)num_seq * state_floats(s)); };
-    if (in_the_way({extent(mq, rows, type), extent(mk, rows, type), extent(mv, rows, type), vector_at(log_decay, heads), states(h0),
-                    vector_at(seq_ptr, (int64_t)num_seq + 1, sizeof(int32_t))},
-                   {extent(mo, rows, type), states(last), vector_at(c.split ? carry : nullptr, c.segments * (int64_t)state_floats(s)),
-                    vector_at(seq_ptr ? status_out : nullptr, 1, sizeof(int32_t)), vector_at(need ? workspace : nullptr, (int64_t)need, 1)}))
+    if (attention::in_the_way({mq, mk, mv}, {mo}, {vector_at(log_decay, heads), states(h0), vector_at(seq_ptr, (int64_t)num_seq + 1, sizeof(int32_t))},
+                              {states(last), vector_at(c.split ? carry : nullptr, c.segments * (int64_t)state_floats(s)),
+                               vector_at(seq_ptr ? status_out : nullptr, 1, sizeof(int32_t)), vector_at(need ? workspace : nullptr, (int64_t)need, 1)},
+                              rows, type))
         return CP_ERR_ARG;
     const hipStream_t st = (hipStream_t)stream;
     if (seq_ptr) hipLaunchKernelGGL(check_kernel, dim3(1), dim3(kThreads), 0, st, seq_ptr, num_seq, rows, status_out);
     if (last && (seq_ptr || rows == 0))
-        hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096)), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
+        hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096), 32), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
                            (int64_t)state_floats(s), h0, last);
     if (rows == 0) return launched();
     Pass p{};
@@ -821,17 +860,18 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
     }
     const auto states = [&](const void *at) { return vector_at(at, (int64_t)num_seq * state_floats(s)); };
-    const auto at = [&](const Heads &m) { return extent(m, rows, type); };
-    if (in_the_way({at(mo), at(mq), at(mk), at(mv), vector_at(log_decay, heads), states(h0), states(dlast),
-                    vector_at(c.split ? carry : nullptr, c.segments * (int64_t)state_floats(s)),
-                    vector_at(seq_ptr, (int64_t)num_seq + 1, sizeof(int32_t))},
-                   {at(nq), at(nk), at(nv), vector_at(dlog_decay, heads), states(dh0), vector_at(seq_ptr ? status_out : nullptr, 1, sizeof(int32_t)),
-                    vector_at(rows > 0 || dlog_decay ? workspace : nullptr, (int64_t)need, 1)}))
+    const bool works = rows > 0 || dlog_decay;
+    if (attention::in_the_way({mo, mq, mk, mv}, {nq, nk, nv},
+                              {vector_at(log_decay, heads), states(h0), states(dlast), vector_at(c.split ? carry : nullptr, c.segments * (int64_t)state_floats(s)),
+                               vector_at(seq_ptr, (int64_t)num_seq + 1, sizeof(int32_t))},
+                              {vector_at(dlog_decay, heads), states(dh0), vector_at(seq_ptr ? status_out : nullptr, 1, sizeof(int32_t)),
+                               vector_at(works ? workspace : nullptr, (int64_t)need, 1)},
+                              rows, type))
         return CP_ERR_ARG;
     const hipStream_t st = (hipStream_t)stream;
     if (seq_ptr) hipLaunchKernelGGL(check_kernel, dim3(1), dim3(kThreads), 0, st, seq_ptr, num_seq, rows, status_out);
     if (dh0 && (seq_ptr || rows == 0))
-        hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096)), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
+        hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096), 32), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
                            (int64_t)state_floats(s), dlast, dh0);
     char *room = (char *)workspace;
     float *gain = (float *)room, *denter = (float *)(room + gain_bytes(s, c));
@@ -866,11 +906,10 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
         pass.o = share, pass.hdo = pass.wb, pass.ldo = (int64_t)heads * pass.wb, pass.wide = true;
         const int code = run(kind, type, pass, nullptr, nullptr, st);
         if (code) return code;
-        const int64_t blocks = (rows * kv_heads * pass.wb + kThreads - 1) / kThreads;
         return by_type(type, [&](auto t) {
             using T = decltype(t);
-            hipLaunchKernelGGL(share_kernel<T>, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(kThreads), 0, st, share, seq_ptr, num_seq, rows, heads,
-                               group, pass.wb, (T *)to, ld, hd);
+            hipLaunchKernelGGL((pass.wb % 4 == 0 ? share_kernel<T, 4> : share_kernel<T, 1>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(kThreads), 0, st,
+                               share, seq_ptr, num_seq, rows, heads, group, pass.wb, (T *)to, ld, hd);
             return launched();
         });
     };
@@ -908,10 +947,8 @@ int cp_linear_attention_step(int32_t num_seq, int32_t heads, int32_t kv_heads, i
     const Heads mq{q, ldq, hdq, heads, width_k, false}, mk{k, ldk, hdk, kv_heads, width_k, false}, mv{v, ldv, hdv, kv_heads, width_v, false},
         mo{o, ldo, hdo, heads, width_v, true};
     if (num_seq > 0 && (!fits(mq, num_seq) || !fits(mk, num_seq) || !fits(mv, num_seq) || !fits(mo, num_seq))) return CP_ERR_SIZE;
-    if (in_the_way({extent(mq, num_seq, type), extent(mk, num_seq, type), extent(mv, num_seq, type), vector_at(log_decay, heads),
-                    vector_at(slots, num_seq, sizeof(int32_t))},
-                   {extent(mo, num_seq, type), vector_at(state, (int64_t)num_slots * state_floats(s)),
-                    vector_at(slots ? status_out : nullptr, 1, sizeof(int32_t))}))
+    if (attention::in_the_way({mq, mk, mv}, {mo}, {vector_at(log_decay, heads), vector_at(slots, num_seq, sizeof(int32_t))},
+                              {vector_at(state, (int64_t)num_slots * state_floats(s)), vector_at(slots ? status_out : nullptr, 1, sizeof(int32_t))}, num_seq, type))
         return CP_ERR_ARG;
     const hipStream_t st = (hipStream_t)stream;
     if (slots) hipLaunchKernelGGL(set_status_kernel, dim3(1), dim3(1), 0, st, status_out, CP_STATUS_OK);
