@@ -618,7 +618,7 @@ Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads, int32_t wk
     constexpr int64_t kWanted = 512;
     const int64_t len = packed ? rows : rows / num_seq;
     const int64_t units = (int64_t)heads * (packed ? 1 : num_seq);
-    int64_t parts = std::max<int64_t>(1, std::min((kWanted + units - 1) / units, len / kLeast));
+    int64_t parts = std::max<int64_t>(1, std::min(kWanted / units, len / kLeast));
     Cut c;
     c.seg_rows = std::max<int64_t>((len + parts - 1) / parts, 1);
     c.seg_rows = (c.seg_rows + 63) / 64 * 64;
@@ -638,7 +638,7 @@ int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t 
     // bf16 heads of up to 128: two workgroups of four wavefronts a compute unit, which have 32 columns each of 128.  The other types' rows leave
     // room for one such in LDS, and those of 256 places for 64 rows only of bf16.
     constexpr bool kHalf = std::is_same_v<T, bf16>;
-    constexpr int R = KB == 8 && !kHalf ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
+    constexpr int R = !kHalf && (KB == 8 || (KB == 4 && COLUMNS == 64)) ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
     if (kind == kGrad) {       // (two states: 16 columns a wavefront)
         hipLaunchKernelGGL((pass_kernel<T, KB, 1, COLUMNS / 16, R, kGrad, EVEN>), grid_of((int64_t)p.segments * p.heads * p.slices), dim3(COLUMNS * 4), 0, st, p,
                            effect, gain);
