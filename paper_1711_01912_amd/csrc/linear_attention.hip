@@ -111,7 +111,7 @@ struct State {
 // KB: blocks of 32 that the state's rows fill; NT: of 16 columns that a wavefront has; WAVES: of a workgroup; R: rows of a chunk;
 // EVEN: widths are multiples of 8
 template <typename T, int KB, int NT, int WAVES, int R, Kind kind, bool EVEN>
-__global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *effect, float *gain) {
+__global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad ? 4 : 2) void pass_kernel(Pass p, float *effect, float *gain) {
     using F = Form<T>;
     using E = typename F::E;
     constexpr int P = F::kPlanes, PS = F::kSplit, PI = kind == kGrad || kind == kLeave ? F::kFine : F::kSplit, PU = F::kFine;
@@ -267,7 +267,14 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void pass_kernel(Pass p, float *e
                     if constexpr (kind == kGrad) {
                         f32x4 other = {0, 0, 0, 0};
 #pragma unroll
-                        for (int k = 0; k < kWide / 32; k++) other = product<true>(x_tile.along(16 * jt, k, lane), d_tile.along(16 * it, k, lane), other);
+                        for (int k0 = 0; k0 < kWide / 32; k0 += 2) {
+                            Frag<E, P> xs[2], ds[2];
+#pragma unroll
+                            for (int k = 0; k < 2; k++) xs[k] = x_tile.along(16 * jt, k0 + k, lane), ds[k] = d_tile.along(16 * it, k0 + k, lane);
+                            asked();
+#pragma unroll
+                            for (int k = 0; k < 2; k++) other = product<true>(xs[k], ds[k], other);
+                        }
                         float sum = 0;
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
@@ -466,15 +473,24 @@ __global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float 
     Pack<float, V> e;
 #pragma unroll
     for (int k = 0; k < V; k++) e.v[k] = 0.0f;
-#pragma unroll 8
-    for (int32_t n = 0; n < segments; n++) {
-        const int32_t s = back ? segments - 1 - n : n;
-        float *here = at + ((int64_t)s * heads + head) * size + i;
-        const Pack<float, V> u = load_pack<float, V>(here);
-        const float by = gain[(int64_t)s * heads + head];
-        store_pack<float, V>(here, e);
+    constexpr int kAhead = 16;                         // segments whose effects are under way at once
+    const auto segment = [&](int32_t n) { return (int64_t)(back ? segments - 1 - n : n) * heads + head; };
+    for (int32_t n0 = 0; n0 < segments; n0 += kAhead) {
+        Pack<float, V> u[kAhead];
+        float by[kAhead];
 #pragma unroll
-        for (int k = 0; k < V; k++) e.v[k] = by == 0.0f ? u.v[k] : fmaf(by, e.v[k], u.v[k]);
+        for (int a = 0; a < kAhead; a++) {
+            const int32_t n = min(n0 + a, segments - 1);
+            u[a] = load_pack<float, V>(at + segment(n) * size + i);
+            by[a] = gain[segment(n)];
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; a++) {
+            if (n0 + a >= segments) break;
+            store_pack<float, V>(at + segment(n0 + a) * size + i, e);
+#pragma unroll
+            for (int k = 0; k < V; k++) e.v[k] = by[a] == 0.0f ? u[a].v[k] : fmaf(by[a], e.v[k], u[a].v[k]);
+        }
     }
 }
 
@@ -499,14 +515,14 @@ __global__ __launch_bounds__(kThreads) void empty_kernel(const int32_t *ptr, int
     }
 }
 
-// Gradients of a head's keys or values from those of the heads that share it, in their order; V neighbouring values a thread
+// Gradients of a head's keys or values from those of the heads that share it, in their order; a wavefront a row, V neighbouring values a lane
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void share_kernel(const float *part, const int32_t *ptr, int32_t num_seq, int64_t rows, int32_t heads, int32_t group,
                                                          int32_t width, T *to, int64_t ld, int64_t hd) {
     const int64_t total = ptr ? min((int64_t)max(ptr[num_seq], 0), rows) : rows;
     const int32_t line = heads / group * width / V;
-    for (int64_t row = blockIdx.x; row < total; row += gridDim.x)
-        for (int32_t i = threadIdx.x; i < line; i += kThreads) {
+    for (int64_t row = (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave; row < total; row += (int64_t)gridDim.x * (kThreads / kWave))
+        for (int32_t i = threadIdx.x % kWave; i < line; i += kWave) {
             const int32_t h = i * V / width, c = i * V % width;
             const float *from = part + (row * heads + (int64_t)h * group) * width + c;
             Pack<float, V> sum = load_pack<float, V>(from);
@@ -615,7 +631,7 @@ struct Cut {
 constexpr int64_t kLeast = 128;
 
 Cut cut_of(int64_t rows, int32_t num_seq, bool packed, int32_t heads, int32_t wk, int32_t wv) {
-    constexpr int64_t kWanted = 512;
+    const int64_t kWanted = std::max(wk, wv) <= 64 ? 1024 : 512;
     const int64_t len = packed ? rows : rows / num_seq;
     const int64_t units = (int64_t)heads * (packed ? 1 : num_seq);
     int64_t parts = std::max<int64_t>(1, std::min(kWanted / units, len / kLeast));
@@ -638,7 +654,7 @@ int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t 
     // bf16 heads of up to 128: two workgroups of four wavefronts a compute unit, which have 32 columns each of 128.  The other types' rows leave
     // room for one such in LDS, and those of 256 places for 64 rows only of bf16.
     constexpr bool kHalf = std::is_same_v<T, bf16>;
-    constexpr int R = !kHalf && (KB == 8 || (KB == 4 && COLUMNS == 64)) ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
+    constexpr int R = (kHalf && KB == 2 && COLUMNS == 64) || (!kHalf && (KB == 8 || (KB == 4 && COLUMNS == 64))) ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
     if (kind == kGrad) {       // (two states: 16 columns a wavefront)
         hipLaunchKernelGGL((pass_kernel<T, KB, 1, COLUMNS / 16, R, kGrad, EVEN>), grid_of((int64_t)p.segments * p.heads * p.slices), dim3(COLUMNS * 4), 0, st, p,
                            effect, gain);
@@ -920,7 +936,7 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
         if (code) return code;
         return by_type(type, [&](auto t) {
             using T = decltype(t);
-            hipLaunchKernelGGL((pass.wb % 4 == 0 ? share_kernel<T, 4> : share_kernel<T, 1>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(kThreads), 0, st,
+            hipLaunchKernelGGL((pass.wb % 4 == 0 ? share_kernel<T, 4> : share_kernel<T, 1>), dim3((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 20)), dim3(kThreads), 0, st,
                                share, seq_ptr, num_seq, rows, heads, group, pass.wb, (T *)to, ld, hd);
             return launched();
         });
