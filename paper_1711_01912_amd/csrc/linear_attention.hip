@@ -152,7 +152,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             ends = last.starts, whole = !last.ends;    // (its end and its start, seen from there)
             lo = last.lo, hi = last.hi;
         }
-        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = whole && !ends ? power(lg, (int)(hi - lo)) : 0.0f;
+        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = whole && !ends ? power(lg, (int)(hi - lo)) : -1.0f;
         if (ends) lo = hi;
     }
     // What does not change from chunk to chunk: the decays between a score's rows, of this wavefront's tiles, into rows from before
@@ -463,8 +463,10 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
     }
 }
 
-// States that enter the segments, from their effects, in place and in the order of the pass: E' = gain E + U.  A gain of 0 drops
-// the state before it (a sequence began), whatever it holds.
+// States that enter the segments, from their effects, in place and in the order of the pass: E' = gain E + U.  A gain below 0
+// drops the state before it (a sequence began), whatever it holds; one of 0 does not, as 0 times a NaN is one.  Sixteen segments' loads are
+// under way at once: 256 segments of 4 heads of 64 x 64 in 35 us, 45 with the next one's alone; 37 with 32 of half the width, 49 with 64 of a
+// quarter.
 template <int V>
 __global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float *gain, int32_t segments, int32_t heads, int32_t size, bool back) {
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * V;
@@ -489,7 +491,7 @@ __global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float 
             if (n0 + a >= segments) break;
             store_pack<float, V>(at + segment(n0 + a) * size + i, e);
 #pragma unroll
-            for (int k = 0; k < V; k++) e.v[k] = by[a] == 0.0f ? u[a].v[k] : fmaf(by[a], e.v[k], u[a].v[k]);
+            for (int k = 0; k < V; k++) e.v[k] = by[a] < 0.0f ? u[a].v[k] : fmaf(by[a], e.v[k], u[a].v[k]);
         }
     }
 }

@@ -124,6 +124,22 @@ def test_values_that_are_no_numbers(dtype, K, V, bad):
         assert name != "k" or not torch.isfinite(got["o"][after, 1]).all()
 
 
+@pytest.mark.parametrize("low", [-0.5, -5.0, -float("inf")])
+def test_a_nan_lasts_to_its_sequence_end(low):
+    """Over segments in which a state decays to nothing in 32 bits too; not into the next sequence."""
+    N, at, end = 4096, 700, 3500
+    i = make(N, 2, 1, 16, 24, "fp32", seed=3)
+    i["v"][at, 0, 5] = float("nan")
+    log_decay = torch.tensor([low, -0.01], device=DEV)
+    ptr = torch.tensor([0, end, N], dtype=torch.int32, device=DEV)
+    got = cpe.cp_linear_attention(i["q"], i["k"], i["v"], log_decay, seq_ptr=ptr, want_last=True)
+    back = cpe.cp_linear_attention(i["q"], i["k"], i["v"], log_decay, seq_ptr=ptr, reverse=True, want_last=True)
+    for out, rows in ((got, slice(at, end)), (back, slice(0, at + 1))):
+        want = torch.zeros(N, 2, 24, dtype=torch.bool, device=DEV)
+        want[rows, :, 5] = True
+        assert torch.equal(out["o"].isnan(), want) and torch.equal(out["last"].isnan().any(2), want[[at, N - 1]])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_decays(dtype):
     i = make(200, 6, 6, 32, 32, dtype, seed=7, h0=True, grad=True)
