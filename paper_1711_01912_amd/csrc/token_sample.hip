@@ -597,6 +597,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
                 }
             });
             __syncthreads();
+            const int count = level > 0 ? counted_ : INT_MAX;          // (read here: it is cleared behind the barriers below)
             // (thread t has steps 256 / THREADS t and on)
             constexpr int kEach = THREADS < kSteps ? kSteps / THREADS : 1;
             uint64_t sum = 0, one[kEach];
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
                 front += one[e];
             }
             __syncthreads();
-            const int step = found_at, count = level > 0 ? counted_ : INT_MAX;
+            const int step = found_at;
             above = found_above;
             if (threadIdx.x == 0) {
                 at[level] = step;
