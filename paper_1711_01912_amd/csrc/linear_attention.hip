@@ -138,6 +138,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
     int64_t lo, hi;
     segment_of(p, seg, lo, hi);
     if (threadIdx.x == 0) odd[0] = odd[1] = 0;
+    __syncthreads();                                   // (before another wavefront finds an infinity in its first rows)
     double decay_sum = 0;
     int turn = 0;
     State<KB, NT> s, r;
