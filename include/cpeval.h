@@ -481,9 +481,10 @@ int cp_ranks(const cp_graph *g, void *workspace, size_t workspace_bytes, void *s
  * A policy that learns where to place a graph's vertices reads them in topological order as a
  * sequence and gives each a row of logits over the devices; partitions are drawn from the rows,
  * cp_eval rates them, and the gradient of their log probabilities, weighted by the ratings,
- * trains the policy.  The entry points below are its sequence layer (cp_recurrence), the joint
- * between its blocks (cp_norm_gate) and its head (cp_token_logprobs), each with its gradient; the
- * matrix products between them are left to the caller's library.
+ * trains the policy.  The entry points below are its sequence layers (cp_recurrence and
+ * cp_linear_attention), the joint between its blocks (cp_norm_gate) and its head
+ * (cp_token_logprobs), each with its gradient, and the draw of tokens from its rows
+ * (cp_token_sample); the matrix products between them are left to the caller's library.
  *
  * Common to them: all arrays are device memory; matrices have rows of contiguous elements and
  * a distance ld between rows, in elements, at least the row's length.  Element types are
@@ -580,9 +581,10 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
  *   carry         [cp_linear_attention_carry_states][heads][width_k][width_v] for the backward pass, or NULL
  *   status_out    device int32, required with seq_ptr: CP_STATUS_BAD_SEQUENCE where seq_ptr does not rise from 0 to at most
  *                 rows (no access leaves the arrays)
- * 16-bit products are exact and summed in 32 bits; states and scores on their way to o as the sum of two bf16, off by at most 2^-15, rows on their way to a state as they
- * are.  An
- * infinity or a NaN makes results from its row to its sequence's end infinite or NaN, of its head alone.
+ * Products of 16-bit elements are exact, and summed in 32 bits.  With 16-bit types, states and scores enter the products for o as
+ * the sum of two bf16, off by at most 2^-15 of their value; rows on their way to a state keep all 24 bits.  An infinity or a NaN
+ * makes what follows from it, from its row to its sequence's end and in its head (or those that share it), infinite or NaN, and
+ * nothing else.
  * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, widths, heads, num_seq < 1, num_seq * heads of equal
  * parts above 2^28, rows no multiple of num_seq without seq_ptr, distances; results whose rows or heads overlap),
  * CP_ERR_NULL, CP_ERR_WORKSPACE, CP_ERR_HIP.
@@ -726,7 +728,8 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
  *   logp          [rows][given], the logarithm of the token's share of the kept mass, or NULL
  *   status_out    device int32, required where a row has settings of its own
  * A row with nothing allowed, or with a NaN or +inf at an allowed place, gets tokens -1 (255 of CP_TOKEN_U8) and logp 0.
- * Probabilities and sums are formed in 64 bits.  Errors: as cp_token_logprobs's; CP_ERR_SIZE where strides put two tokens in one place.
+ * Probabilities and sums are formed in 64 bits.  workspace may be NULL where cp_token_sample_workspace_bytes says 0, as it does for all sizes
+ * now.  Errors: as cp_token_logprobs's; CP_ERR_SIZE where strides put two tokens in one place.
  */
 int cp_token_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t given, size_t *out_bytes);
 int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, double scale, const float *scales,

@@ -2,12 +2,17 @@
 //
 //   S_t = gamma S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t,   gamma = exp(log_decay) of the head
 //
-// in chunks of 64 rows, which makes it matrix products: with S the state that enters a chunk and i, j its rows,
+// in chunks of 32 or 64 rows, which makes it matrix products: with S the state that enters a chunk and i, j its rows,
 //
 //   o_i = scale (gamma^(i+1) q_i S + sum_{j <= i} gamma^(i-j) (q_i . k_j) v_j)
 //   S'  = gamma^n S + sum_j gamma^(n-1-j) k_j^T v_j
 //
-// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS.  The scores, of which only the tiles on and below the diagonal are computed, are shared out among the wavefronts.
+// A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS.  The scores, of which only
+// the tiles on and below the diagonal are computed, are shared out among the wavefronts.
+//
+// What bounds a pass of bf16 heads of 128: 65,536 rows of 16 heads in 365 to 390 us, 1.07 GB at 2.9 TB/s.  Its loads and stores alone take 239 us, its
+// LDS reads and products alone 333 and more (the clock falls under the products), and with two wavefronts a SIMD, which is what LDS and
+// registers leave room for, about half of the issue slots wait for one of them.
 //
 // The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
 //   dq_t = scale do_t S_t^T (the pass with do, v, k in the places of q, k, v),   dv_t = k_t D_t and dk_t = v_t D_t^T (from the last
@@ -392,9 +397,9 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                 }
             }
 
-            // The next chunk is on its way while the state is computed, where there are registers for it.  (Where some go to scratch memory, whose loads wait
-            // for all others before them, it costs more than it gives: 65536 rows of 16 heads of 128 in bf16 443 us for 388; 1,000,000 rows of 4 of 64, where
-            // there are, 3,133 for 3,312, forward and backward.)
+            // The next chunk is on its way while the state is computed, where there are registers for it.  (Where some go to scratch memory, whose
+            // loads wait for all others before them, it costs more than it gives: 65,536 rows of 16 heads of 128 in bf16 443 us for 388; 1,000,000
+            // rows of 4 of 64, where there are, 3,133 for 3,312, forward and backward.)
             if constexpr (kAhead && kind != kEffect) {
                 if (left > 0) fetch();
                 asked();
@@ -568,7 +573,7 @@ struct Step {
 };
 
 // A workgroup has the state of one head of one sequence; a thread V neighbouring columns of every few rows.  It is read once and written
-// once, which is all there is to it.
+// once, which is all there is to it: 512 sequences of 16 heads of 128 x 128 in 217 us, 1.08 GB at 5.0 TB/s, the rate of a copy.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void step_kernel(Step p) {
     __shared__ float sums[kThreads * V], kq[2][256];
@@ -624,8 +629,10 @@ __global__ void set_status_kernel(int32_t *status, int32_t value) { *status = va
 
 constexpr int kMaxWidth = CP_ATTENTION_MAX_WIDTH, kMaxHeads = CP_ATTENTION_MAX_HEADS;
 
-// Segments: workgroups enough for the chip, two a compute unit, of 128 rows at least.  The same for all types and for both
-// directions, since the backward pass reads the states that the forward call kept.
+// Segments: workgroups enough to fill the chip once, two a compute unit, and twice as many for heads of up to 64, of which four fit; of 128 rows at
+// least.  The same for all types and for both directions, since the backward pass reads the states that the forward call kept.  (Forward and
+// backward in bf16: 1,000,000 rows of 4 heads of 64 3.08 ms, 3.26 with half as many; 8 sequences of 4,096 rows of 16 heads of 128 1.15 ms, 1.27
+// with twice as many, whose states cost more than the fuller chip gives.)
 struct Cut {
     int64_t seg_rows;
     int32_t parts, segments;
@@ -654,10 +661,14 @@ int32_t slices_of(int32_t wa, int32_t wb) { return (wb + columns_of(wa, wb) - 1)
 
 template <typename T, int KB, int COLUMNS, bool EVEN>
 int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t st) {
-    // bf16 heads of up to 128: two workgroups of four wavefronts a compute unit, which have 32 columns each of 128.  The other types' rows leave
-    // room for one such in LDS, and those of 256 places for 64 rows only of bf16.
+    // Columns a wavefront: 32 of bf16 heads of up to 128, whose operands then serve two products (65,536 rows of 16 heads of 128 forward 504 us, 605 with 16;
+    // 8 x 4,096 rows forward and backward 1.15 ms, 1.26).  The other types' operands, of two or three parts or in 32 bits, leave no registers for it.
+    // Rows of a chunk: 32 where 64 leave LDS for one workgroup a compute unit, or none, and for bf16 heads of up to 64, of which four
+    // workgroups fit then (1,000,000 rows of 4 heads of 64 3.08 ms, 3.21 with 64; dk and dq of fp16 heads of 48 keys and 80 values, 52,710 rows
+    // of 6, 319 us, 472).  64 otherwise: a state is read and split once for twice the rows.
     constexpr bool kHalf = std::is_same_v<T, bf16>;
-    constexpr int R = (kHalf && KB == 2 && COLUMNS == 64) || (!kHalf && (KB == 8 || (KB == 4 && COLUMNS == 64))) ? 32 : 64, NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
+    constexpr int R = (kHalf && KB == 2 && COLUMNS == 64) || (!kHalf && (KB == 8 || (KB == 4 && COLUMNS == 64))) ? 32 : 64;
+    constexpr int NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;
     if (kind == kGrad) {       // (two states: 16 columns a wavefront)
         hipLaunchKernelGGL((pass_kernel<T, KB, 1, COLUMNS / 16, R, kGrad, EVEN>), grid_of((int64_t)p.segments * p.heads * p.slices), dim3(COLUMNS * 4), 0, st, p,
                            effect, gain);

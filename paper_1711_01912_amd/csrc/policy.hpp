@@ -1,5 +1,5 @@
-// Shared by the operators of a learned placement policy (recurrence.hip, norm_gate.hip, token_logprobs.hip): element types,
-// vectors of them as they are loaded and stored, and sums over a wavefront.
+// Shared by the operators of a learned placement policy (recurrence.hip, linear_attention.hip, norm_gate.hip, token_logprobs.hip,
+// token_sample.hip): element types, vectors of them as they are loaded and stored, and sums over a wavefront.
 #pragma once
 
 #include <hip/hip_runtime.h>
