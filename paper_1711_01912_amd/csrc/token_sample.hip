@@ -41,6 +41,10 @@ struct Draw {
     int64_t t_row, t_step;
     float *logp;                         // [rows][given], or null
     int32_t *status;
+    // of rows that are cut into slices, or 0: what each found
+    int32_t slices, slice_size;
+    uint64_t *found;                     // [rows][slices][kSliced] words of a list, the largest first
+    int32_t *counts;                     // [rows][slices]: how many; or that they had no room, or that there is a NaN or +inf
 };
 
 // one row's settings; false: out of range
@@ -461,6 +465,90 @@ struct Many {
 
 __device__ __forceinline__ uint64_t listed(uint32_t key, int32_t place) { return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)place); }
 
+// Lists the best top_k <= THREADS places and a few more, those of places from `from` on; their number, which may be more than there is room for.
+// The bound that they are at or above is the least of what a few threads' own best places of each wavefront reach; a thread has few of a row's
+// best.  (own, m: of the thread and of all.)
+template <typename T, int THREADS>
+__device__ __forceinline__ int list_best(const Many<T, THREADS> &a, float own, float m, int32_t top_k, int32_t from, uint64_t *list, Block<THREADS> &block, int &counted_) {
+    using M = Many<T, THREADS>;
+    constexpr int kWaves = THREADS / kWave;
+    const int share = (top_k + kWaves - 1) / kWaves;
+    const uint32_t key = M::key(own);
+    uint32_t low = 0, high = M::key(m) + 1;
+    for (int n = 0; n < 32 && high - low > 1; n++) {
+        const uint32_t mid = low + (high - low) / 2;
+        if (__popcll(__ballot(key >= mid)) >= share) low = mid;
+        else high = mid;
+    }
+    if (threadIdx.x % kWave == 0) block.i[threadIdx.x / kWave] = (int32_t)(low ^ 0x80000000u);
+    if (threadIdx.x == 0) counted_ = 0;
+    __syncthreads();
+    int32_t least = block.i[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; w++) least = min(least, block.i[w]);
+    low = (uint32_t)least ^ 0x80000000u;
+    a.template each<4>([&](int32_t v, float x) {
+        if (M::key(x) >= low && x > -INFINITY) {
+            const int at = atomicAdd(&counted_, 1);
+            if (at < kListed) list[at] = listed(M::key(x), from + v);
+        }
+    });
+    __syncthreads();
+    const int count = counted_;
+    __syncthreads();
+    return count;
+}
+
+// Few long rows: a workgroup a slice of a row lists the slice's best top_k, and many_sample_kernel begins with these.
+constexpr int kSliced = 256, kSlices = 64;   // top_k, and slices of a row, at most
+constexpr int32_t kSlice = 8192;             // places of a slice at least
+constexpr int32_t kNoRoom = -1, kOdd = -2;
+__device__ __forceinline__ bool sliced(const Draw &d, const Rule &r) { return d.slices > 0 && r.fine && r.top_k > 0 && r.top_k <= kSliced; }
+// (top_p of 0: the best alone)
+__device__ __forceinline__ Rule row_rule(const Draw &d, int64_t row) {
+    Rule r = rule_of(d.set, row);
+    if (r.top_p == 0.0) r.top_p = 1.0, r.top_k = 1;
+    if (r.top_k >= d.vocab) r.top_k = 0;
+    return r;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSliced) void slice_list_kernel(Draw d) {
+    using M = Many<T, kSliced>;
+    __shared__ uint64_t list[kListed];
+    __shared__ Block<kSliced> block;
+    __shared__ int odd_, counted_;
+    const uint32_t group = group_number();
+    const int64_t row = group / d.slices;
+    if (row >= d.rows) return;
+    const Rule rule = row_rule(d, row);
+    if (!sliced(d, rule)) return;
+    const int32_t from = (int32_t)(group % d.slices) * d.slice_size;
+    const M a{(const T *)d.logits + row * d.ld + from, d.allow ? d.allow + row * d.words + from / 64 : nullptr, min(d.slice_size, d.vocab - from), 0.0f, 0.0};
+    if (threadIdx.x == 0) odd_ = 0;
+    float own = -INFINITY;
+    bool odd = false;
+    a.template each<4>([&](int32_t, float x) { odd |= !(x < INFINITY), own = fmaxf(own, x); });
+    float m = most_of<kWave>(own);
+    if (threadIdx.x % kWave == 0) block.f[threadIdx.x / kWave] = m;
+    __syncthreads();
+    if (odd) odd_ = 1;
+#pragma unroll
+    for (int w = 0; w < kSliced / kWave; w++) m = fmaxf(m, block.f[w]);
+    __syncthreads();
+    int32_t found = kOdd;
+    if (!odd_) {
+        const int count = list_best<T, kSliced>(a, own, m, rule.top_k, from, list, block, counted_);
+        found = kNoRoom;
+        if (count <= kListed) {
+            put_in_order<kSliced>(list, count);
+            found = min(count, rule.top_k);
+            if ((int)threadIdx.x < found) d.found[(int64_t)group * kSliced + threadIdx.x] = list[threadIdx.x];
+        }
+    }
+    if (threadIdx.x == 0) d.counts[group] = found;
+}
+
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_kernel(Draw d) {
     using M = Many<T, THREADS>;
@@ -474,10 +562,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int64_t row = group_number();
     if (row >= d.rows) return;
-    Rule rule = rule_of(d.set, row);
-    if (rule.top_p == 0.0) rule.top_p = 1.0, rule.top_k = 1;       // (the best alone)
+    const Rule rule = row_rule(d, row);
     const int32_t V = d.vocab;
-    if (rule.top_k >= V) rule.top_k = 0;
     M a{(const T *)d.logits + row * d.ld, d.allow ? d.allow + row * d.words : nullptr, V, 0.0f, rule.scale * kLog2eWide};
     const auto draw_of = [&](int32_t g) { return (double)counted(d.u[row * d.u_row + g * d.u_step]); };
     const auto put_logp = [&](int32_t g, float x, double logs) {
@@ -485,16 +571,51 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
     };
 
     if (threadIdx.x == 0) odd_ = counted_ = 0;
-    float m = -INFINITY;
-    bool odd = false;
-    a.template each<4>([&](int32_t, float x) { odd |= !(x < INFINITY), m = fmaxf(m, x); });
-    const float own = m;
-    m = most_of<kWave>(m);
-    if (lane == 0) block.f[wave] = m;
     __syncthreads();
-    if (odd) odd_ = 1;
+    float own = -INFINITY, m = -INFINITY;
+    int32_t have = INT_MAX;                            // words in the list
+    bool whole = true;                                 // whether the row is to be read
+    if (sliced(d, rule)) {
+        // The slices' lists: of each the first words, as many as make top_k together, are at or above a bound
+        const uint64_t *from = d.found + row * d.slices * kSliced;
+        const int32_t *counts = d.counts + row * d.slices;
+        const int32_t mine = lane < d.slices ? counts[lane] : 0, share = (rule.top_k + d.slices - 1) / d.slices;
+        uint64_t bound = lane >= d.slices ? ~0ull : mine >= share ? from[lane * kSliced + share - 1] : 0, best = mine > 0 ? from[lane * kSliced] : 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; w++) m = fmaxf(m, block.f[w]);
+        for (int off = 32; off > 0; off >>= 1) {
+            bound = min(bound, (uint64_t)__shfl_xor((unsigned long long)bound, off));
+            best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, off));
+        }
+        if (__ballot(mine == kOdd)) odd_ = 1, whole = false;
+        else if (!__ballot(mine == kNoRoom)) {
+            whole = false;
+            m = best ? M::value((uint32_t)(best >> 32)) : -INFINITY;
+            for (int i = threadIdx.x; i < d.slices * rule.top_k; i += THREADS) {
+                const int s = i / rule.top_k, k = i - s * rule.top_k;
+                const uint64_t word = k < counts[s] ? from[s * kSliced + k] : 0;
+                if (word && word >= bound) {
+                    const int at = atomicAdd(&counted_, 1);
+                    if (at < kListed) list[at] = word;
+                }
+            }
+        }
+        __syncthreads();
+        have = counted_;
+        if (!whole && have > kListed) whole = true;
+        __syncthreads();
+        if (threadIdx.x == 0) counted_ = 0;
+    }
+    if (whole) {
+        have = INT_MAX;
+        bool odd = false;
+        a.template each<4>([&](int32_t, float x) { odd |= !(x < INFINITY), own = fmaxf(own, x); });
+        m = most_of<kWave>(own);
+        if (lane == 0) block.f[wave] = m;
+        __syncthreads();
+        if (odd) odd_ = 1;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) m = fmaxf(m, block.f[w]);
+    }
     a.m = m;
     __syncthreads();
     if (odd_ || m == -INFINITY || !rule.fine) {
@@ -511,29 +632,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
         if (at < kListed) list[at] = listed(M::key(x), v);
     };
 
-    // Few are left: they are listed, put in order, and all the rest is a matter of the list.  The bound that they are at or above is the least of what a
-    // few threads' own best places of each wavefront reach; a thread has few of a row's best.
+    // Few are left: they are listed, put in order, and all the rest is a matter of the list.
     if (rule.top_k > 0 && rule.top_k <= THREADS) {
-        const int share = (rule.top_k + kWaves - 1) / kWaves;
-        const uint32_t key = M::key(own);
-        uint32_t low = 0, high = M::key(m) + 1;
-        for (int n = 0; n < 32 && high - low > 1; n++) {
-            const uint32_t mid = low + (high - low) / 2;
-            if (__popcll(__ballot(key >= mid)) >= share) low = mid;
-            else high = mid;
-        }
-        if (lane == 0) block.i[wave] = (int32_t)(low ^ 0x80000000u);
-        __syncthreads();
-        int32_t least = block.i[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; w++) least = min(least, block.i[w]);
-        low = (uint32_t)least ^ 0x80000000u;
-        a.template each<4>([&](int32_t v, float x) {
-            if (M::key(x) >= low && x > -INFINITY) note(x, v);
-        });
-        __syncthreads();
-        const int count = counted_;
-        __syncthreads();
+        const int count = have != INT_MAX ? have : list_best<T, THREADS>(a, own, m, rule.top_k, 0, list, block, counted_);
         if (threadIdx.x == 0) counted_ = 0;
         if (count <= kListed) {
             put_in_order<THREADS>(list, count);
@@ -893,6 +994,14 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
 
 constexpr int64_t kFar = 1ll << 28;          // strides; products of these, rows and bytes stay in 64 bits
 
+// Slices of a row, or 0 where rows are not cut
+int32_t slice_size_of(int32_t vocab) { return (int32_t)std::max<int64_t>(((int64_t)vocab + (int64_t)kSlices * kSlice - 1) / ((int64_t)kSlices * kSlice), 1) * kSlice; }
+int32_t slices_of(int64_t rows, int32_t vocab) {
+    if (rows < 1 || rows > 64 || vocab < 4 * kSlice) return 0;
+    return (vocab + slice_size_of(vocab) - 1) / slice_size_of(vocab);
+}
+size_t found_bytes(int64_t rows, int32_t slices) { return align_up((size_t)rows * slices * kSliced * sizeof(uint64_t)); }
+
 __global__ void clear_sampling_kernel(int32_t *status) { *status = CP_STATUS_OK; }
 
 }  // namespace
@@ -906,7 +1015,8 @@ extern "C" {
 int cp_token_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t given, size_t *out_bytes) {
     if (!out_bytes) return CP_ERR_NULL;
     if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > CP_LOGPROBS_MAX_VOCAB || given < 0 || given > CP_LOGPROBS_MAX_GIVEN) return CP_ERR_SIZE;
-    *out_bytes = 0;
+    const int32_t slices = given > 0 ? slices_of(rows, vocab) : 0;
+    *out_bytes = slices ? found_bytes(rows, slices) + align_up((size_t)rows * slices * sizeof(int32_t)) : 0;
     return CP_OK;
 }
 
@@ -925,6 +1035,10 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
     if ((token_type == CP_TOKEN_U8 && vocab > 255) || (rows > 1 && ld < vocab)) return CP_ERR_SIZE;
     const bool own = scales || top_ks || top_ps || min_ps;
     if ((rows > 0 && !logits) || (rows > 0 && given > 0 && (!u || !tokens)) || (own && !status_out)) return CP_ERR_NULL;
+    if (need) {
+        if (!workspace) return CP_ERR_NULL;
+        if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
+    }
     if (rows > 0 && given > 0) {
         // numbers may lie anywhere, tokens apart from each other
         if (u_row_stride < 0 || u_stride < 0 || u_row_stride > kFar || u_stride > kFar || token_row_stride > kFar || token_stride > kFar) return CP_ERR_SIZE;
@@ -937,17 +1051,25 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
         const Extent numbers = vector_at(u, (rows - 1) * u_row_stride + (given - 1) * u_stride + 1);
         if (in_the_way({matrix_at(logits, rows, vocab, ld, type), numbers, vector_at(allow, rows * ((vocab + 63) / 64), 8), vector_at(scales, rows),
                         vector_at(top_ks, rows), vector_at(top_ps, rows), vector_at(min_ps, rows)},
-                       {to, vector_at(logp, rows * given), vector_at(own ? status_out : nullptr, 1)}))
+                       {to, vector_at(logp, rows * given), vector_at(own ? status_out : nullptr, 1), vector_at(need ? workspace : nullptr, (int64_t)need, 1)}))
             return CP_ERR_ARG;
     }
     const hipStream_t st = (hipStream_t)stream;
     if (own) hipLaunchKernelGGL(clear_sampling_kernel, dim3(1), dim3(1), 0, st, status_out);
     if (rows == 0 || given == 0) return launched();
+    // (only where a row may keep few places)
+    const int32_t slices = top_ks || top_ps || (top_k > 0 && top_k <= kSliced) || top_p == 0.0 ? slices_of(rows, vocab) : 0;
     const Draw d{rows, vocab, (vocab + 63) / 64, logits, ld, allow, {scale, top_p, min_p, top_k, scales, top_ps, min_ps, top_ks}, given, u,
-                 u_row_stride, u_stride, tokens, token_type, token_row_stride, token_stride, logp, status_out};
+                 u_row_stride, u_stride, tokens, token_type, token_row_stride, token_stride, logp, status_out, slices, slice_size_of(vocab),
+                 (uint64_t *)workspace, (int32_t *)((char *)workspace + (slices ? found_bytes(rows, slices) : 0))};
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         if (vocab > kFew) {
+            if (slices) {
+                hipLaunchKernelGGL((slice_list_kernel<T>), grid_of(rows * slices), dim3(kSliced), 0, st, d);
+                const int code = launched();
+                if (code) return code;
+            }
             // A workgroup as large as has work for its threads (2048 x 4000 bf16 46 us, 85 of 1,024 threads), two a compute unit where there are more
             // rows than compute units (512 x 65536 181 us, 188 of 1,024 threads; but 8 x 131072 34 us, 36 of 512).
             if (vocab <= 8192) hipLaunchKernelGGL((many_sample_kernel<T, 256>), grid_of(rows), dim3(256), 0, st, d);

@@ -121,6 +121,15 @@ def test_sample_results_where_something_else_lies(lib):
         assert lib.cp_token_sample(*with_(SAMPLE, urs=0, us=0)) not in (ARG, SIZE)
 
 
+def test_sample_workspace(lib):
+    need, long_ = C.c_size_t(0), dict(rows=4, vocab=100000, ld=100000, logits=5 << 44, u=6 << 44, tokens=7 << 44, logp=None)
+    assert lib.cp_token_sample_workspace_bytes(4, 100000, SAMPLE["given"], C.byref(need)) == 0 and need.value > 0
+    for change, code in ((dict(work=None), NULL), (dict(work=(1 << 44) + 8), WORKSPACE), (dict(bytes=need.value - 1), WORKSPACE),
+                         (dict(work=5 << 44), ARG), (dict(work=(7 << 44) - need.value // 512 * 256), ARG)):
+        assert lib.cp_token_sample(*with_(SAMPLE, **{**long_, "work": 1 << 44, "bytes": need.value, **change})) == code, change
+    assert lib.cp_token_sample_workspace_bytes(65, 100000, 1, C.byref(need)) == 0 and need.value == 0
+
+
 def test_sizes(lib):
     out, states = C.c_size_t(0), C.c_int64(0)
     assert lib.cp_linear_attention_workspace_bytes(5000, 1, 1, 2, 1, 64, 64, 1, C.byref(out)) == 0 and out.value > 0

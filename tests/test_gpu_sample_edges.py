@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_1711_01912_amd as cpe
+from paper_1711_01912_amd import policy
 from test_gpu_token_sample import FILTERS, check, inputs
 from workloads import make_workload
 
@@ -40,6 +41,59 @@ def test_more_rows_than_compute_units(V):
     logits, u = inputs(300, V, 1, "bf16", seed=V)
     for f in (dict(top_p=0.9), dict(top_k=30), dict(min_p=0.05)):
         check(logits, u, **f)
+
+
+SLICED = [dict(top_k=1), dict(top_k=50, top_p=0.9), dict(top_k=50, min_p=0.01), dict(top_k=256), dict(top_k=257), dict(top_p=0.0), dict(top_p=0.9), dict(min_p=0.2)]
+
+
+@pytest.mark.parametrize("dtype,V", [("fp32", 32768), ("bf16", 40001), ("fp16", 70000), ("bf16", 524289)])
+def test_few_long_rows(V, dtype):
+    # what is kept lies in one slice, in the last, in all; what is alike has room in no list
+    logits, u = inputs(9, V, 2, dtype, seed=V)
+    logits[1] = 1.0
+    logits[2] = -float("inf")
+    logits[2, V - 3:] = 2.0
+    logits[3] = -float("inf")
+    logits[3, 8190:8194] = torch.tensor([1.0, 2.0, 2.0, 1.0])
+    logits[4] = logits[4].sort().values
+    logits[5] = torch.round(logits[5])
+    logits[6, V // 2], logits[7, V - 1] = float("nan"), float("inf")
+    logits[8] = -float("inf")
+    for f in SLICED:
+        check(logits, u, scale=0.7, **f)
+    allowed = np.random.default_rng(V).random((9, V)) < 0.3
+    allowed[6, V // 2] = allowed[7, V - 1] = False
+    allowed[4, 100:] = False
+    for f in SLICED[1:4]:
+        check(logits, u, allowed, **f)
+
+
+def test_few_long_rows_with_settings_of_their_own():
+    logits, u = inputs(64, 33000, 3, "bf16", seed=4)
+    g = np.random.default_rng(4)
+    k, p = g.choice([0, 1, 3, 50, 255, 256, 257, 1024, 1025, 33000, 40000], 64), g.choice([0.0, 0.3, 0.9, 1.0], 64)
+    check(logits, u, top_k=k, top_p=p, min_p=g.choice([0.0, 0.01], 64))
+    check(logits, u, top_p=p)
+    k[5], p[6] = -1, 1.5
+    out = cpe.cp_token_sample(logits.to(DEV), u.to(DEV), top_k=torch.tensor(k, dtype=torch.int32, device=DEV), top_p=torch.tensor(p, dtype=torch.float32, device=DEV),
+                              check_status=False)
+    assert int(out["status"]) == policy.STATUS_BAD_SAMPLING and bool((out["tokens"][5:7] == -1).all()) and int((out["tokens"] == -1).sum()) == 6
+    # rows of one buffer at odd places, and a graph
+    wide = torch.zeros(8, 33100, dtype=torch.bfloat16, device=DEV)
+    wide[:, 7:33007] = logits[:8].to(DEV)
+    u = u[:8].to(DEV)
+    want = cpe.cp_token_sample(logits[:8].to(DEV), u, top_k=50, top_p=0.9)["tokens"]
+    assert torch.equal(cpe.cp_token_sample(wide[:, 7:33007], u, top_k=50, top_p=0.9)["tokens"], want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = cpe.cp_token_sample(wide[:, 7:33007], u, top_k=50, top_p=0.9)
+    for turn in range(3):
+        u.copy_(torch.rand(u.shape, generator=torch.Generator().manual_seed(turn)))
+        want = cpe.cp_token_sample(wide[:, 7:33007], u, top_k=50, top_p=0.9)["tokens"]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out["tokens"], want)
 
 
 def test_sorted_rows():
