@@ -398,8 +398,7 @@ __device__ __forceinline__ void put_in_order(uint64_t *list, int count) {
 }
 
 // A workgroup a row, which is read from the caches for each of: the maximum; where what is kept ends; the mass of each chunk; the draws.  Only
-// the first reads it from memory.  8 rows of 131,072 in bf16 with top_k 50 take 33 us, which is the latency of two passes by a
-// workgroup; 512 of 65,536 with settings of their own 170 to 180 us.  These are bound by the probabilities (some 16 operations of
+// the first reads it from memory.  512 of 65,536 with settings of their own 170 to 180 us.  These are bound by the probabilities (some 16 operations of
 // 64 bits each) and by the sums of mass by depth, an atomic operation of 64 bits a place in LDS (about 55 us of a row's time).
 template <typename T, int THREADS>
 struct Many {
@@ -499,9 +498,10 @@ __device__ __forceinline__ int list_best(const Many<T, THREADS> &a, float own, f
     return count;
 }
 
-// Few long rows: a workgroup a slice of a row lists the slice's best top_k, and many_sample_kernel begins with these.
-constexpr int kSliced = 256, kSlices = 64;   // top_k, and slices of a row, at most
+// Few long rows of which few places are kept: a workgroup a slice of a row lists the slice's best top_k, and many_sample_kernel begins with these.
+constexpr int kSliced = 128, kSlices = 64;   // top_k, and slices of a row, at most
 constexpr int32_t kSlice = 8192;             // places of a slice at least
+constexpr int kSliceThreads = 256;
 constexpr int32_t kNoRoom = -1, kOdd = -2;
 __device__ __forceinline__ bool sliced(const Draw &d, const Rule &r) { return d.slices > 0 && r.fine && r.top_k > 0 && r.top_k <= kSliced; }
 // (top_p of 0: the best alone)
@@ -513,10 +513,10 @@ __device__ __forceinline__ Rule row_rule(const Draw &d, int64_t row) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSliced) void slice_list_kernel(Draw d) {
-    using M = Many<T, kSliced>;
+__global__ __launch_bounds__(kSliceThreads) void slice_list_kernel(Draw d) {
+    using M = Many<T, kSliceThreads>;
     __shared__ uint64_t list[kListed];
-    __shared__ Block<kSliced> block;
+    __shared__ Block<kSliceThreads> block;
     __shared__ int odd_, counted_;
     const uint32_t group = group_number();
     const int64_t row = group / d.slices;
@@ -534,14 +534,14 @@ __global__ __launch_bounds__(kSliced) void slice_list_kernel(Draw d) {
     __syncthreads();
     if (odd) odd_ = 1;
 #pragma unroll
-    for (int w = 0; w < kSliced / kWave; w++) m = fmaxf(m, block.f[w]);
+    for (int w = 0; w < kSliceThreads / kWave; w++) m = fmaxf(m, block.f[w]);
     __syncthreads();
     int32_t found = kOdd;
     if (!odd_) {
-        const int count = list_best<T, kSliced>(a, own, m, rule.top_k, from, list, block, counted_);
+        const int count = list_best<T, kSliceThreads>(a, own, m, rule.top_k, from, list, block, counted_);
         found = kNoRoom;
         if (count <= kListed) {
-            put_in_order<kSliced>(list, count);
+            put_in_order<kSliceThreads>(list, count);
             found = min(count, rule.top_k);
             if ((int)threadIdx.x < found) d.found[(int64_t)group * kSliced + threadIdx.x] = list[threadIdx.x];
         }
@@ -994,10 +994,12 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
 
 constexpr int64_t kFar = 1ll << 28;          // strides; products of these, rows and bytes stay in 64 bits
 
-// Slices of a row, or 0 where rows are not cut
+// Slices of a row, or 0 where rows are not cut: more rows fill the chip by themselves, and shorter ones are done before a second launch begins.  (bf16,
+// top_k 50 and top_p 0.9: 8 x 131072 23 us, 34 uncut; 64 x 131072 29, 35; 8 x 524288 30, 88; but 8 x 32768 21.4, 19.4.  top_k 128: 8 x 131072 30 us, 37;
+// 256, whose lists are long, 93, 43.)
 int32_t slice_size_of(int32_t vocab) { return (int32_t)std::max<int64_t>(((int64_t)vocab + (int64_t)kSlices * kSlice - 1) / ((int64_t)kSlices * kSlice), 1) * kSlice; }
 int32_t slices_of(int64_t rows, int32_t vocab) {
-    if (rows < 1 || rows > 64 || vocab < 4 * kSlice) return 0;
+    if (rows < 1 || rows > 64 || vocab < 8 * kSlice) return 0;
     return (vocab + slice_size_of(vocab) - 1) / slice_size_of(vocab);
 }
 size_t found_bytes(int64_t rows, int32_t slices) { return align_up((size_t)rows * slices * kSliced * sizeof(uint64_t)); }
@@ -1066,7 +1068,7 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
         using T = decltype(t);
         if (vocab > kFew) {
             if (slices) {
-                hipLaunchKernelGGL((slice_list_kernel<T>), grid_of(rows * slices), dim3(kSliced), 0, st, d);
+                hipLaunchKernelGGL((slice_list_kernel<T>), grid_of(rows * slices), dim3(kSliceThreads), 0, st, d);
                 const int code = launched();
                 if (code) return code;
             }

@@ -43,10 +43,10 @@ def test_more_rows_than_compute_units(V):
         check(logits, u, **f)
 
 
-SLICED = [dict(top_k=1), dict(top_k=50, top_p=0.9), dict(top_k=50, min_p=0.01), dict(top_k=256), dict(top_k=257), dict(top_p=0.0), dict(top_p=0.9), dict(min_p=0.2)]
+SLICED = [dict(top_k=1), dict(top_k=50, top_p=0.9), dict(top_k=50, min_p=0.01), dict(top_k=128), dict(top_k=129), dict(top_k=256), dict(top_p=0.0), dict(top_p=0.9), dict(min_p=0.2)]
 
 
-@pytest.mark.parametrize("dtype,V", [("fp32", 32768), ("bf16", 40001), ("fp16", 70000), ("bf16", 524289)])
+@pytest.mark.parametrize("dtype,V", [("fp32", 65536), ("bf16", 80001), ("fp16", 70000), ("bf16", 524289)])
 def test_few_long_rows(V, dtype):
     # what is kept lies in one slice, in the last, in all; what is alike has room in no list
     logits, u = inputs(9, V, 2, dtype, seed=V)
@@ -69,9 +69,9 @@ def test_few_long_rows(V, dtype):
 
 
 def test_few_long_rows_with_settings_of_their_own():
-    logits, u = inputs(64, 33000, 3, "bf16", seed=4)
+    logits, u = inputs(64, 66000, 3, "bf16", seed=4)
     g = np.random.default_rng(4)
-    k, p = g.choice([0, 1, 3, 50, 255, 256, 257, 1024, 1025, 33000, 40000], 64), g.choice([0.0, 0.3, 0.9, 1.0], 64)
+    k, p = g.choice([0, 1, 3, 50, 127, 128, 129, 256, 1024, 1025, 66000, 70000], 64), g.choice([0.0, 0.3, 0.9, 1.0], 64)
     check(logits, u, top_k=k, top_p=p, min_p=g.choice([0.0, 0.01], 64))
     check(logits, u, top_p=p)
     k[5], p[6] = -1, 1.5
@@ -79,17 +79,17 @@ def test_few_long_rows_with_settings_of_their_own():
                               check_status=False)
     assert int(out["status"]) == policy.STATUS_BAD_SAMPLING and bool((out["tokens"][5:7] == -1).all()) and int((out["tokens"] == -1).sum()) == 6
     # rows of one buffer at odd places, and a graph
-    wide = torch.zeros(8, 33100, dtype=torch.bfloat16, device=DEV)
-    wide[:, 7:33007] = logits[:8].to(DEV)
+    wide = torch.zeros(8, 66100, dtype=torch.bfloat16, device=DEV)
+    wide[:, 7:66007] = logits[:8].to(DEV)
     u = u[:8].to(DEV)
     want = cpe.cp_token_sample(logits[:8].to(DEV), u, top_k=50, top_p=0.9)["tokens"]
-    assert torch.equal(cpe.cp_token_sample(wide[:, 7:33007], u, top_k=50, top_p=0.9)["tokens"], want)
+    assert torch.equal(cpe.cp_token_sample(wide[:, 7:66007], u, top_k=50, top_p=0.9)["tokens"], want)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        out = cpe.cp_token_sample(wide[:, 7:33007], u, top_k=50, top_p=0.9)
+        out = cpe.cp_token_sample(wide[:, 7:66007], u, top_k=50, top_p=0.9)
     for turn in range(3):
         u.copy_(torch.rand(u.shape, generator=torch.Generator().manual_seed(turn)))
-        want = cpe.cp_token_sample(wide[:, 7:33007], u, top_k=50, top_p=0.9)["tokens"]
+        want = cpe.cp_token_sample(wide[:, 7:66007], u, top_k=50, top_p=0.9)["tokens"]
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
