@@ -138,7 +138,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
     const int32_t slice = group % p.slices, head = group / p.slices % p.heads, seg = group / p.slices / p.heads;
     if (seg >= p.segments) return;                     // (the whole workgroup)
     const int c0 = slice * kWide, mine = 16 * NT * wave, col = c0 + mine + l;
-    const float lg = lg_of(p.log_decay ? p.log_decay[head] : 0.0f);
+    const Decay lg = decay_of(p.log_decay ? p.log_decay[head] : 0.0f);
 
     int64_t lo, hi;
     segment_of(p, seg, lo, hi);
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
 
     const RowsOf<T, 32 * KB, R, kThreadsHere, EVEN> a_rows(p.a, head, p.back, 0, p.wa), b_rows(p.b, head, p.back, 0, p.wa);
     const RowsOf<T, kWide, R, kThreadsHere, EVEN> x_rows(p.x, head, p.back, c0, p.wb), d_rows(p.d, head, p.back, c0, p.wb);
-    const bool remembers = lg * R > -40.0f;            // whether what lies before a chunk counts behind it (2^-40: no more in 32 bits)
+    const bool remembers = lg.hi * R > -40.0f;            // whether what lies before a chunk counts behind it (2^-40: no more in 32 bits)
     while (lo < hi) {
         const Piece piece = piece_at(p, lo, hi);
         int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(Step p) {
     const T *k = (const T *)p.k.at + seq * p.k.ld + (head / p.k.group) * p.k.hd;
     const T *v = (const T *)p.v.at + seq * p.v.ld + (head / p.v.group) * p.v.hd;
     for (int c = threadIdx.x; c < p.wk; c += kThreads) kq[0][c] = (float)k[c], kq[1][c] = (float)q[c];
-    const float by = power(lg_of(p.log_decay ? p.log_decay[head] : 0.0f), 1);
+    const float by = power(decay_of(p.log_decay ? p.log_decay[head] : 0.0f), 1);
     const int lanes = (p.wv + V - 1) / V, side = kThreads / lanes;      // (wv is a multiple of V; lanes <= 256)
     const int mine = threadIdx.x % lanes, first = threadIdx.x / lanes;
     float *state = p.state + ((int64_t)slot * p.heads + head) * ((int64_t)p.wk * p.wv) + mine * V;
