@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -30,15 +32,22 @@ def is_stale() -> bool:
 def build_library(force: bool = True, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
-    cmd = [_hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Wall", "-Wno-unused-function",
-           # packed-FP32 instruction forms are kept out of all device code
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True, cwd=CSRC)
+    compile_ = [_hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+                "-Wall", "-Wno-unused-function",
+                # packed-FP32 instruction forms are kept out of all device code
+                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True, cwd=CSRC)
+
+    # Each source by itself, several at once, the longest first: the whole takes as long as linear_attention.hip (1.5 of 6 minutes).
+    with tempfile.TemporaryDirectory() as room, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        objects = {s: os.path.join(room, s + ".o") for s in SOURCES}
+        for done in [pool.submit(run, [*compile_, "-c", os.path.join(CSRC, s), "-o", objects[s]]) for s in reversed(SOURCES)]:
+            done.result()
+        run([_hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *objects.values(), "-o", LIB])
     return LIB
 
 
