@@ -1059,8 +1059,8 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
     const hipStream_t st = (hipStream_t)stream;
     if (own) hipLaunchKernelGGL(clear_sampling_kernel, dim3(1), dim3(1), 0, st, status_out);
     if (rows == 0 || given == 0) return launched();
-    // (only where a row may keep few places)
-    const int32_t slices = top_ks || top_ps || (top_k > 0 && top_k <= kSliced) || top_p == 0.0 ? slices_of(rows, vocab) : 0;
+    // (only where a row may keep few places; not for the sake of a row's own top_p of 0)
+    const int32_t slices = top_ks || (top_k > 0 && top_k <= kSliced) || (!top_ps && top_p == 0.0) ? slices_of(rows, vocab) : 0;
     const Draw d{rows, vocab, (vocab + 63) / 64, logits, ld, allow, {scale, top_p, min_p, top_k, scales, top_ps, min_ps, top_ks}, given, u,
                  u_row_stride, u_stride, tokens, token_type, token_row_stride, token_stride, logp, status_out, slices, slice_size_of(vocab),
                  (uint64_t *)workspace, (int32_t *)((char *)workspace + (slices ? found_bytes(rows, slices) : 0))};
