@@ -581,8 +581,8 @@ int cp_recurrence_step(int32_t num_seq, int32_t width, int type, const void *f, 
  *   carry         [cp_linear_attention_carry_states][heads][width_k][width_v] for the backward pass, or NULL
  *   status_out    device int32, required with seq_ptr: CP_STATUS_BAD_SEQUENCE where seq_ptr does not rise from 0 to at most
  *                 rows (no access leaves the arrays)
- * Products of 16-bit elements are exact, and summed in 32 bits.  With 16-bit types, states and scores enter the products for o as
- * the sum of two bf16, off by at most 2^-15 of their value; rows on their way to a state keep all 24 bits.  An infinity or a NaN
+ * Products of 16-bit elements are exact, and summed in 32 bits.  States, scores and rows on their way to a state enter products with all
+ * 24 bits (against fp16 elements but for what is below 2^-23 of a product).  An infinity or a NaN
  * makes what follows from it, from its row to its sequence's end and in its head (or those that share it), infinite or NaN, and
  * nothing else.
  * Errors: CP_ERR_ARG (type, reverse), CP_ERR_SIZE (rows < 0 or >= 2^31, widths, heads, num_seq < 1, num_seq * heads of equal

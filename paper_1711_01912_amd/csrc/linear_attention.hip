@@ -119,18 +119,21 @@ template <typename T, int KB, int NT, int WAVES, int R, Kind kind, bool EVEN>
 __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad ? 4 : 2) void pass_kernel(Pass p, float *effect, float *gain) {
     using F = Form<T>;
     using E = typename F::E;
-    constexpr int P = F::kPlanes, PS = F::kSplit, PI = kind == kGrad || kind == kLeave ? F::kFine : F::kSplit, PU = F::kFine;
+    constexpr int P = F::kPlanes, PS = F::kSplit;
     constexpr bool kAhead = kind == kEffect || (kind == kGrad ? KB == 2 && sizeof(T) == 2 : KB * NT != 8 || KB == 8);
     constexpr int kThreadsHere = WAVES * kWave, kWide = 16 * NT * WAVES, IT = R / 16, JB = R / 32;
     __shared__ Tile<E, P, 32 * KB, R, false> b_tile;
     __shared__ Tile<E, P, kWide, R, false> x_tile;
-    __shared__ Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R, true> a_tile;
-    // scores [row][place], in the place of q's rows
+    // Scores [row][place] take the place of a's rows (and d's) when these have been read: three parts and the rows together would leave
+    // room for one workgroup of bf16 heads of 128 a compute unit.
     using Scores = Tile<E, PS, kind == kEffect ? 8 : R, kind == kEffect ? 1 : R, true>;
+    using First = Tile<E, P, kind == kEffect ? 8 : 32 * KB, kind == kEffect ? 1 : R, true>;
     using Third = Tile<E, P, kind == kGrad ? kWide : 8, kind == kGrad ? R : 1, true>;
-    __shared__ __attribute__((aligned(16))) char shared_[sizeof(Scores) > sizeof(Third) ? sizeof(Scores) : sizeof(Third)];
+    constexpr size_t kFirst = sizeof(First) + (kind == kGrad ? sizeof(Third) : 0);
+    __shared__ __attribute__((aligned(16))) char shared_[kFirst > sizeof(Scores) ? kFirst : sizeof(Scores)];
+    First &a_tile = *(First *)shared_;
+    Third &d_tile = *(Third *)(shared_ + (kind == kGrad ? sizeof(First) : 0));
     Scores &s_tile = *(Scores *)shared_;
-    Third &d_tile = *(Third *)shared_;
     __shared__ int odd[2];
 
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), l = lane % 16, g = lane / 16;
@@ -183,8 +186,6 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                 const int apart = 16 * (it - jt) + l - 4 * g - e;
                 apart_[k][e] = apart < 0 ? 0.0f : power(lg, apart) * p.s_in;
             }
-            // (right of a diagonal's tile, in its block of 32, lies one that is never written again, unless q's rows are)
-            if (kind != kGrad && it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
         }
 #pragma unroll
         for (int it = 0; it < IT; it++) in_[it] = power(lg, 16 * it + l + 1 - p.shift);
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
 
             f32x4 o[NT][IT];
             if constexpr (kind != kEffect) {
-                // scores of rows i (lanes) and j (places): the tiles on and below the diagonal, shared out
+                // scores of rows i (lanes) and j (places): the tiles on and below the diagonal, shared out, in registers until a's rows have been read
                 f32x4 score[kMine];
 #pragma unroll
                 for (int m = 0; m < kMine; m++) {
@@ -288,18 +289,8 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                             if (apart > 0) sum += (float)apart * c[e] * other[e];
                         }
                         decay_sum += (double)(sum * p.s_out);
-                        score[m] = c;
-                    } else s_tile.keep(16 * it + l, 16 * jt + 4 * g, c);
-                }
-                if constexpr (kind == kGrad) {
-                    __syncthreads();
-#pragma unroll
-                    for (int m = 0; m < kMine; m++) {
-                        int it, jt;
-                        if (!tile_of(m, it, jt)) continue;
-                        s_tile.keep(16 * it + l, 16 * jt + 4 * g, score[m]);
-                        if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
                     }
+                    score[m] = c;
                 }
                 // what the state that enters gives, 32 of its rows at a time
                 f32x4 more[NT][kind == kGrad ? IT : 1];
@@ -322,7 +313,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                     asked();
 #pragma unroll
                     for (int t = 0; t < NT; t++) {
-                        Frag<E, PI> sf;
+                        Frag<E, PS> sf;
                         split(s.at[t][2 * k], s.at[t][2 * k + 1], sf);
                         products<true>(af[k % 2], sf, o[t]);
                         if constexpr (kind == kGrad) {
@@ -360,6 +351,15 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                             decay_sum += (double)(sum * p.s_out);
                         }
                     }
+                }
+                __syncthreads();
+#pragma unroll
+                for (int m = 0; m < kMine; m++) {
+                    int it, jt;
+                    if (!tile_of(m, it, jt)) continue;
+                    s_tile.keep(16 * it + l, 16 * jt + 4 * g, score[m]);
+                    // (right of a diagonal's tile, in its block of 32)
+                    if (it == jt && it % 2 == 0) s_tile.keep(16 * it + l, 16 * jt + 16 + 4 * g, f32x4{0, 0, 0, 0});
                 }
                 __syncthreads();
             }
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
 #pragma unroll
                     for (int e = 0; e < 8; e++) by[e] = power(lg, behind(jb, e, count) + p.shift) * p.s_in;      // (rows behind the chunk's are zeros)
                 }
-                Frag<E, PU> vf[NT];
+                Frag<E, PS> vf[NT];
 #pragma unroll
                 for (int t = 0; t < NT; t++) {
                     float v[8];

@@ -126,23 +126,22 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Elements as the matrix instructions take them.  bf16 as it is; fp16 as the sum of two bf16, which is exact; what is computed in 32
-// bits as the sum of bf16 too: of two, off by at most 2^-15, where the result has 16 bits itself (states and scores on their way to an output),
-// of three, which is exact, where it has 32 (rows on their way to a state, all that the decays' gradient is made of).  float as it is,
-// through the float instructions.
+// bits (states, scores, decayed rows) as the sum of three bf16, which is exact too: two would be off by up to 2^-16, and round an output in 16
+// bits to the wrong side of a middle about once in 500.  float as it is, through the float instructions.
 template <typename T>
 struct Form {
     using E = bf16;
-    static constexpr int kPlanes = 1, kSplit = 2, kFine = 3;
+    static constexpr int kPlanes = 1, kSplit = 3;
 };
 template <>
 struct Form<f16> {
     using E = bf16;
-    static constexpr int kPlanes = 2, kSplit = 2, kFine = 3;
+    static constexpr int kPlanes = 2, kSplit = 3;
 };
 template <>
 struct Form<float> {
     using E = float;
-    static constexpr int kPlanes = 1, kSplit = 1, kFine = 1;
+    static constexpr int kPlanes = 1, kSplit = 1;
 };
 
 // 16 x 32 of a matrix in a wavefront: lane l holds, of row (or column) l % 16, places 4 (l / 16) + 0..3 and 16 + 4 (l / 16) + 0..3.
