@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kFewThreads) void few_sample_kernel(Draw d) {
     __syncthreads();
     // The draws: a wavefront a row where a row has many, else one after the other
     const int64_t row0 = (int64_t)group_number() * kRowsHere;
-    const int rows = (int)min((int64_t)kRowsHere, d.rows - row0);
+    const int rows = (int)min((int64_t)kRowsHere, max(d.rows - row0, (int64_t)0));      // (none of a grid's last row that are too many)
     if (d.given >= kWave) {
         const int wlane = threadIdx.x % kWave;
         for (int r = threadIdx.x / kWave; r < rows; r += kFewThreads / kWave) draw_row<TT>(d, row0 + r, border[r], lp[r], empty[r], wlane, kWave);
