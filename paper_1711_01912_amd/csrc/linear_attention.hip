@@ -779,16 +779,12 @@ bool meet(const Heads &a, const Heads &b, int64_t rows, int type) {
     const bool alike = (rows == 1 || a.ld == b.ld) && (a.heads == 1 || b.heads == 1 || a.hd == b.hd);
     if (!alike || (rows > 1 && a.ld == 0)) return share(extent(a, rows, type), extent(b, rows, type));
     const int64_t ld = a.ld * each, hd = (a.heads > 1 ? a.hd : b.hd) * each, apart = (int64_t)(uintptr_t)b.at - (int64_t)(uintptr_t)a.at;
-    const auto touch = [&](int64_t off) { return off < a.width * each && off > -b.width * each; };
+    const int64_t most = a.width * each - 1, least = 1 - b.width * each;      // how far behind one of a's heads one of b's may begin to touch it
+    const auto upto = [&](int64_t off) { return off >= 0 ? off / ld : -((ld - 1 - off) / ld); };      // whole rows
     for (int64_t h = 1 - (int64_t)b.heads; h < a.heads; h++) {
-        // one of b's heads lies `off` bytes behind one of a's in a row, and `rows` rows on by multiples of ld
+        // one of b's heads lies `off` bytes behind one of a's in a row, and r rows on (a's rows may overlap) off + r ld
         const int64_t off = apart - h * hd;
-        if (rows == 1) {
-            if (touch(off)) return true;
-            continue;
-        }
-        for (int64_t r = -off / ld - 1; r <= -off / ld + 1; r++)
-            if (r > -rows && r < rows && touch(off + r * ld)) return true;
+        if (rows == 1 ? least <= off && off <= most : std::max(-upto(off - least), 1 - rows) <= std::min(upto(most - off), rows - 1)) return true;
     }
     return false;
 }
