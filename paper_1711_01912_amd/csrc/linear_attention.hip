@@ -593,7 +593,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(Step p) {
     const T *k = (const T *)p.k.at + seq * p.k.ld + (head / p.k.group) * p.k.hd;
     const T *v = (const T *)p.v.at + seq * p.v.ld + (head / p.v.group) * p.v.hd;
     for (int c = threadIdx.x; c < p.wk; c += kThreads) kq[0][c] = (float)k[c], kq[1][c] = (float)q[c];
-    const float by = power(decay_of(p.log_decay ? p.log_decay[head] : 0.0f), 1);
+    const Fade fade = fade_of(decay_of(p.log_decay ? p.log_decay[head] : 0.0f), 1);      // (4,000 steps of gamma in 32 bits: 1e-4 off)
     const int lanes = (p.wv + V - 1) / V, side = kThreads / lanes;      // (wv is a multiple of V; lanes <= 256)
     const int mine = threadIdx.x % lanes, first = threadIdx.x / lanes;
     float *state = p.state + ((int64_t)slot * p.heads + head) * ((int64_t)p.wk * p.wv) + mine * V;
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(Step p) {
             Pack<float, V> s = load_pack<float, V>(state + (int64_t)row * p.wv);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                s.v[e] = fmaf(by, s.v[e], kq[0][row] * value[e]);
+                s.v[e] = fmaf(kq[0][row], value[e], faded(s.v[e], fade));
                 sum[e] = fmaf(kq[1][row], s.v[e], sum[e]);
             }
             store_pack<float, V>(state + (int64_t)row * p.wv, s);

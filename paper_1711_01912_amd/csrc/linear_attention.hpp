@@ -119,6 +119,18 @@ __device__ __forceinline__ float power(const Decay &d, int n) {
 // would add up along a head's whole memory
 __device__ __forceinline__ float power_less_one(const Decay &d, int n) { return expm1f(d.log * (float)n); }
 
+// A state times gamma^n: of a decay above a half as S + S (gamma^n - 1), see above; of one below, where that difference would lose what it
+// has fewer bits than, by gamma^n itself
+struct Fade {
+    float by;
+    bool near;
+};
+__device__ __forceinline__ Fade fade_of(const Decay &d, int n) {
+    const float less = power_less_one(d, n);
+    return less >= -0.5f ? Fade{less, true} : Fade{power(d, n), false};
+}
+__device__ __forceinline__ float faded(float s, const Fade &f) { return fmaf(s, f.by, f.near ? s : 0.0f); }
+
 // ---- fragments ---------------------------------------------------------------------------------------
 
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));

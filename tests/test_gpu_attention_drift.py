@@ -1,0 +1,55 @@
+"""States of cp_linear_attention over many steps, segments and chunks: decays close to one, whose rounding would add up, and decays of a state
+alone.
+
+Errors of rounding are as often above as below; what adds up is told by the part of a state's error that points along the state,
+c = <S - ref, ref> / <ref, ref>.  Each rounding is off by at most U = 2^-24 of its value, so that the sum of n roundings of each of M normal values
+has along the state a standard deviation of at most U sqrt(3 n / M), of which six are allowed (Hoeffding: 3e-8 to be further off)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1711_01912_amd as cpe
+from policy_util import TYPES, U, wide
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SLOW = [-1e-5, -1e-6, -7e-6, -3e-5, -2e-4]
+
+
+def along(got, ref):
+    return abs(float(((wide(got) - ref) * ref).sum() / (ref * ref).sum()))
+
+
+def allowed(roundings, values, log_decay, rows):
+    # (gamma^n - 1 is off by at most 2^-21 of itself: expm1 and its argument)
+    return 6 * U * np.sqrt(3 * roundings / values) + 2.0 ** -21 * abs(log_decay) * rows
+
+
+def alike(log_decay, steps):
+    """What the roundings of successive steps add where they are no longer independent of each other.  A step takes m |log_decay| of a state's
+    last places from it, m from 2^23 to 2^24, and what is rounded off is the fraction of that.  Here m changes by 1/64 of itself a step (states of
+    64, what is added of 1): the fraction moves by 2^23 |log_decay| / 64 and more, which makes it another one if that is above a half.  Below, at
+    -1e-6 by 0.13, the same fraction is rounded off again and again, at most half a last place or U of the state each time, the same way.  (The
+    formula with correct rounding, on the CPU, is off by 2.2e-6 there, and by at most 2.2e-7 for the other decays.)"""
+    return steps * U if 2.0 ** 23 * abs(log_decay) / 64 < 0.5 else 0.0
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_steps(dtype):
+    N, H, K = 4000, len(SLOW), 64
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(N, H, K, generator=g).to(TYPES[dtype]) for _ in range(3))
+    h0 = torch.randn(1, H, K, K, generator=g) * 64
+    log_decay = torch.tensor(SLOW)
+    gamma, ref = np.exp(wide(log_decay))[:, None, None], wide(h0)[0]
+    for t in range(N):
+        ref = gamma * ref + wide(k[t])[:, :, None] * wide(v[t])[:, None, :]
+    q, k, v, state, log_decay = (t.to(DEV) for t in (q, k, v, h0, log_decay))
+    last = cpe.cp_linear_attention(q, k, v, log_decay, h0=state, want_last=True)["last"]
+    state = state.clone()
+    for t in range(N):
+        cpe.cp_linear_attention_step(q[t:t + 1], k[t:t + 1], v[t:t + 1], state, log_decay)
+    for h in range(H):
+        # a step rounds a state twice
+        assert along(state[0, h], ref[h]) <= allowed(2 * N, K * K, SLOW[h], N) + alike(SLOW[h], N), ("step", SLOW[h], along(state[0, h], ref[h]))
+        assert along(last[0, h], ref[h]) <= allowed(2 * N, K * K, SLOW[h], N), ("last", SLOW[h], along(last[0, h], ref[h]))
