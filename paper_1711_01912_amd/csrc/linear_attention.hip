@@ -116,7 +116,7 @@ struct State {
 // KB: blocks of 32 that the state's rows fill; NT: of 16 columns that a wavefront has; WAVES: of a workgroup; R: rows of a chunk;
 // EVEN: widths are multiples of 8
 template <typename T, int KB, int NT, int WAVES, int R, Kind kind, bool EVEN>
-__global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad ? 4 : 2) void pass_kernel(Pass p, float *effect, float *gain) {
+__global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad ? 4 : 2) void pass_kernel(Pass p, float *effect, Gain *gain) {
     using F = Form<T>;
     using E = typename F::E;
     constexpr int P = F::kPlanes, PS = F::kSplit;
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             ends = last.starts, whole = !last.ends;    // (its end and its start, seen from there)
             lo = last.lo, hi = last.hi;
         }
-        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = whole && !ends ? power(lg, (int)(hi - lo)) : -1.0f;
+        if (threadIdx.x == 0 && slice == 0) gain[(int64_t)seg * p.heads + head] = {fade_of(lg, (int)(hi - lo)), !whole || ends};
         if (ends) lo = hi;
     }
     // What does not change from chunk to chunk: the decays between a score's rows, of this wavefront's tiles, into rows from before
@@ -469,12 +469,12 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
     }
 }
 
-// States that enter the segments, from their effects, in place and in the order of the pass: E' = gain E + U.  A gain below 0
-// drops the state before it (a sequence began), whatever it holds; one of 0 does not, as 0 times a NaN is one.  Sixteen segments' loads are
-// under way at once: 256 segments of 4 heads of 64 x 64 in 35 us, 45 with the next one's alone; 37 with 32 of half the width, 49 with 64 of a
+// States that enter the segments, from their effects, in place and in the order of the pass: E' = gamma^n E + U.  Where a sequence began, the
+// state before it is dropped, whatever it holds; a gamma^n of 0 does not do that, as 0 times a NaN is one.  (gamma^n in 32 bits is off by
+// the same in every segment: by 3e-5 of a state after 1,024.)  Sixteen segments' loads are under way at once: 256 segments of 4 heads of 64 x 64 in 35 us, 45 with the next one's alone; 37 with 32 of half the width, 49 with 64 of a
 // quarter.
 template <int V>
-__global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float *gain, int32_t segments, int32_t heads, int32_t size, bool back) {
+__global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const Gain *gain, int32_t segments, int32_t heads, int32_t size, bool back) {
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * V;
     if (i >= size) return;
     const int32_t head = blockIdx.y;
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float 
     const auto segment = [&](int32_t n) { return (int64_t)(back ? segments - 1 - n : n) * heads + head; };
     for (int32_t n0 = 0; n0 < segments; n0 += kAhead) {
         Pack<float, V> u[kAhead];
-        float by[kAhead];
+        Gain by[kAhead];
 #pragma unroll
         for (int a = 0; a < kAhead; a++) {
             const int32_t n = min(n0 + a, segments - 1);
@@ -497,7 +497,7 @@ __global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const float 
             if (n0 + a >= segments) break;
             store_pack<float, V>(at + segment(n0 + a) * size + i, e);
 #pragma unroll
-            for (int k = 0; k < V; k++) e.v[k] = by[a] < 0.0f ? u[a].v[k] : fmaf(by[a], e.v[k], u[a].v[k]);
+            for (int k = 0; k < V; k++) e.v[k] = by[a].drops ? u[a].v[k] : faded(e.v[k], by[a].fade) + u[a].v[k];
         }
     }
 }
@@ -660,7 +660,7 @@ int32_t columns_of(int32_t wa, int32_t wb) { return wb > 64 || wa > 128 ? 128 : 
 int32_t slices_of(int32_t wa, int32_t wb) { return (wb + columns_of(wa, wb) - 1) / columns_of(wa, wb); }
 
 template <typename T, int KB, int COLUMNS, bool EVEN>
-int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t st) {
+int run_sized(Kind kind, const Pass &p, float *effect, Gain *gain, hipStream_t st) {
     // Columns a wavefront: 32 of bf16 heads of up to 128, whose operands then serve two products (65,536 rows of 16 heads of 128 forward 504 us, 605 with 16;
     // 8 x 4,096 rows forward and backward 1.15 ms, 1.26).  The other types' operands, of two or three parts or in 32 bits, leave no registers for it.
     // Rows of a chunk: 32 where 64 leave LDS for one workgroup a compute unit, or none, and for bf16 heads of up to 64, of which four
@@ -681,7 +681,7 @@ int run_sized(Kind kind, const Pass &p, float *effect, float *gain, hipStream_t 
     return launched();
 }
 
-int run(Kind kind, int type, Pass p, float *effect, float *gain, hipStream_t st) {
+int run(Kind kind, int type, Pass p, float *effect, Gain *gain, hipStream_t st) {
     const bool even = p.wa % 8 == 0 && p.wb % 8 == 0, wide = columns_of(p.wa, p.wb) == 128;
     p.slices = slices_of(p.wa, p.wb);
     return by_type(type, [&](auto t) {
@@ -695,7 +695,7 @@ int run(Kind kind, int type, Pass p, float *effect, float *gain, hipStream_t st)
 }
 
 // the states that enter the pass's segments, into `at`
-int run_enter(int type, const Pass &p, float *at, float *gain, hipStream_t st) {
+int run_enter(int type, const Pass &p, float *at, Gain *gain, hipStream_t st) {
     const int rc = run(kEffect, type, p, at, gain, st);
     if (rc) return rc;
     const int32_t size = p.wa * p.wb;
@@ -726,7 +726,7 @@ int check(const Shape &s, int reverse) {
 size_t state_floats(const Shape &s) { return (size_t)s.heads * s.wk * s.wv; }
 // of the states that enter segments, and of their gains
 size_t enter_bytes(const Shape &s, const Cut &c) { return c.split ? align_up(c.segments * state_floats(s) * sizeof(float)) : 0; }
-size_t gain_bytes(const Shape &s, const Cut &c) { return c.split ? align_up((size_t)c.segments * s.heads * sizeof(float)) : 0; }
+size_t gain_bytes(const Shape &s, const Cut &c) { return c.split ? align_up((size_t)c.segments * s.heads * sizeof(Gain)) : 0; }
 // (of the passes for dq and dk, both of width_k columns)
 int64_t part_count(const Shape &s, const Cut &c) { return 2 * (int64_t)c.segments * slices_of(s.wv, s.wk); }
 size_t part_bytes(const Shape &s, const Cut &c) { return align_up((size_t)s.heads * part_count(s, c) * sizeof(double)); }
@@ -872,7 +872,8 @@ int cp_linear_attention(int64_t rows, int32_t num_seq, const int32_t *seq_ptr, i
     p.a = {q, ldq, hdq, 1}, p.b = {k, ldk, hdk, heads / kv_heads}, p.x = {v, ldv, hdv, heads / kv_heads};
     p.init = h0, p.last = last, p.o = o, p.ldo = ldo, p.hdo = hdo;
     if (c.split) {
-        float *gain = (float *)workspace, *at = carry ? carry : (float *)((char *)workspace + gain_bytes(s, c));
+        Gain *gain = (Gain *)workspace;
+        float *at = carry ? carry : (float *)((char *)workspace + gain_bytes(s, c));
         rc = run_enter(type, p, at, gain, st);
         if (rc) return rc;
         p.enter = at;
@@ -917,7 +918,8 @@ int cp_linear_attention_backward(int64_t rows, int32_t num_seq, const int32_t *s
         hipLaunchKernelGGL(empty_kernel, dim3((unsigned)std::min(num_seq, 4096), 32), dim3(kThreads), 0, st, seq_ptr, rows / num_seq, num_seq,
                            (int64_t)state_floats(s), dlast, dh0);
     char *room = (char *)workspace;
-    float *gain = (float *)room, *denter = (float *)(room + gain_bytes(s, c));
+    Gain *gain = (Gain *)room;
+    float *denter = (float *)(room + gain_bytes(s, c));
     double *part = (double *)(room + gain_bytes(s, c) + enter_bytes(s, c));
     float *share = (float *)((char *)part + part_bytes(s, c));
     const int32_t group = heads / kv_heads;

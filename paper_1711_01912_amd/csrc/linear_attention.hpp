@@ -131,6 +131,12 @@ __device__ __forceinline__ Fade fade_of(const Decay &d, int n) {
 }
 __device__ __forceinline__ float faded(float s, const Fade &f) { return fmaf(s, f.by, f.near ? s : 0.0f); }
 
+// What a segment does to the state before it
+struct Gain {
+    Fade fade;
+    bool drops;                          // none of it is left: a sequence began
+};
+
 // ---- fragments ---------------------------------------------------------------------------------------
 
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));

@@ -53,3 +53,22 @@ def test_steps(dtype):
         # a step rounds a state twice
         assert along(state[0, h], ref[h]) <= allowed(2 * N, K * K, SLOW[h], N) + alike(SLOW[h], N), ("step", SLOW[h], along(state[0, h], ref[h]))
         assert along(last[0, h], ref[h]) <= allowed(2 * N, K * K, SLOW[h], N), ("last", SLOW[h], along(last[0, h], ref[h]))
+
+
+@pytest.mark.parametrize("low", [-1e-6, -3e-6, -1e-5])
+def test_segments(low):
+    # 1,024 segments of 128 rows of one head: two roundings each, and the last segment's chunks
+    N, K = 131072, 64
+    g = torch.Generator().manual_seed(2)
+    q, k, v, do = (torch.randn(N, 1, K, generator=g) for _ in range(4))
+    h0, dlast = (torch.randn(1, 1, K, K, generator=g) * 4096 for _ in range(2))
+    log_decay = torch.tensor([low])
+    worn = np.exp(float(log_decay[0]) * np.arange(N + 1))
+    last = worn[N] * wide(h0)[0, 0] + (wide(k)[:, 0] * worn[N - 1::-1, None]).T @ wide(v)[:, 0]
+    dh0 = worn[N] * wide(dlast)[0, 0] + (wide(q)[:, 0] * worn[1:, None]).T @ wide(do)[:, 0]
+    q, k, v, do, h0, dlast, log_decay = (t.to(DEV) for t in (q, k, v, do, h0, dlast, log_decay))
+    out = cpe.cp_linear_attention(q, k, v, log_decay, h0=h0, want_last=True, want_carry=True)
+    assert out["carry"].shape[0] == 1024
+    back = cpe.cp_linear_attention_backward(do, q, k, v, log_decay, out["carry"], h0=h0, dlast=dlast)
+    for got, ref, name in ((out["last"], last, "last"), (back["dh0"], dh0, "dh0")):
+        assert along(got[0, 0], ref) <= allowed(2 * 1030, K * K, low, N), (name, along(got[0, 0], ref))
