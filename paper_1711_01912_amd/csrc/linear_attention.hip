@@ -94,14 +94,13 @@ struct State {
         each(p, index, head, col, g, [&](float v, int64_t i) { return sum += (double)(v * with[i]), v; });
         return sum;
     }
-    // (off by half a step of the state: see power_less_one)
-    __device__ __forceinline__ void decay(float less_one) {
+    __device__ __forceinline__ void decay(const Fade &fade) {
 #pragma unroll
         for (int t = 0; t < NT; t++)
 #pragma unroll
             for (int k = 0; k < 2 * KB; k++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) at[t][k][e] = fmaf(at[t][k][e], less_one, at[t][k][e]);
+                for (int e = 0; e < 4; e++) at[t][k][e] = faded(at[t][k][e], fade);
     }
     __device__ __forceinline__ void add(const State &s, float by) {
 #pragma unroll
@@ -195,7 +194,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
     for (int jb = 0; jb < JB; jb++)
 #pragma unroll
         for (int e = 0; e < 8; e++) out_[jb][e] = power(lg, behind(jb, e, R) + p.shift) * p.s_in;
-    const float wane_ = power_less_one(lg, R);
+    const Fade wane_ = fade_of(lg, R);
 
     const RowsOf<T, 32 * KB, R, kThreadsHere, EVEN> a_rows(p.a, head, p.back, 0, p.wa), b_rows(p.b, head, p.back, 0, p.wa);
     const RowsOf<T, kWide, R, kThreadsHere, EVEN> x_rows(p.x, head, p.back, c0, p.wb), d_rows(p.d, head, p.back, c0, p.wb);
@@ -406,8 +405,8 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             }
 
             // the state behind the chunk
-            float wane = wane_;
-            if (count != R) wane = power_less_one(lg, count);
+            Fade wane = wane_;
+            if (count != R) wane = fade_of(lg, count);
             if constexpr (kind == kGrad) {
                 r.add(s, (float)count);
                 r.decay(wane);

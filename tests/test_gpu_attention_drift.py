@@ -72,3 +72,28 @@ def test_segments(low):
     back = cpe.cp_linear_attention_backward(do, q, k, v, log_decay, out["carry"], h0=h0, dlast=dlast)
     for got, ref, name in ((out["last"], last, "last"), (back["dh0"], dh0, "dh0")):
         assert along(got[0, 0], ref) <= allowed(2 * 1030, K * K, low, N), (name, along(got[0, 0], ref))
+
+
+@pytest.mark.parametrize("N", [1, 5, 33, 64, 70, 150])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_state_that_nothing_is_added_to(dtype, N):
+    # each chunk multiplies it by a power of gamma that is off by at most 2^-22, and rounds
+    log_decay = torch.tensor([-0.3, -0.69, -0.7, -2.0, -5.0])
+    H, K, V = 5, 32, 40
+    g = torch.Generator().manual_seed(N)
+    r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    q, k, v, do = r(N, H, K), torch.zeros(N, H, K), r(N, H, V), torch.zeros(N, H, V)
+    q, k, v, do = (t.to(TYPES[dtype]).to(DEV) for t in (q, k, v, do))
+    h0, dlast = r(1, H, K, V), r(1, H, K, V)
+    kw = dict(h0=h0.to(DEV))
+    out = cpe.cp_linear_attention(q, k, v, log_decay.to(DEV), want_last=True, want_carry=True, **kw)
+    back = cpe.cp_linear_attention_backward(do, q, k, v, log_decay.to(DEV), out["carry"], dlast=dlast.to(DEV), **kw)
+    state = h0.to(DEV)
+    for t in range(N):
+        cpe.cp_linear_attention_step(q[t:t + 1], k[t:t + 1], v[t:t + 1], state, log_decay.to(DEV))
+    gamma = np.exp(wide(log_decay) * N)[None, :, None, None]
+    for got, ref, times, name in ((out["last"], gamma * wide(h0), N // 32 + 2, "last"), (back["dh0"], gamma * wide(dlast), N // 32 + 2, "dh0"),
+                                  (state, gamma * wide(h0), N, "state")):
+        # (what is below the least normal number may be 0)
+        off = np.abs(wide(got) - ref) - (times * 2.0 ** -21 * np.abs(ref) + 2.0 ** -126)
+        assert (off <= 0).all(), (name, float((np.abs(wide(got) - ref) / np.abs(ref)).max()))
