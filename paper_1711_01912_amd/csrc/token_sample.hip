@@ -6,7 +6,8 @@
 //
 // The kept places are a beginning of that order: all above a logit, and the first few of those that equal it.  What is drawn is
 // a place, not a value that may be off by a rounding: probabilities and their sums are formed in 64 bits (on this chip
-// at the rate of 32), so that a draw differs from the definition only where u lies within 1e-12 of a border.
+// at the rate of 32), so that a draw differs from the definition only where u or top_p lies within 1e-12 of a border (top_p 2e-12 in
+// rows of 2^26 places).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -80,8 +81,8 @@ __device__ __forceinline__ float float_above(double v) {
     return (double)f < v ? __uint_as_float(__float_as_uint(f) + 1) : f;
 }
 
-// 2^t for t <= 0 with the relative error of a few roundings of 64 bits: Taylor's polynomial of 2^f, |f| <= 1/2, is off by 0.35^12 / 12! = 7e-15
-__device__ __forceinline__ double power_of_two(double t) {
+// 2^(t + up) for t <= 0 with the relative error of a few roundings of 64 bits: Taylor's polynomial of 2^f, |f| <= 1/2, is off by 0.35^12 / 12! = 7e-15
+__device__ __forceinline__ double power_of_two(double t, int up = 0) {
     const double n = __builtin_rint(fmax(t, -1080.0)), f = (fmax(t, -1080.0) - n) * 0.69314718055994530942;
     double p = 1.0 / 39916800;
     p = fma(p, f, 1.0 / 3628800);
@@ -95,7 +96,7 @@ __device__ __forceinline__ double power_of_two(double t) {
     p = fma(p, f, 0.5);
     p = fma(p, f, 1.0);
     p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    return ldexp(p, (int)n + up);
 }
 constexpr double kLog2eWide = 1.44269504088896340736;
 
@@ -626,7 +627,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
         }
         return;
     }
-    // adds a place to the list; true if there was room
+    // adds a place to the list, if there is room
     const auto note = [&](float x, int32_t v) {
         const int at = atomicAdd(&counted_, 1);
         if (at < kListed) list[at] = listed(M::key(x), v);
@@ -673,19 +674,30 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
     // The place in the order where what is kept ends: keys above `key_end`, and `keep_ties` of those that equal it
     uint32_t key_end = 0;
     int64_t keep_ties = INT64_MAX;
-    // mass in units so small that a sum of all places stays below 2^62: whole numbers, which add up the same in any order
-    const double unit = ldexp(1.0, 62 - (32 - __clz(V)));
-    const auto weight = [&](double p) { return (uint64_t)(p * unit + 0.5); };
+    // Masses are added up as whole numbers, which come to the same in any order: those of a step or a digit in units that its sum has just room
+    // for, and these sums in units of 2^-61 to 2^-62 of the whole row's.
+    const auto scale_of = [](double total) { return ldexp(1.0, 61 - ilogb(total)); };
+    const auto in_units = [](double mass, double scale) { return (uint64_t)(mass * scale + 0.5); };
     if (rule.top_p < 1.0 && rule.top_k == 0) {
-        // By how far places lie below the best: 256 steps of a twelfth of a power of two, the step in which top_p is reached again in 256, and so on until the
-        // places of a step are few, which are listed and put in order.
-        constexpr int kDepth = 6;
+        // By how far places lie below the best: 240 steps of a twelfth of a power of two and 16 of one, the step in which top_p is reached again in 256, and so
+        // on until the places of a step are few, which are listed and put in order.  A step's unit is 2^-bits of the mass of a place at its beginning, or
+        // of up to twice that, of which all its places have at least a quarter.  So a row's masses are off by 2^(1 - bits) of themselves, 3e-14 in rows of
+        // 2^20 places and 2e-12 in such of 2^26, however flat they are.  (With one unit for all steps 2e-7 and 1e-3; 512 x 65536 with settings of their own
+        // 186 us; 196 with one a step.)
+        constexpr int kDepth = 6, kFine = 240, kPer = 12, kRest = kFine - kFine / kPer;      // (wide steps: powers + kRest)
+        const int bits = 63 - (32 - __clz(min(V, V / kLanes + THREADS * kVec / kLanes)));      // (of a copy's lanes together, below 2^64)
         __shared__ double from[kDepth + 1], per[kDepth + 1];
         __shared__ int at[kDepth + 1];
         uint64_t above = 0;
-        double want = 0;
-        if (threadIdx.x == 0) from[0] = 0, per[0] = 12.0;
-        const auto step_of = [&](double depth, int level) { return (int)fmin(fmax((depth - from[level]) * per[level], 0.0), kSteps - 1.0); };
+        double want = 0, scale = 0;
+        const auto twelfths = [](int i) { return (int)(__umul24(i, 171) >> 11); };      // i / 12 below 512
+        const auto step_of = [&](double depth, int level) {
+            if (level > 0) return (int)fmin(fmax((depth - from[level]) * per[level], 0.0), kSteps - 1.0);
+            const int i = (int)fmin(depth * kPer, (kSteps - kRest) * kPer - 1.0);
+            return i < kFine ? i : twelfths(i) + kRest;
+        };
+        // whole powers of two that a step begins below the best, or the step that it is part of
+        const auto powers_of = [&](int step, int level) { return level > 0 ? (int)from[level] : step < kFine ? twelfths(step) : step - kRest; };
         const auto inside = [&](double depth, int level) {     // whether it lies in the step of all levels before this one
             bool in = true;
             for (int k = 0; k < level; k++) in &= step_of(depth, k) == at[k];
@@ -698,7 +710,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
             a.template each<2>([&](int32_t v, float x) {
                 const double depth = a.depth(x);
                 if (x > -INFINITY && inside(depth, level)) {
-                    atomicAdd((unsigned long long *)&bins[step_of(depth, level) * kLanes + lane % kLanes], (unsigned long long)weight(power_of_two(-depth)));
+                    const int step = step_of(depth, level);
+                    atomicAdd((unsigned long long *)&bins[step * kLanes + lane % kLanes],
+                              (unsigned long long)(power_of_two(-depth, bits + powers_of(step, level)) + 0.5));
                     if (level > 0) note(x, v);
                 }
             });
@@ -707,14 +721,24 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
             // (thread t has steps 256 / THREADS t and on)
             constexpr int kEach = THREADS < kSteps ? kSteps / THREADS : 1;
             uint64_t sum = 0, one[kEach];
+            double held[kEach], all = 0;
 #pragma unroll
             for (int e = 0; e < kEach; e++) {
-                one[e] = 0;
+                held[e] = 0;
                 const int step = (int)threadIdx.x * kEach + e;
-                if (step < kSteps)
-                    for (int k = 0; k < kLanes; k++) one[e] += bins[step * kLanes + k];
-                sum += one[e];
+                if (step < kSteps) {
+                    for (int k = 0; k < kLanes; k++) held[e] += (double)bins[step * kLanes + k];
+                    held[e] = ldexp(held[e], -bits - powers_of(step, level));
+                }
+                all += held[e];
             }
+            if (level == 0) {
+                double row_mass;
+                block.before(all, row_mass);
+                scale = scale_of(row_mass);
+            }
+#pragma unroll
+            for (int e = 0; e < kEach; e++) sum += one[e] = in_units(held[e], scale);
             uint64_t total;
             uint64_t front = above + block.before(sum, total);
             if (level == 0) want = (double)total * rule.top_p;
@@ -731,8 +755,13 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
             above = found_above;
             if (threadIdx.x == 0) {
                 at[level] = step;
-                from[level + 1] = from[level] + step / per[level];
-                per[level + 1] = step == kSteps - 1 && level == 0 ? kSteps / 1100.0 : per[level] * kSteps;
+                if (level == 0) {
+                    from[1] = step < kFine ? (double)step / kPer : step - kRest;
+                    per[1] = kSteps * (step < kFine ? kPer : step < kSteps - 1 ? 1.0 : 1 / 1100.0);
+                } else {
+                    from[level + 1] = from[level] + step / per[level];
+                    per[level + 1] = per[level] * kSteps;
+                }
                 counted_ = 0;
             }
             __syncthreads();
@@ -753,7 +782,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
             int kept = 0;
             for (int i0 = 0; i0 < few; i0 += THREADS) {
                 const int i = i0 + threadIdx.x;
-                const uint64_t w = i < few ? weight(a.share(M::value((uint32_t)(list[i] >> 32)))) : 0;
+                const uint64_t w = i < few ? in_units(a.share(M::value((uint32_t)(list[i] >> 32))), scale) : 0;
                 uint64_t all;
                 const uint64_t ahead = above + block.before(w, all);
                 kept += __syncthreads_count(i < few && (i == 0 || (double)ahead < want));
@@ -767,8 +796,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
     }
     if (keep_ties == INT64_MAX && (rule.top_k > 0 || rule.top_p < 1.0)) {
         // Many, or all alike: by the digits of their keys, from the highest on, first as many as top_k, then as much as top_p
-        const auto bin = [&](int i) { return bins[i] + bins[kBins + i]; };
-        const auto seek = [&](double want, uint64_t above) {
+        const auto count_in = [&](int i) { return bins[i] + bins[kBins + i]; };
+        const auto seek = [&](auto bin, double want, uint64_t above) {
             // (thread t has the t-th few bins from the top)
             constexpr int kEach = kBins / THREADS;
             uint64_t one[kEach], sum = 0, total;
@@ -800,7 +829,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
                     if (level == 0 || k >> (sh + width) == prefix) atomicAdd((unsigned int *)&bins[lane % kCopies * kBins + (k >> sh & ((1u << width) - 1))], 1u);
                 });
                 __syncthreads();
-                seek((double)rule.top_k, above);
+                seek(count_in, (double)rule.top_k, above);
                 prefix = prefix << width | (uint32_t)found_at, above = found_above;
             }
             key_end = prefix, keep_ties = (int64_t)rule.top_k - (int64_t)above;
@@ -808,9 +837,17 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
         if (rule.top_p < 1.0) {
             const uint32_t least = key_end;
             const int64_t least_ties = keep_ties;
+            // masses in two words: the places of a digit may be of any, so that one has too few bits for rows whose most lies in many unlikely places
+            const int bits = 63 - (32 - __clz(V));
+            const auto add = [&](int at, double mass) {
+                const double units = ldexp(mass, bits), whole = floor(units);
+                atomicAdd((unsigned long long *)&bins[at], (unsigned long long)whole);
+                atomicAdd((unsigned long long *)&bins[kBins + at], (unsigned long long)(ldexp(units - whole, bits) + 0.5));
+            };
+            const auto mass_in = [&](int i) { return ldexp((double)bins[i] + ldexp((double)bins[kBins + i], -bits), -bits); };
             uint64_t above = 0;
             uint32_t prefix = 0;
-            double want = 0;
+            double want = 0, scale = 0;
             for (int level = 0; level < M::kLevels; level++) {
                 const int sh = M::shift(level), width = level == 2 ? 10 : 11;
                 clear();
@@ -818,28 +855,33 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
                     const uint32_t k = M::key(x);
                     // (of those that equal the last of the top_k, added below, only some are left)
                     if (x > -INFINITY && (k > least || least_ties == INT64_MAX) && (level == 0 || k >> (sh + width) == prefix))
-                        atomicAdd((unsigned long long *)&bins[lane % kCopies * kBins + (k >> sh & ((1u << width) - 1))], (unsigned long long)weight(a.share(x)));
+                        add(k >> sh & ((1u << width) - 1), a.share(x));
                 });
                 __syncthreads();
                 if (threadIdx.x == 0 && least_ties != INT64_MAX && (level == 0 || least >> (sh + width) == prefix))
-                    bins[least >> sh & ((1u << width) - 1)] += (uint64_t)least_ties * weight(a.share(M::value(least)));
+                    add(least >> sh & ((1u << width) - 1), (double)least_ties * a.share(M::value(least)));
                 __syncthreads();
+                const auto units_in = [&](int i) { return in_units(mass_in(i), scale); };
                 if (level == 0) {
-                    uint64_t sum = 0, total;
-                    for (int i = threadIdx.x; i < kBins; i += THREADS) sum += bin(i);
-                    block.before(sum, total);
+                    double sum = 0, row_mass;
+                    for (int i = threadIdx.x; i < kBins; i += THREADS) sum += mass_in(i);
+                    block.before(sum, row_mass);
+                    scale = scale_of(row_mass);
+                    uint64_t units = 0, total;
+                    for (int i = threadIdx.x; i < kBins; i += THREADS) units += units_in(i);
+                    block.before(units, total);
                     want = (double)total * rule.top_p;
                 }
-                seek(want, above);
+                seek(units_in, want, above);
                 prefix = prefix << width | (uint32_t)found_at, above = found_above;
             }
             // places that equal the last one: as long as less than `want` lies in front of them, the first in any case
-            const uint64_t each = weight(a.share(M::value(prefix)));
+            const double each = a.share(M::value(prefix)) * scale, front = (double)above;
             int64_t more = V;
             if (each > 0) {
-                more = max((int64_t)((want - (double)above) / (double)each), (int64_t)0);
-                while (more > 0 && !((double)(above + (uint64_t)(more - 1) * each) < want)) more--;
-                while ((double)(above + (uint64_t)more * each) < want) more++;
+                more = (int64_t)fmin(fmax((want - front) / each, 0.0), (double)V);
+                while (more > 0 && !(front + (double)(more - 1) * each < want)) more--;
+                while (more < V && front + (double)more * each < want) more++;
             }
             more = max(more, (int64_t)(above == 0));
             if (prefix == least) more = min(more, least_ties);
