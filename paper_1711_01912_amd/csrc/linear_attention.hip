@@ -217,6 +217,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             if constexpr (kind == kGrad) d_rows.load(d_now, p.d, row, next);
         };
         if (kAhead) fetch();
+        int single = 0;                                // rows of a chunk that go one by one, their part of the decays' gradient being done
         while (left > 0) {
             if (!kAhead) fetch();
             const bool found = x_now.store(x_tile);
@@ -227,12 +228,16 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             }
             if constexpr (kind == kGrad) d_now.store(d_tile);
             __syncthreads();
+            bool sums = true, rest = true;             // what is done: the decays' gradient; all else
             if constexpr (kind != kEffect) {
-                // An infinity or a NaN in x would pass, times a score of 0, to the rows before its own: such chunks go row by row
+                // An infinity or a NaN in x would pass, times a score of 0, to the rows before its own: such chunks go row by row.  (kGrad: behind the sums
+                // of the chunk as a whole, which kLeave's are cut like.)
                 const bool bad = __builtin_amdgcn_readfirstlane(odd[turn]);
                 turn ^= 1;
                 if (threadIdx.x == 0) odd[turn] = 0;
-                if (bad && next > 1) {
+                if constexpr (kind == kGrad) {
+                    sums = single == 0, rest = !(bad && next > 1);
+                } else if (bad && next > 1) {
                     next = 1;
                     __syncthreads();
                     if (kAhead) fetch();
@@ -241,9 +246,12 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             }
             const int count = next;
             const int64_t here = row;
-            left -= count;
-            row += p.back ? -count : count;
-            next = (int)min((int64_t)R, left);
+            if (rest) {
+                left -= count;
+                row += p.back ? -count : count;
+                if (single > 0) single--;
+            } else single = count;
+            next = single > 0 ? 1 : (int)min((int64_t)R, left);
             if constexpr (kind == kEffect) {
                 if (left > 0) fetch();
             }
@@ -285,9 +293,9 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
                             const int apart = 16 * (it - jt) + l - 4 * g - e;
-                            if (apart > 0) sum += (float)apart * c[e] * other[e];
+                            if (apart > 0 && 16 * it + l < count) sum += (float)apart * c[e] * other[e];      // (0 of no row times a NaN is one)
                         }
-                        decay_sum += (double)(sum * p.s_out);
+                        if (sums) decay_sum += (double)(sum * p.s_out);
                     }
                     score[m] = c;
                 }
@@ -332,7 +340,8 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                         for (int e = 0; e < 4; e++) o[t][it][e] *= in_[it];
                         if constexpr (kind == kGrad || kind == kLeave) {
                             const int i = 16 * it + l;
-                            if (i >= count || c >= p.wb) continue;
+                            // (a sequence's last row, whose state no decay follows, has no part even if it holds a NaN)
+                            if (i >= count || c >= p.wb || !sums || (kind == kLeave && i == 0)) continue;
                             const T *from = (const T *)p.d.at + (here + (p.back ? -i : i)) * p.d.ld + (head / p.d.group) * p.d.hd + c;
                             float sum = 0;
                             Pack<T, 4> with{};
@@ -385,7 +394,7 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                     const int c = c0 + mine + 16 * t + 4 * g;
                     const int64_t to = (here + (p.back ? -l : l)) * p.ldo + head * p.hdo + c, step = (p.back ? -16 : 16) * p.ldo;
                     const int places = EVEN ? 4 : p.wb - c;
-                    if (c < p.wb) {
+                    if (c < p.wb && rest) {
 #pragma unroll
                         for (int it = 0; it < IT; it++) {
                             if (16 * it + l >= count) continue;
@@ -408,8 +417,14 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             Fade wane = wane_;
             if (count != R) wane = fade_of(lg, count);
             if constexpr (kind == kGrad) {
-                r.add(s, (float)count);
-                r.decay(wane);
+                if (sums) {
+                    r.add(s, (float)count);
+                    r.decay(wane);
+                }
+                if (!rest) {
+                    __syncthreads();
+                    continue;
+                }
             }
             s.decay(wane);
 #pragma unroll
