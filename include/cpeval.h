@@ -729,7 +729,8 @@ int cp_token_logprobs_backward(int64_t rows, int32_t vocab, int type, const void
  *   status_out    device int32, required where a row has settings of its own
  * A row with nothing allowed, or with a NaN or +inf at an allowed place, gets tokens -1 (255 of CP_TOKEN_U8) and logp 0.
  * Probabilities and sums are formed in 64 bits.  workspace may be NULL where cp_token_sample_workspace_bytes says 0.
- * Errors: as cp_token_logprobs's; CP_ERR_SIZE where strides put two tokens in one place.
+ * Errors: as cp_token_logprobs's; CP_ERR_SIZE where strides put two tokens in one place, or are above 2^28 (a row's where there are several
+ * rows, a number's where there are several).
  */
 int cp_token_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t given, size_t *out_bytes);
 int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, int64_t ld, double scale, const float *scales,

@@ -1083,12 +1083,15 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
         if (!workspace) return CP_ERR_NULL;
         if ((uintptr_t)workspace % kPolicyAlign || workspace_bytes < need) return CP_ERR_WORKSPACE;
     }
+    // (what there is one of is at no distance from another)
+    if (rows == 1) u_row_stride = token_row_stride = 0;
+    if (given == 1) u_stride = token_stride = 0;
     if (rows > 0 && given > 0) {
         // numbers may lie anywhere, tokens apart from each other
         if (u_row_stride < 0 || u_stride < 0 || u_row_stride > kFar || u_stride > kFar || token_row_stride > kFar || token_stride > kFar) return CP_ERR_SIZE;
         const bool apart = token_row_stride >= (given - 1) * token_stride + 1, between = token_stride >= (rows - 1) * token_row_stride + 1;
         if ((given > 1 && token_stride < 1) || (rows > 1 && token_row_stride < 1) || (given > 1 && rows > 1 && !apart && !between)) return CP_ERR_SIZE;
-        const int64_t each = token_type, t_row = rows > 1 ? token_row_stride : 0, t_step = given > 1 ? token_stride : 0;
+        const int64_t each = token_type, t_row = token_row_stride, t_step = token_stride;
         const Extent to = rows == 1   ? Extent{tokens, 1, ((given - 1) * t_step + 1) * each, 0, (size_t)each}
                           : given == 1 || apart ? Extent{tokens, rows, ((given - 1) * t_step + 1) * each, t_row * each, (size_t)each}
                                                 : Extent{tokens, given, ((rows - 1) * t_row + 1) * each, t_step * each, (size_t)each};
