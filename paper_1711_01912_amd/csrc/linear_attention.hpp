@@ -15,7 +15,7 @@ constexpr int kThreads = 256;            // of the kernels beside the pass
 struct Operand {
     const void *at;
     int64_t ld, hd;
-    int32_t group;
+    int32_t group = 1;                   // (heads are divided by it, also of an operand that a pass does not have)
 };
 
 // One pass: S_t = gamma S_{t-1} + s_in b_t^T x_t and o_t = s_out a_t S_t along the rows of each sequence, S of wa x wb.  The forward call
