@@ -379,16 +379,18 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             if constexpr (kind != kEffect) {
                 // and what its own rows give
 #pragma unroll
-                for (int jb = 0; jb < JB; jb++) {
-                    Frag<E, PS> sc[IT];
+                for (int jb = 0; jb < JB; jb++)
 #pragma unroll
-                    for (int it = 2 * jb; it < IT; it++) sc[it] = s_tile.along(16 * it, jb, lane);
-                    asked();
+                    for (int i0 = 2 * jb; i0 < IT; i0 += 2) {
+                        Frag<E, PS> sc[2];
 #pragma unroll
-                    for (int t = 0; t < NT; t++)
+                        for (int k = 0; k < 2; k++) sc[k] = s_tile.along(16 * (i0 + k), jb, lane);
+                        asked();
 #pragma unroll
-                        for (int it = 2 * jb; it < IT; it++) o[t][it] = product(xf[t][jb], sc[it], o[t][it]);
-                }
+                        for (int t = 0; t < NT; t++)
+#pragma unroll
+                            for (int k = 0; k < 2; k++) o[t][i0 + k] = product(xf[t][jb], sc[k], o[t][i0 + k]);
+                    }
 #pragma unroll
                 for (int t = 0; t < NT; t++) {
                     const int c = c0 + mine + 16 * t + 4 * g;
