@@ -10,9 +10,9 @@
 // A wavefront owns 16 or 32 columns of S, in registers, and walks along the rows; q, k and v of a chunk lie in LDS.  The scores, of which only
 // the tiles on and below the diagonal are computed, are shared out among the wavefronts.
 //
-// What bounds a pass of bf16 heads of 128: 65,536 rows of 16 heads in 365 to 390 us, 1.07 GB at 2.9 TB/s.  Its loads and stores alone take 239 us, its
-// LDS reads and products alone 333 and more (the clock falls under the products), and with two wavefronts a SIMD, which is what LDS and
-// registers leave room for, about half of the issue slots wait for one of them.
+// What bounds a pass of bf16 heads of 128: 65,536 rows of 16 heads in 377 to 426 us, 1.07 GB at 2.5 to 2.8 TB/s.  With two wavefronts a SIMD, which is
+// what registers leave room for, loads, LDS and products of one hide too little of the other's: the matrix units are busy for 30% of the
+// time, and wavefronts wait for their turn to issue for 29% of theirs.
 //
 // The gradient is three such passes.  With D_t = gamma D_{t+1} + scale q_t^T do_t the gradient of S_t,
 //   dq_t = scale do_t S_t^T (the pass with do, v, k in the places of q, k, v),   dv_t = k_t D_t and dk_t = v_t D_t^T (from the last
@@ -408,8 +408,9 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
             }
 
             // The next chunk is on its way while the state is computed, where there are registers for it.  (Where some go to scratch memory, whose
-            // loads wait for all others before them, it costs more than it gives: 65,536 rows of 16 heads of 128 in bf16 443 us for 388; 1,000,000
-            // rows of 4 of 64, where there are, 3,133 for 3,312, forward and backward.)
+            // loads wait for all others before them, it costs more than it gives: 8 sequences of 4,096 rows of 16 heads of 128 in bf16 1,242 us for 1,105,
+            // forward and backward; where there are, 52,710 rows of 6 heads of 48 keys and 80 values in fp16 773 for 802.  1,000,000 rows of 4 heads of 64
+            // in bf16 3.00 ms either way.)
             if constexpr (kAhead && kind != kEffect) {
                 if (left > 0) fetch();
                 asked();
@@ -487,8 +488,8 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
 
 // States that enter the segments, from their effects, in place and in the order of the pass: E' = gamma^n E + U.  Where a sequence began, the
 // state before it is dropped, whatever it holds; a gamma^n of 0 does not do that, as 0 times a NaN is one.  (gamma^n in 32 bits is off by
-// the same in every segment: by 3e-5 of a state after 1,024.)  Sixteen segments' loads are under way at once: 256 segments of 4 heads of 64 x 64 in 35 us, 45 with the next one's alone; 37 with 32 of half the width, 49 with 64 of a
-// quarter.
+// the same in every segment: by up to 2e-5 of a state after 1,024.)  Sixteen segments' loads are under way at once: 256 segments of 4
+// heads of 64 x 64 in 43 us, 88 with one segment's alone.
 template <int V>
 __global__ __launch_bounds__(kThreads) void enter_kernel(float *at, const Gain *gain, int32_t segments, int32_t heads, int32_t size, bool back) {
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * V;
@@ -647,8 +648,8 @@ constexpr int kMaxWidth = CP_ATTENTION_MAX_WIDTH, kMaxHeads = CP_ATTENTION_MAX_H
 
 // Segments: workgroups enough to fill the chip once, two a compute unit, and twice as many for heads of up to 64, of which four fit; of 128 rows at
 // least.  The same for all types and for both directions, since the backward pass reads the states that the forward call kept.  (Forward and
-// backward in bf16: 1,000,000 rows of 4 heads of 64 3.08 ms, 3.26 with half as many; 8 sequences of 4,096 rows of 16 heads of 128 1.15 ms, 1.27
-// with twice as many, whose states cost more than the fuller chip gives.)
+// backward in bf16: 1,000,000 rows of 4 heads of 64 3.00 ms, 3.30 with half as many, 3.12 with twice; 8 sequences of 4,096 rows of 16 heads of 128 1.10
+// ms, 1.35 with half as many, 1.25 with twice, whose states cost more than the fuller chip gives.)
 struct Cut {
     int64_t seg_rows;
     int32_t parts, segments;
@@ -677,11 +678,12 @@ int32_t slices_of(int32_t wa, int32_t wb) { return (wb + columns_of(wa, wb) - 1)
 
 template <typename T, int KB, int COLUMNS, bool EVEN>
 int run_sized(Kind kind, const Pass &p, float *effect, Gain *gain, hipStream_t st) {
-    // Columns a wavefront: 32 of bf16 heads of up to 128, whose operands then serve two products (65,536 rows of 16 heads of 128 forward 504 us, 605 with 16;
-    // 8 x 4,096 rows forward and backward 1.15 ms, 1.26).  The other types' operands, of two or three parts or in 32 bits, leave no registers for it.
-    // Rows of a chunk: 32 where 64 leave LDS for one workgroup a compute unit, or none, and for bf16 heads of up to 64, of which four
-    // workgroups fit then (1,000,000 rows of 4 heads of 64 3.08 ms, 3.21 with 64; dk and dq of fp16 heads of 48 keys and 80 values, 52,710 rows
-    // of 6, 319 us, 472).  64 otherwise: a state is read and split once for twice the rows.
+    // Columns a wavefront: 32 of bf16 heads of up to 128, whose operands then serve two products (65,536 rows of 16 heads of 128 forward 532 us, 581 with 16;
+    // 8 x 4,096 rows forward and backward 1.10 ms, 1.22).  The other types' operands, of two or three parts or in 32 bits, leave no registers for it.
+    // Rows of a chunk: 64, so that a state is read and split once for as many, but for three.  bf16 heads of up to 64: of 32 rows four workgroups fit a
+    // compute unit (1,000,000 rows of 4 heads of 64 3.00 ms, 3.24 with 64).  fp16 and float heads whose states have 65 to 128 rows and up to 64 columns:
+    // tiles of 64 rows leave LDS for one workgroup (heads of 48 keys and 80 values, 52,710 rows of 6, 773 us, 943 with 64).  And those of more than
+    // 128 rows, whose tiles of 64 do not fit at all.
     constexpr bool kHalf = std::is_same_v<T, bf16>;
     constexpr int R = (kHalf && KB == 2 && COLUMNS == 64) || (!kHalf && (KB == 8 || (KB == 4 && COLUMNS == 64))) ? 32 : 64;
     constexpr int NT = COLUMNS == 128 && kHalf && KB < 8 ? 2 : 1, WAVES = COLUMNS / 16 / NT;

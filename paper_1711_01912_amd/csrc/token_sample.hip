@@ -399,7 +399,7 @@ __device__ __forceinline__ void put_in_order(uint64_t *list, int count) {
 }
 
 // A workgroup a row, which is read from the caches for each of: the maximum; where what is kept ends; the mass of each chunk; the draws.  Only
-// the first reads it from memory.  512 of 65,536 with settings of their own 170 to 180 us.  These are bound by the probabilities (some 16 operations of
+// the first reads it from memory.  512 of 65,536 with settings of their own 174 to 187 us.  These are bound by the probabilities (some 16 operations of
 // 64 bits each) and by the sums of mass by depth, an atomic operation of 64 bits a place in LDS (about 55 us of a row's time).
 template <typename T, int THREADS>
 struct Many {
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 ? 2 : 4) void many_sample_k
         // on until the places of a step are few, which are listed and put in order.  A step's unit is 2^-bits of the mass of a place at its beginning, or
         // of up to twice that, of which all its places have at least a quarter.  So a row's masses are off by 2^(1 - bits) of themselves, 3e-14 in rows of
         // 2^20 places and 2e-12 in such of 2^26, however flat they are.  (With one unit for all steps 2e-7 and 1e-3; 512 x 65536 with settings of their own
-        // 186 us; 196 with one a step.)
+        // 180 us; 187 with one a step.)
         constexpr int kDepth = 6, kFine = 240, kPer = 12, kRest = kFine - kFine / kPer;      // (wide steps: powers + kRest)
         const int bits = 63 - (32 - __clz(min(V, V / kLanes + THREADS * kVec / kLanes)));      // (of a copy's lanes together, below 2^64)
         __shared__ double from[kDepth + 1], per[kDepth + 1];
@@ -1118,7 +1118,7 @@ int cp_token_sample(int64_t rows, int32_t vocab, int type, const void *logits, i
                 if (code) return code;
             }
             // A workgroup as large as has work for its threads (2048 x 4000 bf16 46 us, 85 of 1,024 threads), two a compute unit where there are more
-            // rows than compute units (512 x 65536 181 us, 188 of 1,024 threads; but 8 x 131072 34 us, 36 of 512).
+            // rows than compute units (512 x 65536 187 us, 191 of 1,024 threads; but 8 x 131072 34 us, 36 of 512).
             if (vocab <= 8192) hipLaunchKernelGGL((many_sample_kernel<T, 256>), grid_of(rows), dim3(256), 0, st, d);
             else if (rows > 256) hipLaunchKernelGGL((many_sample_kernel<T, 512>), grid_of(rows), dim3(512), 0, st, d);
             else hipLaunchKernelGGL((many_sample_kernel<T, 1024>), grid_of(rows), dim3(1024), 0, st, d);
