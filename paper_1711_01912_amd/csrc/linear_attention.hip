@@ -198,7 +198,6 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
 
     const RowsOf<T, 32 * KB, R, kThreadsHere, EVEN> a_rows(p.a, head, p.back, 0, p.wa), b_rows(p.b, head, p.back, 0, p.wa);
     const RowsOf<T, kWide, R, kThreadsHere, EVEN> x_rows(p.x, head, p.back, c0, p.wb), d_rows(p.d, head, p.back, c0, p.wb);
-    const bool remembers = lg.hi * R > -40.0f;            // whether what lies before a chunk counts behind it (2^-40: no more in 32 bits)
     while (lo < hi) {
         const Piece piece = piece_at(p, lo, hi);
         int64_t left = piece.hi - piece.lo, row = p.back ? piece.hi - 1 : piece.lo;
@@ -324,10 +323,8 @@ __global__ __launch_bounds__(WAVES * kWave, R == 32 && KB == 2 && kind != kGrad 
                         split(s.at[t][2 * k], s.at[t][2 * k + 1], sf);
                         products<true>(af[k % 2], sf, o[t]);
                         if constexpr (kind == kGrad) {
-                            if (remembers) {
-                                split(r.at[t][2 * k], r.at[t][2 * k + 1], sf);
-                                products<true>(af[k % 2], sf, more[t]);
-                            }
+                            split(r.at[t][2 * k], r.at[t][2 * k + 1], sf);
+                            products<true>(af[k % 2], sf, more[t]);
                         }
                     }
                 }

@@ -9,7 +9,8 @@ import pytest
 import torch
 
 import paper_1711_01912_amd as cpe
-from policy_util import TYPES, U, wide
+from attention_util import reference
+from policy_util import TYPES, U, half_step, near, wide
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -97,3 +98,23 @@ def test_a_state_that_nothing_is_added_to(dtype, N):
         # (what is below the least normal number may be 0)
         off = np.abs(wide(got) - ref) - (times * 2.0 ** -21 * np.abs(ref) + 2.0 ** -126)
         assert (off <= 0).all(), (name, float((np.abs(wide(got) - ref) / np.abs(ref)).max()))
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("first", [40, 64, 100, 190])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decays_gradient_of_a_state_that_nothing_is_added_to(dtype, first, reverse):
+    # what the outputs from row `first` on read has come through the rows before, each of which counts once more for the decays' gradient
+    N, H, K, V = 200, 6, 24, 40
+    g = torch.Generator().manual_seed(first)
+    r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    q, k, v, do = r(N, H, K), torch.zeros(N, H, K), r(N, H, V), r(N, H, V)
+    do[slice(N - first, N) if reverse else slice(0, first)] = 0
+    q, k, v, do = (t.to(TYPES[dtype]).to(DEV) for t in (q, k, v, do))
+    log_decay, h0 = torch.tensor([-0.01, -0.2, -0.3, -0.44, -0.6, -0.8], device=DEV), r(1, H, K, V).to(DEV)
+    kw = dict(h0=h0, reverse=reverse)
+    carry = cpe.cp_linear_attention(q, k, v, log_decay, want_carry=True, **kw)["carry"]
+    got = cpe.cp_linear_attention_backward(do, q, k, v, log_decay, carry, **kw)
+    ref, tol = reference(q, k, v, log_decay, [0, N], 1.0, h0, reverse, do)
+    # (what is below the least normal number may be 0)
+    near(got["dlog_decay"], ref["dlog_decay"], tol["dlog_decay"] + half_step(torch.float32, ref["dlog_decay"]) + N * N * K * V * 2.0 ** -126, "dlog_decay")
